@@ -228,6 +228,80 @@ int spd_gemm_bf16(const void *a, const void *w, float *c, int32_t M, int32_t N, 
 int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, int32_t N, int32_t K, int32_t batches,
                              int32_t a_batched, int32_t splits, int32_t swap, int32_t *err_flag, void *stream);
 
+/* ---- Paged-cache operators on their own ------------------------------------------------------------
+ *
+ * What a serving program needs next to the stack calls: appending rows to a cache of pages, plain or quantised to 8
+ * bits, reading cached rows back, and the attention of a chunk of new tokens per sequence over such a cache (Sec. 3:
+ * every shard attends over its own heads; a shard's call passes the shard's heads).
+ *
+ * Formats.  A cached row is the head_dim values of one token of one KV head.
+ *   SPD_KV_F32, SPD_KV_BF16 : stored as they are (rounded to nearest where the input is wider)
+ *   SPD_KV_E4M3 : 8-bit floats and one float32 scale s per row, the smallest power of two with max|x| <= 448 s;
+ *                 code = x / s rounded to nearest (exact division); code * s is exact in bfloat16
+ *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 / max|x|) rounded to
+ *                 nearest, half to even, in -127 .. 127
+ * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0. */
+#define SPD_KV_F32 0
+#define SPD_KV_BF16 1
+#define SPD_KV_E4M3 2
+#define SPD_KV_INT8 3
+
+typedef struct {
+    void *k_pages, *v_pages;    /* [n_pages, n_kv_heads, kv_block_size, head_dim], 16-byte aligned           */
+    float *k_scales, *v_scales; /* [n_pages, n_kv_heads, kv_block_size]; 8-bit formats only, else may be null */
+    int32_t n_pages, n_kv_heads, kv_block_size, head_dim; /* head_dim 32, 64 or 128; any block size          */
+    int32_t format;
+} spd_kv_cache;
+
+/* Token rows of a batch of B sequences of unequal lengths: rows cu_new[b] .. cu_new[b+1]-1 of a tensor with n_tokens
+ * rows are sequence b's, at positions seq_lens[b], seq_lens[b]+1, ...  Rows before cu_new[0] or from cu_new[B] on belong
+ * to nobody: they are neither computed nor written.  A sequence without rows is allowed. */
+typedef struct {
+    const int32_t *cu_new;      /* [B + 1] device, not decreasing                                            */
+    const int32_t *seq_lens;    /* [B] device                                                                */
+    const int32_t *block_table; /* [B, max_pages] device                                                     */
+    int32_t B, max_pages, n_tokens;
+} spd_ragged;
+
+/* Append rows to the cache: row i of sequence b becomes the cached row at position seq_lens[b] + i.
+ *   k, v : [n_tokens, n_kv_heads, head_dim], dtype 0 float32 / 1 bfloat16, token rows k_stride / v_stride elements apart
+ *          (slices of one projection output qualify); base and row stride multiples of 16 bytes
+ *   err_flag : device int32; bit 1 a page id outside [0, n_pages), bit 2 a position outside the block table: such rows
+ *          are skipped.  Everything else in the pages stays as it is.  No two rows of a call may name the same slot.
+ * Errors: SPD_ENULL, SPD_EINVAL, SPD_ECUDA. */
+int spd_kv_write(const spd_kv_cache *cache, const spd_ragged *batch, const void *k, const void *v, int64_t k_stride,
+                 int64_t v_stride, int32_t dtype, int32_t *err_flag, void *stream);
+
+/* Read rows back: row i of sequence b of k and v = the cached row at position seq_lens[b] + i, as the values the codes
+ * stand for (code * scale), rounded once to dtype.  seq_lens is the first position to read.  Same layout rules and error
+ * bits as spd_kv_write; rows that cannot be read are left as they are. */
+int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, void *v, int64_t k_stride, int64_t v_stride,
+                int32_t dtype, int32_t *err_flag, void *stream);
+
+/* Attention of new tokens over the cache: query row i of sequence b sits at position p = seq_lens[b] + i and sees the
+ * keys t <= p with t > p - window or t < sinks (window 0: every t <= p):
+ *     out[h] = sum_t softmax_t(scale * q[h] . k_t[h / group]) v_t[h / group],   group = n_q_heads / n_kv_heads
+ * The rows of the new tokens are part of the cache already (spd_kv_write first).  One new token per sequence is a decode
+ * step, all of a prompt with seq_lens 0 a prefill, anything between a chunk, a continued conversation or a check of
+ * drafted tokens.
+ *   q, out : [n_tokens, n_q_heads, head_dim] of dtype (0 float32, 1 bfloat16), strided as in spd_kv_write; must not
+ *            overlap.  A float32 q needs an SPD_KV_F32 or 8-bit cache, a bfloat16 q an SPD_KV_BF16 or 8-bit cache.
+ *   max_new, max_context : host bounds of a sequence's new tokens and of seq_lens[b] + new tokens.  A sequence beyond
+ *            them, or with rows outside the tensor, is skipped with error bit 2.
+ *   window : only pages that hold a visible key are looked up, so that block-table entries of pages that lie wholly
+ *            between the sinks and the window may name anything (the pages may have been given back).
+ *   workspace : device memory, 256-byte aligned, at least spd_paged_attention_workspace_bytes() (may be null where that is
+ *            0); contents before and after do not matter; calls that may run at the same time need one each.
+ * A key that a query does not see has no influence on it, whatever it holds.  Scores, sums and the output are held in
+ * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product.
+ * A page id outside [0, n_pages) sets error bit 1; the output rows that needed it are undefined.
+ * Errors: SPD_ENULL, SPD_EINVAL, SPD_ECAPACITY (max_context beyond the block table), SPD_EWORKSPACE, SPD_ECUDA. */
+int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *batch, const void *q, int64_t q_stride, void *out,
+                        int64_t out_stride, int32_t dtype, int32_t n_q_heads, int32_t max_new, int32_t max_context, float scale,
+                        int32_t window, int32_t sinks, void *workspace, size_t workspace_bytes, int32_t *err_flag, void *stream);
+int spd_paged_attention_workspace_bytes(const spd_kv_cache *cache, int32_t B, int32_t n_tokens, int32_t dtype, int32_t n_q_heads,
+                                        int32_t max_new, int32_t max_context, int32_t window, int32_t sinks, size_t *out_bytes);
+
 /* Replace the per-block mask of a context (same meaning as in spd_create).  A mask with an SPD
  * block needs the larger workspace of such a stack: SPD_EWORKSPACE if the context was created
  * from an all-sync mask.  Drops the captured decode graphs.  Errors: SPD_ENULL, SPD_EWORKSPACE. */

@@ -32,7 +32,8 @@ EXPORTS = ("spd_workspace_bytes", "spd_create", "spd_prefill", "spd_decode_step"
            "spd_set_tuning", "spd_set_mask", "spd_sensitivity_scan", "spd_alg1_plan",
            "spd_head_grouping_stats", "spd_head_scatter", "spd_mlp_match", "spd_timeline_begin", "spd_timeline_read",
            "spd_timeline_end", "spd_tp_region_bytes", "spd_tp_attach", "spd_tp_detach", "spd_tp_decode_step",
-           "spd_tp_prefill", "spd_tp_baseline_decode_step", "spd_tp_baseline_prefill")
+           "spd_tp_prefill", "spd_tp_baseline_decode_step", "spd_tp_baseline_prefill",
+           "spd_kv_write", "spd_kv_read", "spd_paged_attention", "spd_paged_attention_workspace_bytes")
 
 
 class SpdError(RuntimeError):
@@ -52,6 +53,17 @@ class spd_dims(ctypes.Structure):
 class spd_layer(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in WEIGHT_NAMES] + [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)] + \
                [(n, ctypes.c_void_p) for n in BIAS_FIELDS]
+
+
+class spd_kv_cache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("kv_block_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class spd_ragged(ctypes.Structure):
+    _fields_ = [("cu_new", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("B", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
 
 
 _lib = None
@@ -99,6 +111,12 @@ def load_library() -> ctypes.CDLL:
     lib.spd_tp_prefill.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp]
     lib.spd_tp_baseline_decode_step.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, sz, ALLREDUCE_FN, vp, vp]
     lib.spd_tp_baseline_prefill.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, sz, ALLREDUCE_FN, vp, vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    cache, ragged = ctypes.POINTER(spd_kv_cache), ctypes.POINTER(spd_ragged)
+    lib.spd_kv_write.argtypes = [cache, ragged, vp, vp, i64, i64, i32, vp, vp]
+    lib.spd_kv_read.argtypes = [cache, ragged, vp, vp, i64, i64, i32, vp, vp]
+    lib.spd_paged_attention.argtypes = [cache, ragged, vp, i64, vp, i64, i32, i32, i32, i32, f32, i32, i32, vp, sz, vp, vp]
+    lib.spd_paged_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     lib.spd_profile_begin.argtypes = [vp]
     lib.spd_profile_end.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
     lib.spd_timeline_begin.argtypes = [vp, vp]
@@ -181,6 +199,133 @@ def gemm_bf16_sum_static(a: torch.Tensor, w: torch.Tensor, out: torch.Tensor, er
                lib.spd_gemm_bf16_sum_static(a.data_ptr(), w.data_ptr(), out.data_ptr(), M, N, K, batches,
                                             1 if a_batched else 0, splits, 1 if swap else 0, err.data_ptr(),
                                             _stream_ptr()))
+    return out
+
+
+# Storage formats of a paged cache by the pages' dtype (SPD_KV_*); the 8-bit ones have one scale per cached row.
+KV_FORMATS = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _kv_cache(k_pages, v_pages, k_scales, v_scales) -> spd_kv_cache:
+    if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in KV_FORMATS and k_pages.is_contiguous()):
+        raise ValueError("k_pages: contiguous CUDA tensor [n_pages, n_kv_heads, page, head_dim] of float32, bfloat16, float8_e4m3fn or int8")
+    if not (v_pages.dtype == k_pages.dtype and v_pages.shape == k_pages.shape and v_pages.is_contiguous() and v_pages.device == k_pages.device):
+        raise ValueError("v_pages: like k_pages")
+    c = spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, *k_pages.shape, KV_FORMATS[k_pages.dtype])
+    if c.format >= 2:
+        for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if s is None or not (s.device == k_pages.device and s.dtype == torch.float32 and s.shape == k_pages.shape[:3] and s.is_contiguous()):
+                raise ValueError(f"{name}: contiguous float32 [n_pages, n_kv_heads, page] on the pages' device (8-bit caches)")
+        c.k_scales, c.v_scales = k_scales.data_ptr(), v_scales.data_ptr()
+    elif k_scales is not None or v_scales is not None:
+        raise ValueError("k_scales / v_scales: for 8-bit caches only")
+    return c
+
+
+def _ragged(k_pages, cu_new, seq_lens, block_table, n_tokens: int) -> spd_ragged:
+    dev = k_pages.device
+    B = seq_lens.numel()
+    for name, t, n in (("cu_new", cu_new, B + 1), ("seq_lens", seq_lens, B)):
+        if not (t.device == dev and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.numel() == n):
+            raise ValueError(f"{name}: contiguous int32 tensor of {n} values on the pages' device")
+    if not (block_table.device == dev and block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
+            and block_table.shape[0] == B):
+        raise ValueError("block_table: contiguous int32 tensor [B, max_pages] on the pages' device")
+    return spd_ragged(cu_new.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), B, block_table.shape[1], n_tokens)
+
+
+def _rows(name: str, t: torch.Tensor, heads: int, k_pages: torch.Tensor) -> int:
+    """Checks a [n_tokens, heads, head_dim] tensor whose heads lie side by side; returns the elements between its rows."""
+    d = k_pages.shape[3]
+    if not (t.device == k_pages.device and t.dtype in _DTYPES and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d
+            and (t.stride(2) == 1 or d == 1) and (heads == 1 or t.stride(1) == d)):
+        raise ValueError(f"{name}: float32 or bfloat16 [n_tokens, {heads}, {d}] on the pages' device, heads side by side in a row")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _flag(err: torch.Tensor, k_pages: torch.Tensor) -> int:
+    if not (err.device == k_pages.device and err.dtype == torch.int32 and err.numel() >= 1):
+        raise ValueError("err: int32 tensor on the pages' device")
+    return err.data_ptr()
+
+
+def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
+             block_table: torch.Tensor, *, err: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
+             v_scales: Optional[torch.Tensor] = None) -> None:
+    """Append rows to a paged cache, quantised to 8 bits where the pages are float8_e4m3fn or int8; see spd_kv_write.
+
+    k, v: [n_tokens, n_kv_heads, head_dim]; rows cu_new[b] .. cu_new[b+1]-1 are sequence b's, at positions seq_lens[b] on.
+    err: int32 tensor that collects error bits (1 page id out of range, 2 position outside the block table); it is not read
+    back here."""
+    lib = load_library()
+    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v: same dtype and number of rows")
+    r = _ragged(k_pages, cu_new, seq_lens, block_table, k.shape[0])
+    ks, vs = _rows("k", k, c.n_kv_heads, k_pages), _rows("v", v, c.n_kv_heads, k_pages)
+    with torch.cuda.device(k_pages.device):
+        _check("spd_kv_write", lib.spd_kv_write(c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, k_pages), _stream_ptr()))
+
+
+def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *,
+            err: torch.Tensor, n_tokens: Optional[int] = None, dtype: torch.dtype = torch.bfloat16,
+            k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None, out=None):
+    """Cached rows as values: row i of sequence b (rows cu[b] .. cu[b+1]-1) is position starts[b] + i; see spd_kv_read.
+    Returns (k, v), each [n_tokens, n_kv_heads, head_dim] of dtype; `out` gives both tensors instead of n_tokens and dtype.
+    Rows outside every sequence are left as they are (undefined where the tensors are made here)."""
+    lib = load_library()
+    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    if out is None:
+        if n_tokens is None or dtype not in _DTYPES:
+            raise ValueError("n_tokens and a dtype of float32 or bfloat16, or out")
+        k, v = (torch.empty((n_tokens, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_pages.device) for _ in range(2))
+    else:
+        k, v = out
+        if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+            raise ValueError("out: two tensors of one dtype and number of rows")
+    r = _ragged(k_pages, cu, starts, block_table, k.shape[0])
+    ks, vs = _rows("k", k, c.n_kv_heads, k_pages), _rows("v", v, c.n_kv_heads, k_pages)
+    with torch.cuda.device(k_pages.device):
+        _check("spd_kv_read", lib.spd_kv_read(c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, k_pages), _stream_ptr()))
+    return k, v
+
+
+def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
+                    block_table: torch.Tensor, *, max_new: int, max_context: int, err: torch.Tensor, window: int = 0, sinks: int = 0,
+                    scale: Optional[float] = None, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of new tokens over a paged cache (causal; window > 0: the last `window` keys and the first `sinks` ones);
+    see spd_paged_attention.
+
+    q: [n_tokens, n_q_heads, head_dim], rows cu_new[b] .. cu_new[b+1]-1 at positions seq_lens[b] on, whose K/V rows are in
+    the cache already.  max_new, max_context: host bounds of a sequence's new tokens and of its whole length.  scale:
+    1/sqrt(head_dim) by default.  workspace: uint8 tensor to use instead of allocating one (calls that may overlap need
+    one each).  err collects error bits as in kv_write."""
+    lib = load_library()
+    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    n, nq, d = q.shape
+    r = _ragged(k_pages, cu_new, seq_lens, block_table, n)
+    qs = _rows("q", q, nq, k_pages)
+    if out is None:
+        out = torch.empty((n, nq, d), dtype=q.dtype, device=q.device)
+    elif out.dtype != q.dtype or out.shape != q.shape:
+        raise ValueError("out: shape and dtype of q")
+    os_ = _rows("out", out, nq, k_pages)
+    need = ctypes.c_size_t(0)
+    _check("spd_paged_attention_workspace_bytes", lib.spd_paged_attention_workspace_bytes(
+        c, r.B, n, _DTYPES[q.dtype], nq, max_new, max_context, window, sinks, need))
+    ws_ptr = 0
+    if need.value:
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        elif not (workspace.device == q.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()):
+            raise ValueError("workspace: contiguous uint8 tensor on the pages' device")
+        ws_ptr = workspace.data_ptr()
+    with torch.cuda.device(k_pages.device):
+        _check("spd_paged_attention", lib.spd_paged_attention(
+            c, r, q.data_ptr(), qs, out.data_ptr(), os_, _DTYPES[q.dtype], nq, max_new, max_context,
+            d ** -0.5 if scale is None else scale, window, sinks, ws_ptr, workspace.numel() if ws_ptr else 0, _flag(err, k_pages), _stream_ptr()))
     return out
 
 

@@ -1,0 +1,83 @@
+// Paged K/V cache operators: the cache's storage formats, where rows of a ragged batch sit in their sequences and
+// pages, and the launchers of kv_cache.cu, paged_attention.cu, paged_attention_rows.cu and paged_attention_tc.cu.
+#pragma once
+#include "common.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+namespace spd {
+
+enum KvFormat : int { KV_F32 = 0, KV_BF16 = 1, KV_E4M3 = 2, KV_INT8 = 3 };
+
+// [n_pages, n_kv_heads, page, head_dim] elements; 8-bit formats: one float32 scale per (page, head, row).
+struct PagedKv {
+    void *k, *v;
+    float *ks, *vs;
+    int n_pages, nkv, page, d, fmt;
+};
+
+// New rows of B sequences, one sequence after the other: sequence b has rows cu[b] .. cu[b+1]-1 at positions
+// lens[b], lens[b]+1, ...
+struct RaggedBatch {
+    const int32_t *cu, *lens, *table;
+    int B, max_pages, n_tokens;
+};
+
+struct PagedAttnArgs {
+    PagedKv kv;
+    RaggedBatch rb;
+    const void *q;
+    void *out;
+    long q_stride, o_stride;      // elements between token rows
+    int nq, group;                // query heads; query heads per KV head
+    int max_new, max_context;     // host bounds on new and on cached + new tokens of a sequence
+    int window, sinks;            // window 0: everything before the query
+    float scale_log2;             // softmax scale times log2(e)
+    int splits;                   // ranges the keys of a row tile are cut into
+    float *part_o, *part_ml;      // splits > 1: fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
+    int *err;
+};
+
+template <int FMT> struct KvElem;
+template <> struct KvElem<KV_F32> { typedef float type; };
+template <> struct KvElem<KV_BF16> { typedef bf16 type; };
+template <> struct KvElem<KV_E4M3> { typedef uint8_t type; };
+template <> struct KvElem<KV_INT8> { typedef int8_t type; };
+
+// code -> the value it stands for before the row's scale
+template <int FMT> __device__ __forceinline__ float kv_value(typename KvElem<FMT>::type c);
+template <> __device__ __forceinline__ float kv_value<KV_F32>(float c) { return c; }
+template <> __device__ __forceinline__ float kv_value<KV_BF16>(bf16 c) { return __bfloat162float(c); }
+template <> __device__ __forceinline__ float kv_value<KV_E4M3>(uint8_t c)
+{
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));
+}
+template <> __device__ __forceinline__ float kv_value<KV_INT8>(int8_t c) { return (float)c; }
+
+// What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
+__device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
+{
+    row0 = rb.cu[b];
+    n_new = rb.cu[b + 1] - row0;
+    len = rb.lens[b];
+    if (n_new == 0) return false;
+    if (row0 < 0 || n_new < 0 || n_new > rb.n_tokens - row0 || n_new > max_new || len < 0 || len > max_context - n_new) {
+        atomicOr(err, ERR_CAPACITY);
+        n_new = 0;
+        return false;
+    }
+    return true;
+}
+
+cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long k_stride, long v_stride,
+                            int in_bf16, int *err, cudaStream_t st);
+cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, void *v, long k_stride, long v_stride, int out_bf16,
+                           int *err, cudaStream_t st);
+
+// q, out and (for unquantised caches) the pages in one type: bf16 or float32
+cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
+// Adds up the key ranges of a split launch.
+cudaError_t launch_paged_merge(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
+
+} // namespace spd
