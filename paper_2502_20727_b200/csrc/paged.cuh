@@ -55,6 +55,25 @@ template <> __device__ __forceinline__ float kv_value<KV_E4M3>(uint8_t c)
 }
 template <> __device__ __forceinline__ float kv_value<KV_INT8>(int8_t c) { return (float)c; }
 
+// Two 8-bit codes of a word -> bf16x2 of the values they stand for, exactly: bytes 0 and 2 (even), bytes 1 and 3 (odd).
+template <int FMT> __device__ __forceinline__ uint32_t even2(uint32_t w);
+template <int FMT> __device__ __forceinline__ uint32_t odd2(uint32_t w);
+__device__ __forceinline__ uint32_t e4m3_fix(uint32_t x) // sign | 4 exponent bits | 3 mantissa bits in bf16's places: times 2^120
+{
+    const __nv_bfloat162 v = __hmul2(*(const __nv_bfloat162 *)&x, __nv_bfloat162(__ushort_as_bfloat16(0x7b80), __ushort_as_bfloat16(0x7b80)));
+    return *(const uint32_t *)&v;
+}
+__device__ __forceinline__ uint32_t int8_fix(uint32_t w) // codes in bits 0-7 and 16-23
+{
+    const uint32_t x = (w & 0x007f007fu) | 0x43004300u, y = (w & 0x00800080u) | 0x43004300u;
+    const __nv_bfloat162 v = __hsub2(*(const __nv_bfloat162 *)&x, *(const __nv_bfloat162 *)&y);
+    return *(const uint32_t *)&v;
+}
+template <> __device__ __forceinline__ uint32_t even2<KV_E4M3>(uint32_t w) { return e4m3_fix(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u)); }
+template <> __device__ __forceinline__ uint32_t odd2<KV_E4M3>(uint32_t w) { return e4m3_fix(((w >> 4) & 0x07f007f0u) | (w & 0x80008000u)); }
+template <> __device__ __forceinline__ uint32_t even2<KV_INT8>(uint32_t w) { return int8_fix(w); }
+template <> __device__ __forceinline__ uint32_t odd2<KV_INT8>(uint32_t w) { return int8_fix(w >> 8); }
+
 // What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
 __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
 {
@@ -70,6 +89,20 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
     return true;
 }
 
+// A kernel's dynamic shared-memory limit, raised once per device.
+struct SmemLimit {
+    bool done[64] = {};
+    cudaError_t raise(const void *kernel, int bytes)
+    {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+        return e;
+    }
+};
+
 cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long k_stride, long v_stride,
                             int in_bf16, int *err, cudaStream_t st);
 cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, void *v, long k_stride, long v_stride, int out_bf16,
@@ -77,6 +110,8 @@ cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, vo
 
 // q, out and (for unquantised caches) the pages in one type: bf16 or float32
 cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
+// bf16 queries, head_dim 64 or 128, at most 16 rows (new tokens x query heads per KV head) per sequence and KV head
+cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
 // Adds up the key ranges of a split launch.
 cudaError_t launch_paged_merge(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 

@@ -88,6 +88,34 @@ cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cuda
     return q_bf16 ? simt_by_format<bf16>(a, st) : simt_by_format<float>(a, st);
 }
 
+namespace {
+
+enum AttnKernel { ATTN_SIMT, ATTN_ROWS };
+struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; };
+
+// Which kernel serves a call, and into how many ranges the keys of its row tiles are cut.
+AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long n_tokens, int max_new, int max_context, int window, int sinks)
+{
+    AttnPlan p{ATTN_SIMT, 1, 0};
+    if (dtype != 1 || (d != 64 && d != 128)) return p;
+    if (max_new > max_context) max_new = max_context;
+    const long rows = (long)max_new * (nq / nkv);
+    long keys = max_context;
+    if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
+    if (rows <= 16) {
+        p.kernel = ATTN_ROWS;
+        // two thread blocks per SM are resident; ranges of at least 8 blocks of 16 keys
+        const long pairs = (long)(B > 0 ? B : 1) * nkv, want = (2L * sm_count() + pairs - 1) / pairs, most = (keys + 127) / 128;
+        p.splits = (int)(want < most ? want : most);
+        if (p.splits > 64) p.splits = 64;
+        if (p.splits < 1) p.splits = 1;
+    }
+    if (p.splits > 1) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
+    return p;
+}
+
+} // namespace
+
 int check_cache(const spd_kv_cache *c, const spd_ragged *r, PagedKv *kv, RaggedBatch *rb); // kv_cache.cu
 bool rows_ok(const void *p, int64_t stride, int heads, int d, int dtype);
 
@@ -115,8 +143,21 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     a.nq = n_q_heads; a.group = n_q_heads / a.kv.nkv; a.max_new = max_new < max_context ? max_new : max_context; a.max_context = max_context;
     a.window = window; a.sinks = window ? sinks : 0;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.splits = 1; a.err = err_flag;
-    const cudaError_t e = launch_paged_attention_simt(a, dtype, (cudaStream_t)stream);
+    a.err = err_flag;
+    const AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, dtype, a.nq, a.rb.B, a.rb.n_tokens, max_new, max_context, a.window, a.sinks);
+    if (p.workspace && (!workspace || workspace_bytes < p.workspace || ((uintptr_t)workspace & 255))) return SPD_EWORKSPACE;
+    a.splits = p.splits;
+    if (p.splits > 1) {
+        a.part_o = (float *)workspace;
+        a.part_ml = a.part_o + (size_t)p.splits * a.rb.n_tokens * a.nq * a.kv.d;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = cudaSuccess;
+    switch (p.kernel) {
+    case ATTN_SIMT: e = launch_paged_attention_simt(a, dtype, st); break;
+    case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
+    }
+    if (e == cudaSuccess && p.splits > 1) e = launch_paged_merge(a, dtype, st);
     if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }
     return SPD_OK;
 }
@@ -126,6 +167,8 @@ extern "C" int spd_paged_attention_workspace_bytes(const spd_kv_cache *cache, in
 {
     if (!cache || !out_bytes) return SPD_ENULL;
     if (B < 0 || n_tokens < 0 || (dtype != 0 && dtype != 1) || cache->n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % cache->n_kv_heads || max_new < 1 || max_context < 1 || window < 0 || sinks < 0) return SPD_EINVAL;
-    *out_bytes = 0;
+    if (cache->format < SPD_KV_F32 || cache->format > SPD_KV_INT8) return SPD_EINVAL;
+    *out_bytes = plan_attention(cache->format, cache->head_dim, cache->n_kv_heads, dtype, n_q_heads, B, n_tokens, max_new, max_context, window,
+                                window ? sinks : 0).workspace;
     return SPD_OK;
 }

@@ -81,6 +81,15 @@ def test_workspace_refusals(lib):
     for kw in (dict(B=-1), dict(n=-1), dict(nq=0), dict(nq=3), dict(mn=0), dict(mc=0), dict(w=-1), dict(s=-1), dict(dtype=2)):
         assert ask(**kw) == -1, kw
     assert lib.spd_paged_attention_workspace_bytes(None, 1, 1, 1, 1, 1, 1, 0, 0, n) == -2
+    # a single token on a long context is split over thread blocks, and then needs its partial results kept
+    big = cache(n_kv_heads=1, head_dim=128, n_pages=4096)
+    assert ask(big, B=1, n=1, nq=8, mn=1, mc=65536) == 0 and n.value > 0
+    need = n.value
+    r = ragged(B=1, n_tokens=1, max_pages=4096)
+    kw = dict(nq=8, qs=1024, os=1024, max_new=1, max_context=65536)
+    assert attend(lib, c=big, r=r, **kw) == -3
+    assert attend(lib, c=big, r=r, ws=P, wsb=need - 1, **kw) == -3
+    assert attend(lib, c=big, r=r, ws=P + 16, wsb=need + 64, **kw) == -3
 
 
 def test_binding_refuses_what_does_not_match():
