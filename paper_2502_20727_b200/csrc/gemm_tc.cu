@@ -246,6 +246,26 @@ int make_page_map(TcMap *out, const void *ptr, long rows)
     return r == CUDA_SUCCESS ? 0 : -3;
 }
 
+// The same for every storage type of a paged cache, head_dim 64 or 128 (`elem` bytes per element): a {128 bytes or less,
+// 16, halves} box brings 16 token rows of one (page, head) in as tiles of 128-byte rows in the 128-byte swizzle (64-byte
+// rows: 64-byte swizzle), low half of the head dimension first where a row is 256 bytes.
+int make_cache_map(TcMap *out, const void *ptr, long rows, int head_dim, int elem)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return -1;
+    const int row_bytes = head_dim * elem, inner = row_bytes > 128 ? 128 : row_bytes;
+    if (((uintptr_t)ptr & 15) || rows > 0x7fffffffL || (row_bytes != 64 && row_bytes != 128 && row_bytes != 256)) return -2;
+    cuuint64_t dims[3] = {(cuuint64_t)(inner / elem), (cuuint64_t)rows, (cuuint64_t)(row_bytes / inner)};
+    cuuint64_t strides[2] = {(cuuint64_t)row_bytes, 128};
+    cuuint32_t box[3] = {(cuuint32_t)(inner / elem), 16, (cuuint32_t)(row_bytes / inner)};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn((CUtensorMap *)out, elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(ptr),
+                    dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    inner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : -3;
+}
+
 int tc_token_box(bool swap, int tokens)
 {
     if (!swap) return BM;

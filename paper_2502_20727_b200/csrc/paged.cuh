@@ -89,16 +89,18 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
     return true;
 }
 
-// A kernel's dynamic shared-memory limit, raised once per device.
+// A kernel's dynamic shared-memory limit (and leave to run in clusters of more than 8 blocks), raised once per device.
 struct SmemLimit {
-    bool done[64] = {};
-    cudaError_t raise(const void *kernel, int bytes)
+    int done[64] = {};
+    cudaError_t raise(const void *kernel, int bytes, bool wide_cluster = false)
     {
         int dev = 0;
+        const int want = wide_cluster ? 3 : 1;
         cudaError_t e = cudaGetDevice(&dev);
-        if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
+        if (e != cudaSuccess || dev < 0 || dev >= 64 || (done[dev] & want) == want) return e;
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+        if (e == cudaSuccess && wide_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) done[dev] |= want;
         return e;
     }
 };
@@ -110,6 +112,8 @@ cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, vo
 
 // q, out and (for unquantised caches) the pages in one type: bf16 or float32
 cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
+// Key ranges that one thread-block cluster adds up in shared memory; more go through the workspace.
+constexpr int PAGED_MAX_CLUSTER = 16;
 // bf16 queries, head_dim 64 or 128, at most 16 rows (new tokens x query heads per KV head) per sequence and KV head
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
 // Adds up the key ranges of a split launch.

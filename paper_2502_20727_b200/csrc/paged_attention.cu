@@ -104,13 +104,15 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
     if (rows <= 16) {
         p.kernel = ATTN_ROWS;
-        // two thread blocks per SM are resident; ranges of at least 8 blocks of 16 keys
-        const long pairs = (long)(B > 0 ? B : 1) * nkv, want = (2L * sm_count() + pairs - 1) / pairs, most = (keys + 127) / 128;
+        // three thread blocks per SM are resident; twice as many ranges as fill them, since sequences are of unequal length;
+        // ranges of at least 8 blocks of 16 keys.  A cluster's worth of ranges unless they would exceed 2048 keys each.
+        const long pairs = (long)(B > 0 ? B : 1) * nkv, want = (6L * sm_count() + pairs - 1) / pairs, most = (keys + 127) / 128;
         p.splits = (int)(want < most ? want : most);
+        if (p.splits > PAGED_MAX_CLUSTER && keys <= 2048L * PAGED_MAX_CLUSTER) p.splits = PAGED_MAX_CLUSTER;
         if (p.splits > 64) p.splits = 64;
         if (p.splits < 1) p.splits = 1;
     }
-    if (p.splits > 1) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
+    if (p.splits > PAGED_MAX_CLUSTER) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
 }
 
@@ -147,7 +149,7 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     const AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, dtype, a.nq, a.rb.B, a.rb.n_tokens, max_new, max_context, a.window, a.sinks);
     if (p.workspace && (!workspace || workspace_bytes < p.workspace || ((uintptr_t)workspace & 255))) return SPD_EWORKSPACE;
     a.splits = p.splits;
-    if (p.splits > 1) {
+    if (p.workspace) {
         a.part_o = (float *)workspace;
         a.part_ml = a.part_o + (size_t)p.splits * a.rb.n_tokens * a.nq * a.kv.d;
     }
@@ -157,7 +159,7 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     case ATTN_SIMT: e = launch_paged_attention_simt(a, dtype, st); break;
     case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
     }
-    if (e == cudaSuccess && p.splits > 1) e = launch_paged_merge(a, dtype, st);
+    if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, dtype, st);
     if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }
     return SPD_OK;
 }

@@ -1,23 +1,28 @@
 // Paged attention for few query rows (bf16): all rows of a (sequence, KV head) - new tokens times query heads per KV head -
 // fit the 16 rows of one m16n8k16 MMA tile, as in single-token steps and short drafts.
 //
-// Bound: the cache stream.  Per 16 cached keys a warp loads two 16 x head_dim tiles and issues 2 * head_dim / 8 MMAs, a
-// small part of an SM's issue slots at the rate HBM delivers the tiles, so the simple tensor path (mma.sync, registers) is
-// enough and the rest serves the loads:
-//   - every warp works on its own 16-key blocks (j, j + 4, ...) with a private ring of cp.async stages: no block-wide
-//     barrier between the first load and the merge, and about 100 KB in flight per SM (2 thread blocks);
-//   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them (grid z), the
-//     ranges' partial rows are added up by paged_merge_kernel;
+// Bound: the cache stream.  Per 16 cached keys a warp loads two 16 x head_dim tiles and issues head_dim / 4 MMAs, a small
+// part of an SM's issue slots at the rate HBM delivers the tiles, so the simple tensor path (mma.sync, registers) is enough
+// and the rest serves the loads and, for 8-bit caches, the widening of the codes:
+//   - every warp works on its own 16-key blocks (j, j + 4, ...) with a private ring of tiles, one TMA box each for K and V
+//     (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled layout): no block-wide barrier between
+//     the first load and the merge;
+//   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 16 ranges
+//     are one thread-block cluster that adds up its partial rows through shared memory; more go through the workspace and
+//     paged_merge_kernel;
 //   - 8-bit caches stay 8-bit up to the fragment registers.  A 16-byte shared-memory load gives a lane 16 consecutive head
-//     dims of one key; any assignment of dims to the MMA's k index is right as long as Q uses the same one, so the even and
-//     the odd bytes of a 32-bit word become the two B registers of one MMA without a shuffle.  V is loaded as 16 dims of four
-//     keys, whose bytes are interleaved by key pairs; the output columns come out permuted and are stored where they belong.
-//     Row scales multiply the fp32 scores (K) and the softmax weights before they are rounded (V).
-//   - e4m3 -> bf16: sign, exponent and mantissa moved to their places give the value times 2^-120, one bf16x2 product puts
-//     the exponent right (exact, subnormals too).  int8 -> bf16: the low 7 bits over the exponent of 128 give 128 + low, and
-//     128 (or 256 where the sign bit is set) is subtracted (exact).
+//     dims of one key; any assignment of dims to the MMA's k index is right as long as Q uses the same one.  Likewise any
+//     assignment of keys to score columns is right as long as V uses the same one: column 2i of eight keys is key 2i, column
+//     2i + 1 is key (2i) ^ 5, with which both the K loads (lanes = columns) and the V loads (lanes = column pairs) meet every
+//     shared-memory bank once under the swizzle.
+//   - K codes become float16 (exact; one conversion instruction for e4m3; for int8 the code byte under the exponent of 1024,
+//     minus 1152) and so does Q, scaled per row by a power of two to below 2^15: the scaled row keeps bf16's 8 bits for
+//     everything down to 2^-29 of its largest value.  V codes become bfloat16 (exact), because the weights they meet carry
+//     the V scales, whose range float16 does not cover: e4m3 by moving sign, exponent and mantissa to bf16's places (the value
+//     times 2^-120) and one product, int8 as 128 + low 7 bits minus 128 or 256.
 // Softmax: base 2, fp32, per warp; the accumulators follow the running maximum lazily (they are rescaled when it has grown by
 // more than 2^8: weights stay below 2^8, where bf16 rounds as finely as at 1).
+#include "gemm_tc.cuh"
 #include "paged.cuh"
 #include "tc_ptx.cuh"
 
@@ -28,15 +33,16 @@ namespace {
 constexpr int RW = 4, R_THREADS = 32 * RW, BK16 = 16;
 
 template <int FMT, int D> struct RowsCfg {
-    static constexpr int ES = FMT == KV_BF16 ? 2 : 1;
-    static constexpr int RB = D * ES;                      // bytes of a cached row
-    static constexpr int CPR = RB / 16;                    // 16-byte chunks of it
-    static constexpr int SC = FMT == KV_BF16 ? 0 : 128;    // 16 K scales, 16 V scales
-    static constexpr int STAGE = 2 * BK16 * RB + SC;
-    static constexpr int STAGES = FMT == KV_BF16 && D == 128 ? 3 : 6;
-    static constexpr int RING = RW * STAGES * STAGE;
-    static constexpr int MERGE = RW * 16 * (D + 4) * 4;
-    static constexpr int SMEM = (RING > MERGE ? RING : MERGE);
+    static constexpr bool Q8 = FMT != KV_BF16;
+    static constexpr int RB = D * (Q8 ? 1 : 2);            // bytes of a cached row
+    static constexpr int TR = RB > 128 ? 128 : RB;         // bytes of a tile row; 256-byte rows are two tiles
+    static constexpr int TILE = BK16 * RB;                 // K or V of one block
+    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 4 : 6;
+    static constexpr int OFF_SC = RW * STAGES * 2 * TILE;  // 16 K scales, 16 V scales per stage
+    static constexpr int OFF_BAR = OFF_SC + (Q8 ? RW * STAGES * 128 : 0);
+    static constexpr int OFF_PML = OFF_BAR + RW * STAGES * 8 + 16; // abort flag before it; merged [16][2] after
+    static constexpr int SMEM = OFF_PML + 128 + 1024;      // + alignment slack
+    static_assert(RW * 16 * (D + 4) * 4 <= OFF_SC, "merge area fits the rings");
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
@@ -49,22 +55,27 @@ __device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool valid)
     const int n = valid ? 4 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+// 64 bytes, both sides 16-byte aligned
+__device__ __forceinline__ void bulk64(uint32_t dst, const void *src, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 64, [%2];" ::"r"(dst), "l"(src), "r"(bar) : "memory");
+}
 __device__ __forceinline__ uint4 lds128(uint32_t a)
 {
     uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a)
 {
     uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ float2 lds_f2(uint32_t a)
+__device__ __forceinline__ float lds_f(uint32_t a)
 {
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v)
@@ -73,12 +84,16 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v)
 }
 __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+template <bool F16> __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
@@ -92,25 +107,55 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// keys t of a row at position pos (-1: no row) that it sees
+// Two neighbouring codes (low or high half of a word) -> float16x2 of the values they stand for, exactly.
+template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t half_pair(uint32_t w)
+{
+    if (FMT == KV_E4M3) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(HIGH ? w >> 16 : w & 0xffffu), __NV_E4M3);
+        return (uint32_t)h.x | ((uint32_t)h.y << 16);
+    }
+    // w: codes with the sign bit flipped (code + 128)
+    const uint32_t x = __byte_perm(w, 0x64646464u, HIGH ? 0x4342 : 0x4140);
+    const __half2 v = __hsub2(*(const __half2 *)&x, __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480))); // 1024 + 128
+    return *(const uint32_t *)&v;
+}
+
+// keys t that a row at position pos (-1: no row) sees
 __device__ __forceinline__ bool sees(int t, int pos, int window, int sinks) { return t <= pos && (!window || t > pos - window || t < sinks); }
 
-// P16: the page size is a multiple of 16, so a 16-key block lies in one page
-template <int FMT, int D, bool P16>
-__global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(const __grid_constant__ PagedAttnArgs a)
+// key of score column c (0-7) of an 8-column MMA
+__device__ __forceinline__ int key_of(int c) { return c & 1 ? (c & 6) ^ 5 : c; }
+
+template <int FMT, int D, bool TMA>
+__global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+                                                                            const __grid_constant__ PagedAttnArgs a)
 {
     using C = RowsCfg<FMT, D>;
-    constexpr bool Q8 = FMT != KV_BF16;
-    constexpr int NT = D / 8, KS = D / 16;
-    extern __shared__ __align__(128) uint8_t rows_smem[];
-    pdl_launch_dependents();
-    pdl_wait();
+    constexpr bool Q8 = C::Q8;
+    constexpr int NT = D / 8, KS = D / 16, ST = C::STAGES;
+    extern __shared__ uint8_t rows_raw[];
+    uint8_t *gen = rows_raw + ((1024u - (tc::smem_u32(rows_raw) & 1023u)) & 1023u);
+    const uint32_t base = tc::smem_u32(gen);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::OFF_SC + warp * ST * 128, bars = base + C::OFF_BAR + warp * ST * 8;
+    volatile int *abort_flag = (volatile int *)(gen + C::OFF_BAR + RW * ST * 8);
+    pdl_launch_dependents();
+    if (TMA) {
+        if (lane == 0) {
+            for (int s = 0; s < ST; ++s) tc::mbar_init(bars + 8 * s, 1);
+            if (warp == 0) *abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+        }
+        __syncthreads();
+    }
+    pdl_wait();
     const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
     int row0, n_new, len;
-    if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
+    if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return; // the same for a whole cluster
     const int rows = n_new * a.group; // <= 16
-    const int kv_len = len + n_new;
+    const int kv_len = len + n_new, pos_max = kv_len - 1;
     // blocks of 16 keys that hold a key some row sees: sinks, then the window of the first query onwards
     const int lo_min = a.window ? max(0, len - a.window + 1) : 0, first = lo_min / BK16;
     const int n_sink = min((min(a.sinks, lo_min) + BK16 - 1) / BK16, first);
@@ -120,50 +165,72 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
     const int j_begin = split < splits ? (int)((long)n_blocks * split / splits) : 0;
     const int j_end = split < splits ? (int)((long)n_blocks * (split + 1) / splits) : 0;
 
-    const uint32_t ring = tc::smem_u32(rows_smem) + warp * C::STAGES * C::STAGE;
     const int32_t *bt = a.rb.table + (long)b * a.rb.max_pages;
+    const int bpp = a.kv.page / BK16; // TMA: blocks per page
     auto block_of = [&](int j) { return j < n_sink ? j : first + (j - n_sink); };
     auto row_valid = [&](int t) { return t < kv_len && (t >= lo_min || t < a.sinks); };
+    // every row sees every key of the 16 from t0 on
+    auto seen_by_all = [&](int t0) { return t0 + 15 <= len && (!a.window || t0 > pos_max - a.window || t0 + 15 < a.sinks); };
     auto lookup = [&](int t) { // cached row of key t, or -1
         const int pi = t / a.kv.page, page = bt[pi];
         if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); return -1L; }
         return ((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page);
     };
-    // cached row of this lane's key (lane & 15) of block j - P16: of the block's first key
+    // TMA: cached row of the first key of block j (a bad page id: page 0, with the error bit); else of this lane's key (lane & 15), or -1
     auto lookup_block = [&](int j) -> long {
-        const int t0 = block_of(j) * BK16;
-        if (P16) return lookup(t0);
-        const int t = t0 + (lane & 15);
+        const int blk = block_of(j);
+        if (TMA) {
+            const int pi = bpp == 1 ? blk : blk / bpp;
+            int page = bt[pi];
+            if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); page = 0; }
+            return ((long)page * a.kv.nkv + kvh) * a.kv.page + (bpp == 1 ? 0 : (blk - pi * bpp) * BK16);
+        }
+        const int t = blk * BK16 + (lane & 15);
         return row_valid(t) ? lookup(t) : -1L;
     };
-    auto load_block = [&](int j, int stage, long where) {
-        const uint32_t sK = ring + stage * C::STAGE, sV = sK + BK16 * C::RB;
-        const int t0 = block_of(j) * BK16;
-        constexpr int RPI = 32 / C::CPR; // rows per instruction
-        const int c = lane % C::CPR;
+    // 16-byte chunk c of row r of a tile pair / tile, where the copies put it
+    auto at = [&](int r, int c) -> uint32_t {
+        if (C::RB == 256) return (c >> 3) * (BK16 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+        if (C::RB == 128) return r * 128 + ((c ^ (r & 7)) << 4);
+        return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+    };
+    auto load_block = [&](int stage, long where) {
+        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
+        if (TMA) {
+            if (lane == 0) {
+                const uint32_t bar = bars + 8 * stage;
+                tc::mbar_expect_tx(bar, 2 * C::TILE + (Q8 ? 128 : 0));
+                tc::tma_load_3d(sK, (const CUtensorMap *)&k_map, 0, (int)where, 0, bar);
+                tc::tma_load_3d(sV, (const CUtensorMap *)&v_map, 0, (int)where, 0, bar);
+                if (Q8) { bulk64(sS, a.kv.ks + where, bar); bulk64(sS + 64, a.kv.vs + where, bar); }
+            }
+        } else {
+            constexpr int CPR = C::RB / 16, RPI = 32 / CPR; // chunks per row, rows per instruction
+            const int c = lane % CPR;
 #pragma unroll
-        for (int i = 0; i < BK16 / RPI; ++i) {
-            const int r = i * RPI + lane / C::CPR;
-            long row;
-            bool ok;
-            if (P16) { row = where + r; ok = where >= 0 && row_valid(t0 + r); }
-            else { row = __shfl_sync(0xffffffffu, where, r); ok = row >= 0; }
-            const long off = ok ? row * C::RB + c * 16 : 0;
-            const int ck = C::CPR >= 8 ? c ^ ((r & 1) << 2) : c;
-            const int cv = Q8 ? (C::CPR == 8 ? c ^ (r & 6) : c ^ (r & 2)) : c ^ (r & 7);
-            cp16(sK + r * C::RB + ck * 16, (const uint8_t *)a.kv.k + off, ok);
-            cp16(sV + r * C::RB + cv * 16, (const uint8_t *)a.kv.v + off, ok);
-        }
-        if (Q8) {
-            const int r = lane & 15;
-            const long row = P16 ? where + r : where;
-            const bool ok = P16 ? where >= 0 && row_valid(t0 + r) : where >= 0;
-            cp4(sV + BK16 * C::RB + lane * 4, (lane < 16 ? a.kv.ks : a.kv.vs) + (ok ? row : 0), ok);
+            for (int i = 0; i < BK16 / RPI; ++i) {
+                const int r = i * RPI + lane / CPR;
+                const long row = __shfl_sync(0xffffffffu, where, r);
+                const long off = row >= 0 ? row * C::RB + c * 16 : 0;
+                cp16(sK + at(r, c), (const uint8_t *)a.kv.k + off, row >= 0);
+                cp16(sV + at(r, c), (const uint8_t *)a.kv.v + off, row >= 0);
+            }
+            if (Q8) cp4(sS + lane * 4, (lane < 16 ? a.kv.ks : a.kv.vs) + (where >= 0 ? where : 0), where >= 0);
         }
     };
 
-    // Q fragments; rows beyond the tile's are zero
+    const int n_mine = (j_end - j_begin - warp + RW - 1) / RW; // blocks j_begin + warp, + RW, ...
+    auto mine = [&](int i) { return j_begin + warp + i * RW; };
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+        if (s < n_mine) load_block(s, lookup_block(mine(s)));
+        if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    long where = ST < n_mine ? lookup_block(mine(ST)) : 0;
+
+    // Q fragments; rows beyond the tile's are zero.  qs: what turns a score into base-2 units
     uint32_t qf[KS][4];
+    float qs[2];
     int pos[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -171,103 +238,108 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
         const bool live = r < rows;
         const int i = live ? r / a.group : 0, head = live ? r % a.group : 0;
         pos[h] = live ? len + i : -1;
+        qs[h] = a.scale_log2;
         const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
-        if (!Q8) {
+        uint4 u[D / 32];
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) { // a 16-byte K chunk is 8 dims (bf16) or 16 (codes)
+            const int dim = Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
+            u[m] = live ? *(const uint4 *)(qp + dim) : make_uint4(0, 0, 0, 0);
+        }
+        if (Q8) {
+            uint32_t top = 0; // largest magnitude's bits
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
-                const uint4 u = live ? *(const uint4 *)(qp + 32 * m + 8 * t4) : make_uint4(0, 0, 0, 0);
-                qf[2 * m][h] = u.x; qf[2 * m][2 + h] = u.y; qf[2 * m + 1][h] = u.z; qf[2 * m + 1][2 + h] = u.w;
+                const uint32_t w[4] = {u[m].x, u[m].y, u[m].z, u[m].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
             }
-        } else {
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int ex = max((int)(top >> 7), 27) - 127;                         // 2^ex <= largest < 2^(ex + 1), ex >= -100
+            const float f = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);      // to [2^14, 2^15)
+            qs[h] *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
 #pragma unroll
-            for (int m = 0; m < D / 64; ++m) {
+            for (int m = 0; m < D / 32; ++m) {
+                const uint32_t w[4] = {u[m].x, u[m].y, u[m].z, u[m].w};
+                uint32_t x[4];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint4 u = live ? *(const uint4 *)(qp + 64 * m + 16 * t4 + 8 * half) : make_uint4(0, 0, 0, 0);
-                    // dims (0, 2) and (1, 3) of every four: the even and the odd bytes of a cached word
-                    qf[4 * m + 2 * half][h] = __byte_perm(u.x, u.y, 0x5410);
-                    qf[4 * m + 2 * half][2 + h] = __byte_perm(u.x, u.y, 0x7632);
-                    qf[4 * m + 2 * half + 1][h] = __byte_perm(u.z, u.w, 0x5410);
-                    qf[4 * m + 2 * half + 1][2 + h] = __byte_perm(u.z, u.w, 0x7632);
+                for (int e = 0; e < 4; ++e) {
+                    const __half2 v = __floats2half2_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                    x[e] = *(const uint32_t *)&v;
                 }
+                u[m] = make_uint4(x[0], x[1], x[2], x[3]);
             }
         }
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) {
+            qf[2 * m][h] = u[m].x; qf[2 * m][2 + h] = u[m].y; qf[2 * m + 1][h] = u[m].z; qf[2 * m + 1][2 + h] = u[m].w;
+        }
     }
-    const int pos_max = kv_len - 1;
-    // every row sees every key of the 16 from t0 on
-    auto seen_by_all = [&](int t0) { return t0 + 15 <= len && (!a.window || t0 > pos_max - a.window || t0 + 15 < a.sinks); };
 
     float o[NT][4];
 #pragma unroll
     for (int i = 0; i < NT; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
     float m_used[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     bool dirty = false; // a NaN or infinity of V was taken out of a block that not every row sees
-
-    const int n_mine = (j_end - j_begin - warp + RW - 1) / RW; // blocks j_begin + warp, + RW, ...
-    long where = 0;
-    for (int s = 0; s < C::STAGES - 1; ++s) {
-        if (s < n_mine) load_block(j_begin + warp + s * RW, s, lookup_block(j_begin + warp + s * RW));
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    if (C::STAGES - 1 < n_mine) where = lookup_block(j_begin + warp + (C::STAGES - 1) * RW);
-    int stage = 0;
+    bool ok = true;
+    int stage = 0, phase = 0;
     for (int it = 0; it < n_mine; ++it) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
-        __syncwarp();
-        {   // refill the stage read in the previous iteration (STAGES - 1 ahead), page lookups another one ahead
-            const int nx = it + C::STAGES - 1;
-            if (nx < n_mine) load_block(j_begin + warp + nx * RW, stage == 0 ? C::STAGES - 1 : stage - 1, where);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (nx + 1 < n_mine) where = lookup_block(j_begin + warp + (nx + 1) * RW);
+        if (TMA) {
+            ok = tc::mbar_wait(bars + 8 * stage, phase, a.err, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+        } else {
+            asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+            __syncwarp();
         }
-        const uint32_t sK = ring + stage * C::STAGE, sV = sK + BK16 * C::RB, sS = sV + BK16 * C::RB;
-        const int t0 = block_of(j_begin + warp + it * RW) * BK16;
-        float s[2][4];
+        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
+        const int t0 = block_of(mine(it)) * BK16;
+        float s[2][4], ks[2][2], vs[2][2];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-            const int r = nt * 8 + g;
+            const int r = nt * 8 + key_of(g);
             if (!Q8) {
 #pragma unroll
                 for (int m = 0; m < D / 32; ++m) {
-                    const uint4 u = lds128(sK + r * C::RB + (((4 * m + t4) ^ ((r & 1) << 2)) << 4));
-                    mma16816(s[nt], qf[2 * m][0], qf[2 * m][1], qf[2 * m][2], qf[2 * m][3], u.x, u.y);
-                    mma16816(s[nt], qf[2 * m + 1][0], qf[2 * m + 1][1], qf[2 * m + 1][2], qf[2 * m + 1][3], u.z, u.w);
+                    const uint4 u = lds128(sK + at(r, 4 * m + t4));
+                    mma16816<false>(s[nt], qf[2 * m], u.x, u.y);
+                    mma16816<false>(s[nt], qf[2 * m + 1], u.z, u.w);
                 }
             } else {
 #pragma unroll
                 for (int m = 0; m < D / 64; ++m) {
-                    const uint4 u = lds128(sK + r * C::RB + ((C::CPR >= 8 ? (4 * m + t4) ^ ((r & 1) << 2) : t4) << 4));
+                    const uint4 u = lds128(sK + at(r, 4 * m + t4));
                     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int k = 4 * m + i;
-                        mma16816(s[nt], qf[k][0], qf[k][1], qf[k][2], qf[k][3], even2<FMT>(w[i]), odd2<FMT>(w[i]));
+                        const uint32_t x = FMT == KV_INT8 ? w[i] ^ 0x80808080u : w[i];
+                        mma16816<true>(s[nt], qf[4 * m + i], half_pair<FMT, false>(x), half_pair<FMT, true>(x));
                     }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    ks[nt][e] = lds_f(sS + (nt * 8 + key_of(2 * t4 + e)) * 4);
+                    vs[nt][e] = lds_f(sS + 64 + (nt * 8 + key_of(2 * t4 + e)) * 4);
                 }
             }
         }
-        // scores in base 2; masked ones -inf whatever was computed
         const bool all_seen = seen_by_all(t0);
         float mx[2] = {-INFINITY, -INFINITY};
-        float2 kscale[2], vscale[2];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            if (Q8) { kscale[nt] = lds_f2(sS + (nt * 8 + 2 * t4) * 4); vscale[nt] = lds_f2(sS + 64 + (nt * 8 + 2 * t4) * 4); }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int t = t0 + nt * 8 + 2 * t4 + (e & 1), h = e >> 1;
-                float v = s[nt][e] * a.scale_log2;
-                if (Q8) v *= (e & 1) ? kscale[nt].y : kscale[nt].x;
-                if (!all_seen && !sees(t, pos[h], a.window, a.sinks)) v = -INFINITY;
-                s[nt][e] = v;
-                mx[h] = fmaxf(mx[h], v);
+                if (Q8) s[nt][e] *= ks[nt][e & 1];
+                if (!all_seen && !sees(t0 + nt * 8 + key_of(2 * t4 + (e & 1)), pos[e >> 1], a.window, a.sinks)) s[nt][e] = -INFINITY;
+                mx[e >> 1] = fmaxf(mx[e >> 1], s[nt][e]);
             }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2)) * qs[h];
         }
         const bool grow = mx[0] > m_used[0] + 8.f || mx[1] > m_used[1] + 8.f; // first keys of a row included (-inf)
         if (__any_sync(0xffffffffu, grow)) {
@@ -282,18 +354,18 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
 #pragma unroll
             for (int i = 0; i < NT; ++i) { o[i][0] *= f[0]; o[i][1] *= f[0]; o[i][2] *= f[1]; o[i][3] *= f[1]; }
         }
-        const float base[2] = {m_used[0] == -INFINITY ? 0.f : m_used[0], m_used[1] == -INFINITY ? 0.f : m_used[1]};
+        const float mb[2] = {m_used[0] == -INFINITY ? 0.f : m_used[0], m_used[1] == -INFINITY ? 0.f : m_used[1]};
         uint32_t pf[4];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                p[e] = ex2(s[nt][e] - base[e >> 1]);
+                p[e] = ex2(fmaf(s[nt][e], qs[e >> 1], -mb[e >> 1]));
                 l[e >> 1] += p[e];
-                if (Q8) { // a masked key's scale may be anything
-                    const float w = p[e] * ((e & 1) ? vscale[nt].y : vscale[nt].x);
-                    p[e] = s[nt][e] == -INFINITY ? 0.f : w;
+                if (Q8) {
+                    p[e] *= vs[nt][e & 1];
+                    if (!all_seen && s[nt][e] == -INFINITY) p[e] = 0.f; // a masked key's scale may be anything
                 }
             }
             pf[2 * nt] = pack(p[0], p[1]);
@@ -302,11 +374,10 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
         if (!Q8) {
             if (!all_seen) {
                 // 0 * NaN would reach rows that do not see the key: take non-finite values out here, give them back at the end
-                constexpr int RPI = 32 / C::CPR;
 #pragma unroll
-                for (int i = 0; i < BK16 / RPI; ++i) {
-                    const uint32_t at = sV + (i * RPI + lane / C::CPR) * C::RB + (lane % C::CPR) * 16;
-                    uint4 u = lds128(at);
+                for (int i = 0; i < C::TILE / 512; ++i) {
+                    const uint32_t p = sV + (i * 32 + lane) * 16;
+                    const uint4 u = lds128(p);
                     uint32_t w[4] = {u.x, u.y, u.z, u.w};
                     bool bad = false;
 #pragma unroll
@@ -314,29 +385,30 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
                         if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; bad = true; }
                         if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; bad = true; }
                     }
-                    if (bad) { sts128(at, make_uint4(w[0], w[1], w[2], w[3])); dirty = true; }
+                    if (bad) { sts128(p, make_uint4(w[0], w[1], w[2], w[3])); dirty = true; }
                 }
+                tc::fence_proxy_async(); // the tile is refilled by the async proxy
                 __syncwarp();
             }
+            const int c = lane & 7, r = key_of(c) + (((lane >> 3) & 1) << 3);
 #pragma unroll
             for (int dp = 0; dp < D / 16; ++dp) {
                 uint32_t vf[4];
-                const int r = (lane & 7) + (((lane >> 3) & 1) << 3), c = dp * 2 + (lane >> 4);
-                ldsm4t(vf, sV + r * C::RB + ((c ^ (r & 7)) << 4));
-                mma16816(o[2 * dp], pf[0], pf[1], pf[2], pf[3], vf[0], vf[1]);
-                mma16816(o[2 * dp + 1], pf[0], pf[1], pf[2], pf[3], vf[2], vf[3]);
+                ldsm4t(vf, sV + at(r, dp * 2 + (lane >> 4)));
+                mma16816<false>(o[2 * dp], pf, vf[0], vf[1]);
+                mma16816<false>(o[2 * dp + 1], pf, vf[2], vf[3]);
             }
         } else {
-            constexpr int W = D / 32; // words per key and lane
+            constexpr int W = D / 32; // words per key and lane: dims g * D / 8 ..
             uint32_t v[4][W];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = 2 * t4 + (q & 1) + (q >> 1) * 8;
+                const int r = (q >> 1) * 8 + key_of(2 * t4 + (q & 1));
                 if (W == 4) {
-                    const uint4 u = lds128(sV + r * C::RB + ((g ^ (r & 6)) << 4));
+                    const uint4 u = lds128(sV + at(r, g));
                     v[q][0] = u.x; v[q][1] = u.y; v[q][2 % W] = u.z; v[q][3 % W] = u.w;
                 } else {
-                    const uint2 u = lds64(sV + r * C::RB + (((g >> 1) ^ (r & 2)) << 4) + (g & 1) * 8);
+                    const uint2 u = lds64(sV + at(r, g >> 1) + (g & 1) * 8);
                     v[q][0] = u.x; v[q][1] = u.y;
                 }
             }
@@ -345,15 +417,28 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
                 // bytes (k0.0, k0.1, k1.0, k1.1): even bytes = column 0 of keys (k0, k1), odd bytes = column 1
                 const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5410), x1 = __byte_perm(v[2][w], v[3][w], 0x5410);
                 const uint32_t y0 = __byte_perm(v[0][w], v[1][w], 0x7632), y1 = __byte_perm(v[2][w], v[3][w], 0x7632);
-                mma16816(o[4 * w], pf[0], pf[1], pf[2], pf[3], even2<FMT>(x0), even2<FMT>(x1));
-                mma16816(o[4 * w + 1], pf[0], pf[1], pf[2], pf[3], odd2<FMT>(x0), odd2<FMT>(x1));
-                mma16816(o[4 * w + 2], pf[0], pf[1], pf[2], pf[3], even2<FMT>(y0), even2<FMT>(y1));
-                mma16816(o[4 * w + 3], pf[0], pf[1], pf[2], pf[3], odd2<FMT>(y0), odd2<FMT>(y1));
+                mma16816<false>(o[4 * w], pf, even2<FMT>(x0), even2<FMT>(x1));
+                mma16816<false>(o[4 * w + 1], pf, odd2<FMT>(x0), odd2<FMT>(x1));
+                mma16816<false>(o[4 * w + 2], pf, even2<FMT>(y0), even2<FMT>(y1));
+                mma16816<false>(o[4 * w + 3], pf, odd2<FMT>(y0), odd2<FMT>(y1));
             }
         }
-        stage = stage + 1 == C::STAGES ? 0 : stage + 1;
+        __syncwarp(); // every lane has read the stage
+        if (it + ST < n_mine) {
+            load_block(stage, where);
+            if (it + ST + 1 < n_mine) where = lookup_block(mine(it + ST + 1));
+        }
+        if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++stage == ST) { stage = 0; phase ^= 1; }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (!TMA) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (TMA && !ok) { // gave up: the copies still in flight must land before the memory is reused
+        for (int it = 0; it < ST; ++it) {
+            const long long t_end = clock64() + tc::WAIT_LIMIT_CYCLES;
+            while (!tc::mbar_try_wait(bars + 8 * stage, phase) && clock64() < t_end) {}
+            if (++stage == ST) { stage = 0; phase ^= 1; }
+        }
+    }
 
     // the four warps' partial rows, merged through shared memory (the rings are done with)
 #pragma unroll
@@ -362,7 +447,8 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
     }
     const int any_dirty = __syncthreads_or(dirty);
-    float *mo = (float *)rows_smem, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
+    float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
+    float *pml = (float *)(gen + C::OFF_PML);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int r = g + 8 * h;
@@ -380,7 +466,13 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
         }
     }
     __syncthreads();
+    const bool clustered = a.splits > 1 && a.splits <= PAGED_MAX_CLUSTER;
     const long plane = (long)a.rb.n_tokens * a.nq;
+    auto store = [&](int r, int c, float x, float y, float den) {
+        const int i = r / a.group, head = kvh * a.group + r % a.group;
+        const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
+        *(uint32_t *)((bf16 *)a.out + (long)(row0 + i) * a.o_stride + (long)head * D + c) = pack(x * inv, y * inv);
+    };
     for (int idx = threadIdx.x; idx < rows * (D / 2); idx += R_THREADS) {
         const int r = idx / (D / 2), c = idx % (D / 2) * 2;
         float m = -INFINITY, den = 0.f, x = 0.f, y = 0.f;
@@ -410,15 +502,39 @@ __global__ void __launch_bounds__(R_THREADS, 2) paged_attention_rows_kernel(cons
                 }
             }
         }
-        if (a.splits == 1) {
-            const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
-            *(uint32_t *)((bf16 *)a.out + (long)(row0 + i) * a.o_stride + (long)head * D + c) = pack(x * inv, y * inv);
+        if (a.splits == 1) { store(r, c, x, y, den); continue; }
+        if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum: not an empty range
+        if (clustered) { // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
+            *(float2 *)(mo + r * (D + 2) + c) = make_float2(x, y);
+            if (c == 0) { pml[2 * r] = m; pml[2 * r + 1] = den; }
         } else {
-            const long at = (long)split * plane + (long)(row0 + i) * a.nq + head;
-            if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum: not an empty range
-            if (m != -INFINITY) *(float2 *)(a.part_o + at * D + c) = make_float2(x, y);
-            if (c == 0) { a.part_ml[at * 2] = m; a.part_ml[at * 2 + 1] = den; }
+            const long w = (long)split * plane + (long)(row0 + i) * a.nq + head;
+            if (m != -INFINITY) *(float2 *)(a.part_o + w * D + c) = make_float2(x, y);
+            if (c == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
         }
+    }
+    if (clustered) {
+        tc::cluster_sync();
+        const uint32_t mo_addr = base, pml_addr = base + C::OFF_PML;
+        auto peer2 = [](uint32_t addr, int rank) {
+            float2 v;
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(tc::mapa_shared(addr, rank)) : "memory");
+            return v;
+        };
+        for (int idx = split + a.splits * (int)threadIdx.x; idx < rows * (D / 2); idx += a.splits * R_THREADS) {
+            const int r = idx / (D / 2), c = idx % (D / 2) * 2;
+            float m = -INFINITY, den = 0.f, x = 0.f, y = 0.f;
+            for (int s = 0; s < splits; ++s) m = fmaxf(m, peer2(pml_addr + 8 * r, s).x);
+            for (int s = 0; s < splits; ++s) {
+                const float2 q = peer2(pml_addr + 8 * r, s), v = peer2(mo_addr + (r * (D + 2) + c) * 4, s);
+                const float f = q.x == -INFINITY ? 0.f : ex2(q.x - m);
+                den = fmaf(q.y, f, den);
+                x = fmaf(v.x, f, x);
+                y = fmaf(v.y, f, y);
+            }
+            store(r, c, x, y, den);
+        }
+        tc::cluster_sync(); // no block exits while a peer still reads its shared memory
     }
 }
 
@@ -463,19 +579,30 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     for (int e = 0; e < VEC; ++e) dst[e] = from_f<T>(o[e] * inv);
 }
 
-template <int FMT, int D, bool P16> cudaError_t launch_rows(const PagedAttnArgs &a, cudaStream_t st)
+template <int FMT, int D, bool TMA> cudaError_t launch_rows(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
 {
     using C = RowsCfg<FMT, D>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, P16>, C::SMEM);
+    const cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, TMA>, C::SMEM, a.splits > 8);
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_attention_rows_kernel<FMT, D, P16>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(R_THREADS), C::SMEM, st, 0, a);
+    return launch_kernel_z(paged_attention_rows_kernel<FMT, D, TMA>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(R_THREADS), C::SMEM, st,
+                           a.splits <= PAGED_MAX_CLUSTER ? a.splits : 1, km, vm, a);
+}
+template <int FMT, int D> cudaError_t rows_by_copy(const PagedAttnArgs &a, cudaStream_t st)
+{
+    // 16-key blocks as TMA boxes: they lie in one page, row numbers fit a coordinate, scales start on 16 bytes
+    TcMap km{}, vm{};
+    const long rows = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
+    const int es = FMT == KV_BF16 ? 2 : 1;
+    if (a.kv.page % BK16 == 0 && rows <= 0x7fffffffL && !(((uintptr_t)a.kv.ks | (uintptr_t)a.kv.vs) & 15) &&
+        make_cache_map(&km, a.kv.k, rows, D, es) == 0 && make_cache_map(&vm, a.kv.v, rows, D, es) == 0)
+        return launch_rows<FMT, D, true>(a, km, vm, st);
+    return launch_rows<FMT, D, false>(a, km, vm, st);
 }
 template <int FMT> cudaError_t rows_by_dim(const PagedAttnArgs &a, cudaStream_t st)
 {
-    const bool p16 = a.kv.page % 16 == 0;
-    if (a.kv.d == 128) return p16 ? launch_rows<FMT, 128, true>(a, st) : launch_rows<FMT, 128, false>(a, st);
-    if (a.kv.d == 64) return p16 ? launch_rows<FMT, 64, true>(a, st) : launch_rows<FMT, 64, false>(a, st);
+    if (a.kv.d == 128) return rows_by_copy<FMT, 128>(a, st);
+    if (a.kv.d == 64) return rows_by_copy<FMT, 64>(a, st);
     return cudaErrorInvalidValue;
 }
 
