@@ -63,9 +63,18 @@ __device__ __forceinline__ uint32_t e4m3_fix(uint32_t x) // sign | 4 exponent bi
     const __nv_bfloat162 v = __hmul2(*(const __nv_bfloat162 *)&x, __nv_bfloat162(__ushort_as_bfloat16(0x7b80), __ushort_as_bfloat16(0x7b80)));
     return *(const uint32_t *)&v;
 }
+// (a & b) | c in one instruction: with two literals the compiler takes two
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
 __device__ __forceinline__ uint32_t int8_fix(uint32_t w) // codes in bits 0-7 and 16-23
 {
-    const uint32_t x = (w & 0x007f007fu) | 0x43004300u, y = (w & 0x00800080u) | 0x43004300u;
+    uint32_t c128; // bf16x2 of 128, kept in a register
+    asm("mov.b32 %0, 0x43004300;" : "=r"(c128));
+    const uint32_t x = and_or(w, 0x007f007fu, c128), y = and_or(w, 0x00800080u, c128);
     const __nv_bfloat162 v = __hsub2(*(const __nv_bfloat162 *)&x, *(const __nv_bfloat162 *)&y);
     return *(const uint32_t *)&v;
 }

@@ -1,20 +1,23 @@
 // Paged attention for few query rows (bf16): all rows of a (sequence, KV head) - new tokens times query heads per KV head -
-// fit the 16 rows of one m16n8k16 MMA tile, as in single-token steps and short drafts.
+// are the 8 or 16 columns of m16n8k16 MMAs, as in single-token steps and short drafts.
 //
-// Bound: the cache stream.  Per 16 cached keys a warp loads two 16 x head_dim tiles and issues head_dim / 4 MMAs, a small
-// part of an SM's issue slots at the rate HBM delivers the tiles, so the simple tensor path (mma.sync, registers) is enough
-// and the rest serves the loads and, for 8-bit caches, the widening of the codes:
+// Bound: the cache stream.  Keys and head dims are the MMA rows (S^T = K Q^T, O^T = V^T P^T), so that 8 query rows cost no
+// padding: per 16 cached keys a warp issues head_dim / 8 MMAs for 8 query rows, a small part of an SM's issue slots at the
+// rate HBM delivers the keys.  mma.sync and registers are enough, and the rest serves the loads and, for 8-bit caches, the
+// widening of the codes:
 //   - every warp works on its own 16-key blocks (j, j + 4, ...) with a private ring of tiles, one TMA box each for K and V
 //     (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled layout): no block-wide barrier between
 //     the first load and the merge;
 //   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 16 ranges
 //     are one thread-block cluster that adds up its partial rows through shared memory; more go through the workspace and
 //     paged_merge_kernel;
+//   - the weights leave the first product with keys as rows and enter the second with keys as its k index: one 8 x 8
+//     transpose (movmatrix) per 8 keys;
 //   - 8-bit caches stay 8-bit up to the fragment registers.  A 16-byte shared-memory load gives a lane 16 consecutive head
 //     dims of one key; any assignment of dims to the MMA's k index is right as long as Q uses the same one.  Likewise any
-//     assignment of keys to score columns is right as long as V uses the same one: column 2i of eight keys is key 2i, column
-//     2i + 1 is key (2i) ^ 5, with which both the K loads (lanes = columns) and the V loads (lanes = column pairs) meet every
-//     shared-memory bank once under the swizzle.
+//     assignment of keys to score rows is right as long as V uses the same one: row 2i of eight keys is key 2i, row 2i + 1 is
+//     key (2i) ^ 5, with which both the K loads (lanes = rows) and the V loads (lanes = row pairs) meet every shared-memory
+//     bank once under the swizzle.
 //   - K codes become float16 (exact; one conversion instruction for e4m3; for int8 the code byte under the exponent of 1024,
 //     minus 1152) and so does Q, scaled per row by a power of two to below 2^15: the scaled row keeps bf16's 8 bits for
 //     everything down to 2^-29 of its largest value.  V codes become bfloat16 (exact), because the weights they meet carry
@@ -37,7 +40,7 @@ template <int FMT, int D> struct RowsCfg {
     static constexpr int RB = D * (Q8 ? 1 : 2);            // bytes of a cached row
     static constexpr int TR = RB > 128 ? 128 : RB;         // bytes of a tile row; 256-byte rows are two tiles
     static constexpr int TILE = BK16 * RB;                 // K or V of one block
-    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 4 : 6;
+    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : 6;
     static constexpr int OFF_SC = RW * STAGES * 2 * TILE;  // 16 K scales, 16 V scales per stage
     static constexpr int OFF_BAR = OFF_SC + (Q8 ? RW * STAGES * 128 : 0);
     static constexpr int OFF_PML = OFF_BAR + RW * STAGES * 8 + 16; // abort flag before it; merged [16][2] after
@@ -86,14 +89,21 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-template <bool F16> __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     if (F16)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
@@ -123,16 +133,17 @@ template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t half_pair(uint
 // keys t that a row at position pos (-1: no row) sees
 __device__ __forceinline__ bool sees(int t, int pos, int window, int sinks) { return t <= pos && (!window || t > pos - window || t < sinks); }
 
-// key of score column c (0-7) of an 8-column MMA
+// key of score row c (0-7) of eight
 __device__ __forceinline__ int key_of(int c) { return c & 1 ? (c & 6) ^ 5 : c; }
 
-template <int FMT, int D, bool TMA>
-__global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+// NR: groups of 8 query rows
+template <int FMT, int D, int NR, bool TMA>
+__global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                             const __grid_constant__ PagedAttnArgs a)
 {
     using C = RowsCfg<FMT, D>;
     constexpr bool Q8 = C::Q8;
-    constexpr int NT = D / 8, KS = D / 16, ST = C::STAGES;
+    constexpr int MT = D / 16, KS = D / 16, ST = C::STAGES;
     extern __shared__ uint8_t rows_raw[];
     uint8_t *gen = rows_raw + ((1024u - (tc::smem_u32(rows_raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(gen);
@@ -154,7 +165,7 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
     const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
     int row0, n_new, len;
     if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return; // the same for a whole cluster
-    const int rows = n_new * a.group; // <= 16
+    const int rows = n_new * a.group; // <= 8 NR
     const int kv_len = len + n_new, pos_max = kv_len - 1;
     // blocks of 16 keys that hold a key some row sees: sinks, then the window of the first query onwards
     const int lo_min = a.window ? max(0, len - a.window + 1) : 0, first = lo_min / BK16;
@@ -228,17 +239,16 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
     }
     long where = ST < n_mine ? lookup_block(mine(ST)) : 0;
 
-    // Q fragments; rows beyond the tile's are zero.  qs: what turns a score into base-2 units
-    uint32_t qf[KS][4];
-    float qs[2];
-    int pos[2];
+    // Q fragments (column g of a group of 8 rows); rows beyond the tile's are zero.  qs: what turns the scores of this lane's
+    // columns 2 t4 and 2 t4 + 1 into base-2 units
+    uint32_t qf[NR][KS][2];
+    float qs[NR][2];
+    int pos[NR][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = g + 8 * h;
+    for (int n = 0; n < NR; ++n) {
+        const int r = g + 8 * n;
         const bool live = r < rows;
         const int i = live ? r / a.group : 0, head = live ? r % a.group : 0;
-        pos[h] = live ? len + i : -1;
-        qs[h] = a.scale_log2;
         const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
         uint4 u[D / 32];
 #pragma unroll
@@ -246,6 +256,7 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
             const int dim = Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
             u[m] = live ? *(const uint4 *)(qp + dim) : make_uint4(0, 0, 0, 0);
         }
+        float my_qs = a.scale_log2;
         if (Q8) {
             uint32_t top = 0; // largest magnitude's bits
 #pragma unroll
@@ -258,7 +269,7 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int ex = max((int)(top >> 7), 27) - 127;                         // 2^ex <= largest < 2^(ex + 1), ex >= -100
             const float f = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);      // to [2^14, 2^15)
-            qs[h] *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+            my_qs *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
                 const uint32_t w[4] = {u[m].x, u[m].y, u[m].z, u[m].w};
@@ -273,14 +284,32 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
         }
 #pragma unroll
         for (int m = 0; m < D / 32; ++m) {
-            qf[2 * m][h] = u[m].x; qf[2 * m][2 + h] = u[m].y; qf[2 * m + 1][h] = u[m].z; qf[2 * m + 1][2 + h] = u[m].w;
+            qf[n][2 * m][0] = u[m].x; qf[n][2 * m][1] = u[m].y; qf[n][2 * m + 1][0] = u[m].z; qf[n][2 * m + 1][1] = u[m].w;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = 8 * n + 2 * t4 + e;
+            pos[n][e] = c < rows ? len + c / a.group : -1;
+            qs[n][e] = __shfl_sync(0xffffffffu, my_qs, (2 * t4 + e) * 4);
         }
     }
 
-    float o[NT][4];
+    // where this lane reads in a stage; chunk bits above the lane's own are XORs, rows + 8 a fixed distance
+    const uint32_t lane_k = at(key_of(g), t4);
+    const int vc = lane & 7;
+    const uint32_t lane_v0 = Q8 ? (D == 128 ? at(key_of(2 * t4), g) : at(key_of(2 * t4), g >> 1) + (g & 1) * 8) : at(key_of(vc) + (lane & 8), lane >> 4);
+    const uint32_t lane_v1 = Q8 ? (D == 128 ? at(key_of(2 * t4 + 1), g) : at(key_of(2 * t4 + 1), g >> 1) + (g & 1) * 8) : 0u;
+    const uint32_t lane_s = key_of(g) * 4;
+
+    float o[NR][MT][4];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
-    float m_used[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) { o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f; }
+    }
+    float m_used[NR][2], l[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) { m_used[n][0] = m_used[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
     bool dirty = false; // a NaN or infinity of V was taken out of a block that not every row sees
     bool ok = true;
     int stage = 0, phase = 0;
@@ -295,81 +324,98 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
         }
         const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
         const int t0 = block_of(mine(it)) * BK16;
-        float s[2][4], ks[2][2], vs[2][2];
+        float s[NR][4], ks[2], vs[2]; // rows g and g + 8
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-            const int r = nt * 8 + key_of(g);
-            if (!Q8) {
+        for (int n = 0; n < NR; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        if (!Q8) {
 #pragma unroll
-                for (int m = 0; m < D / 32; ++m) {
-                    const uint4 u = lds128(sK + at(r, 4 * m + t4));
-                    mma16816<false>(s[nt], qf[2 * m], u.x, u.y);
-                    mma16816<false>(s[nt], qf[2 * m + 1], u.z, u.w);
+            for (int m = 0; m < D / 32; ++m) {
+                const uint32_t p = ((sK + lane_k) ^ ((m & 1) << 6)) + (m >> 1) * (BK16 * 128);
+                const uint4 u = lds128(p), w = lds128(p + 8 * C::TR);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    mma16816<false>(s[n], u.x, w.x, u.y, w.y, qf[n][2 * m][0], qf[n][2 * m][1]);
+                    mma16816<false>(s[n], u.z, w.z, u.w, w.w, qf[n][2 * m + 1][0], qf[n][2 * m + 1][1]);
                 }
-            } else {
+            }
+        } else {
 #pragma unroll
-                for (int m = 0; m < D / 64; ++m) {
-                    const uint4 u = lds128(sK + at(r, 4 * m + t4));
-                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            for (int m = 0; m < D / 64; ++m) {
+                const uint32_t p = (sK + lane_k) ^ (m << 6);
+                const uint4 u0 = lds128(p), u1 = lds128(p + 8 * C::TR);
+                const uint32_t w0[4] = {u0.x, u0.y, u0.z, u0.w}, w1[4] = {u1.x, u1.y, u1.z, u1.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = FMT == KV_INT8 ? w[i] ^ 0x80808080u : w[i];
-                        mma16816<true>(s[nt], qf[4 * m + i], half_pair<FMT, false>(x), half_pair<FMT, true>(x));
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x0 = FMT == KV_INT8 ? w0[i] ^ 0x80808080u : w0[i], x1 = FMT == KV_INT8 ? w1[i] ^ 0x80808080u : w1[i];
+                    const uint32_t a0 = half_pair<FMT, false>(x0), a1 = half_pair<FMT, false>(x1), a2 = half_pair<FMT, true>(x0), a3 = half_pair<FMT, true>(x1);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) mma16816<true>(s[n], a0, a1, a2, a3, qf[n][4 * m + i][0], qf[n][4 * m + i][1]);
                 }
+            }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    ks[nt][e] = lds_f(sS + (nt * 8 + key_of(2 * t4 + e)) * 4);
-                    vs[nt][e] = lds_f(sS + 64 + (nt * 8 + key_of(2 * t4 + e)) * 4);
-                }
+            for (int h = 0; h < 2; ++h) { ks[h] = lds_f(sS + lane_s + h * 32); vs[h] = lds_f(sS + lane_s + 64 + h * 32); }
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= ks[e >> 1];
             }
         }
         const bool all_seen = seen_by_all(t0);
-        float mx[2] = {-INFINITY, -INFINITY};
+        if (!all_seen) { // masked scores are -inf whatever was computed
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+            for (int n = 0; n < NR; ++n) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (Q8) s[nt][e] *= ks[nt][e & 1];
-                if (!all_seen && !sees(t0 + nt * 8 + key_of(2 * t4 + (e & 1)), pos[e >> 1], a.window, a.sinks)) s[nt][e] = -INFINITY;
-                mx[e >> 1] = fmaxf(mx[e >> 1], s[nt][e]);
+                for (int e = 0; e < 4; ++e)
+                    if (!sees(t0 + 8 * (e >> 1) + key_of(g), pos[n][e & 1], a.window, a.sinks)) s[n][e] = -INFINITY;
             }
         }
+        float mx[NR][2];
+        bool grow = false;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2)) * qs[h];
+        for (int n = 0; n < NR; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float m = fmaxf(s[n][e], s[n][2 + e]);
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                mx[n][e] = m * qs[n][e];
+                grow |= mx[n][e] > m_used[n][e] + 8.f; // first keys of a row included (-inf)
+            }
         }
-        const bool grow = mx[0] > m_used[0] + 8.f || mx[1] > m_used[1] + 8.f; // first keys of a row included (-inf)
         if (__any_sync(0xffffffffu, grow)) {
-            float f[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float nm = fmaxf(m_used[h], mx[h]);
-                f[h] = m_used[h] == -INFINITY ? 0.f : ex2(m_used[h] - nm);
-                m_used[h] = nm;
-                l[h] *= f[h];
+            for (int n = 0; n < NR; ++n) {
+                float f[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float nm = fmaxf(m_used[n][e], mx[n][e]);
+                    f[e] = m_used[n][e] == -INFINITY ? 0.f : ex2(m_used[n][e] - nm);
+                    m_used[n][e] = nm;
+                    l[n][e] *= f[e];
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
             }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) { o[i][0] *= f[0]; o[i][1] *= f[0]; o[i][2] *= f[1]; o[i][3] *= f[1]; }
         }
-        const float mb[2] = {m_used[0] == -INFINITY ? 0.f : m_used[0], m_used[1] == -INFINITY ? 0.f : m_used[1]};
-        uint32_t pf[4];
+        uint32_t pf[NR][2];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int n = 0; n < NR; ++n) {
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                p[e] = ex2(fmaf(s[nt][e], qs[e >> 1], -mb[e >> 1]));
-                l[e >> 1] += p[e];
-                if (Q8) {
-                    p[e] *= vs[nt][e & 1];
-                    if (!all_seen && s[nt][e] == -INFINITY) p[e] = 0.f; // a masked key's scale may be anything
-                }
+                const float mb = m_used[n][e & 1] == -INFINITY ? 0.f : m_used[n][e & 1];
+                p[e] = ex2(fmaf(s[n][e], qs[n][e & 1], -mb));
+                l[n][e & 1] += p[e];
+                if (Q8) p[e] *= vs[e >> 1];
             }
-            pf[2 * nt] = pack(p[0], p[1]);
-            pf[2 * nt + 1] = pack(p[2], p[3]);
+            if (Q8 && !all_seen) { // 0 times the scale of a masked key, which may be anything
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (s[n][e] == -INFINITY) p[e] = 0.f;
+            }
+            pf[n][0] = transpose8x8(pack(p[0], p[1]));
+            pf[n][1] = transpose8x8(pack(p[2], p[3]));
         }
         if (!Q8) {
             if (!all_seen) {
@@ -390,37 +436,39 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
                 tc::fence_proxy_async(); // the tile is refilled by the async proxy
                 __syncwarp();
             }
-            const int c = lane & 7, r = key_of(c) + (((lane >> 3) & 1) << 3);
 #pragma unroll
-            for (int dp = 0; dp < D / 16; ++dp) {
-                uint32_t vf[4];
-                ldsm4t(vf, sV + at(r, dp * 2 + (lane >> 4)));
-                mma16816<false>(o[2 * dp], pf, vf[0], vf[1]);
-                mma16816<false>(o[2 * dp + 1], pf, vf[2], vf[3]);
+            for (int i = 0; i < MT; ++i) {
+                uint32_t vf[4]; // (keys 0-7, dims 0-7), (keys 8-15, dims 0-7), (keys 0-7, dims 8-15), (keys 8-15, dims 8-15)
+                ldsm4t(vf, ((sV + lane_v0) ^ ((i & 3) << 5)) + (i >> 2) * (BK16 * 128));
+#pragma unroll
+                for (int n = 0; n < NR; ++n) mma16816<false>(o[n][i], vf[0], vf[2], vf[1], vf[3], pf[n][0], pf[n][1]);
             }
         } else {
             constexpr int W = D / 32; // words per key and lane: dims g * D / 8 ..
             uint32_t v[4][W];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = (q >> 1) * 8 + key_of(2 * t4 + (q & 1));
+                const uint32_t p = sV + (q & 1 ? lane_v1 : lane_v0) + (q >> 1) * 8 * C::TR;
                 if (W == 4) {
-                    const uint4 u = lds128(sV + at(r, g));
+                    const uint4 u = lds128(p);
                     v[q][0] = u.x; v[q][1] = u.y; v[q][2 % W] = u.z; v[q][3 % W] = u.w;
                 } else {
-                    const uint2 u = lds64(sV + at(r, g >> 1) + (g & 1) * 8);
+                    const uint2 u = lds64(p);
                     v[q][0] = u.x; v[q][1] = u.y;
                 }
             }
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                // bytes (k0.0, k0.1, k1.0, k1.1): even bytes = column 0 of keys (k0, k1), odd bytes = column 1
+                // bytes (k0.0, k0.1, k1.0, k1.1): even bytes = dim 0 of keys (k0, k1), odd bytes = dim 1
                 const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5410), x1 = __byte_perm(v[2][w], v[3][w], 0x5410);
                 const uint32_t y0 = __byte_perm(v[0][w], v[1][w], 0x7632), y1 = __byte_perm(v[2][w], v[3][w], 0x7632);
-                mma16816<false>(o[4 * w], pf, even2<FMT>(x0), even2<FMT>(x1));
-                mma16816<false>(o[4 * w + 1], pf, odd2<FMT>(x0), odd2<FMT>(x1));
-                mma16816<false>(o[4 * w + 2], pf, even2<FMT>(y0), even2<FMT>(y1));
-                mma16816<false>(o[4 * w + 3], pf, odd2<FMT>(y0), odd2<FMT>(y1));
+                const uint32_t a0 = even2<FMT>(x0), a1 = odd2<FMT>(x0), a2 = even2<FMT>(x1), a3 = odd2<FMT>(x1);
+                const uint32_t b0 = even2<FMT>(y0), b1 = odd2<FMT>(y0), b2 = even2<FMT>(y1), b3 = odd2<FMT>(y1);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    mma16816<false>(o[n][2 * w], a0, a1, a2, a3, pf[n][0], pf[n][1]);
+                    mma16816<false>(o[n][2 * w + 1], b0, b1, b2, b3, pf[n][0], pf[n][1]);
+                }
             }
         }
         __syncwarp(); // every lane has read the stage
@@ -442,27 +490,31 @@ __global__ void __launch_bounds__(R_THREADS, 3) paged_attention_rows_kernel(cons
 
     // the four warps' partial rows, merged through shared memory (the rings are done with)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 4);
+            l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 8);
+            l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 16);
+        }
     }
     const int any_dirty = __syncthreads_or(dirty);
     float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
     float *pml = (float *)(gen + C::OFF_PML);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = g + 8 * h;
-        if (r < rows) {
-            float *dst = mo + (warp * 16 + r) * (D + 2);
+    for (int n = 0; n < NR; ++n) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (!Q8) *(float2 *)(dst + nt * 8 + 2 * t4) = make_float2(o[nt][2 * h], o[nt][2 * h + 1]);
-                else { // column n of MMA nt = dim n * D / 8 + nt
-                    dst[(2 * t4) * (D / 8) + nt] = o[nt][2 * h];
-                    dst[(2 * t4 + 1) * (D / 8) + nt] = o[nt][2 * h + 1];
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * n + 2 * t4 + e;
+            if (r < rows) {
+                float *dst = mo + (warp * 16 + r) * (D + 2);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if (!Q8) { dst[16 * i + g] = o[n][i][e]; dst[16 * i + 8 + g] = o[n][i][2 + e]; }
+                    else *(float2 *)(dst + g * (D / 8) + 2 * i) = make_float2(o[n][i][e], o[n][i][2 + e]); // MMA row g: dims g D/8 + 2i, row g + 8: + 1
                 }
+                if (g == 0) { ml[(warp * 16 + r) * 2] = m_used[n][e]; ml[(warp * 16 + r) * 2 + 1] = l[n][e]; }
             }
-            if (t4 == 0) { ml[(warp * 16 + r) * 2] = m_used[h]; ml[(warp * 16 + r) * 2 + 1] = l[h]; }
         }
     }
     __syncthreads();
@@ -579,13 +631,13 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     for (int e = 0; e < VEC; ++e) dst[e] = from_f<T>(o[e] * inv);
 }
 
-template <int FMT, int D, bool TMA> cudaError_t launch_rows(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
+template <int FMT, int D, int NR, bool TMA> cudaError_t launch_rows(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
 {
     using C = RowsCfg<FMT, D>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, TMA>, C::SMEM, a.splits > 8);
+    const cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, NR, TMA>, C::SMEM, a.splits > 8);
     if (e != cudaSuccess) return e;
-    return launch_kernel_z(paged_attention_rows_kernel<FMT, D, TMA>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(R_THREADS), C::SMEM, st,
+    return launch_kernel_z(paged_attention_rows_kernel<FMT, D, NR, TMA>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(R_THREADS), C::SMEM, st,
                            a.splits <= PAGED_MAX_CLUSTER ? a.splits : 1, km, vm, a);
 }
 template <int FMT, int D> cudaError_t rows_by_copy(const PagedAttnArgs &a, cudaStream_t st)
@@ -596,8 +648,8 @@ template <int FMT, int D> cudaError_t rows_by_copy(const PagedAttnArgs &a, cudaS
     const int es = FMT == KV_BF16 ? 2 : 1;
     if (a.kv.page % BK16 == 0 && rows <= 0x7fffffffL && !(((uintptr_t)a.kv.ks | (uintptr_t)a.kv.vs) & 15) &&
         make_cache_map(&km, a.kv.k, rows, D, es) == 0 && make_cache_map(&vm, a.kv.v, rows, D, es) == 0)
-        return launch_rows<FMT, D, true>(a, km, vm, st);
-    return launch_rows<FMT, D, false>(a, km, vm, st);
+        return a.max_new * a.group <= 8 ? launch_rows<FMT, D, 1, true>(a, km, vm, st) : launch_rows<FMT, D, 2, true>(a, km, vm, st);
+    return launch_rows<FMT, D, 2, false>(a, km, vm, st);
 }
 template <int FMT> cudaError_t rows_by_dim(const PagedAttnArgs &a, cudaStream_t st)
 {
