@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspd_b200.so")
 
 SPD_OK = 0
+SPD_EWORKSPACE = -3
 STATUS_NAMES = {0: "SPD_OK", -1: "SPD_EINVAL", -2: "SPD_ENULL", -3: "SPD_EWORKSPACE", -4: "SPD_ECAPACITY",
                 -5: "SPD_ECUDA", -6: "SPD_EDEVICE", -7: "SPD_ECALLBACK"}
 ALLREDUCE_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
@@ -207,47 +208,67 @@ KV_FORMATS = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
+# These run once per layer and token of a serving loop, so their checks stay cheap: device indices instead of device objects,
+# one comparison where one says it.
 def _kv_cache(k_pages, v_pages, k_scales, v_scales) -> spd_kv_cache:
-    if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.dtype in KV_FORMATS and k_pages.is_contiguous()):
+    dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
+    fmt = KV_FORMATS.get(dtype)
+    if fmt is None or len(shape) != 4 or dev < 0 or not k_pages.is_contiguous():
         raise ValueError("k_pages: contiguous CUDA tensor [n_pages, n_kv_heads, page, head_dim] of float32, bfloat16, float8_e4m3fn or int8")
-    if not (v_pages.dtype == k_pages.dtype and v_pages.shape == k_pages.shape and v_pages.is_contiguous() and v_pages.device == k_pages.device):
+    if v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev or not v_pages.is_contiguous():
         raise ValueError("v_pages: like k_pages")
-    c = spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, *k_pages.shape, KV_FORMATS[k_pages.dtype])
-    if c.format >= 2:
+    if fmt >= 2:
         for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
-            if s is None or not (s.device == k_pages.device and s.dtype == torch.float32 and s.shape == k_pages.shape[:3] and s.is_contiguous()):
+            if s is None or s.get_device() != dev or s.dtype is not torch.float32 or s.shape != shape[:3] or not s.is_contiguous():
                 raise ValueError(f"{name}: contiguous float32 [n_pages, n_kv_heads, page] on the pages' device (8-bit caches)")
-        c.k_scales, c.v_scales = k_scales.data_ptr(), v_scales.data_ptr()
-    elif k_scales is not None or v_scales is not None:
+        return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *shape, fmt)
+    if k_scales is not None or v_scales is not None:
         raise ValueError("k_scales / v_scales: for 8-bit caches only")
-    return c
+    return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, *shape, fmt)
 
 
-def _ragged(k_pages, cu_new, seq_lens, block_table, n_tokens: int) -> spd_ragged:
-    dev = k_pages.device
-    B = seq_lens.numel()
-    for name, t, n in (("cu_new", cu_new, B + 1), ("seq_lens", seq_lens, B)):
-        if not (t.device == dev and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.numel() == n):
-            raise ValueError(f"{name}: contiguous int32 tensor of {n} values on the pages' device")
-    if not (block_table.device == dev and block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
-            and block_table.shape[0] == B):
-        raise ValueError("block_table: contiguous int32 tensor [B, max_pages] on the pages' device")
-    return spd_ragged(cu_new.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), B, block_table.shape[1], n_tokens)
+def _int32(name: str, t: torch.Tensor, dev: int, shape) -> int:
+    if t.dtype is not torch.int32 or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 tensor {list(shape)} on the pages' device")
+    return t.data_ptr()
 
 
-def _rows(name: str, t: torch.Tensor, heads: int, k_pages: torch.Tensor) -> int:
+def _ragged(dev: int, cu_new, seq_lens, block_table, n_tokens: int) -> spd_ragged:
+    if block_table.dim() != 2:
+        raise ValueError("block_table: [B, max_pages]")
+    B, width = block_table.shape
+    return spd_ragged(_int32("cu_new", cu_new, dev, (B + 1,)), _int32("seq_lens", seq_lens, dev, (B,)),
+                      _int32("block_table", block_table, dev, (B, width)), B, width, n_tokens)
+
+
+def _rows(name: str, t: torch.Tensor, dev: int, heads: int, d: int) -> int:
     """Checks a [n_tokens, heads, head_dim] tensor whose heads lie side by side; returns the elements between its rows."""
-    d = k_pages.shape[3]
-    if not (t.device == k_pages.device and t.dtype in _DTYPES and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d
-            and (t.stride(2) == 1 or d == 1) and (heads == 1 or t.stride(1) == d)):
+    n, h, e = t.shape
+    row, head, one = t.stride()
+    if t.get_device() != dev or t.dtype not in _DTYPES or h != heads or e != d or one != 1 or (head != d and heads > 1):
         raise ValueError(f"{name}: float32 or bfloat16 [n_tokens, {heads}, {d}] on the pages' device, heads side by side in a row")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return row if n > 1 else heads * d
 
 
-def _flag(err: torch.Tensor, k_pages: torch.Tensor) -> int:
-    if not (err.device == k_pages.device and err.dtype == torch.int32 and err.numel() >= 1):
+def _flag(err: torch.Tensor, dev: int) -> int:
+    if err.get_device() != dev or err.dtype is not torch.int32 or err.numel() < 1:
         raise ValueError("err: int32 tensor on the pages' device")
     return err.data_ptr()
+
+
+try:
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+except AttributeError:  # a torch built without CUDA
+    def _raw_stream(dev: int) -> int:
+        return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _call_on(dev: int, fn, *args) -> int:
+    """fn(*args, stream) with `dev` current, on its current stream."""
+    if torch.cuda.current_device() == dev:
+        return fn(*args, _raw_stream(dev))
+    with torch.cuda.device(dev):
+        return fn(*args, _raw_stream(dev))
 
 
 def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
@@ -260,12 +281,14 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     back here."""
     lib = load_library()
     c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
-    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
-        raise ValueError("k and v: same dtype and number of rows")
-    r = _ragged(k_pages, cu_new, seq_lens, block_table, k.shape[0])
-    ks, vs = _rows("k", k, c.n_kv_heads, k_pages), _rows("v", v, c.n_kv_heads, k_pages)
-    with torch.cuda.device(k_pages.device):
-        _check("spd_kv_write", lib.spd_kv_write(c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, k_pages), _stream_ptr()))
+    dev = k_pages.get_device()
+    if k.dtype is not v.dtype or k.shape != v.shape:
+        raise ValueError("k and v: same dtype and shape")
+    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
+    r = _ragged(dev, cu_new, seq_lens, block_table, k.shape[0])
+    rc = _call_on(dev, lib.spd_kv_write, c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, dev))
+    if rc:
+        _check("spd_kv_write", rc)
 
 
 def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *,
@@ -276,18 +299,21 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, star
     Rows outside every sequence are left as they are (undefined where the tensors are made here)."""
     lib = load_library()
     c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    dev = k_pages.get_device()
     if out is None:
         if n_tokens is None or dtype not in _DTYPES:
             raise ValueError("n_tokens and a dtype of float32 or bfloat16, or out")
-        k, v = (torch.empty((n_tokens, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_pages.device) for _ in range(2))
+        k = torch.empty((n_tokens, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_pages.device)
+        v = torch.empty_like(k)
     else:
         k, v = out
-        if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
-            raise ValueError("out: two tensors of one dtype and number of rows")
-    r = _ragged(k_pages, cu, starts, block_table, k.shape[0])
-    ks, vs = _rows("k", k, c.n_kv_heads, k_pages), _rows("v", v, c.n_kv_heads, k_pages)
-    with torch.cuda.device(k_pages.device):
-        _check("spd_kv_read", lib.spd_kv_read(c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, k_pages), _stream_ptr()))
+        if k.dtype is not v.dtype or k.shape != v.shape:
+            raise ValueError("out: two tensors of one dtype and shape")
+    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
+    r = _ragged(dev, cu, starts, block_table, k.shape[0])
+    rc = _call_on(dev, lib.spd_kv_read, c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, dev))
+    if rc:
+        _check("spd_kv_read", rc)
     return k, v
 
 
@@ -300,32 +326,38 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
 
     q: [n_tokens, n_q_heads, head_dim], rows cu_new[b] .. cu_new[b+1]-1 at positions seq_lens[b] on, whose K/V rows are in
     the cache already.  max_new, max_context: host bounds of a sequence's new tokens and of its whole length.  scale:
-    1/sqrt(head_dim) by default.  workspace: uint8 tensor to use instead of allocating one (calls that may overlap need
-    one each).  err collects error bits as in kv_write."""
+    1/sqrt(head_dim) by default.  workspace: uint8 tensor to use instead of allocating one where the call needs one (calls
+    that may overlap need one each).  err collects error bits as in kv_write."""
     lib = load_library()
     c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    dev = k_pages.get_device()
     n, nq, d = q.shape
-    r = _ragged(k_pages, cu_new, seq_lens, block_table, n)
-    qs = _rows("q", q, nq, k_pages)
+    qs = _rows("q", q, dev, nq, c.head_dim)
     if out is None:
-        out = torch.empty((n, nq, d), dtype=q.dtype, device=q.device)
-    elif out.dtype != q.dtype or out.shape != q.shape:
-        raise ValueError("out: shape and dtype of q")
-    os_ = _rows("out", out, nq, k_pages)
-    need = ctypes.c_size_t(0)
-    _check("spd_paged_attention_workspace_bytes", lib.spd_paged_attention_workspace_bytes(
-        c, r.B, n, _DTYPES[q.dtype], nq, max_new, max_context, window, sinks, need))
-    ws_ptr = 0
-    if need.value:
-        if workspace is None:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        elif not (workspace.device == q.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()):
+        out = q.new_empty((n, nq, d))
+        os_ = nq * d
+    else:
+        if out.dtype is not q.dtype or out.shape != q.shape:
+            raise ValueError("out: shape and dtype of q")
+        os_ = _rows("out", out, dev, nq, d)
+    r = _ragged(dev, cu_new, seq_lens, block_table, n)
+    dtype = _DTYPES[q.dtype]
+    ws_ptr = ws_bytes = 0
+    if workspace is not None:
+        if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
             raise ValueError("workspace: contiguous uint8 tensor on the pages' device")
-        ws_ptr = workspace.data_ptr()
-    with torch.cuda.device(k_pages.device):
-        _check("spd_paged_attention", lib.spd_paged_attention(
-            c, r, q.data_ptr(), qs, out.data_ptr(), os_, _DTYPES[q.dtype], nq, max_new, max_context,
-            d ** -0.5 if scale is None else scale, window, sinks, ws_ptr, workspace.numel() if ws_ptr else 0, _flag(err, k_pages), _stream_ptr()))
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    args = (c, r, q.data_ptr(), qs, out.data_ptr(), os_, dtype, nq, max_new, max_context, d ** -0.5 if scale is None else scale, window, sinks)
+    flag = _flag(err, dev)
+    rc = _call_on(dev, lib.spd_paged_attention, *args, ws_ptr, ws_bytes, flag)
+    if rc == SPD_EWORKSPACE and workspace is None:  # nothing ran: this call wants one
+        need = ctypes.c_size_t(0)
+        _check("spd_paged_attention_workspace_bytes", lib.spd_paged_attention_workspace_bytes(
+            c, r.B, n, dtype, nq, max_new, max_context, window, sinks, need))
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        rc = _call_on(dev, lib.spd_paged_attention, *args, workspace.data_ptr(), need.value, flag)
+    if rc:
+        _check("spd_paged_attention", rc)
     return out
 
 

@@ -35,7 +35,8 @@ struct PagedAttnArgs {
     int window, sinks;            // window 0: everything before the query
     float scale_log2;             // softmax scale times log2(e)
     int splits;                   // ranges the keys of a row tile are cut into
-    float *part_o, *part_ml;      // splits > 1: fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
+    int stages;                   // paged_attention_rows.cu: set by its launcher
+    float *part_o, *part_ml;      // ranges that no cluster adds up (else null): fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
     int *err;
 };
 
@@ -56,8 +57,15 @@ template <> __device__ __forceinline__ float kv_value<KV_E4M3>(uint8_t c)
 template <> __device__ __forceinline__ float kv_value<KV_INT8>(int8_t c) { return (float)c; }
 
 // Two 8-bit codes of a word -> bf16x2 of the values they stand for, exactly: bytes 0 and 2 (even), bytes 1 and 3 (odd).
-template <int FMT> __device__ __forceinline__ uint32_t even2(uint32_t w);
-template <int FMT> __device__ __forceinline__ uint32_t odd2(uint32_t w);
+// c128: widen_const(), kept in a register by the caller.
+template <int FMT> __device__ __forceinline__ uint32_t even2(uint32_t w, uint32_t c128);
+template <int FMT> __device__ __forceinline__ uint32_t odd2(uint32_t w, uint32_t c128);
+__device__ __forceinline__ uint32_t widen_const() // bf16x2 of 128, which the compiler does not turn back into a literal
+{
+    uint32_t c;
+    asm volatile("mov.b32 %0, 0x43004300;" : "=r"(c));
+    return c;
+}
 __device__ __forceinline__ uint32_t e4m3_fix(uint32_t x) // sign | 4 exponent bits | 3 mantissa bits in bf16's places: times 2^120
 {
     const __nv_bfloat162 v = __hmul2(*(const __nv_bfloat162 *)&x, __nv_bfloat162(__ushort_as_bfloat16(0x7b80), __ushort_as_bfloat16(0x7b80)));
@@ -70,18 +78,16 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
-__device__ __forceinline__ uint32_t int8_fix(uint32_t w) // codes in bits 0-7 and 16-23
+__device__ __forceinline__ uint32_t int8_fix(uint32_t w, uint32_t c128) // codes in bits 0-7 and 16-23
 {
-    uint32_t c128; // bf16x2 of 128, kept in a register
-    asm("mov.b32 %0, 0x43004300;" : "=r"(c128));
     const uint32_t x = and_or(w, 0x007f007fu, c128), y = and_or(w, 0x00800080u, c128);
     const __nv_bfloat162 v = __hsub2(*(const __nv_bfloat162 *)&x, *(const __nv_bfloat162 *)&y);
     return *(const uint32_t *)&v;
 }
-template <> __device__ __forceinline__ uint32_t even2<KV_E4M3>(uint32_t w) { return e4m3_fix(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u)); }
-template <> __device__ __forceinline__ uint32_t odd2<KV_E4M3>(uint32_t w) { return e4m3_fix(((w >> 4) & 0x07f007f0u) | (w & 0x80008000u)); }
-template <> __device__ __forceinline__ uint32_t even2<KV_INT8>(uint32_t w) { return int8_fix(w); }
-template <> __device__ __forceinline__ uint32_t odd2<KV_INT8>(uint32_t w) { return int8_fix(w >> 8); }
+template <> __device__ __forceinline__ uint32_t even2<KV_E4M3>(uint32_t w, uint32_t) { return e4m3_fix(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u)); }
+template <> __device__ __forceinline__ uint32_t odd2<KV_E4M3>(uint32_t w, uint32_t) { return e4m3_fix(((w >> 4) & 0x07f007f0u) | (w & 0x80008000u)); }
+template <> __device__ __forceinline__ uint32_t even2<KV_INT8>(uint32_t w, uint32_t c128) { return int8_fix(w, c128); }
+template <> __device__ __forceinline__ uint32_t odd2<KV_INT8>(uint32_t w, uint32_t c128) { return int8_fix(w >> 8, c128); }
 
 // What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
 __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
@@ -98,18 +104,16 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
     return true;
 }
 
-// A kernel's dynamic shared-memory limit (and leave to run in clusters of more than 8 blocks), raised once per device.
+// A kernel's dynamic shared-memory limit, raised once per device.
 struct SmemLimit {
-    int done[64] = {};
-    cudaError_t raise(const void *kernel, int bytes, bool wide_cluster = false)
+    bool done[64] = {};
+    cudaError_t raise(const void *kernel, int bytes)
     {
         int dev = 0;
-        const int want = wide_cluster ? 3 : 1;
         cudaError_t e = cudaGetDevice(&dev);
-        if (e != cudaSuccess || dev < 0 || dev >= 64 || (done[dev] & want) == want) return e;
+        if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e == cudaSuccess && wide_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e == cudaSuccess) done[dev] |= want;
+        if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
         return e;
     }
 };
@@ -122,7 +126,7 @@ cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, vo
 // q, out and (for unquantised caches) the pages in one type: bf16 or float32
 cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 // Key ranges that one thread-block cluster adds up in shared memory; more go through the workspace.
-constexpr int PAGED_MAX_CLUSTER = 16;
+constexpr int PAGED_MAX_CLUSTER = 8;
 // bf16 queries, head_dim 64 or 128, at most 16 rows (new tokens x query heads per KV head) per sequence and KV head
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
 // Adds up the key ranges of a split launch.

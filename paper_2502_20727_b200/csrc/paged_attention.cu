@@ -104,13 +104,17 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
     if (rows <= 16) {
         p.kernel = ATTN_ROWS;
-        // three thread blocks per SM are resident; twice as many ranges as fill them, since sequences are of unequal length;
-        // ranges of at least 8 blocks of 16 keys.  A cluster's worth of ranges unless they would exceed 2048 keys each.
-        const long pairs = (long)(B > 0 ? B : 1) * nkv, want = (6L * sm_count() + pairs - 1) / pairs, most = (keys + 127) / 128;
-        p.splits = (int)(want < most ? want : most);
-        if (p.splits > PAGED_MAX_CLUSTER && keys <= 2048L * PAGED_MAX_CLUSTER) p.splits = PAGED_MAX_CLUSTER;
-        if (p.splits > 64) p.splits = 64;
-        if (p.splits < 1) p.splits = 1;
+        // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
+        // the resident ones; at least one per 2560 keys, which evens out sequences of unequal length; none under 256 keys.
+        // More than a cluster's worth cost a second kernel (about 2 us) and pay from 512 keys each.  Measured, 8 KV heads of
+        // 8 query heads, bf16, us by ranges: 1 x 4096 keys 8: 11.2, 20: 12.8; 1 x 16384 8: 24.9, 20: 22.4; 4 x 4096 2: 24.7,
+        // 4: 18.9, 8: 19.1; 16 x 4096 2: 49, 8: 61.
+        const long pairs = (long)(B > 0 ? B : 1) * nkv, sms = sm_count(), resident = fmt != KV_BF16 && rows <= 8 ? 4 : 3;
+        long s = sms / pairs >= 2 ? sms / pairs : resident * sms / pairs;
+        if (s > (keys + 255) / 256) s = (keys + 255) / 256;
+        if (s < (keys + 2559) / 2560) s = (keys + 2559) / 2560;
+        if (s > PAGED_MAX_CLUSTER && keys < 512 * s) s = PAGED_MAX_CLUSTER;
+        p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     }
     if (p.splits > PAGED_MAX_CLUSTER) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;

@@ -8,7 +8,7 @@
 //   - every warp works on its own 16-key blocks (j, j + 4, ...) with a private ring of tiles, one TMA box each for K and V
 //     (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled layout): no block-wide barrier between
 //     the first load and the merge;
-//   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 16 ranges
+//   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 8 ranges
 //     are one thread-block cluster that adds up its partial rows through shared memory; more go through the workspace and
 //     paged_merge_kernel;
 //   - the weights leave the first product with keys as rows and enter the second with keys as its k index: one 8 x 8
@@ -33,19 +33,22 @@ namespace spd {
 
 namespace {
 
-constexpr int RW = 4, R_THREADS = 32 * RW, BK16 = 16;
+constexpr int BK16 = 16;
 
-template <int FMT, int D> struct RowsCfg {
+// RW warps per thread block; `stages` tiles per warp (TMA: as many as the launch has shared memory for)
+template <int FMT, int D, int RW> struct RowsCfg {
     static constexpr bool Q8 = FMT != KV_BF16;
     static constexpr int RB = D * (Q8 ? 1 : 2);            // bytes of a cached row
     static constexpr int TR = RB > 128 ? 128 : RB;         // bytes of a tile row; 256-byte rows are two tiles
     static constexpr int TILE = BK16 * RB;                 // K or V of one block
-    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : 6;
-    static constexpr int OFF_SC = RW * STAGES * 2 * TILE;  // 16 K scales, 16 V scales per stage
-    static constexpr int OFF_BAR = OFF_SC + (Q8 ? RW * STAGES * 128 : 0);
-    static constexpr int OFF_PML = OFF_BAR + RW * STAGES * 8 + 16; // abort flag before it; merged [16][2] after
-    static constexpr int SMEM = OFF_PML + 128 + 1024;      // + alignment slack
-    static_assert(RW * 16 * (D + 4) * 4 <= OFF_SC, "merge area fits the rings");
+    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : 6; // with the most thread blocks resident
+    static constexpr int MAX_STAGES = 8;
+    static constexpr int MERGE = RW * 16 * (D + 4) * 4;    // the warps' partial rows, over the tiles
+    // after the tiles: 16 K scales, 16 V scales per stage; a barrier per stage; abort flag; merged [16][2]
+    static constexpr int off_sc(int st) { return RW * st * 2 * TILE > MERGE ? RW * st * 2 * TILE : (MERGE + 1023) / 1024 * 1024; }
+    static constexpr int off_bar(int st) { return off_sc(st) + (Q8 ? RW * st * 128 : 0); }
+    static constexpr int off_pml(int st) { return off_bar(st) + RW * st * 8 + 16; }
+    static constexpr int smem(int st) { return off_pml(st) + 128 + 1024; } // + alignment slack
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
@@ -137,19 +140,20 @@ __device__ __forceinline__ bool sees(int t, int pos, int window, int sinks) { re
 __device__ __forceinline__ int key_of(int c) { return c & 1 ? (c & 6) ^ 5 : c; }
 
 // NR: groups of 8 query rows
-template <int FMT, int D, int NR, bool TMA>
-__global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+template <int FMT, int D, int NR, int RW, bool TMA>
+__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF16 ? 4 : 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                             const __grid_constant__ PagedAttnArgs a)
 {
-    using C = RowsCfg<FMT, D>;
+    using C = RowsCfg<FMT, D, RW>;
     constexpr bool Q8 = C::Q8;
-    constexpr int MT = D / 16, KS = D / 16, ST = C::STAGES;
+    constexpr int MT = D / 16, KS = D / 16, R_THREADS = 32 * RW;
+    const int ST = TMA ? a.stages : C::STAGES;
     extern __shared__ uint8_t rows_raw[];
     uint8_t *gen = rows_raw + ((1024u - (tc::smem_u32(rows_raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(gen);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::OFF_SC + warp * ST * 128, bars = base + C::OFF_BAR + warp * ST * 8;
-    volatile int *abort_flag = (volatile int *)(gen + C::OFF_BAR + RW * ST * 8);
+    const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::off_sc(ST) + warp * ST * 128, bars = base + C::off_bar(ST) + warp * ST * 8;
+    volatile int *abort_flag = (volatile int *)(gen + C::off_bar(ST) + RW * ST * 8);
     pdl_launch_dependents();
     if (TMA) {
         if (lane == 0) {
@@ -232,7 +236,6 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
 
     const int n_mine = (j_end - j_begin - warp + RW - 1) / RW; // blocks j_begin + warp, + RW, ...
     auto mine = [&](int i) { return j_begin + warp + i * RW; };
-#pragma unroll
     for (int s = 0; s < ST; ++s) {
         if (s < n_mine) load_block(s, lookup_block(mine(s)));
         if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
     const int vc = lane & 7;
     const uint32_t lane_v0 = Q8 ? (D == 128 ? at(key_of(2 * t4), g) : at(key_of(2 * t4), g >> 1) + (g & 1) * 8) : at(key_of(vc) + (lane & 8), lane >> 4);
     const uint32_t lane_v1 = Q8 ? (D == 128 ? at(key_of(2 * t4 + 1), g) : at(key_of(2 * t4 + 1), g >> 1) + (g & 1) * 8) : 0u;
-    const uint32_t lane_s = key_of(g) * 4;
+    const uint32_t lane_s = key_of(g) * 4, c128 = widen_const();
 
     float o[NR][MT][4];
 #pragma unroll
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
         } else {
-            asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
             __syncwarp();
         }
         const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
@@ -462,8 +465,8 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
                 // bytes (k0.0, k0.1, k1.0, k1.1): even bytes = dim 0 of keys (k0, k1), odd bytes = dim 1
                 const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5410), x1 = __byte_perm(v[2][w], v[3][w], 0x5410);
                 const uint32_t y0 = __byte_perm(v[0][w], v[1][w], 0x7632), y1 = __byte_perm(v[2][w], v[3][w], 0x7632);
-                const uint32_t a0 = even2<FMT>(x0), a1 = odd2<FMT>(x0), a2 = even2<FMT>(x1), a3 = odd2<FMT>(x1);
-                const uint32_t b0 = even2<FMT>(y0), b1 = odd2<FMT>(y0), b2 = even2<FMT>(y1), b3 = odd2<FMT>(y1);
+                const uint32_t a0 = even2<FMT>(x0, c128), a1 = odd2<FMT>(x0, c128), a2 = even2<FMT>(x1, c128), a3 = odd2<FMT>(x1, c128);
+                const uint32_t b0 = even2<FMT>(y0, c128), b1 = odd2<FMT>(y0, c128), b2 = even2<FMT>(y1, c128), b3 = odd2<FMT>(y1, c128);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     mma16816<false>(o[n][2 * w], a0, a1, a2, a3, pf[n][0], pf[n][1]);
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
     }
     const int any_dirty = __syncthreads_or(dirty);
     float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
-    float *pml = (float *)(gen + C::OFF_PML);
+    float *pml = (float *)(gen + C::off_pml(ST));
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
@@ -518,7 +521,7 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
         }
     }
     __syncthreads();
-    const bool clustered = a.splits > 1 && a.splits <= PAGED_MAX_CLUSTER;
+    const bool clustered = a.splits > 1 && !a.part_o;
     const long plane = (long)a.rb.n_tokens * a.nq;
     auto store = [&](int r, int c, float x, float y, float den) {
         const int i = r / a.group, head = kvh * a.group + r % a.group;
@@ -567,7 +570,7 @@ __global__ void __launch_bounds__(R_THREADS, NR == 1 && FMT != KV_BF16 ? 4 : 3) 
     }
     if (clustered) {
         tc::cluster_sync();
-        const uint32_t mo_addr = base, pml_addr = base + C::OFF_PML;
+        const uint32_t mo_addr = base, pml_addr = base + C::off_pml(ST);
         auto peer2 = [](uint32_t addr, int rank) {
             float2 v;
             asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(tc::mapa_shared(addr, rank)) : "memory");
@@ -610,20 +613,41 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     if (before < 1 || before > a.rb.B) return;
     int row0, n_new, len;
     if (!batch_row(a.rb, before - 1, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
-    float m = -INFINITY;
-    for (int s = lane; s < a.splits; s += 32) m = fmaxf(m, __ldcg(a.part_ml + ((long)s * plane + w) * 2));
-    m = warp_max(m);
-    float o[VEC], den = 0.f;
+    // the ranges' maxima and sums in the lanes (two each), then their rows eight at a time
+    float mr[2], wr[2], den = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int s = lane + 32 * k;
+        const float2 v = s < a.splits ? __ldcg((const float2 *)(a.part_ml + ((long)s * plane + w) * 2)) : make_float2(-INFINITY, 0.f);
+        mr[k] = v.x; wr[k] = v.y;
+    }
+    const float m = warp_max(fmaxf(mr[0], mr[1]));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float f = mr[k] == -INFINITY ? 0.f : ex2(mr[k] - m); // an empty range has no rows
+        den = fmaf(wr[k], f, den);
+        wr[k] = f;
+    }
+    den = warp_sum(den);
+    float o[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) o[e] = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const long at = (long)s * plane + w;
-        const float ms = __ldcg(a.part_ml + at * 2);
-        if (ms == -INFINITY) continue; // an empty range: nothing was written
-        const float f = ex2(ms - m);
-        den = fmaf(__ldcg(a.part_ml + at * 2 + 1), f, den);
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {
+        float v[8][VEC], f[8];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] = fmaf(__ldcg(a.part_o + at * D + lane * VEC + e), f, o[e]);
+        for (int k = 0; k < 8; ++k) {
+            const int s = s0 + k;
+            f[k] = __shfl_sync(0xffffffffu, s < 32 ? wr[0] : wr[1], s & 31);
+            const bool empty = __shfl_sync(0xffffffffu, s < 32 ? mr[0] : mr[1], s & 31) == -INFINITY || s >= a.splits;
+            const float *p = a.part_o + ((long)(empty ? 0 : s) * plane + w) * D + lane * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[k][e] = empty ? 0.f : __ldcg(p + e);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o[e] = fmaf(v[k][e], f[k], o[e]);
+        }
     }
     const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
     T *dst = (T *)a.out + (long)t * a.o_stride + (long)head * D + lane * VEC;
@@ -631,30 +655,42 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     for (int e = 0; e < VEC; ++e) dst[e] = from_f<T>(o[e] * inv);
 }
 
-template <int FMT, int D, int NR, bool TMA> cudaError_t launch_rows(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
+template <int FMT, int D, int NR, int RW, bool TMA>
+cudaError_t launch_rows(PagedAttnArgs a, const TcMap &km, const TcMap &vm, cudaStream_t st)
 {
-    using C = RowsCfg<FMT, D>;
+    using C = RowsCfg<FMT, D, RW>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, NR, TMA>, C::SMEM, a.splits > 8);
+    // deep rings where few thread blocks share an SM
+    a.stages = C::STAGES;
+    const long per_sm = ((long)a.kv.nkv * a.rb.B * a.splits + sm_count() - 1) / sm_count();
+    while (TMA && a.stages < C::MAX_STAGES && C::smem(a.stages + 1) * per_sm <= 220 * 1024) ++a.stages;
+    cudaError_t e = limit.raise((const void *)paged_attention_rows_kernel<FMT, D, NR, RW, TMA>,
+                                C::smem(C::MAX_STAGES) < 227 * 1024 ? C::smem(C::MAX_STAGES) : 227 * 1024);
     if (e != cudaSuccess) return e;
-    return launch_kernel_z(paged_attention_rows_kernel<FMT, D, NR, TMA>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(R_THREADS), C::SMEM, st,
-                           a.splits <= PAGED_MAX_CLUSTER ? a.splits : 1, km, vm, a);
+    return launch_kernel_z(paged_attention_rows_kernel<FMT, D, NR, RW, TMA>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(32 * RW), C::smem(a.stages), st,
+                           a.part_o ? 1 : a.splits, km, vm, a);
 }
-template <int FMT, int D> cudaError_t rows_by_copy(const PagedAttnArgs &a, cudaStream_t st)
+template <int FMT, int D, int NR> cudaError_t rows_by_copy(const PagedAttnArgs &a, cudaStream_t st)
 {
     // 16-key blocks as TMA boxes: they lie in one page, row numbers fit a coordinate, scales start on 16 bytes
     TcMap km{}, vm{};
     const long rows = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
     const int es = FMT == KV_BF16 ? 2 : 1;
     if (a.kv.page % BK16 == 0 && rows <= 0x7fffffffL && !(((uintptr_t)a.kv.ks | (uintptr_t)a.kv.vs) & 15) &&
-        make_cache_map(&km, a.kv.k, rows, D, es) == 0 && make_cache_map(&vm, a.kv.v, rows, D, es) == 0)
-        return a.max_new * a.group <= 8 ? launch_rows<FMT, D, 1, true>(a, km, vm, st) : launch_rows<FMT, D, 2, true>(a, km, vm, st);
-    return launch_rows<FMT, D, 2, false>(a, km, vm, st);
+        make_cache_map(&km, a.kv.k, rows, D, es) == 0 && make_cache_map(&vm, a.kv.v, rows, D, es) == 0) {
+        if ((long)a.kv.nkv * a.rb.B * a.splits <= sm_count()) return launch_rows<FMT, D, NR, 8, true>(a, km, vm, st);
+        return launch_rows<FMT, D, NR, 4, true>(a, km, vm, st);
+    }
+    return launch_rows<FMT, D, 2, 4, false>(a, km, vm, st);
+}
+template <int FMT, int D> cudaError_t rows_by_count(const PagedAttnArgs &a, cudaStream_t st)
+{
+    return a.max_new * a.group <= 8 ? rows_by_copy<FMT, D, 1>(a, st) : rows_by_copy<FMT, D, 2>(a, st);
 }
 template <int FMT> cudaError_t rows_by_dim(const PagedAttnArgs &a, cudaStream_t st)
 {
-    if (a.kv.d == 128) return rows_by_copy<FMT, 128>(a, st);
-    if (a.kv.d == 64) return rows_by_copy<FMT, 64>(a, st);
+    if (a.kv.d == 128) return rows_by_count<FMT, 128>(a, st);
+    if (a.kv.d == 64) return rows_by_count<FMT, 64>(a, st);
     return cudaErrorInvalidValue;
 }
 
