@@ -105,16 +105,20 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     if (rows <= 16) {
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
-        // the resident ones; at least one per 2560 keys, which evens out sequences of unequal length; none under 256 keys.
+        // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
         // More than a cluster's worth cost a second kernel (about 2 us) and pay from 512 keys each.  Measured, 8 KV heads of
         // 8 query heads, bf16, us by ranges: 1 x 4096 keys 8: 11.2, 20: 12.8; 1 x 16384 8: 24.9, 20: 22.4; 4 x 4096 2: 24.7,
         // 4: 18.9, 8: 19.1; 16 x 4096 2: 49, 8: 61.
         const long pairs = (long)(B > 0 ? B : 1) * nkv, sms = sm_count(), resident = fmt != KV_BF16 && rows <= 8 ? 4 : 3;
         long s = sms / pairs >= 2 ? sms / pairs : resident * sms / pairs;
         if (s > (keys + 255) / 256) s = (keys + 255) / 256;
-        if (s < (keys + 2559) / 2560) s = (keys + 2559) / 2560;
-        if (s > PAGED_MAX_CLUSTER && keys < 512 * s) s = PAGED_MAX_CLUSTER;
-        p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+        if (s < (keys + 2047) / 2048) s = (keys + 2047) / 2048;
+        if (s > PAGED_MAX_CLUSTER) {
+            if (s > keys / 512) s = keys / 512;
+            if (s > 64) s = 64;
+            if (s < 12) s = PAGED_MAX_CLUSTER;
+        }
+        p.splits = (int)(s < 1 ? 1 : s);
     }
     if (p.splits > PAGED_MAX_CLUSTER) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
