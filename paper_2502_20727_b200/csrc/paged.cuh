@@ -129,6 +129,8 @@ cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cuda
 constexpr int PAGED_MAX_CLUSTER = 8;
 // bf16 queries, head_dim 64 or 128, at most 16 rows (new tokens x query heads per KV head) per sequence and KV head
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
+// bf16 queries, head_dim 64 or 128, any number of rows
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st);
 // Adds up the key ranges of a split launch.
 cudaError_t launch_paged_merge(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 

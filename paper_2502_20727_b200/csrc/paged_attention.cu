@@ -90,7 +90,7 @@ cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cuda
 
 namespace {
 
-enum AttnKernel { ATTN_SIMT, ATTN_ROWS };
+enum AttnKernel { ATTN_SIMT, ATTN_ROWS, ATTN_TC };
 struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; };
 
 // Which kernel serves a call, and into how many ranges the keys of its row tiles are cut.
@@ -120,7 +120,15 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         }
         p.splits = (int)(s < 1 ? 1 : s);
     }
-    if (p.splits > PAGED_MAX_CLUSTER) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
+    else {
+        // one thread block per SM: ranges where the row tiles leave SMs idle, of at least four tiles of 128 keys
+        p.kernel = ATTN_TC;
+        const long blocks = (rows + (rows > 128 ? 255 : 127)) / (rows > 128 ? 256 : 128) * nkv * (B > 0 ? B : 1);
+        long s = sm_count() / blocks;
+        if (s > (keys + 511) / 512) s = (keys + 511) / 512;
+        p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    }
+    if (p.kernel == ATTN_TC ? p.splits > 1 : p.splits > PAGED_MAX_CLUSTER) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
 }
 
@@ -166,6 +174,7 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     switch (p.kernel) {
     case ATTN_SIMT: e = launch_paged_attention_simt(a, dtype, st); break;
     case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
+    case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
     }
     if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, dtype, st);
     if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }

@@ -1,0 +1,663 @@
+// Paged attention for many query rows (bf16, head_dim 64 or 128) on the tcgen05 tensor cores: chunks of prompts on a cached
+// context, drafts of many tokens, grouped-query batches.
+//
+// The rows of a (sequence, KV head) are packed: row r = new token r / group, query head r % group of the KV head, so that the
+// query heads of a group share every K/V tile.  A thread block serves two 128-row tiles A and B (PAIR), which take turns on the
+// tensor cores: while one tile's softmax runs, the other's products do.  Where a (sequence, KV head) has at most 128 rows, A and
+// B are the same rows on alternate key tiles (each with a maximum, a sum and an accumulator of its own, added up at the end), so
+// that the products of one key tile run under the softmax of the other there too.
+// Per tile of 128 keys and 128 rows:
+//   S = Q K^T      tcgen05.mma, Q and K as K-major 128B-swizzled tiles, accumulator in tensor memory
+//   P = softmax    thread = row: a pass over the row's 128 scores in tensor memory for the maximum, a second one for the
+//                  weights, which go back to tensor memory as bf16 over the scores already read
+//   O += P V       tcgen05.mma with P read from tensor memory and V as the MN-major operand ([key][dim] rows as they are
+//                  stored); O stays in tensor memory and is rescaled there only when the row maximum has grown by more than 2^8
+// Tensor memory (512 columns): S/P of A and B at 0 and 128, O of A and B at 256 and 384.
+// Warps: 0-3 softmax of A, 4-7 of B, 8-11 load, 12 issues the MMAs.  K and V tiles have rings of two; a K tile is free once S is
+// computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims; 8-bit pages (and bf16 pages
+// of other sizes) by the four load warps, which widen the codes to bf16 on the way into shared memory.  The pairs that widening
+// a 32-bit word gives are (0, 2) and (1, 3) of its four codes: the head dims of Q, K and V all sit in that order, and the output
+// is put right when it is stored.  Row scales multiply the scores (K) and the weights (V) in fp32.
+// A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
+// shared memory before the product, and rows that do see them get them back at the end.
+// Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
+#include "gemm_tc.cuh"
+#include "paged.cuh"
+#include "tc_ptx.cuh"
+
+namespace spd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int TQ = 128, TK = 128, T_THREADS = 13 * 32, HALF = 128 * 128; // bytes of [128 rows][64 bf16]
+constexpr uint32_t T_COLS = 512;
+enum { BAR_LOAD = 3, BAR_SOFT = 4 };
+
+template <int D> struct TcCfg {
+    static constexpr int TILE = 128 * D * 2;
+    static constexpr int OFF_Q = 0, OFF_K = 2 * TILE, OFF_V = OFF_K + 2 * TILE;
+    static constexpr int OFF_SC = OFF_V + 2 * TILE;            // [8][256] K and V scales of a tile
+    static constexpr int OFF_ROW = OFF_SC + 8 * 1024;          // [2][128] cached rows of a tile's keys
+    static constexpr int OFF_BAR = OFF_ROW + 2 * 1024;
+    static constexpr int OFF_ML = OFF_BAR + 512;               // [128][2] maximum and sum of B
+    static constexpr int SMEM = OFF_ML + 1024 + 1024;          // + alignment slack
+};
+
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t lbo, uint32_t sbo)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3FFFF) >> 4);
+    d |= (uint64_t)(lbo >> 4) << 16;
+    d |= (uint64_t)(sbo >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// D[tmem] (+)= A[tmem] B[shared]
+__device__ __forceinline__ void umma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t ta, float (&v)[32])
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(ta) : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t ta, const uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(ta), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+                   "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+template <int ID, int N> __device__ __forceinline__ void named_bar() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *(const uint32_t *)&v;
+}
+// Waits a bounded time whatever the abort flag says: copies and products in flight before the memory is given up.
+__device__ __forceinline__ void settle(uint32_t bar, uint32_t parity)
+{
+    const long long t_end = clock64() + WAIT_LIMIT_CYCLES;
+    while (!mbar_try_wait(bar, parity) && clock64() < t_end) {}
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
+{
+    const int n = valid ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// byte offset of 16-byte chunk c (8 dims) of row r in a K-major tile of 64-dim halves
+__device__ __forceinline__ uint32_t tile_at(int r, int c) { return (uint32_t)((c >> 3) * HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+
+__device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities out; true: there were some
+{
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; bad = true; }
+        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; bad = true; }
+    }
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+    return bad;
+}
+
+template <int FMT, int D, bool PAIR, bool TMA>
+__global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+                                                                          const __grid_constant__ PagedAttnArgs a)
+{
+    using C = TcCfg<D>;
+    constexpr bool Q8 = FMT != KV_BF16;
+    extern __shared__ uint8_t tc_raw[];
+    uint8_t *gen = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(gen), bars = base + C::OFF_BAR;
+    const uint32_t q_full = bars;
+    auto k_full = [&](int s) { return bars + 8u * (1 + s); };
+    auto k_empty = [&](int s) { return bars + 8u * (3 + s); };
+    auto v_full = [&](int s) { return bars + 8u * (5 + s); };
+    auto v_empty = [&](int s) { return bars + 8u * (7 + s); };
+    auto v_clean = [&](int s) { return bars + 8u * (9 + s); };
+    auto s_full = [&](int u) { return bars + 8u * (11 + u); };
+    auto p_ready = [&](int u) { return bars + 8u * (13 + u); };
+    auto o_done = [&](int u) { return bars + 8u * (15 + u); };
+    auto sc_full = [&](int s) { return bars + 8u * (17 + s); };
+    const uint32_t drain = bars + 8u * 25;
+    uint32_t *tmem_slot = (uint32_t *)(gen + C::OFF_BAR + 8 * 32);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    volatile int *dirty = (volatile int *)(tmem_slot + 2);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
+    int row0, n_new, len;
+    if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
+    constexpr int ROWS = PAIR ? 2 * TQ : TQ;
+    const int all_rows = n_new * a.group;
+    const int tile = (int)gridDim.x - 1 - (int)blockIdx.x; // the longest rows first
+    const int r0 = tile * ROWS;
+    if (r0 >= all_rows) return;
+    const int rows = min(ROWS, all_rows - r0);
+    const int pos_first = len + r0 / a.group, pos_last = len + (r0 + rows - 1) / a.group;
+    const int kv_len = pos_last + 1;
+    // tiles of 128 keys that hold a key some row sees: sinks, then the window of the first row onwards
+    const int lo_min = a.window ? max(0, pos_first - a.window + 1) : 0, first = lo_min / TK;
+    const int n_sink = min((min(a.sinks, lo_min) + TK - 1) / TK, first);
+    const int n_all = n_sink + (kv_len + TK - 1) / TK - first;
+    const int j_begin = (int)((long)n_all * split / a.splits), n_tiles = (int)((long)n_all * (split + 1) / a.splits) - j_begin;
+    auto key0 = [&](int j) { return ((j_begin + j) < n_sink ? (j_begin + j) : first + (j_begin + j) - n_sink) * TK; };
+    auto key_needed = [&](int t) { return t < kv_len && (t >= lo_min || t < a.sinks); };
+    // some row does not see some key of the tile
+    auto partial = [&](int t0) { return !(t0 + TK - 1 <= pos_first && (!a.window || t0 > pos_last - a.window || t0 + TK - 1 < a.sinks)); };
+    const int32_t *bt = a.rb.table + (long)b * a.rb.max_pages;
+
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        *dirty = 0;
+        mbar_init(q_full, 128);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(k_full(s), TMA ? 1 : 128);
+            mbar_init(v_full(s), TMA ? 1 : 128);
+            mbar_init(k_empty(s), 1);
+            mbar_init(v_empty(s), 1);
+            mbar_init(v_clean(s), 2);
+            mbar_init(s_full(s), 1);
+            mbar_init(p_ready(s), 4);
+            mbar_init(o_done(s), 1);
+        }
+        for (int s = 0; s < 8; ++s) mbar_init(sc_full(s), 128);
+        mbar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(T_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // unit u (A, B) takes tiles unit_tile(u, 0), unit_tile(u, 1), ...
+    auto unit_tile = [&](int u, int i) { return PAIR ? i : 2 * i + u; };
+    auto unit_count = [&](int u) { return PAIR ? n_tiles : (n_tiles - u + 1) / 2; };
+
+    if (warp >= 8 && warp < 12) {
+        const int tid = threadIdx.x - 256;
+        if (TMA && (warp == 8 || warp == 9) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 9 ? &v_map : &k_map) : "memory");
+        // one box = 16 keys x 64 dims; lane = (16 keys, half of the head); 16 keys that no row needs come as zeros (a row beyond the map)
+        constexpr int BOXES = 8 * (D / 64);
+        auto tma_tile = [&](int j, bool is_v) {
+            const int s = j & 1;
+            const uint32_t full = is_v ? v_full(s) : k_full(s);
+            const int t = key0(j) + (lane & 7) * 16, h = lane >> 3;
+            long row = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
+            if (t < kv_len && (t + 15 >= lo_min || t < a.sinks)) {
+                const int pi = t / a.kv.page;
+                int page = bt[pi];
+                if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); page = 0; }
+                row = ((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page);
+            }
+            bool ok = true;
+            if (j >= 2) ok = mbar_wait(is_v ? v_empty(s) : k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+            if (!__all_sync(0xffffffffu, ok)) return false;
+            if (lane == 0) mbar_expect_tx(full, C::TILE);
+            __syncwarp();
+            if (lane < BOXES)
+                tma_load_3d(base + (is_v ? C::OFF_V : C::OFF_K) + s * C::TILE + h * HALF + (lane & 7) * 2048, (const CUtensorMap *)(is_v ? &v_map : &k_map),
+                            h * 64, (int)row, 0, full);
+            return true;
+        };
+        int issued = 0; // tiles this warp has asked for (TMA)
+        bool ok = true;
+        if (TMA && warp < 10)
+            for (; issued < 2 && issued < n_tiles; ++issued) tma_tile(issued, warp == 9);
+        // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
+        if (n_tiles > 0) {
+            constexpr int CH = D / 8;
+            for (int idx = tid; idx < ROWS * CH; idx += 128) {
+                const int r = idx / CH, c = idx % CH, rr = r0 + r;
+                uint4 u = make_uint4(0, 0, 0, 0);
+                if (r < rows) u = *(const uint4 *)((const bf16 *)a.q + (long)(row0 + rr / a.group) * a.q_stride + (long)(kvh * a.group + rr % a.group) * D + c * 8);
+                if (Q8)
+                    u = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632), __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
+                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c), u);
+            }
+        }
+        fence_proxy_async();
+        mbar_arrive(q_full);
+        if (TMA) {
+            if (warp < 10) {
+                for (; ok && issued < n_tiles; ++issued) ok = tma_tile(issued, warp == 9);
+                if (!ok) // copies in flight land before the block ends
+                    for (int j = max(0, issued - 2); j < issued; ++j) settle((warp == 9 ? v_full(j & 1) : k_full(j & 1)), (j >> 1) & 1);
+            } else {
+                // pass every V tile on to the MMA warp; those with keys that not every row sees without the values that 0
+                // would not cancel
+                for (int j = 0; ok && j < n_tiles; ++j) {
+                    ok = mbar_wait(v_full(j & 1), (j >> 1) & 1, a.err, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (partial(key0(j))) {
+                        bool bad = false;
+                        for (int i = tid - 64; i < C::TILE / 16; i += 64) {
+                            uint4 u = lds128(base + C::OFF_V + (j & 1) * C::TILE + i * 16);
+                            if (clean16(u)) { sts128(base + C::OFF_V + (j & 1) * C::TILE + i * 16, u); bad = true; }
+                        }
+                        if (bad) *dirty = 1;
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
+                    if (lane == 0) mbar_arrive(v_clean(j & 1));
+                }
+            }
+        } else {
+            long *rowoff = (long *)(gen + C::OFF_ROW);
+            float *sc = (float *)(gen + C::OFF_SC);
+            auto rows_of = [&](int j) { // cached rows (-1: no row needs the key) and scales of the tile's keys
+                const int t = key0(j) + tid;
+                long row = -1;
+                if (key_needed(t)) {
+                    const int pi = t / a.kv.page, page = bt[pi];
+                    if (page < 0 || page >= a.kv.n_pages) atomicOr(a.err, ERR_PAGE_RANGE);
+                    else row = ((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page);
+                }
+                rowoff[(j & 1) * 128 + tid] = row;
+                if (Q8) {
+                    sc[(j & 7) * 256 + tid] = row >= 0 ? a.kv.ks[row] : 0.f;
+                    sc[(j & 7) * 256 + 128 + tid] = row >= 0 ? a.kv.vs[row] : 0.f;
+                    mbar_arrive(sc_full(j & 7)); // eight tiles later the slot's scores have long been weighted
+                }
+                named_bar<BAR_LOAD, 128>();
+            };
+            if (Q8) {
+                constexpr int CPR = D / 16, N = 128 * CPR / 128; // 16-code chunks per row, per thread
+                const uint32_t c128 = widen_const();
+                const int c = tid % CPR;
+                auto fetch = [&](int j, const void *pages, uint4 (&u)[N]) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const long row = rowoff[(j & 1) * 128 + i * (128 / CPR) + tid / CPR];
+                        u[i] = row >= 0 ? *(const uint4 *)((const uint8_t *)pages + row * D + c * 16) : make_uint4(0, 0, 0, 0);
+                    }
+                };
+                auto widen = [&](uint32_t tile_base, const uint4 (&u)[N]) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int r = i * (128 / CPR) + tid / CPR;
+                        const uint4 lo = make_uint4(even2<FMT>(u[i].x, c128), odd2<FMT>(u[i].x, c128), even2<FMT>(u[i].y, c128), odd2<FMT>(u[i].y, c128));
+                        const uint4 hi = make_uint4(even2<FMT>(u[i].z, c128), odd2<FMT>(u[i].z, c128), even2<FMT>(u[i].w, c128), odd2<FMT>(u[i].w, c128));
+                        const bool swap = (c >> 2) & 1; // the two halves of the head in turn: other banks
+                        sts128(tile_base + tile_at(r, 2 * c + swap), swap ? hi : lo);
+                        sts128(tile_base + tile_at(r, 2 * c + !swap), swap ? lo : hi);
+                    }
+                    fence_proxy_async();
+                };
+                uint4 uk[N], uv[N];
+                if (n_tiles > 0) { rows_of(0); fetch(0, a.kv.k, uk); }
+                for (int j = 0; j < n_tiles; ++j) {
+                    const int s = j & 1;
+                    fetch(j, a.kv.v, uv);
+                    if (j >= 2 && ok) ok = mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    if (ok) widen(base + C::OFF_K + s * C::TILE, uk);
+                    mbar_arrive(k_full(s));
+                    if (j + 1 < n_tiles) { rows_of(j + 1); fetch(j + 1, a.kv.k, uk); }
+                    if (j >= 2 && ok) ok = mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    if (ok) widen(base + C::OFF_V + s * C::TILE, uv);
+                    mbar_arrive(v_full(s));
+                }
+            } else {
+                // cp.async, one operand tile behind
+                constexpr int CH = D / 8;
+                auto copy = [&](int j, const void *pages, uint32_t tile_base) {
+                    for (int i = tid; i < 128 * CH; i += 128) {
+                        const int r = i / CH, c = i % CH;
+                        const long row = rowoff[(j & 1) * 128 + r];
+                        cp16(tile_base + tile_at(r, c), (const bf16 *)pages + (row >= 0 ? row * D + c * 8 : 0), row >= 0);
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                };
+                auto landed_v = [&](int j) {
+                    if (partial(key0(j))) { // this thread's own chunks
+                        bool bad = false;
+                        for (int i = tid; i < 128 * CH; i += 128) {
+                            const uint32_t p = base + C::OFF_V + (j & 1) * C::TILE + tile_at(i / CH, i % CH);
+                            uint4 u = lds128(p);
+                            if (clean16(u)) { sts128(p, u); bad = true; }
+                        }
+                        if (bad) *dirty = 1;
+                    }
+                    fence_proxy_async();
+                    mbar_arrive(v_full(j & 1));
+                };
+                for (int j = 0; j < n_tiles; ++j) {
+                    const int s = j & 1;
+                    rows_of(j);
+                    if (j >= 2 && ok) ok = mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    copy(j, a.kv.k, base + C::OFF_K + s * C::TILE);
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    if (j) landed_v(j - 1);
+                    if (j >= 2 && ok) ok = mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    copy(j, a.kv.v, base + C::OFF_V + s * C::TILE);
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    fence_proxy_async();
+                    mbar_arrive(k_full(s));
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                if (n_tiles) landed_v(n_tiles - 1);
+            }
+        }
+    } else if (warp == 12) {
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = make_idesc(TK), idesc_o = make_idesc(D) | (1u << 16); // V: MN-major
+            auto issue_s = [&](int u, int j) { // S of unit u on key tile j
+                const uint32_t q = base + C::OFF_Q + (PAIR ? u : 0) * C::TILE, k = base + C::OFF_K + (j & 1) * C::TILE;
+#pragma unroll
+                for (int kk = 0; kk < D / UMMA_K; ++kk)
+                    umma(tmem + u * 128u, make_desc(q + (kk >> 2) * HALF) + (uint64_t)((kk & 3) * 2), make_desc(k + (kk >> 2) * HALF) + (uint64_t)((kk & 3) * 2),
+                         idesc_s, kk > 0);
+                umma_commit(s_full(u));
+            };
+            auto issue_o = [&](int u, int j, bool acc) {
+                const uint32_t v = base + C::OFF_V + (j & 1) * C::TILE;
+#pragma unroll
+                for (int kk = 0; kk < TK / UMMA_K; ++kk)
+                    umma_ta(tmem + 256u + u * 128u, tmem + u * 128u + kk * 8u, desc_mn(v + kk * UMMA_K * 128, HALF, 1024), idesc_o, acc || kk > 0);
+            };
+            bool ok = n_tiles > 0 && mbar_wait(q_full, 0, a.err, abort_flag);
+            for (int u = 0; ok && u < 2; ++u)
+                if (unit_count(u) > 0) {
+                    const int j = unit_tile(u, 0);
+                    ok = mbar_wait(k_full(j & 1), 0, a.err, abort_flag);
+                    if (!ok) break;
+                    fence_after();
+                    issue_s(u, j);
+                    if (!PAIR || u == 1) umma_commit(k_empty(j & 1));
+                }
+            for (int i = 0; ok && i < unit_count(0); ++i)
+                for (int u = 0; ok && u < 2; ++u) {
+                    if (i >= unit_count(u)) break;
+                    const int j = unit_tile(u, i), s = j & 1;
+                    ok = mbar_wait(p_ready(u), i & 1, a.err, abort_flag) && mbar_wait(TMA ? v_clean(s) : v_full(s), (j >> 1) & 1, a.err, abort_flag);
+                    if (!ok) break;
+                    fence_after();
+                    issue_o(u, j, i > 0);
+                    if (!PAIR || u == 1) umma_commit(v_empty(s));
+                    if (i + 1 < unit_count(u)) {
+                        const int jn = unit_tile(u, i + 1);
+                        ok = mbar_wait(k_full(jn & 1), (jn >> 1) & 1, a.err, abort_flag);
+                        if (!ok) break;
+                        fence_after();
+                        issue_s(u, jn);
+                        if (!PAIR || u == 1) umma_commit(k_empty(jn & 1));
+                    } else
+                        umma_commit(o_done(u));
+                }
+            if (!ok && n_tiles > 0) { // products in flight end before tensor memory is freed
+                umma_commit(drain);
+                settle(drain, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int u = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + lanes + u * 128u, t_o = tmem + lanes + 256u + u * 128u;
+        const int rr = (PAIR ? u * TQ : 0) + row, gr = r0 + rr; // row of the tiles, of the (sequence, KV head)
+        const bool live = rr < rows;
+        const int pos = live ? len + gr / a.group : -1;
+        const float qs = a.scale_log2;
+        const float *sc = (const float *)(gen + C::OFF_SC);
+        float m_used = -INFINITY, l = 0.f;
+        bool ok = true;
+        const int count = unit_count(u);
+        for (int i = 0; i < count; ++i) {
+            const int j = unit_tile(u, i), t0 = key0(j);
+            ok = mbar_wait(s_full(u), i & 1, a.err, abort_flag);
+            if (Q8 && ok) ok = mbar_wait(sc_full(j & 7), (j >> 3) & 1, a.err, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            fence_after();
+            const bool masked = partial(t0);
+            const int hi = pos - t0, lo = a.window ? pos - a.window + 1 - t0 : -1, sk = a.sinks - t0; // columns c <= hi with c >= lo or c < sk
+            const float *ks = sc + (j & 7) * 256, *vs = ks + 128;
+            auto scores = [&](int c0, float (&v)[32]) {
+                tmem_ld32(t_s + c0, v);
+                if (Q8) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 f = *(const float4 *)(ks + c0 + e);
+                        v[e] *= f.x; v[e + 1] *= f.y; v[e + 2] *= f.z; v[e + 3] *= f.w;
+                    }
+                }
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c0 + e > hi || (c0 + e < lo && c0 + e >= sk)) v[e] = -INFINITY;
+                }
+            };
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int c0 = 0; c0 < TK; c0 += 32) {
+                float v[32], m0 = -INFINITY, m1 = -INFINITY;
+                scores(c0, v);
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) { m0 = fmaxf(fmaxf(m0, v[e]), v[e + 1]); m1 = fmaxf(fmaxf(m1, v[e + 2]), v[e + 3]); }
+                mx = fmaxf(mx, fmaxf(m0, m1));
+            }
+            mx *= qs;
+            float f = 1.f;
+            if (m_used == -INFINITY) m_used = mx; // nothing accumulated yet
+            else if (mx > m_used + 8.f) { f = ex2(m_used - mx); m_used = mx; l *= f; }
+            if (__any_sync(0xffffffffu, f != 1.f)) {
+                // every product so far is complete: S of this tile was issued after them
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float v[32];
+                    uint32_t w[16];
+                    tmem_ld32(t_o + c0, v);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[16 * h + e] * f);
+                        tmem_st16(t_o + c0 + 16 * h, w);
+                    }
+                }
+                tmem_st_wait();
+            }
+            const float mb = m_used == -INFINITY ? 0.f : m_used;
+            float l0 = 0.f, l1 = 0.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < TK; c0 += 32) {
+                float v[32];
+                uint32_t w[16];
+                scores(c0, v);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    float p0 = ex2(fmaf(v[e], qs, -mb)), p1 = ex2(fmaf(v[e + 1], qs, -mb));
+                    l0 += p0;
+                    l1 += p1;
+                    if (Q8) {
+                        const float2 g = *(const float2 *)(vs + c0 + e);
+                        p0 = masked && v[e] == -INFINITY ? 0.f : p0 * g.x; // a masked key's scale may be anything
+                        p1 = masked && v[e + 1] == -INFINITY ? 0.f : p1 * g.y;
+                    }
+                    w[e >> 1] = pack(p0, p1);
+                }
+                tmem_st16(t_s + (c0 >> 1), w);
+            }
+            l += l0 + l1;
+            tmem_st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_ready(u));
+        }
+        if (ok && count > 0) {
+            ok = mbar_wait(o_done(u), 0, a.err, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            fence_after();
+        }
+        float *ob = (float *)(gen + C::OFF_K), *ml = (float *)(gen + C::OFF_ML); // B's rows for A: [dim][row], over the K (and V) tiles
+        const bool both = !PAIR && n_tiles > 1;
+        if (both) {
+            if (u == 1) {
+                if (ok) ok = mbar_wait(o_done(0), 0, a.err, abort_flag); // A's products read these tiles too
+                ok = __all_sync(0xffffffffu, ok);
+                if (ok) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        float v[32];
+                        tmem_ld32(t_o + c0, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) ob[(c0 + e) * 128 + row] = v[e];
+                    }
+                }
+                ml[2 * row] = m_used;
+                ml[2 * row + 1] = l;
+            }
+            named_bar<BAR_SOFT, 256>();
+        }
+        if (ok && (PAIR || u == 0)) {
+            float fa = 1.f, fb = 0.f, m = m_used, den = l;
+            if (both) {
+                const float mo = ml[2 * row], lo = ml[2 * row + 1];
+                m = fmaxf(m_used, mo);
+                fa = m_used == -INFINITY ? 0.f : ex2(m_used - m);
+                fb = mo == -INFINITY ? 0.f : ex2(mo - m);
+                den = fmaf(l, fa, lo * fb);
+            }
+            if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum
+            const float inv = a.part_o ? 1.f : (den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den));
+            const int head = kvh * a.group + gr % a.group;
+            const long token = row0 + gr / a.group;
+            const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
+            bf16 *dst = (bf16 *)a.out + token * a.o_stride + (long)head * D;
+            if (a.part_o && live) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
+            const bool give_back = !Q8 && *dirty;
+#pragma unroll 1
+            for (int c0 = 0; c0 < D && n_tiles > 0; c0 += 32) {
+                float v[32], x[32];
+                tmem_ld32(t_o + c0, v); // warp-wide: lanes without a row load too
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] *= fa;
+                if (both) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = fmaf(ob[(c0 + e) * 128 + row], fb, v[e]);
+                }
+                if (!live) continue;
+                if (give_back) {
+                    for (int j = 0; j < n_tiles; ++j) {
+                        const int t0 = key0(j);
+                        for (int t = t0; t < t0 + TK && partial(t0); ++t) {
+                            if (t > pos || (a.window && t <= pos - a.window && t >= a.sinks)) continue;
+                            const int pi = t / a.kv.page, page = bt[pi];
+                            if (page < 0 || page >= a.kv.n_pages) continue;
+                            const bf16 *src = (const bf16 *)a.kv.v + (((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page)) * D + c0;
+#pragma unroll 1
+                            for (int e = 0; e < 32; ++e) {
+                                const float y = __bfloat162float(src[e]);
+                                if (!isfinite(y)) {
+#pragma unroll
+                                    for (int k = 0; k < 32; ++k)
+                                        if (k == e) v[k] += y;
+                                }
+                            }
+                        }
+                    }
+                }
+                // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
+                if (a.part_o) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        *(uint4 *)(dst + c0 + e) = make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7]));
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 12) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_COLS) : "memory");
+    }
+}
+
+template <int FMT, int D, bool PAIR, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
+{
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise((const void *)paged_attention_tc_kernel<FMT, D, PAIR, TMA>, TcCfg<D>::SMEM);
+    if (e != cudaSuccess) return e;
+    const int rows = PAIR ? 256 : 128;
+    const long tiles = ((long)a.max_new * a.group + rows - 1) / rows;
+    return launch_kernel(paged_attention_tc_kernel<FMT, D, PAIR, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(T_THREADS),
+                         TcCfg<D>::SMEM, st, 0, km, vm, a);
+}
+template <int FMT, int D, bool PAIR> cudaError_t tc_by_copy(const PagedAttnArgs &a, cudaStream_t st)
+{
+    TcMap km{}, vm{};
+    if constexpr (FMT == KV_BF16) {
+        const long rows = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
+        if (a.kv.page % 16 == 0 && rows < 0x7fffff00L && make_operand_map(&km, a.kv.k, D, rows, 1, D, 0, 16) == 0 &&
+            make_operand_map(&vm, a.kv.v, D, rows, 1, D, 0, 16) == 0)
+            return launch_tc<FMT, D, PAIR, true>(a, km, vm, st);
+    }
+    return launch_tc<FMT, D, PAIR, false>(a, km, vm, st);
+}
+template <int FMT> cudaError_t tc_by_dim(const PagedAttnArgs &a, cudaStream_t st)
+{
+    const bool pair = (long)a.max_new * a.group > TQ;
+    if (a.kv.d == 128) return pair ? tc_by_copy<FMT, 128, true>(a, st) : tc_by_copy<FMT, 128, false>(a, st);
+    if (a.kv.d == 64) return pair ? tc_by_copy<FMT, 64, true>(a, st) : tc_by_copy<FMT, 64, false>(a, st);
+    return cudaErrorInvalidValue;
+}
+
+} // namespace
+
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st)
+{
+    switch (a.kv.fmt) {
+    case KV_BF16: return tc_by_dim<KV_BF16>(a, st);
+    case KV_E4M3: return tc_by_dim<KV_E4M3>(a, st);
+    case KV_INT8: return tc_by_dim<KV_INT8>(a, st);
+    default: return cudaErrorInvalidValue;
+    }
+}
+
+} // namespace spd
