@@ -8,16 +8,18 @@
 // that the products of one key tile run under the softmax of the other there too.
 // Per tile of 128 keys and 128 rows:
 //   S = Q K^T      tcgen05.mma, Q and K as K-major 128B-swizzled tiles, accumulator in tensor memory
-//   P = softmax    thread = row: a pass over the row's 128 scores in tensor memory for the maximum, a second one for the
-//                  weights, which go back to tensor memory as bf16 over the scores already read
+//   P = softmax    thread = row and half of the keys: maximum (joined with the other half's), then the weights, which go back
+//                  to tensor memory as bf16 over the scores already read
 //   O += P V       tcgen05.mma with P read from tensor memory and V as the MN-major operand ([key][dim] rows as they are
 //                  stored); O stays in tensor memory and is rescaled there only when the row maximum has grown by more than 2^8
 // Tensor memory (512 columns): S/P of A and B at 0 and 128, O of A and B at 256 and 384.
-// Warps: 0-3 softmax of A, 4-7 of B, 8-11 load, 12 issues the MMAs.  K and V tiles have rings of two; a K tile is free once S is
-// computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims; 8-bit pages (and bf16 pages
-// of other sizes) by the four load warps, which widen the codes to bf16 on the way into shared memory.  The pairs that widening
-// a 32-bit word gives are (0, 2) and (1, 3) of its four codes: the head dims of Q, K and V all sit in that order, and the output
-// is put right when it is stored.  Row scales multiply the scores (K) and the weights (V) in fp32.
+// Warps: 0-15 softmax (two threads per row, four warps per scheduler: one thread per row left the schedulers waiting on their
+// own instructions' latencies), then the load warps, then two that issue the MMAs of A and of B.  K and V tiles have rings of two;
+// a K tile is free once S is computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a
+// second load warp looks after V, see below); 8-bit pages (and bf16 pages of other sizes) by four load warps, which widen the
+// codes to bf16 on the way into shared memory.  The pairs that widening a 32-bit word gives are (0, 2) and (1, 3) of its four
+// codes: the head dims of Q, K and V all sit in that order, and the output is put right when it is stored.  Row scales multiply
+// the scores (K) and the weights (V) in fp32.
 // A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
 // shared memory before the product, and rows that do see them get them back at the end.
 // Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
@@ -31,9 +33,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int TQ = 128, TK = 128, T_THREADS = 13 * 32, HALF = 128 * 128; // bytes of [128 rows][64 bf16]
+constexpr int TQ = 128, TK = 128, HALF = 128 * 128; // bytes of [128 rows][64 bf16]
+constexpr int SOFT_WARPS = 16, SOFT_THREADS = 32 * SOFT_WARPS;
 constexpr uint32_t T_COLS = 512;
-enum { BAR_LOAD = 3, BAR_SOFT = 4 };
+enum { BAR_LOAD = 3, BAR_SOFT = 4, BAR_A = 5, BAR_B = 6, BAR_PAIR = 8 }; // BAR_PAIR .. + 7
 
 template <int D> struct TcCfg {
     static constexpr int TILE = 128 * D * 2;
@@ -41,26 +44,37 @@ template <int D> struct TcCfg {
     static constexpr int OFF_SC = OFF_V + 2 * TILE;            // [8][256] K and V scales of a tile
     static constexpr int OFF_ROW = OFF_SC + 8 * 1024;          // [2][128] cached rows of a tile's keys
     static constexpr int OFF_BAR = OFF_ROW + 2 * 1024;
-    static constexpr int OFF_ML = OFF_BAR + 512;               // [128][2] maximum and sum of B
-    static constexpr int SMEM = OFF_ML + 1024 + 1024;          // + alignment slack
+    static constexpr int OFF_RED = OFF_BAR + 512;              // [2 parities][2 units][2 halves][128] maxima; sums at the end
+    static constexpr int OFF_ML = OFF_RED + 4096;              // [128] maximum of B
+    static constexpr int SMEM = OFF_ML + 512 + 1024;           // + alignment slack
 };
 
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t lbo, uint32_t sbo)
+// Shared-memory descriptors in two words: 128B-swizzled tiles, 8-row groups 1024 bytes apart.  Word 0 holds the address / 16 (and,
+// for the MN-major V tile, the distance of its 64-dim blocks), so a step inside a tile is an addition to it.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) { return ((addr & 0x3FFFFu) >> 4) | (lead << 16); }
+// The products are issued by one elected lane of a converged warp whose operands are the same in all lanes: they then live in
+// uniform registers, and the issue loop keeps ahead of the tensor cores (with a single-lane branch it did not).
+// D[tmem] (+)= A[shared] B[shared]
+__device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc)
 {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr & 0x3FFFF) >> 4);
-    d |= (uint64_t)(lbo >> 4) << 16;
-    d |= (uint64_t)(sbo >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI) : "memory");
 }
 // D[tmem] (+)= A[tmem] B[shared]
-__device__ __forceinline__ void umma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\t"
+                 "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(DESC_HI) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t ta, float (&v)[32])
 {
@@ -76,17 +90,46 @@ __device__ __forceinline__ void tmem_ld32(uint32_t ta, float (&v)[32])
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_st16(uint32_t ta, const uint32_t (&v)[16])
+// The same without the wait: the registers may be read after tmem_wait32 on them only.
+__device__ __forceinline__ void tmem_ask32(uint32_t ta, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(ta) : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) // the registers pass through, so that no use of them moves before the wait
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t ta, const uint32_t *v)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  ::"r"(ta), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
                    "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16u(uint32_t ta, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(ta) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 template <int ID, int N> __device__ __forceinline__ void named_bar() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
+template <int ID, int N> __device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -97,6 +140,45 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *(const uint32_t *)&v;
+}
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(unsigned long long *)&d)
+        : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b), "l"(*(const unsigned long long *)&c));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
+    return d;
+}
+// 2^t of two values on the FMA pipes, for t <= 127 (t below -126 counts as -126): t = n + f with n = round(t), |f| <= 1/2; a
+// polynomial of degree 4 for 2^f (least maximum relative error over the interval by a Lawson iteration: 2.6e-6) whose exponent
+// field n is added to.
+__device__ __forceinline__ float2 exp2_poly2(float2 t)
+{
+    const float2 magic = make_float2(12582912.f, 12582912.f); // 1.5 * 2^23: the sum's low bits are n
+    t = make_float2(fmaxf(t.x, -126.f), fmaxf(t.y, -126.f));
+    const float2 z = add2(t, magic), n = add2(z, make_float2(-12582912.f, -12582912.f));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), t);
+    float2 p = fma2(make_float2(0.009570102207362652f, 0.009570102207362652f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+    p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    p = make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(z.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(z.y) << 23)));
+    // at -126 the polynomial gives just under 1, hence a subnormal number here: flushed, so that -inf gives 0
+    float2 d;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&p), "l"(0x3f8000003f800000ull));
+    return d;
 }
 // Waits a bounded time whatever the abort flag says: copies and products in flight before the memory is given up.
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity)
@@ -135,12 +217,20 @@ __device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities o
     return bad;
 }
 
+constexpr bool TURNS = true;
+// Column (from the unit's first) of the weights of keys k, k + 1: each 32 keys' go over columns of their own half's scores, the
+// second 32 over the last 16, so that the first 32 scores can be read again after them.
+__device__ __forceinline__ constexpr uint32_t weight_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 48 : 0) + ((k & 31) >> 1)); }
+constexpr int load_warps(bool tma) { return tma ? 2 : 4; }
+constexpr int tc_threads(bool tma) { return SOFT_THREADS + 32 * (load_warps(tma) + 2); } // 640 x 96 or 704 x 80 registers
+
 template <int FMT, int D, bool PAIR, bool TMA>
-__global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+__global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                           const __grid_constant__ PagedAttnArgs a)
 {
     using C = TcCfg<D>;
     constexpr bool Q8 = FMT != KV_BF16;
+    constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA);
     extern __shared__ uint8_t tc_raw[];
     uint8_t *gen = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(gen), bars = base + C::OFF_BAR;
@@ -151,11 +241,12 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
     auto v_empty = [&](int s) { return bars + 8u * (7 + s); };
     auto v_clean = [&](int s) { return bars + 8u * (9 + s); };
     auto s_full = [&](int u) { return bars + 8u * (11 + u); };
-    auto p_ready = [&](int u) { return bars + 8u * (13 + u); };
+    auto p_ready = [&](int u) { return bars + 8u * (13 + u); };      // weights of a tile's first 64 keys
+    auto p_rest = [&](int u) { return bars + 8u * (26 + u); };       // ... of the others
     auto o_done = [&](int u) { return bars + 8u * (15 + u); };
     auto sc_full = [&](int s) { return bars + 8u * (17 + s); };
-    const uint32_t drain = bars + 8u * 25;
-    uint32_t *tmem_slot = (uint32_t *)(gen + C::OFF_BAR + 8 * 32);
+    auto drain = [&](int u) { return bars + 8u * (28 + u); };
+    uint32_t *tmem_slot = (uint32_t *)(gen + C::OFF_BAR + 8 * 40);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     volatile int *dirty = (volatile int *)(tmem_slot + 2);
 
@@ -187,22 +278,24 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         *dirty = 0;
-        mbar_init(q_full, 128);
+        mbar_init(q_full, SOFT_THREADS);
         for (int s = 0; s < 2; ++s) {
             mbar_init(k_full(s), TMA ? 1 : 128);
             mbar_init(v_full(s), TMA ? 1 : 128);
-            mbar_init(k_empty(s), 1);
-            mbar_init(v_empty(s), 1);
-            mbar_init(v_clean(s), 2);
+            mbar_init(k_empty(s), PAIR ? 2 : 1); // both units read a tile, or one
+            mbar_init(v_empty(s), PAIR ? 2 : 1);
+            mbar_init(v_clean(s), 1);
             mbar_init(s_full(s), 1);
             mbar_init(p_ready(s), 4);
+            mbar_init(p_rest(s), 4);
             mbar_init(o_done(s), 1);
         }
         for (int s = 0; s < 8; ++s) mbar_init(sc_full(s), 128);
-        mbar_init(drain, 1);
+        mbar_init(drain(0), 1);
+        mbar_init(drain(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == W_MMA) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(T_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -214,9 +307,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
     auto unit_tile = [&](int u, int i) { return PAIR ? i : 2 * i + u; };
     auto unit_count = [&](int u) { return PAIR ? n_tiles : (n_tiles - u + 1) / 2; };
 
-    if (warp >= 8 && warp < 12) {
-        const int tid = threadIdx.x - 256;
-        if (TMA && (warp == 8 || warp == 9) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 9 ? &v_map : &k_map) : "memory");
+    if (warp >= W_LOAD && warp < W_MMA) {
+        const int tid = threadIdx.x - 32 * W_LOAD;
         // one box = 16 keys x 64 dims; lane = (16 keys, half of the head); 16 keys that no row needs come as zeros (a row beyond the map)
         constexpr int BOXES = 8 * (D / 64);
         auto tma_tile = [&](int j, bool is_v) {
@@ -240,43 +332,42 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
                             h * 64, (int)row, 0, full);
             return true;
         };
-        int issued = 0; // tiles this warp has asked for (TMA)
         bool ok = true;
-        if (TMA && warp < 10)
-            for (; issued < 2 && issued < n_tiles; ++issued) tma_tile(issued, warp == 9);
-        // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
-        if (n_tiles > 0) {
-            constexpr int CH = D / 8;
-            for (int idx = tid; idx < ROWS * CH; idx += 128) {
-                const int r = idx / CH, c = idx % CH, rr = r0 + r;
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (r < rows) u = *(const uint4 *)((const bf16 *)a.q + (long)(row0 + rr / a.group) * a.q_stride + (long)(kvh * a.group + rr % a.group) * D + c * 8);
-                if (Q8)
-                    u = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632), __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
-                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c), u);
-            }
-        }
-        fence_proxy_async();
-        mbar_arrive(q_full);
         if (TMA) {
-            if (warp < 10) {
-                for (; ok && issued < n_tiles; ++issued) ok = tma_tile(issued, warp == 9);
-                if (!ok) // copies in flight land before the block ends
-                    for (int j = max(0, issued - 2); j < issued; ++j) settle((warp == 9 ? v_full(j & 1) : k_full(j & 1)), (j >> 1) & 1);
+            if (warp == W_LOAD) {
+                int k_in = 0, v_in = 0; // tiles asked for
+                for (int j = 0; ok && j < n_tiles; ++j) {
+                    ok = tma_tile(j, false);
+                    k_in += ok;
+                    ok = ok && tma_tile(j, true);
+                    v_in += ok;
+                }
+                if (!ok) { // copies in flight land before the block ends
+                    for (int j = max(0, k_in - 2); j < k_in; ++j) settle(k_full(j & 1), (j >> 1) & 1);
+                    for (int j = max(0, v_in - 2); j < v_in; ++j) settle(v_full(j & 1), (j >> 1) & 1);
+                }
             } else {
-                // pass every V tile on to the MMA warp; those with keys that not every row sees without the values that 0
+                // pass every V tile on to the MMA warps; those with keys that not every row sees without the values that 0
                 // would not cancel
                 for (int j = 0; ok && j < n_tiles; ++j) {
                     ok = mbar_wait(v_full(j & 1), (j >> 1) & 1, a.err, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     if (partial(key0(j))) {
-                        bool bad = false;
-                        for (int i = tid - 64; i < C::TILE / 16; i += 64) {
-                            uint4 u = lds128(base + C::OFF_V + (j & 1) * C::TILE + i * 16);
-                            if (clean16(u)) { sts128(base + C::OFF_V + (j & 1) * C::TILE + i * 16, u); bad = true; }
+                        const uint32_t v = base + C::OFF_V + (j & 1) * C::TILE + lane * 16;
+                        uint32_t top = 0; // largest magnitude bits of either half
+#pragma unroll 16
+                        for (int i = 0; i < C::TILE / 512; ++i) {
+                            const uint4 x = lds128(v + i * 512);
+                            top = __vmaxu2(top, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
                         }
-                        if (bad) *dirty = 1;
+                        if ((top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u) {
+                            for (int i = 0; i < C::TILE / 512; ++i) {
+                                uint4 x = lds128(v + i * 512);
+                                if (clean16(x)) sts128(v + i * 512, x);
+                            }
+                            *dirty = 1;
+                        }
                         fence_proxy_async();
                         __syncwarp();
                     }
@@ -303,39 +394,44 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
                 named_bar<BAR_LOAD, 128>();
             };
             if (Q8) {
-                constexpr int CPR = D / 16, N = 128 * CPR / 128; // 16-code chunks per row, per thread
+                constexpr int CPR = D / 16, N = CPR / 2; // 16-code chunks per row; per thread and half a tile (64 keys)
                 const uint32_t c128 = widen_const();
                 const int c = tid % CPR;
-                auto fetch = [&](int j, const void *pages, uint4 (&u)[N]) {
+                auto fetch = [&](int j, int h, const void *pages, uint4 (&x)[N]) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const long row = rowoff[(j & 1) * 128 + i * (128 / CPR) + tid / CPR];
-                        u[i] = row >= 0 ? *(const uint4 *)((const uint8_t *)pages + row * D + c * 16) : make_uint4(0, 0, 0, 0);
+                        const long row = rowoff[(j & 1) * 128 + h * 64 + i * (128 / CPR) + tid / CPR];
+                        x[i] = row >= 0 ? *(const uint4 *)((const uint8_t *)pages + row * D + c * 16) : make_uint4(0, 0, 0, 0);
                     }
                 };
-                auto widen = [&](uint32_t tile_base, const uint4 (&u)[N]) {
+                auto widen = [&](uint32_t tile_base, int h, const uint4 (&x)[N]) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const int r = i * (128 / CPR) + tid / CPR;
-                        const uint4 lo = make_uint4(even2<FMT>(u[i].x, c128), odd2<FMT>(u[i].x, c128), even2<FMT>(u[i].y, c128), odd2<FMT>(u[i].y, c128));
-                        const uint4 hi = make_uint4(even2<FMT>(u[i].z, c128), odd2<FMT>(u[i].z, c128), even2<FMT>(u[i].w, c128), odd2<FMT>(u[i].w, c128));
+                        const int r = h * 64 + i * (128 / CPR) + tid / CPR;
+                        const uint4 lo = make_uint4(even2<FMT>(x[i].x, c128), odd2<FMT>(x[i].x, c128), even2<FMT>(x[i].y, c128), odd2<FMT>(x[i].y, c128));
+                        const uint4 hi = make_uint4(even2<FMT>(x[i].z, c128), odd2<FMT>(x[i].z, c128), even2<FMT>(x[i].w, c128), odd2<FMT>(x[i].w, c128));
                         const bool swap = (c >> 2) & 1; // the two halves of the head in turn: other banks
                         sts128(tile_base + tile_at(r, 2 * c + swap), swap ? hi : lo);
                         sts128(tile_base + tile_at(r, 2 * c + !swap), swap ? lo : hi);
                     }
-                    fence_proxy_async();
                 };
-                uint4 uk[N], uv[N];
-                if (n_tiles > 0) { rows_of(0); fetch(0, a.kv.k, uk); }
+                uint4 x0[N], x1[N]; // one batch is on its way while the other is widened
+                if (n_tiles > 0) { rows_of(0); fetch(0, 0, a.kv.k, x0); }
                 for (int j = 0; j < n_tiles; ++j) {
                     const int s = j & 1;
-                    fetch(j, a.kv.v, uv);
-                    if (j >= 2 && ok) ok = mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    if (ok) widen(base + C::OFF_K + s * C::TILE, uk);
+                    fetch(j, 1, a.kv.k, x1);
+                    if (j >= 2) mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    widen(base + C::OFF_K + s * C::TILE, 0, x0);
+                    fetch(j, 0, a.kv.v, x0);
+                    widen(base + C::OFF_K + s * C::TILE, 1, x1);
+                    fence_proxy_async();
                     mbar_arrive(k_full(s));
-                    if (j + 1 < n_tiles) { rows_of(j + 1); fetch(j + 1, a.kv.k, uk); }
-                    if (j >= 2 && ok) ok = mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    if (ok) widen(base + C::OFF_V + s * C::TILE, uv);
+                    fetch(j, 1, a.kv.v, x1);
+                    if (j >= 2) mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+                    widen(base + C::OFF_V + s * C::TILE, 0, x0);
+                    if (j + 1 < n_tiles) { rows_of(j + 1); fetch(j + 1, 0, a.kv.k, x0); }
+                    widen(base + C::OFF_V + s * C::TILE, 1, x1);
+                    fence_proxy_async();
                     mbar_arrive(v_full(s));
                 }
             } else {
@@ -379,180 +475,233 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
                 if (n_tiles) landed_v(n_tiles - 1);
             }
         }
-    } else if (warp == 12) {
-        if (lane == 0) {
+    } else if (warp >= W_MMA) {
+        {
+            // One warp for the products of A, one for those of B.  A wait that gives up raises the abort flag, after which
+            // every wait returns at once: the loops run out on whatever is there, and the block ends with the error bit set.
+            const int u = warp - W_MMA, count = unit_count(u);
             constexpr uint32_t idesc_s = make_idesc(TK), idesc_o = make_idesc(D) | (1u << 16); // V: MN-major
-            auto issue_s = [&](int u, int j) { // S of unit u on key tile j
-                const uint32_t q = base + C::OFF_Q + (PAIR ? u : 0) * C::TILE, k = base + C::OFF_K + (j & 1) * C::TILE;
+            const uint32_t q_lo = desc_lo(base + C::OFF_Q + (PAIR ? u * C::TILE : 0), 1), k_lo = desc_lo(base + C::OFF_K, 1), v_lo = desc_lo(base + C::OFF_V, HALF >> 4);
+            const uint32_t t_s = tmem + u * 128u, t_o = tmem + 256u + u * 128u;
+            auto wait = [&](uint32_t bar, int parity) { mbar_wait(bar, parity, a.err, abort_flag); };
+            auto issue_s = [&](int s) { // S on K slot s
 #pragma unroll
                 for (int kk = 0; kk < D / UMMA_K; ++kk)
-                    umma(tmem + u * 128u, make_desc(q + (kk >> 2) * HALF) + (uint64_t)((kk & 3) * 2), make_desc(k + (kk >> 2) * HALF) + (uint64_t)((kk & 3) * 2),
-                         idesc_s, kk > 0);
-                umma_commit(s_full(u));
+                    umma_ss(t_s, q_lo + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, k_lo + s * (C::TILE >> 4) + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, idesc_s, kk > 0);
+                commit(s_full(u));
+                commit(k_empty(s));
             };
-            auto issue_o = [&](int u, int j, bool acc) {
-                const uint32_t v = base + C::OFF_V + (j & 1) * C::TILE;
+            auto issue_o = [&](int s, int kk0, bool acc) { // 64 keys
 #pragma unroll
-                for (int kk = 0; kk < TK / UMMA_K; ++kk)
-                    umma_ta(tmem + 256u + u * 128u, tmem + u * 128u + kk * 8u, desc_mn(v + kk * UMMA_K * 128, HALF, 1024), idesc_o, acc || kk > 0);
+                for (int kk = kk0; kk < kk0 + 64 / UMMA_K; ++kk)
+                    umma_ts(t_o, t_s + weight_column(16 * kk), v_lo + s * (C::TILE >> 4) + kk * (UMMA_K * 128 >> 4), idesc_o, acc || kk > 0);
             };
-            bool ok = n_tiles > 0 && mbar_wait(q_full, 0, a.err, abort_flag);
-            for (int u = 0; ok && u < 2; ++u)
-                if (unit_count(u) > 0) {
-                    const int j = unit_tile(u, 0);
-                    ok = mbar_wait(k_full(j & 1), 0, a.err, abort_flag);
-                    if (!ok) break;
-                    fence_after();
-                    issue_s(u, j);
-                    if (!PAIR || u == 1) umma_commit(k_empty(j & 1));
-                }
-            for (int i = 0; ok && i < unit_count(0); ++i)
-                for (int u = 0; ok && u < 2; ++u) {
-                    if (i >= unit_count(u)) break;
-                    const int j = unit_tile(u, i), s = j & 1;
-                    ok = mbar_wait(p_ready(u), i & 1, a.err, abort_flag) && mbar_wait(TMA ? v_clean(s) : v_full(s), (j >> 1) & 1, a.err, abort_flag);
-                    if (!ok) break;
-                    fence_after();
-                    issue_o(u, j, i > 0);
-                    if (!PAIR || u == 1) umma_commit(v_empty(s));
-                    if (i + 1 < unit_count(u)) {
-                        const int jn = unit_tile(u, i + 1);
-                        ok = mbar_wait(k_full(jn & 1), (jn >> 1) & 1, a.err, abort_flag);
-                        if (!ok) break;
-                        fence_after();
-                        issue_s(u, jn);
-                        if (!PAIR || u == 1) umma_commit(k_empty(jn & 1));
-                    } else
-                        umma_commit(o_done(u));
-                }
-            if (!ok && n_tiles > 0) { // products in flight end before tensor memory is freed
-                umma_commit(drain);
-                settle(drain, 0);
+            if (count > 0) {
+                wait(q_full, 0);
+                wait(k_full(PAIR ? 0 : u), 0);
+                __syncwarp();
+                fence_after();
+                issue_s(PAIR ? 0 : u);
+            }
+            for (int i = 0; i < count; ++i) {
+                const int s = PAIR ? i & 1 : u, use = PAIR ? i >> 1 : i; // slot of tile i of the unit, how often it was filled before
+                const int sn = PAIR ? (i + 1) & 1 : u, use_n = PAIR ? (i + 1) >> 1 : i + 1;
+                // the tiles first: they have normally long been there
+                wait(TMA ? v_clean(s) : v_full(s), use & 1);
+                if (i + 1 < count) wait(k_full(sn), use_n & 1);
+                wait(p_ready(u), i & 1);
+                __syncwarp();
+                fence_after();
+                issue_o(s, 0, i > 0);
+                wait(p_rest(u), i & 1);
+                __syncwarp();
+                fence_after();
+                issue_o(s, 64 / UMMA_K, true);
+                commit(v_empty(s));
+                if (i + 1 < count) issue_s(sn);
+                else commit(o_done(u));
+            }
+            if (*abort_flag && count > 0) { // products in flight end before tensor memory is freed
+                __syncwarp();
+                commit(drain(u));
+                settle(drain(u), 0);
             }
         }
         __syncwarp();
     } else {
-        const int u = warp >> 2, row = threadIdx.x & 127;
+        const int u = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + u * 4 + (warp & 3);
+        // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
+        {
+            constexpr int CH = D / 8;
+            for (int idx = threadIdx.x; idx < ROWS * CH; idx += SOFT_THREADS) {
+                const int r = idx / CH, c = idx % CH, rr = r0 + r;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < rows) x = *(const uint4 *)((const bf16 *)a.q + (long)(row0 + rr / a.group) * a.q_stride + (long)(kvh * a.group + rr % a.group) * D + c * 8);
+                if (Q8)
+                    x = make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
+                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c), x);
+            }
+            fence_proxy_async();
+            mbar_arrive(q_full);
+        }
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + u * 128u, t_o = tmem + lanes + 256u + u * 128u;
+        const uint32_t t_s = tmem + lanes + u * 128u + half * 64u; // this thread's scores: 64 columns; its weights: the first 32 of them
+        const uint32_t t_o = tmem + lanes + 256u + u * 128u + half * (D / 2);
         const int rr = (PAIR ? u * TQ : 0) + row, gr = r0 + rr; // row of the tiles, of the (sequence, KV head)
         const bool live = rr < rows;
         const int pos = live ? len + gr / a.group : -1;
         const float qs = a.scale_log2;
         const float *sc = (const float *)(gen + C::OFF_SC);
+        float *red = (float *)(gen + C::OFF_RED);
         float m_used = -INFINITY, l = 0.f;
-        bool ok = true;
         const int count = unit_count(u);
+        if (TURNS && u == 1) bar_arrive<BAR_A, SOFT_THREADS>(); // A's first turn
         for (int i = 0; i < count; ++i) {
-            const int j = unit_tile(u, i), t0 = key0(j);
-            ok = mbar_wait(s_full(u), i & 1, a.err, abort_flag);
-            if (Q8 && ok) ok = mbar_wait(sc_full(j & 7), (j >> 3) & 1, a.err, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+            const int j = unit_tile(u, i), t0 = key0(j) + half * 64;
+            mbar_wait(s_full(u), i & 1, a.err, abort_flag); // see the MMA warps about waits that give up
+            if (Q8) mbar_wait(sc_full(j & 7), (j >> 3) & 1, a.err, abort_flag);
+            __syncwarp();
             fence_after();
-            const bool masked = partial(t0);
+            const bool masked = partial(key0(j));
             const int hi = pos - t0, lo = a.window ? pos - a.window + 1 - t0 : -1, sk = a.sinks - t0; // columns c <= hi with c >= lo or c < sk
-            const float *ks = sc + (j & 7) * 256, *vs = ks + 128;
-            auto scores = [&](int c0, float (&v)[32]) {
-                tmem_ld32(t_s + c0, v);
+            const float *ks = sc + (j & 7) * 256 + half * 64, *vs = ks + 128;
+            // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
+            auto finish = [&](int c0, uint32_t (&r)[32]) {
                 if (Q8) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
-                        const float4 f = *(const float4 *)(ks + c0 + e);
-                        v[e] *= f.x; v[e + 1] *= f.y; v[e + 2] *= f.z; v[e + 3] *= f.w;
+                        const float4 k4 = *(const float4 *)(ks + c0 + e);
+                        const float2 x = mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(k4.x, k4.y));
+                        const float2 y = mul2(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), make_float2(k4.z, k4.w));
+                        r[e] = __float_as_uint(x.x); r[e + 1] = __float_as_uint(x.y); r[e + 2] = __float_as_uint(y.x); r[e + 3] = __float_as_uint(y.y);
                     }
                 }
                 if (masked) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (c0 + e > hi || (c0 + e < lo && c0 + e >= sk)) v[e] = -INFINITY;
+                        if (c0 + e > hi || (c0 + e < lo && c0 + e >= sk)) r[e] = 0xff800000u;
                 }
             };
-            float mx = -INFINITY;
-#pragma unroll 1
-            for (int c0 = 0; c0 < TK; c0 += 32) {
-                float v[32], m0 = -INFINITY, m1 = -INFINITY;
-                scores(c0, v);
+            auto max_of = [&](const uint32_t (&r)[32]) {
+                float x0 = -INFINITY, x1 = -INFINITY, x2 = -INFINITY, x3 = -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) { m0 = fmaxf(fmaxf(m0, v[e]), v[e + 1]); m1 = fmaxf(fmaxf(m1, v[e + 2]), v[e + 3]); }
-                mx = fmaxf(mx, fmaxf(m0, m1));
-            }
-            mx *= qs;
-            float f = 1.f;
-            if (m_used == -INFINITY) m_used = mx; // nothing accumulated yet
-            else if (mx > m_used + 8.f) { f = ex2(m_used - mx); m_used = mx; l *= f; }
-            if (__any_sync(0xffffffffu, f != 1.f)) {
-                // every product so far is complete: S of this tile was issued after them
-#pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += 32) {
-                    float v[32];
-                    uint32_t w[16];
-                    tmem_ld32(t_o + c0, v);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[16 * h + e] * f);
-                        tmem_st16(t_o + c0 + 16 * h, w);
-                    }
+                for (int e = 0; e < 32; e += 8) {
+                    x0 = fmaxf(fmaxf(x0, __uint_as_float(r[e])), __uint_as_float(r[e + 1]));
+                    x1 = fmaxf(fmaxf(x1, __uint_as_float(r[e + 2])), __uint_as_float(r[e + 3]));
+                    x2 = fmaxf(fmaxf(x2, __uint_as_float(r[e + 4])), __uint_as_float(r[e + 5]));
+                    x3 = fmaxf(fmaxf(x3, __uint_as_float(r[e + 6])), __uint_as_float(r[e + 7]));
                 }
-                tmem_st_wait();
+                return fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+            };
+            constexpr bool KEEP = TMA; // 96 registers hold the 64 scores; with 80 they are read a second time
+            uint32_t ra[32], rb[32];
+            float mx;
+            tmem_ask32(t_s, ra);
+            tmem_wait32(ra);
+            if (KEEP) tmem_ask32(t_s + 32, rb);
+            finish(0, ra);
+            mx = max_of(ra);
+            if (!KEEP) tmem_ask32(t_s + 32, rb);
+            tmem_wait32(rb);
+            finish(32, rb);
+            mx = fmaxf(mx, max_of(rb)) * qs;
+            // join with the other half's maximum: both threads of a row then take the same decision
+            float *rm = red + ((i & 1) * 2 + u) * 256 + row;
+            rm[half * 128] = mx;
+            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            mx = fmaxf(mx, rm[(half ^ 1) * 128]);
+            const bool up = mx > m_used + 8.f; // -inf: a row's first keys
+            if (__any_sync(0xffffffffu, up)) {
+                float f = 1.f;
+                if (up) { f = m_used == -INFINITY ? 1.f : ex2(m_used - mx); m_used = mx; l *= f; }
+                if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+                    // every product so far is complete: S of this tile was issued after them
+#pragma unroll 1
+                    for (int d0 = 0; d0 < D / 2; d0 += 16) {
+                        uint32_t x[16];
+                        tmem_ld16u(t_o + d0, x);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+                        tmem_st16(t_o + d0, x);
+                    }
+                    tmem_st_wait();
+                    fence_before();
+                    asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory"); // the other half's columns too
+                }
             }
+            // A and B take turns at the weights: one tile's run under the other's products, not against its weights
+            if (TURNS) { if (u == 0) named_bar<BAR_A, SOFT_THREADS>(); else named_bar<BAR_B, SOFT_THREADS>(); }
             const float mb = m_used == -INFINITY ? 0.f : m_used;
-            float l0 = 0.f, l1 = 0.f;
-#pragma unroll 1
-            for (int c0 = 0; c0 < TK; c0 += 32) {
-                float v[32];
+            const float2 q2 = make_float2(qs, qs), m2 = make_float2(-mb, -mb);
+            float2 ls = make_float2(0.f, 0.f);
+            auto weigh = [&](int c0, uint32_t (&r)[32]) {
                 uint32_t w[16];
-                scores(c0, v);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    float p0 = ex2(fmaf(v[e], qs, -mb)), p1 = ex2(fmaf(v[e + 1], qs, -mb));
-                    l0 += p0;
-                    l1 += p1;
-                    if (Q8) {
-                        const float2 g = *(const float2 *)(vs + c0 + e);
-                        p0 = masked && v[e] == -INFINITY ? 0.f : p0 * g.x; // a masked key's scale may be anything
-                        p1 = masked && v[e + 1] == -INFINITY ? 0.f : p1 * g.y;
-                    }
-                    w[e >> 1] = pack(p0, p1);
+                for (int k = 0; k < 16; ++k) {
+                    const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
+                    // every fourth pair on the FMA pipes, which the exponentials otherwise leave idle
+                    float2 p = k % 4 == 3 ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
+                    ls = add2(ls, p);
+                    if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
+                    w[k] = pack(p.x, p.y);
                 }
-                tmem_st16(t_s + (c0 >> 1), w);
+                if (Q8 && masked) { // 0 times the scale of an unseen key, which may be anything
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int e = c0 + 2 * k;
+                        if (e > hi || (e < lo && e >= sk)) w[k] &= 0xffff0000u;
+                        if (e + 1 > hi || (e + 1 < lo && e + 1 >= sk)) w[k] &= 0xffffu;
+                    }
+                }
+                tmem_st16(t_s + weight_column(c0), w);
+            };
+            if (KEEP) {
+                weigh(0, ra);
+                weigh(32, rb);
+            } else {
+                weigh(32, rb);
+                tmem_ask32(t_s, ra);
+                tmem_wait32(ra);
+                finish(0, ra);
+                weigh(0, ra);
             }
-            l += l0 + l1;
+            l += ls.x + ls.y;
             tmem_st_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_ready(u));
+            if (lane == 0) mbar_arrive(half ? p_rest(u) : p_ready(u));
+            if (TURNS) { if (u == 0) bar_arrive<BAR_B, SOFT_THREADS>(); else bar_arrive<BAR_A, SOFT_THREADS>(); }
         }
-        if (ok && count > 0) {
+        bool ok = true;
+        if (count > 0) {
             ok = mbar_wait(o_done(u), 0, a.err, abort_flag);
+            if (!PAIR && u == 1) ok = mbar_wait(o_done(0), 0, a.err, abort_flag) && ok; // A's products read the tiles that B's rows go over
             ok = __all_sync(0xffffffffu, ok);
             fence_after();
         }
-        float *ob = (float *)(gen + C::OFF_K), *ml = (float *)(gen + C::OFF_ML); // B's rows for A: [dim][row], over the K (and V) tiles
+        named_bar<BAR_SOFT, SOFT_THREADS>();
+        // sums of the halves; B's rows for A: [dim][row] over the K tiles
+        float *ob = (float *)(gen + C::OFF_K), *mlb = (float *)(gen + C::OFF_ML);
         const bool both = !PAIR && n_tiles > 1;
-        if (both) {
-            if (u == 1) {
-                if (ok) ok = mbar_wait(o_done(0), 0, a.err, abort_flag); // A's products read these tiles too
-                ok = __all_sync(0xffffffffu, ok);
-                if (ok) {
+        red[(u * 2 + half) * 128 + row] = l;
+        if (both && u == 1) {
+            if (half == 0) mlb[row] = m_used;
+            if (ok) {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        float v[32];
-                        tmem_ld32(t_o + c0, v);
+                for (int c0 = 0; c0 < D / 2; c0 += 16) {
+                    uint32_t x[16];
+                    tmem_ld16u(t_o + c0, x);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) ob[(c0 + e) * 128 + row] = v[e];
-                    }
+                    for (int e = 0; e < 16; ++e) ob[(half * (D / 2) + c0 + e) * 128 + row] = __uint_as_float(x[e]);
                 }
-                ml[2 * row] = m_used;
-                ml[2 * row + 1] = l;
             }
-            named_bar<BAR_SOFT, 256>();
         }
+        named_bar<BAR_SOFT, SOFT_THREADS>();
         if (ok && (PAIR || u == 0)) {
+            l = red[u * 256 + row] + red[u * 256 + 128 + row];
             float fa = 1.f, fb = 0.f, m = m_used, den = l;
             if (both) {
-                const float mo = ml[2 * row], lo = ml[2 * row + 1];
+                const float mo = mlb[row], lo = red[256 + row] + red[256 + 128 + row];
                 m = fmaxf(m_used, mo);
                 fa = m_used == -INFINITY ? 0.f : ex2(m_used - m);
                 fb = mo == -INFINITY ? 0.f : ex2(mo - m);
@@ -564,19 +713,19 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
             const long token = row0 + gr / a.group;
             const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
             bf16 *dst = (bf16 *)a.out + token * a.o_stride + (long)head * D;
-            if (a.part_o && live) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
+            if (a.part_o && live && half == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
             const bool give_back = !Q8 && *dirty;
 #pragma unroll 1
-            for (int c0 = 0; c0 < D && n_tiles > 0; c0 += 32) {
-                float v[32], x[32];
-                tmem_ld32(t_o + c0, v); // warp-wide: lanes without a row load too
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] *= fa;
-                if (both) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = fmaf(ob[(c0 + e) * 128 + row], fb, v[e]);
-                }
+            for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2) && n_tiles > 0; c0 += 16) {
+                uint32_t y[16];
+                float v[16], x[16];
+                tmem_ld16u(tmem + lanes + 256u + u * 128u + c0, y); // warp-wide: lanes without a row load too
                 if (!live) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    v[e] = __uint_as_float(y[e]) * fa;
+                    if (both) v[e] = fmaf(ob[(c0 + e) * 128 + row], fb, v[e]);
+                }
                 if (give_back) {
                     for (int j = 0; j < n_tiles; ++j) {
                         const int t0 = key0(j);
@@ -586,12 +735,12 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
                             if (page < 0 || page >= a.kv.n_pages) continue;
                             const bf16 *src = (const bf16 *)a.kv.v + (((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page)) * D + c0;
 #pragma unroll 1
-                            for (int e = 0; e < 32; ++e) {
-                                const float y = __bfloat162float(src[e]);
-                                if (!isfinite(y)) {
+                            for (int e = 0; e < 16; ++e) {
+                                const float z = __bfloat162float(src[e]);
+                                if (!isfinite(z)) {
 #pragma unroll
-                                    for (int k = 0; k < 32; ++k)
-                                        if (k == e) v[k] += y;
+                                    for (int k = 0; k < 16; ++k)
+                                        if (k == e) v[k] += z;
                                 }
                             }
                         }
@@ -599,13 +748,13 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
                 }
                 // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
+                for (int e = 0; e < 16; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
                 if (a.part_o) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    for (int e = 0; e < 16; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
+                    for (int e = 0; e < 16; e += 8)
                         *(uint4 *)(dst + c0 + e) = make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7]));
                 }
             }
@@ -613,7 +762,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) paged_attention_tc_kernel(const 
     }
     fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == W_MMA) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_COLS) : "memory");
     }
@@ -626,7 +775,7 @@ template <int FMT, int D, bool PAIR, bool TMA> cudaError_t launch_tc(const Paged
     if (e != cudaSuccess) return e;
     const int rows = PAIR ? 256 : 128;
     const long tiles = ((long)a.max_new * a.group + rows - 1) / rows;
-    return launch_kernel(paged_attention_tc_kernel<FMT, D, PAIR, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(T_THREADS),
+    return launch_kernel(paged_attention_tc_kernel<FMT, D, PAIR, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA)),
                          TcCfg<D>::SMEM, st, 0, km, vm, a);
 }
 template <int FMT, int D, bool PAIR> cudaError_t tc_by_copy(const PagedAttnArgs &a, cudaStream_t st)
