@@ -36,7 +36,8 @@ using namespace tc;
 constexpr int TQ = 128, TK = 128, HALF = 128 * 128; // bytes of [128 rows][64 bf16]
 constexpr int SOFT_WARPS = 16, SOFT_THREADS = 32 * SOFT_WARPS;
 constexpr uint32_t T_COLS = 512;
-enum { BAR_LOAD = 3, BAR_SOFT = 4, BAR_A = 5, BAR_B = 6, BAR_PAIR = 8 }; // BAR_PAIR .. + 7
+// named barriers: each always with the same number of threads, and no arrival left over
+enum { BAR_OUT_A = 1, BAR_OUT_B = 2, BAR_LOAD = 3, BAR_SOFT = 4, BAR_A = 5, BAR_B = 6, BAR_PAIR = 8 }; // BAR_PAIR .. + 7
 
 template <int D> struct TcCfg {
     static constexpr int TILE = 128 * D * 2;
@@ -217,7 +218,6 @@ __device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities o
     return bad;
 }
 
-constexpr bool TURNS = true;
 // Column (from the unit's first) of the weights of keys k, k + 1: each 32 keys' go over columns of their own half's scores, the
 // second 32 over the last 16, so that the first 32 scores can be read again after them.
 __device__ __forceinline__ constexpr uint32_t weight_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 48 : 0) + ((k & 31) >> 1)); }
@@ -262,6 +262,12 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
     const int r0 = tile * ROWS;
     if (r0 >= all_rows) return;
     const int rows = min(ROWS, all_rows - r0);
+    // new token and head of the tiles' row r.  A quotient of small numbers by way of their floats: (n + 1/2) / group is off by less
+    // than the 1 / (2 group) that could change it while n < 2^22, and n < group + 256
+    const int tok0 = r0 / a.group, head0 = r0 - tok0 * a.group;
+    const float inv_group = 1.f / (float)a.group;
+    auto token_of = [&](int r) { return (int)(((float)(head0 + r) + 0.5f) * inv_group); }; // after tok0
+    auto head_of = [&](int r, int token) { return head0 + r - token * a.group; };
     const int pos_first = len + r0 / a.group, pos_last = len + (r0 + rows - 1) / a.group;
     const int kv_len = pos_last + 1;
     // tiles of 128 keys that hold a key some row sees: sinks, then the window of the first row onwards
@@ -532,14 +538,20 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
         const int u = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + u * 4 + (warp & 3);
         // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
         {
-            constexpr int CH = D / 8;
-            for (int idx = threadIdx.x; idx < ROWS * CH; idx += SOFT_THREADS) {
-                const int r = idx / CH, c = idx % CH, rr = r0 + r;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < rows) x = *(const uint4 *)((const bf16 *)a.q + (long)(row0 + rr / a.group) * a.q_stride + (long)(kvh * a.group + rr % a.group) * D + c * 8);
-                if (Q8)
-                    x = make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
-                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c), x);
+            constexpr int CH = D / 8, N = ROWS * CH / SOFT_THREADS;
+            uint4 x[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int idx = k * SOFT_THREADS + threadIdx.x, r = idx / CH, c = idx % CH, t = token_of(r);
+                x[k] = make_uint4(0, 0, 0, 0);
+                if (r < rows) x[k] = *(const uint4 *)((const bf16 *)a.q + (long)(row0 + tok0 + t) * a.q_stride + (long)(kvh * a.group + head_of(r, t)) * D + c * 8);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int idx = k * SOFT_THREADS + threadIdx.x, r = idx / CH, c = idx % CH;
+                const uint4 y = x[k];
+                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c),
+                       Q8 ? make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.z, y.w, 0x7632)) : y);
             }
             fence_proxy_async();
             mbar_arrive(q_full);
@@ -547,15 +559,15 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + u * 128u + half * 64u; // this thread's scores: 64 columns; its weights: the first 32 of them
         const uint32_t t_o = tmem + lanes + 256u + u * 128u + half * (D / 2);
-        const int rr = (PAIR ? u * TQ : 0) + row, gr = r0 + rr; // row of the tiles, of the (sequence, KV head)
+        const int rr = (PAIR ? u * TQ : 0) + row, my_token = token_of(rr);
         const bool live = rr < rows;
-        const int pos = live ? len + gr / a.group : -1;
+        const int pos = live ? len + tok0 + my_token : -1;
         const float qs = a.scale_log2;
         const float *sc = (const float *)(gen + C::OFF_SC);
         float *red = (float *)(gen + C::OFF_RED);
         float m_used = -INFINITY, l = 0.f;
         const int count = unit_count(u);
-        if (TURNS && u == 1) bar_arrive<BAR_A, SOFT_THREADS>(); // A's first turn
+        if (u == 1 && unit_count(0) > 0) bar_arrive<BAR_A, SOFT_THREADS>(); // A's first turn
         for (int i = 0; i < count; ++i) {
             const int j = unit_tile(u, i), t0 = key0(j) + half * 64;
             mbar_wait(s_full(u), i & 1, a.err, abort_flag); // see the MMA warps about waits that give up
@@ -563,7 +575,12 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
             __syncwarp();
             fence_after();
             const bool masked = partial(key0(j));
-            const int hi = pos - t0, lo = a.window ? pos - a.window + 1 - t0 : -1, sk = a.sinks - t0; // columns c <= hi with c >= lo or c < sk
+            unsigned long long seen = ~0ull; // this thread's columns whose keys the row sees: c <= pos - t0 with c >= lo or c < sinks - t0
+            if (masked) {
+                auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
+                seen = below(pos - t0 + 1);
+                if (a.window) seen &= ~below(pos - a.window + 1 - t0) | below(a.sinks - t0);
+            }
             const float *ks = sc + (j & 7) * 256 + half * 64, *vs = ks + 128;
             // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
             auto finish = [&](int c0, uint32_t (&r)[32]) {
@@ -579,7 +596,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 if (masked) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (c0 + e > hi || (c0 + e < lo && c0 + e >= sk)) r[e] = 0xff800000u;
+                        if (!((uint32_t)(seen >> c0) & (1u << e))) r[e] = 0xff800000u;
                 }
             };
             auto max_of = [&](const uint32_t (&r)[32]) {
@@ -612,8 +629,9 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
             mx = fmaxf(mx, rm[(half ^ 1) * 128]);
             const bool up = mx > m_used + 8.f; // -inf: a row's first keys
             if (__any_sync(0xffffffffu, up)) {
+                // all rows of the warp follow, so that rows whose first keys were few or low do not come one by one
                 float f = 1.f;
-                if (up) { f = m_used == -INFINITY ? 1.f : ex2(m_used - mx); m_used = mx; l *= f; }
+                if (mx > m_used) { f = m_used == -INFINITY ? 1.f : ex2(m_used - mx); m_used = mx; l *= f; }
                 if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
                     // every product so far is complete: S of this tile was issued after them
 #pragma unroll 1
@@ -630,7 +648,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 }
             }
             // A and B take turns at the weights: one tile's run under the other's products, not against its weights
-            if (TURNS) { if (u == 0) named_bar<BAR_A, SOFT_THREADS>(); else named_bar<BAR_B, SOFT_THREADS>(); }
+            if (u == 0) named_bar<BAR_A, SOFT_THREADS>(); else named_bar<BAR_B, SOFT_THREADS>();
             const float mb = m_used == -INFINITY ? 0.f : m_used;
             const float2 q2 = make_float2(qs, qs), m2 = make_float2(-mb, -mb);
             float2 ls = make_float2(0.f, 0.f);
@@ -640,7 +658,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 for (int k = 0; k < 16; ++k) {
                     const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
                     // every fourth pair on the FMA pipes, which the exponentials otherwise leave idle
-                    float2 p = k % 4 == 3 ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
+                    float2 p = (TMA ? k % 2 == 1 : k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
                     ls = add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
                     w[k] = pack(p.x, p.y);
@@ -648,9 +666,8 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 if (Q8 && masked) { // 0 times the scale of an unseen key, which may be anything
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const int e = c0 + 2 * k;
-                        if (e > hi || (e < lo && e >= sk)) w[k] &= 0xffff0000u;
-                        if (e + 1 > hi || (e + 1 < lo && e + 1 >= sk)) w[k] &= 0xffffu;
+                        if (!((uint32_t)(seen >> c0) & (1u << (2 * k)))) w[k] &= 0xffff0000u;
+                        if (!((uint32_t)(seen >> c0) & (2u << (2 * k)))) w[k] &= 0xffffu;
                     }
                 }
                 tmem_st16(t_s + weight_column(c0), w);
@@ -670,7 +687,8 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(half ? p_rest(u) : p_ready(u));
-            if (TURNS) { if (u == 0) bar_arrive<BAR_B, SOFT_THREADS>(); else bar_arrive<BAR_A, SOFT_THREADS>(); }
+            if (u == 0) { if (i < unit_count(1)) bar_arrive<BAR_B, SOFT_THREADS>(); }
+            else if (i + 1 < unit_count(0)) bar_arrive<BAR_A, SOFT_THREADS>();
         }
         bool ok = true;
         if (count > 0) {
@@ -709,10 +727,9 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
             }
             if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum
             const float inv = a.part_o ? 1.f : (den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den));
-            const int head = kvh * a.group + gr % a.group;
-            const long token = row0 + gr / a.group;
+            const int head = kvh * a.group + head_of(rr, my_token);
+            const long token = row0 + tok0 + my_token;
             const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
-            bf16 *dst = (bf16 *)a.out + token * a.o_stride + (long)head * D;
             if (a.part_o && live && half == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
             const bool give_back = !Q8 && *dirty;
 #pragma unroll 1
@@ -752,10 +769,23 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 if (a.part_o) {
 #pragma unroll
                     for (int e = 0; e < 16; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                } else {
+                } else { // through the Q tile, so that whole rows leave together
 #pragma unroll
                     for (int e = 0; e < 16; e += 8)
-                        *(uint4 *)(dst + c0 + e) = make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7]));
+                        sts128(base + C::OFF_Q + (PAIR ? u * C::TILE : 0) + tile_at(row, (c0 + e) >> 3),
+                               make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7])));
+                }
+            }
+            if (!a.part_o && n_tiles > 0) {
+                if (u == 0) named_bar<BAR_OUT_A, SOFT_THREADS / 2>(); else named_bar<BAR_OUT_B, SOFT_THREADS / 2>();
+                constexpr int CH = D / 8;
+                const int first_row = PAIR ? u * TQ : 0;
+#pragma unroll 4
+                for (int idx = threadIdx.x & 255; idx < 128 * CH; idx += SOFT_THREADS / 2) {
+                    const int r = idx / CH, c = idx % CH, t = token_of(first_row + r);
+                    if (first_row + r >= rows) continue;
+                    *(uint4 *)((bf16 *)a.out + (long)(row0 + tok0 + t) * a.o_stride + (long)(kvh * a.group + head_of(first_row + r, t)) * D + c * 8) =
+                        lds128(base + C::OFF_Q + (PAIR ? u * C::TILE : 0) + tile_at(r, c));
                 }
             }
         }
