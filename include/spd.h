@@ -237,9 +237,10 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  * Formats.  A cached row is the head_dim values of one token of one KV head.
  *   SPD_KV_F32, SPD_KV_BF16 : stored as they are (rounded to nearest where the input is wider)
  *   SPD_KV_E4M3 : 8-bit floats and one float32 scale s per row, the smallest power of two with max|x| <= 448 s;
- *                 code = x / s rounded to nearest (exact division); code * s is exact in bfloat16
+ *                 code = x / s rounded to nearest (exact division; within a factor of two of the
+ *                 largest float, codes stop where code * s is still finite); code * s is exact in bfloat16
  *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 / max|x|) rounded to
- *                 nearest, half to even, in -127 .. 127
+ *                 nearest in -127 .. 127 (the factor is within two units in its last place)
  * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0. */
 #define SPD_KV_F32 0
 #define SPD_KV_BF16 1
