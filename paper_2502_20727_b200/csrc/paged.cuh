@@ -35,6 +35,7 @@ struct PagedAttnArgs {
     int window, sinks;            // window 0: everything before the query
     float scale_log2;             // softmax scale times log2(e)
     int splits;                   // ranges the keys of a row tile are cut into
+    int row_tile;                 // general kernel: rows of a thread block (16, 32, 64)
     int stages;                   // paged_attention_rows.cu: set by its launcher
     float *part_o, *part_ml;      // ranges that no cluster adds up (else null): fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
     int *err;
@@ -123,8 +124,8 @@ cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const void
 cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, void *v, long k_stride, long v_stride, int out_bf16,
                            int *err, cudaStream_t st);
 
-// q, out and (for unquantised caches) the pages in one type: bf16 or float32
-cudaError_t launch_paged_attention_simt(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
+// float32 queries, or bf16 ones with head_dim 32
+cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 // Key ranges that one thread-block cluster adds up in shared memory; more go through the workspace.
 constexpr int PAGED_MAX_CLUSTER = 8;
 // bf16 queries, head_dim 64 or 128, at most 16 rows (new tokens x query heads per KV head) per sequence and KV head

@@ -709,9 +709,12 @@ cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st)
 cudaError_t launch_paged_merge(const PagedAttnArgs &a, int q_bf16, cudaStream_t st)
 {
     const dim3 grid((unsigned)(((long)a.rb.n_tokens * a.nq + 3) / 4));
-    if (q_bf16 && a.kv.d == 128) return launch_kernel(paged_merge_kernel<bf16, 128>, grid, dim3(128), 0, st, 0, a);
-    if (q_bf16 && a.kv.d == 64) return launch_kernel(paged_merge_kernel<bf16, 64>, grid, dim3(128), 0, st, 0, a);
-    return cudaErrorInvalidValue;
+    switch (a.kv.d) {
+    case 128: return q_bf16 ? launch_kernel(paged_merge_kernel<bf16, 128>, grid, dim3(128), 0, st, 0, a) : launch_kernel(paged_merge_kernel<float, 128>, grid, dim3(128), 0, st, 0, a);
+    case 64: return q_bf16 ? launch_kernel(paged_merge_kernel<bf16, 64>, grid, dim3(128), 0, st, 0, a) : launch_kernel(paged_merge_kernel<float, 64>, grid, dim3(128), 0, st, 0, a);
+    case 32: return q_bf16 ? launch_kernel(paged_merge_kernel<bf16, 32>, grid, dim3(128), 0, st, 0, a) : launch_kernel(paged_merge_kernel<float, 32>, grid, dim3(128), 0, st, 0, a);
+    default: return cudaErrorInvalidValue;
+    }
 }
 
 } // namespace spd
