@@ -283,11 +283,11 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
     if (dtype != 1 || d == 32) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64: 64 rows 38.7 us, 32
-        // rows 57); ranges where the tiles do not give every SM two thread blocks, of at least four tiles of 64 keys
+        // rows 57); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);
         p.row_tile = rows <= 32 ? 16 : 64;
-        long s = 2L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
-        if (s > (keys + 255) / 256) s = (keys + 255) / 256;
+        long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
+        if (s > (keys + 127) / 128) s = (keys + 127) / 128;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     } else     if (rows <= 16) {
         p.kernel = ATTN_ROWS;
