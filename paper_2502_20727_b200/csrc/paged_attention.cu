@@ -17,7 +17,7 @@ namespace {
 // in shared memory.  Thread (tx, ty) computes the scores of rows ty RPT .. and keys tx + 16 j, four head dims at a time (eight
 // products per 16-byte shared-memory load), the row maxima and sums over its half warp, and the output columns 4 tx + 64 j.
 // Bound: for chunks the FMA pipes, for few rows (RPT 1) the cache reads, which are cut into key ranges over thread blocks.
-// One warp per row, without tiles, took 259 us for 4 ragged chunks of up to 256 tokens where this takes 21 (head_dim 64).
+// One warp per row, without tiles, took 259 us for 4 ragged chunks of up to 256 tokens where this takes 29 (head_dim 64).
 constexpr int GK = 64, G_THREADS = 256;
 
 // float32 caches: the next tile is on its way (cp.async) while this one is computed
@@ -289,7 +289,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
         if (s > (keys + 127) / 128) s = (keys + 127) / 128;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-    } else     if (rows <= 16) {
+    } else     if (rows <= PAGED_MAX_FEW_ROWS) {
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
         // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
@@ -308,10 +308,10 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         p.splits = (int)(s < 1 ? 1 : s);
     }
     else {
-        // one thread block per SM: ranges where the row tiles leave SMs idle, of at least four tiles of 128 keys
+        // two thread blocks per SM: ranges where the row tiles leave some idle, of at least four tiles of 128 keys
         p.kernel = ATTN_TC;
-        const long blocks = (rows + (rows > 128 ? 255 : 127)) / (rows > 128 ? 256 : 128) * nkv * (B > 0 ? B : 1);
-        long s = sm_count() / blocks;
+        const long blocks = (rows + 127) / 128 * nkv * (B > 0 ? B : 1);
+        long s = 2L * sm_count() / blocks;
         if (s > (keys + 511) / 512) s = (keys + 511) / 512;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     }

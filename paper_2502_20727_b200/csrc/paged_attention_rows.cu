@@ -44,11 +44,11 @@ template <int FMT, int D, int RW> struct RowsCfg {
     static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : 6; // with the most thread blocks resident
     static constexpr int MAX_STAGES = 8;
     static constexpr int MERGE = RW * 16 * (D + 4) * 4;    // the warps' partial rows, over the tiles
-    // after the tiles: 16 K scales, 16 V scales per stage; a barrier per stage; abort flag; merged [16][2]
+    // after the tiles: 16 K scales, 16 V scales per stage; a barrier per stage; abort flag; merged [16][2], weights [16][RW], rows' places [16], ranges' weights [16][8]
     static constexpr int off_sc(int st) { return RW * st * 2 * TILE > MERGE ? RW * st * 2 * TILE : (MERGE + 1023) / 1024 * 1024; }
     static constexpr int off_bar(int st) { return off_sc(st) + (Q8 ? RW * st * 128 : 0); }
-    static constexpr int off_pml(int st) { return off_bar(st) + RW * st * 8 + 16; }
-    static constexpr int smem(int st) { return off_pml(st) + 128 + 1024; } // + alignment slack
+    static constexpr int off_pml(int st) { return (off_bar(st) + RW * st * 8 + 16 + 15) / 16 * 16; }
+    static constexpr int smem(int st) { return off_pml(st) + 128 + 16 * RW * 4 + 128 + 16 * PAGED_MAX_CLUSTER * 4 + 1024; } // + alignment slack
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
@@ -177,8 +177,9 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     const int n_blocks = n_sink + (kv_len + BK16 - 1) / BK16 - first;
     // short sequences are cut into fewer ranges, of at least 8 blocks
     const int splits = min(a.splits, (n_blocks + 7) / 8);
-    const int j_begin = split < splits ? (int)((long)n_blocks * split / splits) : 0;
-    const int j_end = split < splits ? (int)((long)n_blocks * (split + 1) / splits) : 0;
+    const int per = splits > 1 ? n_blocks / splits : n_blocks, extra = n_blocks - per * splits; // the first `extra` ranges get one more
+    const int j_begin = split < splits ? split * per + min(split, extra) : 0;
+    const int j_end = split < splits ? j_begin + per + (split < extra ? 1 : 0) : 0;
 
     const int32_t *bt = a.rb.table + (long)b * a.rb.max_pages;
     const int bpp = a.kv.page / BK16; // TMA: blocks per page
@@ -192,14 +193,13 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         return ((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page);
     };
     // TMA: cached row of the first key of block j (a bad page id: page 0, with the error bit); else of this lane's key (lane & 15), or -1
+    auto row_of = [&](int blk, int page) -> long {
+        if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); page = 0; }
+        return ((long)page * a.kv.nkv + kvh) * a.kv.page + (bpp == 1 ? 0 : blk % bpp * BK16);
+    };
     auto lookup_block = [&](int j) -> long {
         const int blk = block_of(j);
-        if (TMA) {
-            const int pi = bpp == 1 ? blk : blk / bpp;
-            int page = bt[pi];
-            if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); page = 0; }
-            return ((long)page * a.kv.nkv + kvh) * a.kv.page + (bpp == 1 ? 0 : (blk - pi * bpp) * BK16);
-        }
+        if (TMA) return row_of(blk, bt[bpp == 1 ? blk : blk / bpp]);
         const int t = blk * BK16 + (lane & 15);
         return row_valid(t) ? lookup(t) : -1L;
     };
@@ -236,9 +236,33 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
 
     const int n_mine = (j_end - j_begin - warp + RW - 1) / RW; // blocks j_begin + warp, + RW, ...
     auto mine = [&](int i) { return j_begin + warp + i * RW; };
+    // The tiles and Q are asked for together: page ids of the first tiles (one lane each), Q as it lies, then the tiles.
+    int first_page = 0;
+    if (TMA) {
+        const int blk = block_of(j_begin + warp + lane * RW);
+        if (lane < ST && lane < n_mine) first_page = bt[bpp == 1 ? blk : blk / bpp];
+    }
+    uint4 q_raw[NR][D / 32];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        const int r = g + 8 * n;
+        const bool live = r < rows;
+        const int i = live ? r / a.group : 0, head = live ? r - i * a.group : 0;
+        const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) { // a 16-byte K chunk is 8 dims (bf16) or 16 (codes)
+            const int dim = Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
+            q_raw[n][m] = live ? *(const uint4 *)(qp + dim) : make_uint4(0, 0, 0, 0);
+        }
+    }
     for (int s = 0; s < ST; ++s) {
-        if (s < n_mine) load_block(s, lookup_block(mine(s)));
-        if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+        if (TMA) {
+            const int page = __shfl_sync(0xffffffffu, first_page, s & 31);
+            if (s < n_mine) load_block(s, row_of(block_of(mine(s)), page));
+        } else {
+            if (s < n_mine) load_block(s, lookup_block(mine(s)));
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
     }
     long where = ST < n_mine ? lookup_block(mine(ST)) : 0;
 
@@ -249,16 +273,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     int pos[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        const int r = g + 8 * n;
-        const bool live = r < rows;
-        const int i = live ? r / a.group : 0, head = live ? r % a.group : 0;
-        const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
-        uint4 u[D / 32];
-#pragma unroll
-        for (int m = 0; m < D / 32; ++m) { // a 16-byte K chunk is 8 dims (bf16) or 16 (codes)
-            const int dim = Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
-            u[m] = live ? *(const uint4 *)(qp + dim) : make_uint4(0, 0, 0, 0);
-        }
+        uint4 (&u)[D / 32] = q_raw[n];
         float my_qs = a.scale_log2;
         if (Q8) {
             uint32_t top = 0; // largest magnitude's bits
@@ -521,29 +536,43 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         }
     }
     __syncthreads();
+    // per row: the warps' weights relative to the block's maximum, its maximum and sum, where the row goes
     const bool clustered = a.splits > 1 && !a.part_o;
     const long plane = (long)a.rb.n_tokens * a.nq;
-    auto store = [&](int r, int c, float x, float y, float den) {
-        const int i = r / a.group, head = kvh * a.group + r % a.group;
-        const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
-        *(uint32_t *)((bf16 *)a.out + (long)(row0 + i) * a.o_stride + (long)head * D + c) = pack(x * inv, y * inv);
-    };
-    for (int idx = threadIdx.x; idx < rows * (D / 2); idx += R_THREADS) {
-        const int r = idx / (D / 2), c = idx % (D / 2) * 2;
-        float m = -INFINITY, den = 0.f, x = 0.f, y = 0.f;
+    float *wt = pml + 32;                // [16][RW]
+    long *dst_of = (long *)(wt + 16 * RW); // [16]
+    float *cw = (float *)(dst_of + 16);    // [16][ranges of a cluster]
+    if (threadIdx.x < rows) {
+        const int r = threadIdx.x, i = r / a.group, head = kvh * a.group + r - i * a.group;
+        float m = -INFINITY, den = 0.f;
 #pragma unroll
         for (int w = 0; w < RW; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
 #pragma unroll
         for (int w = 0; w < RW; ++w) {
             const float mw = ml[(w * 16 + r) * 2], f = mw == -INFINITY ? 0.f : ex2(mw - m);
+            wt[r * RW + w] = f;
             den = fmaf(ml[(w * 16 + r) * 2 + 1], f, den);
+        }
+        if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum: not an empty range
+        pml[2 * r] = m;
+        pml[2 * r + 1] = den;
+        dst_of[r] = a.part_o ? (long)split * plane + (long)(row0 + i) * a.nq + head : (long)(row0 + i) * a.o_stride + (long)head * D;
+    }
+    __syncthreads();
+    auto inverse = [](float den) { return den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den); };
+#pragma unroll 4
+    for (int idx = threadIdx.x; idx < rows * (D / 2); idx += R_THREADS) {
+        const int r = idx / (D / 2), c = idx % (D / 2) * 2;
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 0; w < RW; ++w) {
+            const float f = wt[r * RW + w];
             const float2 v = *(const float2 *)(mo + (w * 16 + r) * (D + 2) + c);
             x = fmaf(v.x, f, x);
             y = fmaf(v.y, f, y);
         }
-        const int i = r / a.group, head = kvh * a.group + r % a.group;
         if (!Q8 && any_dirty) { // the values taken out above, for the rows that see them
-            const int p = len + i;
+            const int p = len + r / a.group;
             for (int j = j_begin; j < j_end; ++j) {
                 const int t0 = block_of(j) * BK16;
                 for (int t = t0; t < t0 + BK16 && !seen_by_all(t0); ++t) {
@@ -557,15 +586,15 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 }
             }
         }
-        if (a.splits == 1) { store(r, c, x, y, den); continue; }
-        if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum: not an empty range
-        if (clustered) { // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
+        if (a.splits == 1) {
+            const float inv = inverse(pml[2 * r + 1]);
+            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x * inv, y * inv);
+        } else if (clustered) // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
             *(float2 *)(mo + r * (D + 2) + c) = make_float2(x, y);
-            if (c == 0) { pml[2 * r] = m; pml[2 * r + 1] = den; }
-        } else {
-            const long w = (long)split * plane + (long)(row0 + i) * a.nq + head;
-            if (m != -INFINITY) *(float2 *)(a.part_o + w * D + c) = make_float2(x, y);
-            if (c == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
+        else {
+            const float m = pml[2 * r];
+            if (m != -INFINITY) *(float2 *)(a.part_o + dst_of[r] * D + c) = make_float2(x, y);
+            if (c == 0) *(float2 *)(a.part_ml + dst_of[r] * 2) = make_float2(m, pml[2 * r + 1]);
         }
     }
     if (clustered) {
@@ -576,18 +605,39 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(tc::mapa_shared(addr, rank)) : "memory");
             return v;
         };
+        // per row: the ranges' weights, with the sum's reciprocal in them (over the warps' weights, which have been used)
+        if (threadIdx.x < rows) {
+            const int r = threadIdx.x;
+            float2 q[PAGED_MAX_CLUSTER];
+            float m = -INFINITY, den = 0.f;
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) q[s] = s < splits ? peer2(pml_addr + 8 * r, s) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) m = fmaxf(m, q[s].x);
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) {
+                q[s].x = q[s].x == -INFINITY ? 0.f : ex2(q[s].x - m);
+                den = fmaf(q[s].y, q[s].x, den);
+            }
+            const float inv = inverse(den);
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s)
+                if (s < splits) cw[r * PAGED_MAX_CLUSTER + s] = q[s].x * inv;
+        }
+        __syncthreads();
         for (int idx = split + a.splits * (int)threadIdx.x; idx < rows * (D / 2); idx += a.splits * R_THREADS) {
             const int r = idx / (D / 2), c = idx % (D / 2) * 2;
-            float m = -INFINITY, den = 0.f, x = 0.f, y = 0.f;
-            for (int s = 0; s < splits; ++s) m = fmaxf(m, peer2(pml_addr + 8 * r, s).x);
-            for (int s = 0; s < splits; ++s) {
-                const float2 q = peer2(pml_addr + 8 * r, s), v = peer2(mo_addr + (r * (D + 2) + c) * 4, s);
-                const float f = q.x == -INFINITY ? 0.f : ex2(q.x - m);
-                den = fmaf(q.y, f, den);
-                x = fmaf(v.x, f, x);
-                y = fmaf(v.y, f, y);
+            float2 v[PAGED_MAX_CLUSTER];
+            float x = 0.f, y = 0.f;
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) v[s] = s < splits ? peer2(mo_addr + (r * (D + 2) + c) * 4, s) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) {
+                const float f = s < splits ? cw[r * PAGED_MAX_CLUSTER + s] : 0.f;
+                x = fmaf(v[s].x, f, x);
+                y = fmaf(v[s].y, f, y);
             }
-            store(r, c, x, y, den);
+            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x, y);
         }
         tc::cluster_sync(); // no block exits while a peer still reads its shared memory
     }

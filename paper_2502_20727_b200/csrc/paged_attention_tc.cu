@@ -2,20 +2,19 @@
 // context, drafts of many tokens, grouped-query batches.
 //
 // The rows of a (sequence, KV head) are packed: row r = new token r / group, query head r % group of the KV head, so that the
-// query heads of a group share every K/V tile.  A thread block serves two 128-row tiles A and B (PAIR), which take turns on the
-// tensor cores: while one tile's softmax runs, the other's products do.  Where a (sequence, KV head) has at most 128 rows, A and
-// B are the same rows on alternate key tiles (each with a maximum, a sum and an accumulator of its own, added up at the end), so
-// that the products of one key tile run under the softmax of the other there too.
+// query heads of a group share every K/V tile.  A thread block serves one tile of 128 rows, and two blocks share an SM (each 256
+// columns of tensor memory and 110 KB of shared memory): one's products run under the other's softmax, start and end.  One block
+// with two tiles that shared their K/V tiles and took turns was no faster on long contexts (2048 tokens on 14336, 64 heads: 1168
+// us against 1041) and slower on short ones (window of 1024: 181 against 141 us), where it waited for itself at both ends.
 // Per tile of 128 keys and 128 rows:
 //   S = Q K^T      tcgen05.mma, Q and K as K-major 128B-swizzled tiles, accumulator in tensor memory
 //   P = softmax    thread = row and half of the keys: maximum (joined with the other half's), then the weights, which go back
 //                  to tensor memory as bf16 over the scores already read
 //   O += P V       tcgen05.mma with P read from tensor memory and V as the MN-major operand ([key][dim] rows as they are
 //                  stored); O stays in tensor memory and is rescaled there only when the row maximum has grown by more than 2^8
-// Tensor memory (512 columns): S/P of A and B at 0 and 128, O of A and B at 256 and 384.
-// Warps: 0-15 softmax (two threads per row, four warps per scheduler: one thread per row left the schedulers waiting on their
-// own instructions' latencies), then the load warps, then two that issue the MMAs of A and of B.  K and V tiles have rings of two;
-// a K tile is free once S is computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a
+// Tensor memory: S and P at column 0, O at 128.
+// Warps: 0-7 softmax (two threads per row: one per row left the schedulers waiting on their own instructions' latencies), then the
+// load warps, then one that issues the MMAs.  There is one K and one V slot; K is free once S is computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a
 // second load warp looks after V, see below); 8-bit pages (and bf16 pages of other sizes) by four load warps, which widen the
 // codes to bf16 on the way into shared memory.  The pairs that widening a 32-bit word gives are (0, 2) and (1, 3) of its four
 // codes: the head dims of Q, K and V all sit in that order, and the output is put right when it is stored.  Row scales multiply
@@ -34,20 +33,17 @@ namespace {
 using namespace tc;
 
 constexpr int TQ = 128, TK = 128, HALF = 128 * 128; // bytes of [128 rows][64 bf16]
-constexpr int SOFT_WARPS = 16, SOFT_THREADS = 32 * SOFT_WARPS;
-constexpr uint32_t T_COLS = 512;
 // named barriers: each always with the same number of threads, and no arrival left over
-enum { BAR_OUT_A = 1, BAR_OUT_B = 2, BAR_LOAD = 3, BAR_SOFT = 4, BAR_A = 5, BAR_B = 6, BAR_PAIR = 8 }; // BAR_PAIR .. + 7
+enum { BAR_OUT = 1, BAR_LOAD = 2, BAR_PAIR = 4 }; // BAR_PAIR .. + 3
 
 template <int D> struct TcCfg {
     static constexpr int TILE = 128 * D * 2;
-    static constexpr int OFF_Q = 0, OFF_K = 2 * TILE, OFF_V = OFF_K + 2 * TILE;
-    static constexpr int OFF_SC = OFF_V + 2 * TILE;            // [8][256] K and V scales of a tile
+    static constexpr int OFF_Q = 0, OFF_K = TILE, OFF_V = OFF_K + TILE;
+    static constexpr int OFF_SC = OFF_V + TILE;                //  [8][256] K and V scales of a tile
     static constexpr int OFF_ROW = OFF_SC + 8 * 1024;          // [2][128] cached rows of a tile's keys
     static constexpr int OFF_BAR = OFF_ROW + 2 * 1024;
-    static constexpr int OFF_RED = OFF_BAR + 512;              // [2 parities][2 units][2 halves][128] maxima; sums at the end
-    static constexpr int OFF_ML = OFF_RED + 4096;              // [128] maximum of B
-    static constexpr int SMEM = OFF_ML + 512 + 1024;           // + alignment slack
+    static constexpr int OFF_RED = OFF_BAR + 512;              // [2 parities][2 halves][128] maxima; sums at the end
+    static constexpr int SMEM = OFF_RED + 2048 + 1024;         // + alignment slack
 };
 
 // Shared-memory descriptors in two words: 128B-swizzled tiles, 8-row groups 1024 bytes apart.  Word 0 holds the address / 16 (and,
@@ -130,7 +126,6 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 template <int ID, int N> __device__ __forceinline__ void named_bar() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
-template <int ID, int N> __device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -222,30 +217,24 @@ __device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities o
 // second 32 over the last 16, so that the first 32 scores can be read again after them.
 __device__ __forceinline__ constexpr uint32_t weight_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 48 : 0) + ((k & 31) >> 1)); }
 constexpr int load_warps(bool tma) { return tma ? 2 : 4; }
-constexpr int tc_threads(bool tma) { return SOFT_THREADS + 32 * (load_warps(tma) + 2); } // 640 x 96 or 704 x 80 registers
+constexpr int SOFT_WARPS = 8, SOFT_THREADS = 32 * SOFT_WARPS;
+constexpr int tc_threads(bool tma) { return SOFT_THREADS + 32 * (load_warps(tma) + 1); } // two blocks: 80 registers a thread, or 72
 
-template <int FMT, int D, bool PAIR, bool TMA>
-__global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+template <int FMT, int D, bool TMA>
+__global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                           const __grid_constant__ PagedAttnArgs a)
 {
     using C = TcCfg<D>;
     constexpr bool Q8 = FMT != KV_BF16;
+    constexpr uint32_t T_COLS = 256, T_O = 128;
     constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA);
     extern __shared__ uint8_t tc_raw[];
     uint8_t *gen = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(gen), bars = base + C::OFF_BAR;
-    const uint32_t q_full = bars;
-    auto k_full = [&](int s) { return bars + 8u * (1 + s); };
-    auto k_empty = [&](int s) { return bars + 8u * (3 + s); };
-    auto v_full = [&](int s) { return bars + 8u * (5 + s); };
-    auto v_empty = [&](int s) { return bars + 8u * (7 + s); };
-    auto v_clean = [&](int s) { return bars + 8u * (9 + s); };
-    auto s_full = [&](int u) { return bars + 8u * (11 + u); };
-    auto p_ready = [&](int u) { return bars + 8u * (13 + u); };      // weights of a tile's first 64 keys
-    auto p_rest = [&](int u) { return bars + 8u * (26 + u); };       // ... of the others
-    auto o_done = [&](int u) { return bars + 8u * (15 + u); };
-    auto sc_full = [&](int s) { return bars + 8u * (17 + s); };
-    auto drain = [&](int u) { return bars + 8u * (28 + u); };
+    const uint32_t q_full = bars, k_full = bars + 8, k_empty = bars + 16, v_full = bars + 24, v_empty = bars + 32, v_clean = bars + 40, s_full = bars + 48;
+    const uint32_t p_ready = bars + 56, p_rest = bars + 64; // weights of a tile's first 64 keys, of the others
+    const uint32_t o_done = bars + 72, drain = bars + 80;
+    auto sc_full = [&](int s) { return bars + 8u * (11 + s); };
     uint32_t *tmem_slot = (uint32_t *)(gen + C::OFF_BAR + 8 * 40);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     volatile int *dirty = (volatile int *)(tmem_slot + 2);
@@ -256,7 +245,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
     const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
     int row0, n_new, len;
     if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
-    constexpr int ROWS = PAIR ? 2 * TQ : TQ;
+    constexpr int ROWS = TQ;
     const int all_rows = n_new * a.group;
     const int tile = (int)gridDim.x - 1 - (int)blockIdx.x; // the longest rows first
     const int r0 = tile * ROWS;
@@ -285,20 +274,17 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
         *abort_flag = 0;
         *dirty = 0;
         mbar_init(q_full, SOFT_THREADS);
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(k_full(s), TMA ? 1 : 128);
-            mbar_init(v_full(s), TMA ? 1 : 128);
-            mbar_init(k_empty(s), PAIR ? 2 : 1); // both units read a tile, or one
-            mbar_init(v_empty(s), PAIR ? 2 : 1);
-            mbar_init(v_clean(s), 1);
-            mbar_init(s_full(s), 1);
-            mbar_init(p_ready(s), 4);
-            mbar_init(p_rest(s), 4);
-            mbar_init(o_done(s), 1);
-        }
+        mbar_init(k_full, TMA ? 1 : 128);
+        mbar_init(v_full, TMA ? 1 : 128);
+        mbar_init(k_empty, 1);
+        mbar_init(v_empty, 1);
+        mbar_init(v_clean, 1);
+        mbar_init(s_full, 1);
+        mbar_init(p_ready, 4);
+        mbar_init(p_rest, 4);
+        mbar_init(o_done, 1);
+        mbar_init(drain, 1);
         for (int s = 0; s < 8; ++s) mbar_init(sc_full(s), 128);
-        mbar_init(drain(0), 1);
-        mbar_init(drain(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == W_MMA) {
@@ -309,17 +295,12 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
     __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_slot;
-    // unit u (A, B) takes tiles unit_tile(u, 0), unit_tile(u, 1), ...
-    auto unit_tile = [&](int u, int i) { return PAIR ? i : 2 * i + u; };
-    auto unit_count = [&](int u) { return PAIR ? n_tiles : (n_tiles - u + 1) / 2; };
-
     if (warp >= W_LOAD && warp < W_MMA) {
         const int tid = threadIdx.x - 32 * W_LOAD;
         // one box = 16 keys x 64 dims; lane = (16 keys, half of the head); 16 keys that no row needs come as zeros (a row beyond the map)
         constexpr int BOXES = 8 * (D / 64);
         auto tma_tile = [&](int j, bool is_v) {
-            const int s = j & 1;
-            const uint32_t full = is_v ? v_full(s) : k_full(s);
+            const uint32_t full = is_v ? v_full : k_full;
             const int t = key0(j) + (lane & 7) * 16, h = lane >> 3;
             long row = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
             if (t < kv_len && (t + 15 >= lo_min || t < a.sinks)) {
@@ -329,38 +310,34 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 row = ((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page);
             }
             bool ok = true;
-            if (j >= 2) ok = mbar_wait(is_v ? v_empty(s) : k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
+            if (j > 0) ok = mbar_wait(is_v ? v_empty : k_empty, (j - 1) & 1, a.err, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) return false;
             if (lane == 0) mbar_expect_tx(full, C::TILE);
             __syncwarp();
             if (lane < BOXES)
-                tma_load_3d(base + (is_v ? C::OFF_V : C::OFF_K) + s * C::TILE + h * HALF + (lane & 7) * 2048, (const CUtensorMap *)(is_v ? &v_map : &k_map),
+                tma_load_3d(base + (is_v ? C::OFF_V : C::OFF_K) + h * HALF + (lane & 7) * 2048, (const CUtensorMap *)(is_v ? &v_map : &k_map),
                             h * 64, (int)row, 0, full);
             return true;
         };
         bool ok = true;
         if (TMA) {
+            // The first warp asks for the K tiles, the second for the V tiles.  It also passes them on to the MMA warps: those with
+            // keys that not every row sees without the values that 0 would not cancel.
             if (warp == W_LOAD) {
-                int k_in = 0, v_in = 0; // tiles asked for
-                for (int j = 0; ok && j < n_tiles; ++j) {
-                    ok = tma_tile(j, false);
-                    k_in += ok;
-                    ok = ok && tma_tile(j, true);
-                    v_in += ok;
-                }
-                if (!ok) { // copies in flight land before the block ends
-                    for (int j = max(0, k_in - 2); j < k_in; ++j) settle(k_full(j & 1), (j >> 1) & 1);
-                    for (int j = max(0, v_in - 2); j < v_in; ++j) settle(v_full(j & 1), (j >> 1) & 1);
-                }
+                int in = 0;
+                for (; ok && in < n_tiles; in += ok) ok = tma_tile(in, false);
+                if (!ok && in > 0) settle(k_full, (in - 1) & 1); // a copy in flight lands before the block ends
             } else {
-                // pass every V tile on to the MMA warps; those with keys that not every row sees without the values that 0
-                // would not cancel
-                for (int j = 0; ok && j < n_tiles; ++j) {
-                    ok = mbar_wait(v_full(j & 1), (j >> 1) & 1, a.err, abort_flag);
+                int in = 0;
+                for (; ok && in < n_tiles; ) {
+                    ok = tma_tile(in, true);
+                    if (!ok) break;
+                    const int j = in++;
+                    ok = mbar_wait(v_full, j & 1, a.err, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     if (partial(key0(j))) {
-                        const uint32_t v = base + C::OFF_V + (j & 1) * C::TILE + lane * 16;
+                        const uint32_t v = base + C::OFF_V + lane * 16;
                         uint32_t top = 0; // largest magnitude bits of either half
 #pragma unroll 16
                         for (int i = 0; i < C::TILE / 512; ++i) {
@@ -377,8 +354,9 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                         fence_proxy_async();
                         __syncwarp();
                     }
-                    if (lane == 0) mbar_arrive(v_clean(j & 1));
+                    if (lane == 0) mbar_arrive(v_clean);
                 }
+                if (!ok && in > 0) settle(v_full, (in - 1) & 1);
             }
         } else {
             long *rowoff = (long *)(gen + C::OFF_ROW);
@@ -424,21 +402,20 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 uint4 x0[N], x1[N]; // one batch is on its way while the other is widened
                 if (n_tiles > 0) { rows_of(0); fetch(0, 0, a.kv.k, x0); }
                 for (int j = 0; j < n_tiles; ++j) {
-                    const int s = j & 1;
                     fetch(j, 1, a.kv.k, x1);
-                    if (j >= 2) mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    widen(base + C::OFF_K + s * C::TILE, 0, x0);
+                    if (j > 0) mbar_wait(k_empty, (j - 1) & 1, a.err, abort_flag);
+                    widen(base + C::OFF_K, 0, x0);
                     fetch(j, 0, a.kv.v, x0);
-                    widen(base + C::OFF_K + s * C::TILE, 1, x1);
+                    widen(base + C::OFF_K, 1, x1);
                     fence_proxy_async();
-                    mbar_arrive(k_full(s));
+                    mbar_arrive(k_full);
                     fetch(j, 1, a.kv.v, x1);
-                    if (j >= 2) mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    widen(base + C::OFF_V + s * C::TILE, 0, x0);
+                    if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
+                    widen(base + C::OFF_V, 0, x0);
                     if (j + 1 < n_tiles) { rows_of(j + 1); fetch(j + 1, 0, a.kv.k, x0); }
-                    widen(base + C::OFF_V + s * C::TILE, 1, x1);
+                    widen(base + C::OFF_V, 1, x1);
                     fence_proxy_async();
-                    mbar_arrive(v_full(s));
+                    mbar_arrive(v_full);
                 }
             } else {
                 // cp.async, one operand tile behind
@@ -455,87 +432,79 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                     if (partial(key0(j))) { // this thread's own chunks
                         bool bad = false;
                         for (int i = tid; i < 128 * CH; i += 128) {
-                            const uint32_t p = base + C::OFF_V + (j & 1) * C::TILE + tile_at(i / CH, i % CH);
+                            const uint32_t p = base + C::OFF_V + tile_at(i / CH, i % CH);
                             uint4 u = lds128(p);
                             if (clean16(u)) { sts128(p, u); bad = true; }
                         }
                         if (bad) *dirty = 1;
                     }
                     fence_proxy_async();
-                    mbar_arrive(v_full(j & 1));
+                    mbar_arrive(v_full);
                 };
                 for (int j = 0; j < n_tiles; ++j) {
-                    const int s = j & 1;
                     rows_of(j);
-                    if (j >= 2 && ok) ok = mbar_wait(k_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    copy(j, a.kv.k, base + C::OFF_K + s * C::TILE);
+                    if (j > 0) mbar_wait(k_empty, (j - 1) & 1, a.err, abort_flag);
+                    copy(j, a.kv.k, base + C::OFF_K);
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     if (j) landed_v(j - 1);
-                    if (j >= 2 && ok) ok = mbar_wait(v_empty(s), ((j >> 1) - 1) & 1, a.err, abort_flag);
-                    copy(j, a.kv.v, base + C::OFF_V + s * C::TILE);
+                    if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
+                    copy(j, a.kv.v, base + C::OFF_V);
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     fence_proxy_async();
-                    mbar_arrive(k_full(s));
+                    mbar_arrive(k_full);
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
                 if (n_tiles) landed_v(n_tiles - 1);
             }
         }
     } else if (warp >= W_MMA) {
-        {
-            // One warp for the products of A, one for those of B.  A wait that gives up raises the abort flag, after which
-            // every wait returns at once: the loops run out on whatever is there, and the block ends with the error bit set.
-            const int u = warp - W_MMA, count = unit_count(u);
-            constexpr uint32_t idesc_s = make_idesc(TK), idesc_o = make_idesc(D) | (1u << 16); // V: MN-major
-            const uint32_t q_lo = desc_lo(base + C::OFF_Q + (PAIR ? u * C::TILE : 0), 1), k_lo = desc_lo(base + C::OFF_K, 1), v_lo = desc_lo(base + C::OFF_V, HALF >> 4);
-            const uint32_t t_s = tmem + u * 128u, t_o = tmem + 256u + u * 128u;
-            auto wait = [&](uint32_t bar, int parity) { mbar_wait(bar, parity, a.err, abort_flag); };
-            auto issue_s = [&](int s) { // S on K slot s
+        // A wait that gives up raises the abort flag, after which every wait returns at once: the loops run out on whatever is there,
+        // and the block ends with the error bit set.
+        constexpr uint32_t idesc_s = make_idesc(TK), idesc_o = make_idesc(D) | (1u << 16); // V: MN-major
+        const uint32_t q_lo = desc_lo(base + C::OFF_Q, 1), k_lo = desc_lo(base + C::OFF_K, 1), v_lo = desc_lo(base + C::OFF_V, HALF >> 4);
+        auto wait = [&](uint32_t bar, int parity) {
+            mbar_wait(bar, parity, a.err, abort_flag);
+            __syncwarp();
+            fence_after();
+        };
+        auto issue_s = [&] {
 #pragma unroll
-                for (int kk = 0; kk < D / UMMA_K; ++kk)
-                    umma_ss(t_s, q_lo + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, k_lo + s * (C::TILE >> 4) + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, idesc_s, kk > 0);
-                commit(s_full(u));
-                commit(k_empty(s));
-            };
-            auto issue_o = [&](int s, int kk0, bool acc) { // 64 keys
+            for (int kk = 0; kk < D / UMMA_K; ++kk)
+                umma_ss(tmem, q_lo + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, k_lo + (kk >> 2) * (HALF >> 4) + (kk & 3) * 2, idesc_s, kk > 0);
+            commit(s_full);
+            commit(k_empty);
+        };
+        auto issue_o = [&](int kk0, bool acc) { // 64 keys
 #pragma unroll
-                for (int kk = kk0; kk < kk0 + 64 / UMMA_K; ++kk)
-                    umma_ts(t_o, t_s + weight_column(16 * kk), v_lo + s * (C::TILE >> 4) + kk * (UMMA_K * 128 >> 4), idesc_o, acc || kk > 0);
-            };
-            if (count > 0) {
-                wait(q_full, 0);
-                wait(k_full(PAIR ? 0 : u), 0);
-                __syncwarp();
-                fence_after();
-                issue_s(PAIR ? 0 : u);
-            }
-            for (int i = 0; i < count; ++i) {
-                const int s = PAIR ? i & 1 : u, use = PAIR ? i >> 1 : i; // slot of tile i of the unit, how often it was filled before
-                const int sn = PAIR ? (i + 1) & 1 : u, use_n = PAIR ? (i + 1) >> 1 : i + 1;
-                // the tiles first: they have normally long been there
-                wait(TMA ? v_clean(s) : v_full(s), use & 1);
-                if (i + 1 < count) wait(k_full(sn), use_n & 1);
-                wait(p_ready(u), i & 1);
-                __syncwarp();
-                fence_after();
-                issue_o(s, 0, i > 0);
-                wait(p_rest(u), i & 1);
-                __syncwarp();
-                fence_after();
-                issue_o(s, 64 / UMMA_K, true);
-                commit(v_empty(s));
-                if (i + 1 < count) issue_s(sn);
-                else commit(o_done(u));
-            }
-            if (*abort_flag && count > 0) { // products in flight end before tensor memory is freed
-                __syncwarp();
-                commit(drain(u));
-                settle(drain(u), 0);
-            }
+            for (int kk = kk0; kk < kk0 + 64 / UMMA_K; ++kk)
+                umma_ts(tmem + T_O, tmem + weight_column(16 * kk), v_lo + kk * (UMMA_K * 128 >> 4), idesc_o, acc || kk > 0);
+        };
+        if (n_tiles > 0) {
+            wait(q_full, 0);
+            wait(k_full, 0);
+            issue_s();
+        }
+        for (int j = 0; j < n_tiles; ++j) {
+            wait(TMA ? v_clean : v_full, j & 1);
+            wait(p_ready, j & 1);
+            issue_o(0, j > 0);
+            wait(p_rest, j & 1);
+            issue_o(64 / UMMA_K, true);
+            commit(v_empty);
+            if (j + 1 < n_tiles) {
+                wait(k_full, (j + 1) & 1);
+                issue_s();
+            } else
+                commit(o_done);
+        }
+        if (*abort_flag && n_tiles > 0) { // products in flight end before tensor memory is freed
+            __syncwarp();
+            commit(drain);
+            settle(drain, 0);
         }
         __syncwarp();
     } else {
-        const int u = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + u * 4 + (warp & 3);
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + (warp & 3);
         // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
         {
             constexpr int CH = D / 8, N = ROWS * CH / SOFT_THREADS;
@@ -550,27 +519,25 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
             for (int k = 0; k < N; ++k) {
                 const int idx = k * SOFT_THREADS + threadIdx.x, r = idx / CH, c = idx % CH;
                 const uint4 y = x[k];
-                sts128(base + C::OFF_Q + (r >> 7) * C::TILE + tile_at(r & 127, c),
+                sts128(base + C::OFF_Q + tile_at(r, c),
                        Q8 ? make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.z, y.w, 0x7632)) : y);
             }
             fence_proxy_async();
             mbar_arrive(q_full);
         }
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + u * 128u + half * 64u; // this thread's scores: 64 columns; its weights: the first 32 of them
-        const uint32_t t_o = tmem + lanes + 256u + u * 128u + half * (D / 2);
-        const int rr = (PAIR ? u * TQ : 0) + row, my_token = token_of(rr);
-        const bool live = rr < rows;
+        const uint32_t t_s = tmem + lanes + half * 64u; // this thread's scores: 64 columns; its weights: the first 32 of them
+        const uint32_t t_o = tmem + lanes + T_O + half * (D / 2);
+        const int my_token = token_of(row);
+        const bool live = row < rows;
         const int pos = live ? len + tok0 + my_token : -1;
         const float qs = a.scale_log2;
         const float *sc = (const float *)(gen + C::OFF_SC);
         float *red = (float *)(gen + C::OFF_RED);
         float m_used = -INFINITY, l = 0.f;
-        const int count = unit_count(u);
-        if (u == 1 && unit_count(0) > 0) bar_arrive<BAR_A, SOFT_THREADS>(); // A's first turn
-        for (int i = 0; i < count; ++i) {
-            const int j = unit_tile(u, i), t0 = key0(j) + half * 64;
-            mbar_wait(s_full(u), i & 1, a.err, abort_flag); // see the MMA warps about waits that give up
+        for (int j = 0; j < n_tiles; ++j) {
+            const int t0 = key0(j) + half * 64;
+            mbar_wait(s_full, j & 1, a.err, abort_flag); // see the MMA warp about waits that give up
             if (Q8) mbar_wait(sc_full(j & 7), (j >> 3) & 1, a.err, abort_flag);
             __syncwarp();
             fence_after();
@@ -610,20 +577,18 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 }
                 return fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
             };
-            constexpr bool KEEP = TMA; // 96 registers hold the 64 scores; with 80 they are read a second time
-            uint32_t ra[32], rb[32];
+            uint32_t ra[32], rb[32]; // the first 32 scores are read twice: 64 would not stay in the registers of two blocks
             float mx;
             tmem_ask32(t_s, ra);
             tmem_wait32(ra);
-            if (KEEP) tmem_ask32(t_s + 32, rb);
             finish(0, ra);
             mx = max_of(ra);
-            if (!KEEP) tmem_ask32(t_s + 32, rb);
+            tmem_ask32(t_s + 32, rb);
             tmem_wait32(rb);
             finish(32, rb);
             mx = fmaxf(mx, max_of(rb)) * qs;
             // join with the other half's maximum: both threads of a row then take the same decision
-            float *rm = red + ((i & 1) * 2 + u) * 256 + row;
+            float *rm = red + (j & 1) * 256 + row;
             rm[half * 128] = mx;
             asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
             mx = fmaxf(mx, rm[(half ^ 1) * 128]);
@@ -632,7 +597,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 // all rows of the warp follow, so that rows whose first keys were few or low do not come one by one
                 float f = 1.f;
                 if (mx > m_used) { f = m_used == -INFINITY ? 1.f : ex2(m_used - mx); m_used = mx; l *= f; }
-                if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+                if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
                     // every product so far is complete: S of this tile was issued after them
 #pragma unroll 1
                     for (int d0 = 0; d0 < D / 2; d0 += 16) {
@@ -647,8 +612,6 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                     asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory"); // the other half's columns too
                 }
             }
-            // A and B take turns at the weights: one tile's run under the other's products, not against its weights
-            if (u == 0) named_bar<BAR_A, SOFT_THREADS>(); else named_bar<BAR_B, SOFT_THREADS>();
             const float mb = m_used == -INFINITY ? 0.f : m_used;
             const float2 q2 = make_float2(qs, qs), m2 = make_float2(-mb, -mb);
             float2 ls = make_float2(0.f, 0.f);
@@ -672,77 +635,45 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 }
                 tmem_st16(t_s + weight_column(c0), w);
             };
-            if (KEEP) {
-                weigh(0, ra);
-                weigh(32, rb);
-            } else {
-                weigh(32, rb);
-                tmem_ask32(t_s, ra);
-                tmem_wait32(ra);
-                finish(0, ra);
-                weigh(0, ra);
-            }
+            weigh(32, rb);
+            tmem_ask32(t_s, ra);
+            tmem_wait32(ra);
+            finish(0, ra);
+            weigh(0, ra);
             l += ls.x + ls.y;
             tmem_st_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(half ? p_rest(u) : p_ready(u));
-            if (u == 0) { if (i < unit_count(1)) bar_arrive<BAR_B, SOFT_THREADS>(); }
-            else if (i + 1 < unit_count(0)) bar_arrive<BAR_A, SOFT_THREADS>();
+            if (lane == 0) mbar_arrive(half ? p_rest : p_ready);
         }
         bool ok = true;
-        if (count > 0) {
-            ok = mbar_wait(o_done(u), 0, a.err, abort_flag);
-            if (!PAIR && u == 1) ok = mbar_wait(o_done(0), 0, a.err, abort_flag) && ok; // A's products read the tiles that B's rows go over
+        if (n_tiles > 0) {
+            ok = mbar_wait(o_done, 0, a.err, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             fence_after();
         }
-        named_bar<BAR_SOFT, SOFT_THREADS>();
-        // sums of the halves; B's rows for A: [dim][row] over the K tiles
-        float *ob = (float *)(gen + C::OFF_K), *mlb = (float *)(gen + C::OFF_ML);
-        const bool both = !PAIR && n_tiles > 1;
-        red[(u * 2 + half) * 128 + row] = l;
-        if (both && u == 1) {
-            if (half == 0) mlb[row] = m_used;
-            if (ok) {
-#pragma unroll 1
-                for (int c0 = 0; c0 < D / 2; c0 += 16) {
-                    uint32_t x[16];
-                    tmem_ld16u(t_o + c0, x);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) ob[(half * (D / 2) + c0 + e) * 128 + row] = __uint_as_float(x[e]);
-                }
-            }
-        }
-        named_bar<BAR_SOFT, SOFT_THREADS>();
-        if (ok && (PAIR || u == 0)) {
-            l = red[u * 256 + row] + red[u * 256 + 128 + row];
-            float fa = 1.f, fb = 0.f, m = m_used, den = l;
-            if (both) {
-                const float mo = mlb[row], lo = red[256 + row] + red[256 + 128 + row];
-                m = fmaxf(m_used, mo);
-                fa = m_used == -INFINITY ? 0.f : ex2(m_used - m);
-                fb = mo == -INFINITY ? 0.f : ex2(mo - m);
-                den = fmaf(l, fa, lo * fb);
-            }
+        // the sums of a row's two threads
+        asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory"); // the maxima have been read
+        red[half * 128 + row] = l;
+        asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+        {
+            const float den = l + red[(half ^ 1) * 128 + row];
+            float m = m_used;
             if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum
             const float inv = a.part_o ? 1.f : (den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den));
-            const int head = kvh * a.group + head_of(rr, my_token);
+            const int head = kvh * a.group + head_of(row, my_token);
             const long token = row0 + tok0 + my_token;
             const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
             if (a.part_o && live && half == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
             const bool give_back = !Q8 && *dirty;
 #pragma unroll 1
-            for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2) && n_tiles > 0; c0 += 16) {
+            for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2) && n_tiles > 0 && ok; c0 += 16) {
                 uint32_t y[16];
                 float v[16], x[16];
-                tmem_ld16u(tmem + lanes + 256u + u * 128u + c0, y); // warp-wide: lanes without a row load too
+                tmem_ld16u(tmem + lanes + T_O + c0, y); // warp-wide: lanes without a row load too
                 if (!live) continue;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    v[e] = __uint_as_float(y[e]) * fa;
-                    if (both) v[e] = fmaf(ob[(c0 + e) * 128 + row], fb, v[e]);
-                }
+                for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(y[e]);
                 if (give_back) {
                     for (int j = 0; j < n_tiles; ++j) {
                         const int t0 = key0(j);
@@ -772,20 +703,19 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
                 } else { // through the Q tile, so that whole rows leave together
 #pragma unroll
                     for (int e = 0; e < 16; e += 8)
-                        sts128(base + C::OFF_Q + (PAIR ? u * C::TILE : 0) + tile_at(row, (c0 + e) >> 3),
+                        sts128(base + C::OFF_Q + tile_at(row, (c0 + e) >> 3),
                                make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7])));
                 }
             }
             if (!a.part_o && n_tiles > 0) {
-                if (u == 0) named_bar<BAR_OUT_A, SOFT_THREADS / 2>(); else named_bar<BAR_OUT_B, SOFT_THREADS / 2>();
+                named_bar<BAR_OUT, SOFT_THREADS>();
                 constexpr int CH = D / 8;
-                const int first_row = PAIR ? u * TQ : 0;
 #pragma unroll 4
-                for (int idx = threadIdx.x & 255; idx < 128 * CH; idx += SOFT_THREADS / 2) {
-                    const int r = idx / CH, c = idx % CH, t = token_of(first_row + r);
-                    if (first_row + r >= rows) continue;
-                    *(uint4 *)((bf16 *)a.out + (long)(row0 + tok0 + t) * a.o_stride + (long)(kvh * a.group + head_of(first_row + r, t)) * D + c * 8) =
-                        lds128(base + C::OFF_Q + (PAIR ? u * C::TILE : 0) + tile_at(r, c));
+                for (int idx = threadIdx.x; idx < 128 * CH; idx += SOFT_THREADS) {
+                    const int r = idx / CH, c = idx % CH, t = token_of(r);
+                    if (r >= rows || !ok) continue;
+                    *(uint4 *)((bf16 *)a.out + (long)(row0 + tok0 + t) * a.o_stride + (long)(kvh * a.group + head_of(r, t)) * D + c * 8) =
+                        lds128(base + C::OFF_Q + tile_at(r, c));
                 }
             }
         }
@@ -798,32 +728,30 @@ __global__ void __launch_bounds__(tc_threads(TMA), 1) paged_attention_tc_kernel(
     }
 }
 
-template <int FMT, int D, bool PAIR, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
+template <int FMT, int D, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
 {
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_tc_kernel<FMT, D, PAIR, TMA>, TcCfg<D>::SMEM);
+    const cudaError_t e = limit.raise((const void *)paged_attention_tc_kernel<FMT, D, TMA>, TcCfg<D>::SMEM);
     if (e != cudaSuccess) return e;
-    const int rows = PAIR ? 256 : 128;
-    const long tiles = ((long)a.max_new * a.group + rows - 1) / rows;
-    return launch_kernel(paged_attention_tc_kernel<FMT, D, PAIR, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA)),
+    const long tiles = ((long)a.max_new * a.group + TQ - 1) / TQ;
+    return launch_kernel(paged_attention_tc_kernel<FMT, D, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA)),
                          TcCfg<D>::SMEM, st, 0, km, vm, a);
 }
-template <int FMT, int D, bool PAIR> cudaError_t tc_by_copy(const PagedAttnArgs &a, cudaStream_t st)
+template <int FMT, int D> cudaError_t tc_by_copy(const PagedAttnArgs &a, cudaStream_t st)
 {
     TcMap km{}, vm{};
     if constexpr (FMT == KV_BF16) {
         const long rows = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
         if (a.kv.page % 16 == 0 && rows < 0x7fffff00L && make_operand_map(&km, a.kv.k, D, rows, 1, D, 0, 16) == 0 &&
             make_operand_map(&vm, a.kv.v, D, rows, 1, D, 0, 16) == 0)
-            return launch_tc<FMT, D, PAIR, true>(a, km, vm, st);
+            return launch_tc<FMT, D, true>(a, km, vm, st);
     }
-    return launch_tc<FMT, D, PAIR, false>(a, km, vm, st);
+    return launch_tc<FMT, D, false>(a, km, vm, st);
 }
 template <int FMT> cudaError_t tc_by_dim(const PagedAttnArgs &a, cudaStream_t st)
 {
-    const bool pair = (long)a.max_new * a.group > TQ;
-    if (a.kv.d == 128) return pair ? tc_by_copy<FMT, 128, true>(a, st) : tc_by_copy<FMT, 128, false>(a, st);
-    if (a.kv.d == 64) return pair ? tc_by_copy<FMT, 64, true>(a, st) : tc_by_copy<FMT, 64, false>(a, st);
+    if (a.kv.d == 128) return tc_by_copy<FMT, 128>(a, st);
+    if (a.kv.d == 64) return tc_by_copy<FMT, 64>(a, st);
     return cudaErrorInvalidValue;
 }
 
