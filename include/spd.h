@@ -115,6 +115,26 @@ int spd_create(const spd_dims *dims, const uint8_t *sync_mask, const spd_layer *
 int spd_prefill(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t *block_table,
                 int32_t max_pages, void *out, void *stream);
 
+/* Extend cached sequences: S new tokens for each of B sequences, which follow its seq_lens[b] cached ones - the next chunk of a
+ * prompt, a continued conversation, the check of S drafted tokens.  Writes their K/V to positions seq_lens[b] .. seq_lens[b]+S-1
+ * and the last block's output to `out`; each new token attends to the cached ones and to the new ones up to itself.  The caller
+ * advances seq_lens (by as many tokens as it keeps).
+ *   x, out      : [B, S, hidden] storage dtype; must not alias
+ *   seq_lens    : [B] int32 device
+ *   max_context : host-side upper bound of seq_lens[b] + S over the batch (<= max_seq_len)
+ * A sequence whose seq_lens[b] + S exceeds max_context has no attention output and sets the device error flag (bit 2); K/V
+ * positions beyond the block-table row are not written.  Launched directly (no graph replay).
+ * Errors: SPD_ENULL, SPD_EINVAL (B > max_batch, max_context < S), SPD_ECAPACITY, SPD_ECUDA. */
+int spd_extend(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t *seq_lens, const int32_t *block_table,
+               int32_t max_pages, int32_t max_context, void *out, void *stream);
+
+/* Sliding attention window of a context, for every later call that runs blocks (prefill, extend, decode, the rank mode): a token at
+ * position p attends to the keys t <= p with t > p - window or t < sinks.  window 0 (default): all t <= p.  K/V pages that lie
+ * wholly between the sinks and the window are no longer looked up and may be given back.  The attention launches of such calls
+ * take no part in spd_timeline_*.  Drops the captured decode graphs.
+ * Errors: SPD_ENULL, SPD_EINVAL (negative). */
+int spd_set_window(spd_ctx *ctx, int32_t window, int32_t sinks);
+
 /* One decode step: one new token per sequence.  Appends the token's K/V at position
  * seq_lens[b] and attends over seq_lens[b] + 1 tokens; the caller advances seq_lens.
  *   x, out       : [B, hidden] storage dtype; must not alias
@@ -238,7 +258,8 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  *   SPD_KV_F32, SPD_KV_BF16 : stored as they are (rounded to nearest where the input is wider)
  *   SPD_KV_E4M3 : 8-bit floats and one float32 scale s per row, the smallest power of two with max|x| <= 448 s;
  *                 code = x / s rounded to nearest (exact division; within a factor of two of the
- *                 largest float, codes stop where code * s is still finite); code * s is exact in bfloat16
+ *                 largest float, codes stop where code * s is still finite); code * s is exact in bfloat16;
+ *                 the codes 0x7f and 0xff (NaN) are never written and must not be in a row that is read
  *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 / max|x|) rounded to
  *                 nearest in -127 .. 127 (the factor is within two units in its last place)
  * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0. */

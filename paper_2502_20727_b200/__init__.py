@@ -34,7 +34,7 @@ EXPORTS = ("spd_workspace_bytes", "spd_create", "spd_prefill", "spd_decode_step"
            "spd_head_grouping_stats", "spd_head_scatter", "spd_mlp_match", "spd_timeline_begin", "spd_timeline_read",
            "spd_timeline_end", "spd_tp_region_bytes", "spd_tp_attach", "spd_tp_detach", "spd_tp_decode_step",
            "spd_tp_prefill", "spd_tp_baseline_decode_step", "spd_tp_baseline_prefill",
-           "spd_kv_write", "spd_kv_read", "spd_paged_attention", "spd_paged_attention_workspace_bytes")
+           "spd_extend", "spd_set_window", "spd_kv_write", "spd_kv_read", "spd_paged_attention", "spd_paged_attention_workspace_bytes")
 
 
 class SpdError(RuntimeError):
@@ -84,6 +84,8 @@ def load_library() -> ctypes.CDLL:
     lib.spd_create.argtypes = [ctypes.POINTER(spd_dims), vp, ctypes.POINTER(spd_layer), i32, vp, sz,
                                ctypes.POINTER(vp)]
     lib.spd_prefill.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp]
+    lib.spd_extend.argtypes = [vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
+    lib.spd_set_window.argtypes = [vp, i32, i32]
     lib.spd_decode_step.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp]
     lib.spd_sync_points.argtypes = [vp]
     lib.spd_launches_per_decode_step.argtypes = [vp]
@@ -539,6 +541,32 @@ class SpdStack:
             _check("spd_prefill", self.lib.spd_prefill(self._ctx, x.data_ptr(), B, S, block_table.data_ptr(),
                                                         block_table.shape[1], out.data_ptr(), _stream_ptr()))
         return out
+
+    def extend(self, x: torch.Tensor, seq_lens: torch.Tensor, block_table: torch.Tensor, max_context: int,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [B, S, hidden]: S new tokens per sequence behind its seq_lens[b] cached ones; see spd_extend."""
+        B, S, H = x.shape
+        self._check_io(x, block_table)
+        if not (seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.numel() == B):
+            raise ValueError("seq_lens: int32 CUDA tensor [B]")
+        out = torch.empty_like(x) if out is None else out
+        with torch.cuda.device(self.device):
+            _check("spd_extend", self.lib.spd_extend(self._ctx, x.data_ptr(), B, S, seq_lens.data_ptr(), block_table.data_ptr(),
+                                                      block_table.shape[1], int(max_context), out.data_ptr(), _stream_ptr()))
+        return out
+
+    def set_window(self, window: int, sinks: int = 0):
+        """Attend to the last `window` tokens and the first `sinks` ones from now on (0: to all); see spd_set_window."""
+        _check("spd_set_window", self.lib.spd_set_window(self._ctx, int(window), int(sinks)))
+
+    def read_cache(self, layer: int, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *, n_tokens: int, err: torch.Tensor):
+        """Cached K and V rows of one layer, e.g. to keep a prefix or to move a sequence; see kv_read."""
+        return kv_read(self.k_pages[layer], self.v_pages[layer], cu, starts, block_table, n_tokens=n_tokens, dtype=self.dtype, err=err)
+
+    def write_cache(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *,
+                    err: torch.Tensor):
+        """Put K and V rows into one layer's pages at positions starts[b] on, e.g. a kept prefix; see kv_write."""
+        kv_write(k, v, self.k_pages[layer], self.v_pages[layer], cu, starts, block_table, err=err)
 
     def decode_step(self, x: torch.Tensor, seq_lens: torch.Tensor, block_table: torch.Tensor, max_context: int,
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:

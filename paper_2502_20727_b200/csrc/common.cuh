@@ -120,6 +120,7 @@ __device__ __forceinline__ float warp_max(float v)
 // Where the tokens of a launch sit in their sequences.
 //   prefill chunk: token m = bi * ns + si is position s0 + si of sequence b0 + bi
 //   decode       : token m is position seq_lens[m] of sequence m
+//   extension    : as a prefill chunk, but sequence b's new tokens follow its seq_lens[b] cached ones
 struct TokMap {
     int decode;
     int b0, ns, s0;
@@ -127,7 +128,7 @@ struct TokMap {
     __device__ __forceinline__ void locate(int m, int &b, int &pos) const
     {
         if (decode) { b = m; pos = seq_lens[m]; }
-        else { b = b0 + m / ns; pos = s0 + m % ns; }
+        else { b = b0 + m / ns; pos = s0 + m % ns + (seq_lens ? seq_lens[b] : 0); }
     }
 };
 

@@ -18,10 +18,11 @@ struct PagedKv {
 };
 
 // New rows of B sequences, one sequence after the other: sequence b has rows cu[b] .. cu[b+1]-1 at positions
-// lens[b], lens[b]+1, ...
+// lens[b], lens[b]+1, ...  The stack's own batches (attention only): cu null = `uniform` rows each; lens null = 0; plus `first`.
 struct RaggedBatch {
     const int32_t *cu, *lens, *table;
     int B, max_pages, n_tokens;
+    int uniform, first;
 };
 
 struct PagedAttnArgs {
@@ -93,9 +94,9 @@ template <> __device__ __forceinline__ uint32_t odd2<KV_INT8>(uint32_t w, uint32
 // What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
 __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
 {
-    row0 = rb.cu[b];
-    n_new = rb.cu[b + 1] - row0;
-    len = rb.lens[b];
+    row0 = rb.cu ? rb.cu[b] : b * rb.uniform;
+    n_new = rb.cu ? rb.cu[b + 1] - row0 : rb.uniform;
+    len = (rb.lens ? rb.lens[b] : 0) + rb.first;
     if (n_new == 0) return false;
     if (row0 < 0 || n_new < 0 || n_new > rb.n_tokens - row0 || n_new > max_new || len < 0 || len > max_context - n_new) {
         atomicOr(err, ERR_CAPACITY);
@@ -133,6 +134,9 @@ constexpr int PAGED_MAX_FEW_ROWS = 16;
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
 // bf16 queries, head_dim 64 or 128, any number of rows
 cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st);
+// Chooses a kernel and launches it (and the merge).  part_o / part_ml: room for `part_splits` ranges of partial rows, or null and 0;
+// more ranges than that are not made (a cluster's worth needs none).
+cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, cudaStream_t st);
 // Adds up the key ranges of a split launch.
 cudaError_t launch_paged_merge(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 

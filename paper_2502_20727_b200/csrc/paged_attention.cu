@@ -321,6 +321,27 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
 
 } // namespace
 
+cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, cudaStream_t st)
+{
+    AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, q_bf16, a.nq, a.rb.B, a.rb.n_tokens, a.max_new, a.max_context, a.window, a.sinks);
+    if (p.workspace && p.splits > part_splits) {
+        const int own = p.kernel == ATTN_ROWS ? PAGED_MAX_CLUSTER : 1; // ranges that need no workspace
+        p.splits = part_splits > own ? part_splits : own;
+        p.workspace = p.splits > own;
+    }
+    a.splits = p.splits;
+    a.row_tile = p.row_tile;
+    if (!p.workspace) a.part_o = a.part_ml = nullptr;
+    cudaError_t e = cudaSuccess;
+    switch (p.kernel) {
+    case ATTN_GENERAL: e = launch_paged_attention_general(a, q_bf16, st); break;
+    case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
+    case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
+    }
+    if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, q_bf16, st);
+    return e;
+}
+
 int check_cache(const spd_kv_cache *c, const spd_ragged *r, PagedKv *kv, RaggedBatch *rb); // kv_cache.cu
 bool rows_ok(const void *p, int64_t stride, int heads, int d, int dtype);
 
@@ -351,20 +372,11 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     a.err = err_flag;
     const AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, dtype, a.nq, a.rb.B, a.rb.n_tokens, max_new, max_context, a.window, a.sinks);
     if (p.workspace && (!workspace || workspace_bytes < p.workspace || ((uintptr_t)workspace & 255))) return SPD_EWORKSPACE;
-    a.splits = p.splits;
-    a.row_tile = p.row_tile;
     if (p.workspace) {
         a.part_o = (float *)workspace;
         a.part_ml = a.part_o + (size_t)p.splits * a.rb.n_tokens * a.nq * a.kv.d;
     }
-    cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = cudaSuccess;
-    switch (p.kernel) {
-    case ATTN_GENERAL: e = launch_paged_attention_general(a, dtype, st); break;
-    case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
-    case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
-    }
-    if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, dtype, st);
+    const cudaError_t e = run_paged_attention(a, dtype, p.workspace ? p.splits : 0, (cudaStream_t)stream);
     if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }
     return SPD_OK;
 }

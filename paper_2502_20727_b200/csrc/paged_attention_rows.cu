@@ -654,8 +654,8 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     const long w = (long)blockIdx.x * 4 + (threadIdx.x >> 5), plane = (long)a.rb.n_tokens * a.nq;
     if (w >= plane) return;
     const int t = (int)(w / a.nq), head = (int)(w % a.nq);
-    int before = 0;
-    for (int i0 = 0; i0 <= a.rb.B; i0 += 32) {
+    int before = a.rb.cu ? 0 : t / a.rb.uniform + 1;
+    for (int i0 = 0; a.rb.cu && i0 <= a.rb.B; i0 += 32) {
         const unsigned mk = __ballot_sync(0xffffffffu, i0 + lane <= a.rb.B && a.rb.cu[i0 + lane] <= t);
         before += __popc(mk);
         if (mk != 0xffffffffu) break;

@@ -5,6 +5,7 @@
 #include "gemm_tc.cuh"
 #include "gemm_decode.cuh"
 #include "gemm_prefill.cuh"
+#include "paged.cuh"
 #include "tp_prefill.cuh"
 
 #include <math.h>
@@ -139,6 +140,7 @@ struct Ctx {
     int prefill_rescale_log2;    // tcgen05 prefill attention: growth of the row maximum (log2) that triggers a rescale
     int peer_wait_ms;            // rank mode: how long a rank waits for its peers' partial sums
     int prefill_group_m;         // prompt projections: token tiles per group of the tile order (0 = default)
+    int window, sinks;           // attention window (0: none) and the first tokens that stay visible
     int prefill_pairs;           // prompt projections: CTA pairs (256-token tiles) where a launch has more than 128 tokens
     int launches_last;
     TpState tp;
@@ -472,6 +474,31 @@ const TcMap *act_map(Ctx *c, ActBuf buf, int box)
     const TcMap *var = (expr);                     \
     if (!var) { g_last_cuda_error = (int)cudaErrorInvalidValue; return SPD_ECUDA; }
 
+// Attention of one launch.  Prompts from position 0 and single-token steps without a window: the stack's own kernels; extensions
+// of cached sequences and windows: the paged attention, whose key ranges may use the decode step's partial-result buffers.
+template <typename T> cudaError_t attention(Ctx *c, const AttnArgs &a, bool decode, int max_context, int &launches, cudaStream_t st)
+{
+    const bool extension = !a.tm.decode && a.tm.seq_lens;
+    if (!c->window && !extension) return decode ? launch_decode_attention<T>(a, st) : launch_prefill_attention<T>(a, st);
+    if (((uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15) return cudaErrorMisalignedAddress;
+    PagedAttnArgs p{};
+    p.kv = PagedKv{const_cast<void *>(a.k_pages), const_cast<void *>(a.v_pages), nullptr, nullptr, a.pt.n_pages, a.pt.n_kv_heads, a.pt.block, a.head_dim,
+                   sizeof(T) == 2 ? KV_BF16 : KV_F32};
+    const int ns = a.tm.decode ? 1 : a.tm.ns, b0 = a.tm.decode ? 0 : a.tm.b0;
+    p.rb = RaggedBatch{nullptr, a.tm.seq_lens ? a.tm.seq_lens + b0 : nullptr, a.pt.block_table + (long)b0 * a.pt.max_pages, a.M / ns, a.pt.max_pages,
+                       a.M, ns, a.tm.decode ? 0 : a.tm.s0};
+    p.q = a.q; p.out = a.out; p.q_stride = p.o_stride = (long)a.n_q_heads * a.head_dim;
+    p.nq = a.n_q_heads; p.group = a.n_q_heads / a.pt.n_kv_heads;
+    p.max_new = ns; p.max_context = max_context; p.window = c->window; p.sinks = c->window ? c->sinks : 0;
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
+    p.err = a.err;
+    p.part_o = a.part_o; p.part_ml = a.part_ml;
+    // the buffers hold 32 ranges of max_batch tokens
+    const cudaError_t e = run_paged_attention(p, sizeof(T) == 2, (int)(32L * c->d.max_batch / a.M), st);
+    if (p.part_o) ++launches; // the ranges were added up by a second kernel
+    return e;
+}
+
 template <typename T>
 int run_tokens(Ctx *c, const void *x, void *out, int M, TokMap tm, const int32_t *bt, int max_pages,
                bool decode, int max_context, cudaStream_t st)
@@ -546,8 +573,7 @@ int run_tokens(Ctx *c, const void *x, void *out, int M, TokMap tm, const int32_t
                 MAP_OR_FAIL(qm, act_map(c, AB_Q, 128));
                 a.q_map = qm; a.k_map = &c->maps[l].kpages; a.v_map = &c->maps[l].vpages; a.rescale_log2 = (float)c->prefill_rescale_log2;
             }
-            if (decode) LAUNCH(K_ATTN, launch_decode_attention<T>(a, st));
-            else LAUNCH(K_ATTN, launch_prefill_attention<T>(a, st));
+            LAUNCH(K_ATTN, attention<T>(c, a, decode, max_context, launches, st));
         }
         // a5: row-split output projection.  Plane (i, j) holds the part of Y_i that comes from
         // sub-range j of shard i's K slice.  A synchronous block in prefill needs only the sum:
@@ -721,8 +747,7 @@ int run_tp_baseline(Ctx *c, const void *x, void *out, int M, TokMap tm, const in
                 MAP_OR_FAIL(qm, act_map(c, AB_Q, 128));
                 t.q_map = qm; t.k_map = &lm.kpages; t.v_map = &lm.vpages; t.rescale_log2 = (float)c->prefill_rescale_log2;
             }
-            if (decode) LAUNCH(K_ATTN, launch_decode_attention<bf16>(t, st));
-            else LAUNCH(K_ATTN, launch_prefill_attention<bf16>(t, st));
+            LAUNCH(K_ATTN, attention<bf16>(c, t, decode, max_context, launches, st));
         }
         {   // a5: the rank's partial attention output Y_r, in K-range planes, then as one [M][H] buffer
             const TcMap *wmaps[1] = {&lm.wo_full};
@@ -834,7 +859,7 @@ int run_decode_fused(Ctx *c, const void *x, void *out, int M, TokMap tm, const i
             a.M = M; a.n_q_heads = d.n_q_heads; a.head_dim = d.head_dim; a.B = M; a.splits = p.attn_splits;
             a.max_context = max_context; a.part_o = c->part_o; a.part_ml = c->part_ml; a.counters = c->attn_cnt; a.err = c->err;
             if (d.head_dim == 128 && d.kv_block_size == 16) { a.k_map = &c->maps[l].kpage_whole; a.v_map = &c->maps[l].vpage_whole; }
-            LAUNCH_S(K_ATTN, a, launch_decode_attention<bf16>(a, st));
+            LAUNCH_S(K_ATTN, a, attention<bf16>(c, a, true, max_context, launches, st));
         }
         {   // a5 - a7: shard i's K slice gives the plane group Y_i
             DecGemmArgs g = base_args();
@@ -957,7 +982,7 @@ int run_tp(Ctx *c, const void *x, void *out, long out_stride, int M, TokMap tm, 
             a.M = M; a.n_q_heads = d.n_q_heads; a.head_dim = d.head_dim; a.B = M; a.splits = p.attn_splits;
             a.max_context = max_context; a.part_o = c->part_o; a.part_ml = c->part_ml; a.counters = c->attn_cnt; a.err = c->err;
             if (d.head_dim == 128 && d.kv_block_size == 16) { a.k_map = &c->maps[l].kpage_whole; a.v_map = &c->maps[l].vpage_whole; }
-            LAUNCH_S(K_ATTN, a, launch_decode_attention<bf16>(a, st));
+            LAUNCH_S(K_ATTN, a, attention<bf16>(c, a, true, max_context, launches, st));
         }
         {   // a5 - a7: Y_z from the rank's own heads.  TP block: R = X + sum over ranks (sync-point 1);
             // SPD block: the sync-point is dropped, R_z = X + Y_z feeds the rank's MLP and Y_z is kept for a10
@@ -1095,7 +1120,7 @@ int run_tp_prefill(Ctx *c, const void *x, void *out, long out_stride, int M, Tok
                 MAP_OR_FAIL(qm, act_map(c, AB_Q, 128));
                 a.q_map = qm; a.k_map = &lm.kpages; a.v_map = &lm.vpages; a.rescale_log2 = (float)c->prefill_rescale_log2;
             }
-            LAUNCH_S(K_ATTN, a, launch_prefill_attention<bf16>(a, st));
+            LAUNCH_S(K_ATTN, a, attention<bf16>(c, a, false, max_context, launches, st));
         }
         int mlp_tiles = 1;
         MAP_OR_FAIL(attn_map, act_map(c, AB_ATTN_SHARD, 128));
@@ -1226,7 +1251,7 @@ int run_prefill_fused(Ctx *c, const void *x, void *out, int M, TokMap tm, const 
                 MAP_OR_FAIL(qm, act_map(c, AB_Q, 128));
                 a.q_map = qm; a.k_map = &c->maps[l].kpages; a.v_map = &c->maps[l].vpages; a.rescale_log2 = (float)c->prefill_rescale_log2;
             }
-            LAUNCH_S(K_ATTN, a, launch_prefill_attention<bf16>(a, st));
+            LAUNCH_S(K_ATTN, a, attention<bf16>(c, a, false, max_context, launches, st));
         }
         int mlp_tiles, mlp_groups;
         if (sync) {   // a5 - a7, sync block: sum_i Y_i is the K accumulation over all heads
@@ -1524,6 +1549,7 @@ int spd_create(const spd_dims *dims, const uint8_t *sync_mask, const spd_layer *
     c.prefill_rescale_log2 = 8;
     c.peer_wait_ms = 1000;
     c.prefill_pairs = 1;
+    c.window = c.sinks = 0;
     c.prefill_group_m = 0;
     c.ring_stages = 0;
     c.oproj_planes = 0;
@@ -1606,6 +1632,72 @@ int spd_prefill(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t
     return SPD_OK;
 }
 
+int spd_extend(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t *seq_lens, const int32_t *block_table, int32_t max_pages,
+               int32_t max_context, void *out, void *stream)
+{
+    if (!ctx || !x || !seq_lens || !block_table || !out) return SPD_ENULL;
+    Ctx &c = ctx->c;
+    const spd_dims &d = c.d;
+    if (B < 1 || S < 1 || B > d.max_batch || x == out || max_context < S) return SPD_EINVAL;
+    if (max_context > d.max_seq_len || (long)max_pages * d.kv_block_size < max_context) return SPD_ECAPACITY;
+    cudaStream_t st = (cudaStream_t)stream;
+    const size_t es = esize(d);
+    const bool fused = d.dtype == 1 && (d.block_kind == 0 || c.bias_fused);
+    // One token tile of the weight-streaming projections (a decode step's) beats the 128-token tiles of a prompt; two tiles read
+    // the weights twice.  Two 70B-shaped blocks, 2048 cached tokens, us: 4 tokens 571 and 999, 64 tokens 678 and 1036, 96 tokens
+    // 1146 and 1107.
+    const bool few = fused && B * (long)S <= (c.Mcap < 64 ? c.Mcap : 64);
+    const int Mp = few ? B * S : d.max_prefill_tokens;
+    int total_launches = 0;
+    CU_TRY(timeline_restart(&c, st));
+    auto run = [&](int b0, int nb, int s0, int ns) -> int {
+        TokMap tm{0, b0, ns, s0, seq_lens};
+        const size_t off = ((size_t)b0 * S + s0) * d.hidden * es;
+        const char *xi = (const char *)x + off;
+        char *xo = (char *)out + off;
+        int rc = d.dtype == 0         ? run_tokens<float>(&c, xi, xo, nb * ns, tm, block_table, max_pages, false, max_context, st)
+                 : few                ? run_decode_fused(&c, xi, xo, nb * ns, tm, block_table, max_pages, max_context, st)
+                 : fused && d.hidden % 16 == 0 ? run_prefill_fused(&c, xi, xo, nb * ns, tm, block_table, max_pages, max_context, st)
+                                      : run_tokens<bf16>(&c, xi, xo, nb * ns, tm, block_table, max_pages, false, max_context, st);
+        total_launches += c.launches_last;
+        return rc;
+    };
+    // chunks of at most Mp tokens, as in spd_prefill
+    if (S <= Mp) {
+        const int nb = Mp / S;
+        for (int b0 = 0; b0 < B; b0 += nb) {
+            const int rc = run(b0, (B - b0 < nb) ? B - b0 : nb, 0, S);
+            if (rc) return rc;
+        }
+    } else {
+        for (int b = 0; b < B; ++b)
+            for (int s0 = 0; s0 < S; s0 += Mp) {
+                const int rc = run(b, 1, s0, (S - s0 < Mp) ? S - s0 : Mp);
+                if (rc) return rc;
+            }
+    }
+    c.launches_last = total_launches;
+    CU_TRY(timeline_fold(&c, st));
+    return SPD_OK;
+}
+
+static void drop_graphs(Ctx &c)
+{
+    for (GraphEntry &g : c.graphs) cudaGraphExecDestroy(g.exec);
+    c.graphs.clear();
+}
+
+int spd_set_window(spd_ctx *ctx, int32_t window, int32_t sinks)
+{
+    if (!ctx) return SPD_ENULL;
+    if (window < 0 || sinks < 0) return SPD_EINVAL;
+    Ctx &c = ctx->c;
+    c.window = window;
+    c.sinks = window ? sinks : 0;
+    drop_graphs(c);
+    return SPD_OK;
+}
+
 int spd_decode_step(spd_ctx *ctx, const void *x, int32_t B, const int32_t *seq_lens, const int32_t *block_table,
                     int32_t max_pages, int32_t max_context, void *out, void *stream)
 {
@@ -1646,12 +1738,6 @@ int spd_decode_step(spd_ctx *ctx, const void *x, int32_t B, const int32_t *seq_l
         rc = capture_ahead(c, ahead, run_at(next_bucket), st);
     }
     return rc;
-}
-
-static void drop_graphs(Ctx &c)
-{
-    for (GraphEntry &g : c.graphs) cudaGraphExecDestroy(g.exec);
-    c.graphs.clear();
 }
 
 int spd_set_mask(spd_ctx *ctx, const uint8_t *sync_mask)
