@@ -18,11 +18,15 @@
 //     assignment of keys to score rows is right as long as V uses the same one: row 2i of eight keys is key 2i, row 2i + 1 is
 //     key (2i) ^ 5, with which both the K loads (lanes = rows) and the V loads (lanes = row pairs) meet every shared-memory
 //     bank once under the swizzle.
-//   - K codes become float16 (exact; one conversion instruction for e4m3; for int8 the code byte under the exponent of 1024,
-//     minus 1152) and so does Q, scaled per row by a power of two to below 2^15: the scaled row keeps bf16's 8 bits for
-//     everything down to 2^-29 of its largest value.  V codes become bfloat16 (exact), because the weights they meet carry
-//     the V scales, whose range float16 does not cover: e4m3 by moving sign, exponent and mantissa to bf16's places (the value
-//     times 2^-120) and one product, int8 as 128 + low 7 bits minus 128 or 256.
+//   - K codes become float16 (exact, e4m3 up to a power of two; see half_of) and so does Q, scaled per row by a power of two to
+//     below 2^15: the scaled row keeps bf16's 8 bits for everything down to 2^-29 of its largest value.  V codes become bfloat16
+//     (exact), because the weights they meet carry the V scales and reach from 1 to where they vanish, a range that float16 does
+//     not cover: e4m3 by moving sign, exponent and mantissa to bf16's places (the value times 2^-120) and one product, int8 as
+//     128 + low 7 bits minus 128 or 256;
+//   - weights are rounded to bf16.  With int8 scales, which are not powers of two, even a row's only weight is off, and the errors
+//     came to 1.5 times that of the output's own rounding: there the rest of each weight is a second bf16 with products of its own
+//     (32 sequences of 9 to 16 thousand tokens: 192 us, 182 without; the same for the other formats cost 2 to 8 % and
+//     would take errors of 1.05 to 1.2 times, at most 1.45, to 1).
 // Softmax: base 2, fp32, per warp; the accumulators follow the running maximum lazily (they are rescaled when it has grown by
 // more than 2^8: weights stay below 2^8, where bf16 rounds as finely as at 1).
 #include "gemm_tc.cuh"
@@ -120,16 +124,15 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Two neighbouring codes (low or high half of a word) -> float16x2 of the values they stand for, exactly.
-template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t half_pair(uint32_t w)
+// Two K codes of a word -> float16x2.  int8: codes with the sign bit flipped (code + 128), bytes 0, 1 or (SECOND) 2, 3, under the
+// exponent of 1024, minus 1152.  e4m3: bytes 0, 2 or 1, 3, sign, exponent and mantissa moved to float16's places: the value
+// times E4M3_UNIT = 2^-8, exactly (64 sequences of ragged lengths: 33.3 us, with a conversion instruction per pair 34.1).
+constexpr float E4M3_UNIT = 0x1p-8f;
+template <int FMT, bool SECOND> __device__ __forceinline__ uint32_t half_of(uint32_t w)
 {
-    if (FMT == KV_E4M3) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(HIGH ? w >> 16 : w & 0xffffu), __NV_E4M3);
-        return (uint32_t)h.x | ((uint32_t)h.y << 16);
-    }
-    // w: codes with the sign bit flipped (code + 128)
-    const uint32_t x = __byte_perm(w, 0x64646464u, HIGH ? 0x4342 : 0x4140);
-    const __half2 v = __hsub2(*(const __half2 *)&x, __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480))); // 1024 + 128
+    if (FMT == KV_E4M3) return SECOND ? ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u) : ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u);
+    const uint32_t x = __byte_perm(w, 0x64646464u, SECOND ? 0x4342 : 0x4140);
+    const __half2 v = __hsub2(*(const __half2 *)&x, __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
     return *(const uint32_t *)&v;
 }
 
@@ -287,7 +290,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int ex = max((int)(top >> 7), 27) - 127;                         // 2^ex <= largest < 2^(ex + 1), ex >= -100
             const float f = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);      // to [2^14, 2^15)
-            my_qs *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+            my_qs *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * (FMT == KV_E4M3 ? 1.f / E4M3_UNIT : 1.f);
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
                 const uint32_t w[4] = {u[m].x, u[m].y, u[m].z, u[m].w};
@@ -302,7 +305,12 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         }
 #pragma unroll
         for (int m = 0; m < D / 32; ++m) {
-            qf[n][2 * m][0] = u[m].x; qf[n][2 * m][1] = u[m].y; qf[n][2 * m + 1][0] = u[m].z; qf[n][2 * m + 1][1] = u[m].w;
+            if (FMT == KV_E4M3) { // as half_of pairs the codes
+                qf[n][2 * m][0] = __byte_perm(u[m].x, u[m].y, 0x5410); qf[n][2 * m][1] = __byte_perm(u[m].x, u[m].y, 0x7632);
+                qf[n][2 * m + 1][0] = __byte_perm(u[m].z, u[m].w, 0x5410); qf[n][2 * m + 1][1] = __byte_perm(u[m].z, u[m].w, 0x7632);
+            } else {
+                qf[n][2 * m][0] = u[m].x; qf[n][2 * m][1] = u[m].y; qf[n][2 * m + 1][0] = u[m].z; qf[n][2 * m + 1][1] = u[m].w;
+            }
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -365,7 +373,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t x0 = FMT == KV_INT8 ? w0[i] ^ 0x80808080u : w0[i], x1 = FMT == KV_INT8 ? w1[i] ^ 0x80808080u : w1[i];
-                    const uint32_t a0 = half_pair<FMT, false>(x0), a1 = half_pair<FMT, false>(x1), a2 = half_pair<FMT, true>(x0), a3 = half_pair<FMT, true>(x1);
+                    const uint32_t a0 = half_of<FMT, false>(x0), a1 = half_of<FMT, false>(x1), a2 = half_of<FMT, true>(x0), a3 = half_of<FMT, true>(x1);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) mma16816<true>(s[n], a0, a1, a2, a3, qf[n][4 * m + i][0], qf[n][4 * m + i][1]);
                 }
@@ -416,7 +424,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 for (int i = 0; i < MT; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
             }
         }
-        uint32_t pf[NR][2];
+        uint32_t pf[NR][2], pl[NR][2]; // pl: what rounding left, int8
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             float p[4];
@@ -434,6 +442,14 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             }
             pf[n][0] = transpose8x8(pack(p[0], p[1]));
             pf[n][1] = transpose8x8(pack(p[2], p[3]));
+            if (FMT == KV_INT8) {
+                auto left = [](float lo, float hi) { // lo, hi minus their bf16s
+                    const uint32_t w = pack(lo, hi);
+                    return pack(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xffff0000u));
+                };
+                pl[n][0] = transpose8x8(left(p[0], p[1]));
+                pl[n][1] = transpose8x8(left(p[2], p[3]));
+            }
         }
         if (!Q8) {
             if (!all_seen) {
@@ -486,6 +502,10 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 for (int n = 0; n < NR; ++n) {
                     mma16816<false>(o[n][2 * w], a0, a1, a2, a3, pf[n][0], pf[n][1]);
                     mma16816<false>(o[n][2 * w + 1], b0, b1, b2, b3, pf[n][0], pf[n][1]);
+                    if (FMT == KV_INT8) {
+                        mma16816<false>(o[n][2 * w], a0, a1, a2, a3, pl[n][0], pl[n][1]);
+                        mma16816<false>(o[n][2 * w + 1], b0, b1, b2, b3, pl[n][0], pl[n][1]);
+                    }
                 }
             }
         }

@@ -18,7 +18,10 @@
 // second load warp looks after V, see below); 8-bit pages (and bf16 pages of other sizes) by four load warps, which widen the
 // codes to bf16 on the way into shared memory.  The pairs that widening a 32-bit word gives are (0, 2) and (1, 3) of its four
 // codes: the head dims of Q, K and V all sit in that order, and the output is put right when it is stored.  Row scales multiply
-// the scores (K) and the weights (V) in fp32.
+// the scores (K) and the weights (V) in fp32.  A weight that carries an int8 row's scale is off by up to 2^-8 even where it is the
+// row's only one, and such errors came to 1.5 times the output's own rounding: there what rounding left is a second bf16 with a
+// product of its own (ragged chunks of up to 700 tokens on up to 1000, 40 heads: 266 us, 211 without; e4m3, whose scales are powers
+// of two, 215).
 // A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
 // shared memory before the product, and rows that do see them get them back at the end.
 // Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
@@ -216,6 +219,8 @@ __device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities o
 // Column (from the unit's first) of the weights of keys k, k + 1: each 32 keys' go over columns of their own half's scores, the
 // second 32 over the last 16, so that the first 32 scores can be read again after them.
 __device__ __forceinline__ constexpr uint32_t weight_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 48 : 0) + ((k & 31) >> 1)); }
+// ... and of what rounding left of it (int8): the rest of those scores' columns
+__device__ __forceinline__ constexpr uint32_t rest_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 32 : 16) + ((k & 31) >> 1)); }
 constexpr int load_warps(bool tma) { return tma ? 2 : 4; }
 constexpr int SOFT_WARPS = 8, SOFT_THREADS = 32 * SOFT_WARPS;
 constexpr int tc_threads(bool tma) { return SOFT_THREADS + 32 * (load_warps(tma) + 1); } // two blocks: 80 registers a thread, or 72
@@ -478,6 +483,11 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
 #pragma unroll
             for (int kk = kk0; kk < kk0 + 64 / UMMA_K; ++kk)
                 umma_ts(tmem + T_O, tmem + weight_column(16 * kk), v_lo + kk * (UMMA_K * 128 >> 4), idesc_o, acc || kk > 0);
+            if (FMT == KV_INT8) {
+#pragma unroll
+                for (int kk = kk0; kk < kk0 + 64 / UMMA_K; ++kk)
+                    umma_ts(tmem + T_O, tmem + rest_column(16 * kk), v_lo + kk * (UMMA_K * 128 >> 4), idesc_o, 1);
+            }
         };
         if (n_tiles > 0) {
             wait(q_full, 0);
@@ -625,6 +635,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
                     ls = add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
                     w[k] = pack(p.x, p.y);
+                    if (FMT == KV_INT8) { r[2 * k] = __float_as_uint(p.x); r[2 * k + 1] = __float_as_uint(p.y); }
                 }
                 if (Q8 && masked) { // 0 times the scale of an unseen key, which may be anything
 #pragma unroll
@@ -634,6 +645,17 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
                     }
                 }
                 tmem_st16(t_s + weight_column(c0), w);
+                if (FMT == KV_INT8) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        w[k] = pack(__uint_as_float(r[2 * k]) - __uint_as_float(w[k] << 16), __uint_as_float(r[2 * k + 1]) - __uint_as_float(w[k] & 0xffff0000u));
+                        if (masked) {
+                            if (!((uint32_t)(seen >> c0) & (1u << (2 * k)))) w[k] &= 0xffff0000u;
+                            if (!((uint32_t)(seen >> c0) & (2u << (2 * k)))) w[k] &= 0xffffu;
+                        }
+                    }
+                    tmem_st16(t_s + rest_column(c0), w);
+                }
             };
             weigh(32, rb);
             tmem_ask32(t_s, ra);
