@@ -131,7 +131,7 @@ int spd_extend(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t 
 /* Sliding attention window of a context, for every later call that runs blocks (prefill, extend, decode, the rank mode): a token at
  * position p attends to the keys t <= p with t > p - window or t < sinks.  window 0 (default): all t <= p.  K/V pages that lie
  * wholly between the sinks and the window are no longer looked up and may be given back.  The attention launches of such calls
- * take no part in spd_timeline_*.  Drops the captured decode graphs.
+ * take no part in spd_timeline_*; spd_head_grouping_stats goes on looking at whole prompts.  Drops the captured decode graphs.
  * Errors: SPD_ENULL, SPD_EINVAL (negative). */
 int spd_set_window(spd_ctx *ctx, int32_t window, int32_t sinks);
 
@@ -308,7 +308,7 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  * drafted tokens.
  *   q, out : [n_tokens, n_q_heads, head_dim] of dtype (0 float32, 1 bfloat16), strided as in spd_kv_write; must not
  *            overlap.  A float32 q needs an SPD_KV_F32 or 8-bit cache, a bfloat16 q an SPD_KV_BF16 or 8-bit cache.
- *   max_new, max_context : host bounds of a sequence's new tokens and of seq_lens[b] + new tokens.  A sequence beyond
+ *   max_new, max_context : host bounds of a sequence's new tokens and of seq_lens[b] + new tokens (at most 2^30).  A sequence beyond
  *            them, or with rows outside the tensor, is skipped with error bit 2.
  *   window : only pages that hold a visible key are looked up, so that block-table entries of pages that lie wholly
  *            between the sinks and the window may name anything (the pages may have been given back).

@@ -547,9 +547,12 @@ class SpdStack:
         """x [B, S, hidden]: S new tokens per sequence behind its seq_lens[b] cached ones; see spd_extend."""
         B, S, H = x.shape
         self._check_io(x, block_table)
-        if not (seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.numel() == B):
-            raise ValueError("seq_lens: int32 CUDA tensor [B]")
-        out = torch.empty_like(x) if out is None else out
+        if not (seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,) and seq_lens.is_contiguous()):
+            raise ValueError("seq_lens: contiguous int32 CUDA tensor [B]")
+        if out is None:
+            out = torch.empty_like(x)
+        elif out.shape != x.shape or out.dtype != x.dtype or not (out.is_cuda and out.is_contiguous()):
+            raise ValueError("out: like x")
         with torch.cuda.device(self.device):
             _check("spd_extend", self.lib.spd_extend(self._ctx, x.data_ptr(), B, S, seq_lens.data_ptr(), block_table.data_ptr(),
                                                       block_table.shape[1], int(max_context), out.data_ptr(), _stream_ptr()))

@@ -129,6 +129,8 @@ cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, vo
 cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, cudaStream_t st);
 // Key ranges that one thread-block cluster adds up in shared memory; more go through the workspace.
 constexpr int PAGED_MAX_CLUSTER = 8;
+// Longest sequence: positions and what is added to them (windows' ends, tiles) stay within 32 bits.
+constexpr int PAGED_MAX_CONTEXT = 1 << 30;
 // bf16 queries, head_dim 64 or 128, few rows (new tokens x query heads per KV head) per sequence and KV head
 constexpr int PAGED_MAX_FEW_ROWS = 16;
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);

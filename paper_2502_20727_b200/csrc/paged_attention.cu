@@ -17,7 +17,7 @@ namespace {
 // in shared memory.  Thread (tx, ty) computes the scores of rows ty RPT .. and keys tx + 16 j, four head dims at a time (eight
 // products per 16-byte shared-memory load), the row maxima and sums over its half warp, and the output columns 4 tx + 64 j.
 // Bound: for chunks the FMA pipes, for few rows (RPT 1) the cache reads, which are cut into key ranges over thread blocks.
-// One warp per row, without tiles, took 259 us for 4 ragged chunks of up to 256 tokens where this takes 29 (head_dim 64).
+// One warp per row, without tiles, took 259 us for 4 ragged chunks of up to 256 tokens where this takes 30 (head_dim 64).
 constexpr int GK = 64, G_THREADS = 256;
 
 // float32 caches: the next tile is on its way (cp.async) while this one is computed
@@ -359,7 +359,7 @@ extern "C" int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *
     if (!err_flag) return SPD_ENULL;
     if ((dtype != 0 && dtype != 1) || n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % a.kv.nkv || a.rb.B > 65535) return SPD_EINVAL;
     if ((a.kv.fmt == KV_F32 && dtype != 0) || (a.kv.fmt == KV_BF16 && dtype != 1)) return SPD_EINVAL;
-    if (max_new < 1 || max_context < 1 || window < 0 || sinks < 0 || !(scale > 0.f) || !isfinite(scale)) return SPD_EINVAL;
+    if (max_new < 1 || max_context < 1 || max_context > PAGED_MAX_CONTEXT || window < 0 || sinks < 0 || !(scale > 0.f) || !isfinite(scale)) return SPD_EINVAL;
     if ((int64_t)a.rb.max_pages * a.kv.page < max_context) return SPD_ECAPACITY;
     if (a.rb.B == 0 || a.rb.n_tokens == 0) return SPD_OK;
     if (!q || !out) return SPD_ENULL;

@@ -31,3 +31,12 @@ def test_null_context_is_refused():
     lib = spd.load_library()
     assert lib.spd_extend(None, 16, 1, 1, 16, 16, 1, 1, 32, None) == -2
     assert lib.spd_set_window(None, 4, 0) == -2
+
+
+def test_attention_refuses_contexts_beyond_its_positions():
+    spd_build.build()
+    lib = spd.load_library()
+    c = spd.spd_kv_cache(0x10000, 0x10000, None, None, 4, 2, 1 << 20, 64, 1)
+    r = spd.spd_ragged(0x10000, 0x10000, 0x10000, 2, 4096, 0)  # no tokens: a call that is allowed does nothing
+    for max_context, rc in ((1 << 30, 0), ((1 << 30) + 1, -1), (2 ** 31 - 1, -1)):
+        assert lib.spd_paged_attention(c, r, 0x10000, 256, 0x20000, 256, 1, 4, 1, max_context, 0.1, 0, 0, None, 0, 0x10000, None) == rc
