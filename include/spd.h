@@ -130,8 +130,8 @@ int spd_extend(spd_ctx *ctx, const void *x, int32_t B, int32_t S, const int32_t 
 
 /* Sliding attention window of a context, for every later call that runs blocks (prefill, extend, decode, the rank mode): a token at
  * position p attends to the keys t <= p with t > p - window or t < sinks.  window 0 (default): all t <= p.  K/V pages that lie
- * wholly between the sinks and the window are no longer looked up and may be given back.  The attention launches of such calls
- * take no part in spd_timeline_*; spd_head_grouping_stats goes on looking at whole prompts.  Drops the captured decode graphs.
+ * wholly between the sinks and the window are no longer looked up and may be given back.  spd_head_grouping_stats goes on looking
+ * at whole prompts.  Drops the captured decode graphs.
  * Errors: SPD_ENULL, SPD_EINVAL (negative). */
 int spd_set_window(spd_ctx *ctx, int32_t window, int32_t sinks);
 

@@ -40,6 +40,7 @@ struct PagedAttnArgs {
     int stages;                   // paged_attention_rows.cu: set by its launcher
     float *part_o, *part_ml;      // ranges that no cluster adds up (else null): fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
     int *err;
+    unsigned long long *stamp;    // the stack's launch timeline, or null
 };
 
 template <int FMT> struct KvElem;

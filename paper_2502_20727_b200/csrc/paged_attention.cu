@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(G_THREADS) paged_attention_general_kernel(cons
     constexpr int RT = C::RT, LD = C::LD, LP = C::LP, OC = D < 64 ? 1 : D / 64; // groups of 4 output columns per thread (D 32: half the threads)
     extern __shared__ __align__(16) float gsm[];
     float *sQ = gsm, *sKV = sQ + RT * LD, *sP = sKV + C::BUFS * 2 * GK * LD;
+    if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
     pdl_wait();
     const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
@@ -219,6 +220,7 @@ __global__ void __launch_bounds__(G_THREADS) paged_attention_general_kernel(cons
             }
         }
     }
+    if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
 template <typename T, int FMT, int D, int RPT> cudaError_t launch_general(const PagedAttnArgs &a, cudaStream_t st)

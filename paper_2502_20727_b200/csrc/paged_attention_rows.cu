@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::off_sc(ST) + warp * ST * 128, bars = base + C::off_bar(ST) + warp * ST * 8;
     volatile int *abort_flag = (volatile int *)(gen + C::off_bar(ST) + RW * ST * 8);
+    if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
     if (TMA) {
         if (lane == 0) {
@@ -661,6 +662,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         }
         tc::cluster_sync(); // no block exits while a peer still reads its shared memory
     }
+    if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
 // Adds up the key ranges of a split launch: one warp per (token, query head), the ranges' weights in its lanes.
@@ -723,6 +725,7 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     T *dst = (T *)a.out + (long)t * a.o_stride + (long)head * D + lane * VEC;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dst[e] = from_f<T>(o[e] * inv);
+    if (lane == 0) stamp_exit(a.stamp); // the slot's start is the ranges' launch
 }
 
 template <int FMT, int D, int NR, int RW, bool TMA>

@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
     volatile int *dirty = (volatile int *)(tmem_slot + 2);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
     pdl_wait();
     const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
@@ -748,6 +749,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_COLS) : "memory");
     }
+    if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
 template <int FMT, int D, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)

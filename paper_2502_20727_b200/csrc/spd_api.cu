@@ -492,6 +492,7 @@ template <typename T> cudaError_t attention(Ctx *c, const AttnArgs &a, bool deco
     p.max_new = ns; p.max_context = max_context; p.window = c->window; p.sinks = c->window ? c->sinks : 0;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
     p.err = a.err;
+    p.stamp = a.stamp;
     p.part_o = a.part_o; p.part_ml = a.part_ml;
     // the buffers hold 32 ranges of max_batch tokens
     const cudaError_t e = run_paged_attention(p, sizeof(T) == 2, (int)(32L * c->d.max_batch / a.M), st);

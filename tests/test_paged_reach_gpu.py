@@ -99,3 +99,31 @@ def test_extend_captured_and_replayed():
         del g
     assert st.device_error() == 0
     st.close()
+
+
+def test_timeline_and_profile_of_extensions_and_windows():
+    """The launch timeline knows these attention launches too: one per layer, with time of their own within the call's span."""
+    w = si.Workload("wide", "bf16", 3, 1024, 16, 2, 128, 2048, 2, (0, 1, 0), 2, 16, 4)
+    p = Pair(w, B=2, max_len=1024)
+    st = p.stack
+    p.fill_cache([900, 700])
+    seq = torch.tensor([900, 700], dtype=torch.int32, device=p.device)
+    for S, window in ((4, 0), (60, 0), (60, 100), (1, 300)):
+        st.set_window(window, 4)
+        x = si.make_hidden(w, (2, S, w.hidden), "cpu", 0, S).to(p.device)
+        run = (lambda: st.extend(x, seq, p.block_table, 1000)) if S > 1 else (lambda: st.decode_step(x[:, 0].contiguous(), seq, p.block_table, 1000))
+        plain = run().clone()
+        st.timeline_begin()
+        for _ in range(3):
+            out = run()
+        launches, span, calls = st.timeline_read()
+        st.timeline_end()
+        own = [t for kind, t in launches if kind == "attention"]
+        assert calls == 3 and len(own) == 3 and all(t > 0 for t in own) and sum(t for _, t in launches) <= span
+        assert torch.equal(out, plain)
+        st.profile_begin()
+        run()
+        prof = st.profile_end()
+        assert prof["attention"]["launches"] >= 3 and prof["attention"]["ms"] > 0
+    assert st.device_error() == 0
+    st.close()
