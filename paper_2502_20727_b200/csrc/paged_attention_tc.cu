@@ -140,6 +140,12 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *(const uint32_t *)&v;
 }
+__device__ __forceinline__ float max_nan(float a, float b) // NaN if either is
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 // two fp32 operations per instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
@@ -581,12 +587,12 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
                 float x0 = -INFINITY, x1 = -INFINITY, x2 = -INFINITY, x3 = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
-                    x0 = fmaxf(fmaxf(x0, __uint_as_float(r[e])), __uint_as_float(r[e + 1]));
-                    x1 = fmaxf(fmaxf(x1, __uint_as_float(r[e + 2])), __uint_as_float(r[e + 3]));
-                    x2 = fmaxf(fmaxf(x2, __uint_as_float(r[e + 4])), __uint_as_float(r[e + 5]));
-                    x3 = fmaxf(fmaxf(x3, __uint_as_float(r[e + 6])), __uint_as_float(r[e + 7]));
+                    x0 = max_nan(max_nan(x0, __uint_as_float(r[e])), __uint_as_float(r[e + 1]));
+                    x1 = max_nan(max_nan(x1, __uint_as_float(r[e + 2])), __uint_as_float(r[e + 3]));
+                    x2 = max_nan(max_nan(x2, __uint_as_float(r[e + 4])), __uint_as_float(r[e + 5]));
+                    x3 = max_nan(max_nan(x3, __uint_as_float(r[e + 6])), __uint_as_float(r[e + 7]));
                 }
-                return fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+                return max_nan(max_nan(x0, x1), max_nan(x2, x3));
             };
             uint32_t ra[32], rb[32]; // the first 32 scores are read twice: 64 would not stay in the registers of two blocks
             float mx;
@@ -597,12 +603,13 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
             tmem_ask32(t_s + 32, rb);
             tmem_wait32(rb);
             finish(32, rb);
-            mx = fmaxf(mx, max_of(rb)) * qs;
+            mx = max_nan(mx, max_of(rb)) * qs;
             // join with the other half's maximum: both threads of a row then take the same decision
             float *rm = red + (j & 1) * 256 + row;
             rm[half * 128] = mx;
             asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
-            mx = fmaxf(mx, rm[(half ^ 1) * 128]);
+            mx = max_nan(mx, rm[(half ^ 1) * 128]);
+            if (mx != mx) l = mx; // a NaN among the scores: exp2_poly2 would lose it
             const bool up = mx > m_used + 8.f; // -inf: a row's first keys
             if (__any_sync(0xffffffffu, up)) {
                 // all rows of the warp follow, so that rows whose first keys were few or low do not come one by one
