@@ -15,13 +15,14 @@
 // Tensor memory: S and P at column 0, O at 128.
 // Warps: 0-7 softmax (two threads per row: one per row left the schedulers waiting on their own instructions' latencies), then the
 // load warps, then one that issues the MMAs.  There is one K and one V slot; K is free once S is computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a
-// second load warp looks after V, see below); 8-bit pages (and bf16 pages of other sizes) by four load warps, which widen the
+// second load warp looks after V, see below); bf16 pages of other sizes by four load warps; 8-bit pages by eight (212 us with
+// four where eight take 187), which widen the
 // codes to bf16 on the way into shared memory.  The pairs that widening a 32-bit word gives are (0, 2) and (1, 3) of its four
 // codes: the head dims of Q, K and V all sit in that order, and the output is put right when it is stored.  Row scales multiply
 // the scores (K) and the weights (V) in fp32.  A weight that carries an int8 row's scale is off by up to 2^-8 even where it is the
 // row's only one, and such errors came to 1.5 times the output's own rounding: there what rounding left is a second bf16 with a
-// product of its own (ragged chunks of up to 700 tokens on up to 1000, 40 heads: 266 us, 211 without; e4m3, whose scales are powers
-// of two, 215).
+// product of its own (ragged chunks of up to 700 tokens on up to 1000, 40 heads: 243 us; e4m3, whose scales are powers of two and
+// whose weights are single bf16s, 187; bf16 124).
 // A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
 // shared memory before the product, and rows that do see them get them back at the end.
 // Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
@@ -227,18 +228,22 @@ __device__ __forceinline__ bool clean16(uint4 &u) // takes NaNs and infinities o
 __device__ __forceinline__ constexpr uint32_t weight_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 48 : 0) + ((k & 31) >> 1)); }
 // ... and of what rounding left of it (int8): the rest of those scores' columns
 __device__ __forceinline__ constexpr uint32_t rest_column(int k) { return (uint32_t)((k >> 6) * 64 + (k & 32 ? 32 : 16) + ((k & 31) >> 1)); }
-constexpr int load_warps(bool tma) { return tma ? 2 : 4; }
+constexpr int load_warps(bool tma, bool q8) { return tma ? 2 : q8 ? 8 : 4; }
 constexpr int SOFT_WARPS = 8, SOFT_THREADS = 32 * SOFT_WARPS;
-constexpr int tc_threads(bool tma) { return SOFT_THREADS + 32 * (load_warps(tma) + 1); } // two blocks: 80 registers a thread, or 72
+constexpr int tc_threads(bool tma, bool q8) { return SOFT_THREADS + 32 * (load_warps(tma, q8) + 1); } // two blocks: 80 registers a thread, 72 or 56
+// 8-bit caches: the load warps' way from one tile to the next is the longest, so there are eight of them, and of the 56 registers a thread
+// that 17 warps leave they give 16 to the softmax warps: 8 x 72 + 8 x 40 + 56 = 17 x 56
+constexpr int Q8_LAUNCH_REGS = 56, Q8_SOFT_REGS = 72, Q8_LOAD_REGS = 40;
+static_assert(8 * Q8_SOFT_REGS + 8 * Q8_LOAD_REGS + Q8_LAUNCH_REGS <= 17 * Q8_LAUNCH_REGS);
 
 template <int FMT, int D, bool TMA>
-__global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
+__global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_attention_tc_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                           const __grid_constant__ PagedAttnArgs a)
 {
     using C = TcCfg<D>;
     constexpr bool Q8 = FMT != KV_BF16;
     constexpr uint32_t T_COLS = 256, T_O = 128;
-    constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA);
+    constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA, Q8), LT = 32 * load_warps(TMA, Q8);
     extern __shared__ uint8_t tc_raw[];
     uint8_t *gen = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(gen), bars = base + C::OFF_BAR;
@@ -286,8 +291,8 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
         *abort_flag = 0;
         *dirty = 0;
         mbar_init(q_full, SOFT_THREADS);
-        mbar_init(k_full, TMA ? 1 : 128);
-        mbar_init(v_full, TMA ? 1 : 128);
+        mbar_init(k_full, TMA ? 1 : LT);
+        mbar_init(v_full, TMA ? 1 : LT);
         mbar_init(k_empty, 1);
         mbar_init(v_empty, 1);
         mbar_init(v_clean, 1);
@@ -308,6 +313,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
     fence_after();
     const uint32_t tmem = *tmem_slot;
     if (warp >= W_LOAD && warp < W_MMA) {
+        if (Q8) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Q8_LOAD_REGS));
         const int tid = threadIdx.x - 32 * W_LOAD;
         // one box = 16 keys x 64 dims; lane = (16 keys, half of the head); 16 keys that no row needs come as zeros (a row beyond the map)
         constexpr int BOXES = 8 * (D / 64);
@@ -374,6 +380,10 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
             long *rowoff = (long *)(gen + C::OFF_ROW);
             float *sc = (float *)(gen + C::OFF_SC);
             auto rows_of = [&](int j) { // cached rows (-1: no row needs the key) and scales of the tile's keys
+                if (LT > 128 && tid >= 128) {
+                    named_bar<BAR_LOAD, LT>();
+                    return;
+                }
                 const int t = key0(j) + tid;
                 long row = -1;
                 if (key_needed(t)) {
@@ -387,23 +397,23 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
                     sc[(j & 7) * 256 + 128 + tid] = row >= 0 ? a.kv.vs[row] : 0.f;
                     mbar_arrive(sc_full(j & 7)); // eight tiles later the slot's scores have long been weighted
                 }
-                named_bar<BAR_LOAD, 128>();
+                named_bar<BAR_LOAD, LT>();
             };
             if (Q8) {
-                constexpr int CPR = D / 16, N = CPR / 2; // 16-code chunks per row; per thread and half a tile (64 keys)
+                constexpr int CPR = D / 16, N = 64 * CPR / LT; // 16-code chunks per row; per thread and half a tile (64 keys)
                 const uint32_t c128 = widen_const();
                 const int c = tid % CPR;
                 auto fetch = [&](int j, int h, const void *pages, uint4 (&x)[N]) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const long row = rowoff[(j & 1) * 128 + h * 64 + i * (128 / CPR) + tid / CPR];
+                        const long row = rowoff[(j & 1) * 128 + h * 64 + i * (LT / CPR) + tid / CPR];
                         x[i] = row >= 0 ? *(const uint4 *)((const uint8_t *)pages + row * D + c * 16) : make_uint4(0, 0, 0, 0);
                     }
                 };
                 auto widen = [&](uint32_t tile_base, int h, const uint4 (&x)[N]) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const int r = h * 64 + i * (128 / CPR) + tid / CPR;
+                        const int r = h * 64 + i * (LT / CPR) + tid / CPR;
                         const uint4 lo = make_uint4(even2<FMT>(x[i].x, c128), odd2<FMT>(x[i].x, c128), even2<FMT>(x[i].y, c128), odd2<FMT>(x[i].y, c128));
                         const uint4 hi = make_uint4(even2<FMT>(x[i].z, c128), odd2<FMT>(x[i].z, c128), even2<FMT>(x[i].w, c128), odd2<FMT>(x[i].w, c128));
                         const bool swap = (c >> 2) & 1; // the two halves of the head in turn: other banks
@@ -521,6 +531,7 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
         }
         __syncwarp();
     } else {
+        if (Q8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Q8_SOFT_REGS));
         const int half = warp >> 2, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + (warp & 3);
         // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
         {
@@ -762,10 +773,18 @@ __global__ void __launch_bounds__(tc_threads(TMA), 2) paged_attention_tc_kernel(
 template <int FMT, int D, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a, const TcMap &km, const TcMap &vm, cudaStream_t st)
 {
     static SmemLimit limit;
+    if (FMT != KV_BF16) { // the registers that the warps pass on have to be there
+        static const cudaError_t fits = [] {
+            cudaFuncAttributes f{};
+            const cudaError_t e = cudaFuncGetAttributes(&f, (const void *)paged_attention_tc_kernel<FMT, D, TMA>);
+            return e != cudaSuccess ? e : f.numRegs == Q8_LAUNCH_REGS ? cudaSuccess : cudaErrorInvalidKernelImage;
+        }();
+        if (fits != cudaSuccess) return fits;
+    }
     const cudaError_t e = limit.raise((const void *)paged_attention_tc_kernel<FMT, D, TMA>, TcCfg<D>::SMEM);
     if (e != cudaSuccess) return e;
     const long tiles = ((long)a.max_new * a.group + TQ - 1) / TQ;
-    return launch_kernel(paged_attention_tc_kernel<FMT, D, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA)),
+    return launch_kernel(paged_attention_tc_kernel<FMT, D, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA, FMT != KV_BF16)),
                          TcCfg<D>::SMEM, st, 0, km, vm, a);
 }
 template <int FMT, int D> cudaError_t tc_by_copy(const PagedAttnArgs &a, cudaStream_t st)
