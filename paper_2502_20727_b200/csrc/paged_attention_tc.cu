@@ -14,9 +14,9 @@
 //                  stored); O stays in tensor memory and is rescaled there only when the row maximum has grown by more than 2^8
 // Tensor memory: S and P at column 0, O at 128.
 // Warps: 0-7 softmax (two threads per row: one per row left the schedulers waiting on their own instructions' latencies), then the
-// load warps, then one that issues the MMAs.  There is one K and one V slot; K is free once S is computed.  bf16 pages of a multiple of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a
-// second load warp looks after V, see below); bf16 pages of other sizes by four load warps; 8-bit pages by eight (212 us with
-// four where eight take 187), which widen the
+// load warps, then one that issues the MMAs.  There is one K and one V slot; K is free once S is computed.  bf16 pages of a multiple
+// of 16 tokens arrive by TMA, one box per 16 keys and 64 dims (a second load warp looks after V, see below); bf16 pages of other
+// sizes by four load warps; 8-bit pages by eight (four took 212 us where eight take 187), which widen the
 // codes to bf16 on the way into shared memory.  The pairs that widening a 32-bit word gives are (0, 2) and (1, 3) of its four
 // codes: the head dims of Q, K and V all sit in that order, and the output is put right when it is stored.  Row scales multiply
 // the scores (K) and the weights (V) in fp32.  A weight that carries an int8 row's scale is off by up to 2^-8 even where it is the
