@@ -36,7 +36,7 @@ struct PagedAttnArgs {
     int window, sinks;            // window 0: everything before the query
     float scale_log2;             // softmax scale times log2(e)
     int splits;                   // ranges the keys of a row tile are cut into
-    int row_tile;                 // general kernel: rows of a thread block (16, 32, 64)
+    int row_tile;                 // general kernel: rows of a thread block (16 or 64)
     int stages;                   // paged_attention_rows.cu: set by its launcher
     float *part_o, *part_ml;      // ranges that no cluster adds up (else null): fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
     int *err;

@@ -291,7 +291,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
         if (s > (keys + 127) / 128) s = (keys + 127) / 128;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-    } else     if (rows <= PAGED_MAX_FEW_ROWS) {
+    } else if (rows <= PAGED_MAX_FEW_ROWS) {
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
         // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
@@ -308,8 +308,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
             if (s < 12) s = PAGED_MAX_CLUSTER;
         }
         p.splits = (int)(s < 1 ? 1 : s);
-    }
-    else {
+    } else {
         // two thread blocks per SM: ranges where the row tiles leave some idle, of at least four tiles of 128 keys
         p.kernel = ATTN_TC;
         const long blocks = (rows + 127) / 128 * nkv * (B > 0 ? B : 1);
