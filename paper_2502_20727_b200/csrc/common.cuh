@@ -29,10 +29,15 @@ template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
 
-// Programmatic dependent launch.  Every kernel of the library signals at its very top that the
-// next kernel in the stream may be scheduled, and waits for the completion (and memory
-// visibility) of the previous one before it touches anything a predecessor wrote or may still
-// read.  Both are no-ops for a kernel launched without the attribute.
+// Programmatic dependent launch.  A kernel of the library signals at its top that the next kernel in the stream may be scheduled,
+// and waits for the completion (and memory visibility) of the previous one before it touches anything a predecessor wrote or may
+// still read.  Both are no-ops for a kernel launched without the attribute.
+// Tensor memory: the GEMMs allocate theirs before they wait and hold it until then, and tcgen05.alloc waits without a limit.  So a
+// kernel that waits before it allocates signals only once it owns its columns: the next kernel, which starts when every block has
+// signalled or ended, then cannot take columns that a block of this one still needs.  Kernels that allocate at their top may signal
+// first, because no mix of them that shares an SM is short of columns: those with all 512 columns need more than 190 KB of shared
+// memory and share with none; a GEMM's block of 128 columns needs 75 KB or more, of fewer 56 KB or more, so that at most four
+// blocks with 512 columns in all fit.
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

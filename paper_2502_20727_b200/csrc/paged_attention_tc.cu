@@ -243,8 +243,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) stamp_entry(a.stamp);
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_wait(); // pdl_launch_dependents: below, once the block owns its tensor memory
     const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
     int row0, n_new, len;
     if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
@@ -298,6 +297,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_slot;
+    pdl_launch_dependents();
     if (warp >= W_LOAD && warp < W_MMA) {
         if (Q8) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Q8_LOAD_REGS));
         const int tid = threadIdx.x - 32 * W_LOAD;
