@@ -260,8 +260,8 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  *                 code = x / s rounded to nearest (exact division; within a factor of two of the
  *                 largest float, codes stop where code * s is still finite); code * s is exact in bfloat16;
  *                 the codes 0x7f and 0xff (NaN) are never written and must not be in a row that is read
- *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 / max|x|) rounded to
- *                 nearest in -127 .. 127 (the factor is within two units in its last place)
+ *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 * (1 / max|x|)), the
+ *                 reciprocal and both products rounded to float32, rounded to nearest (half to even) in -127 .. 127
  * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0. */
 #define SPD_KV_F32 0
 #define SPD_KV_BF16 1

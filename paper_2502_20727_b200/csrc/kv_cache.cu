@@ -4,7 +4,8 @@
 //   e4m3 : s = the smallest power of two with max|x| <= 448 s; code = x / s rounded to e4m3.  The division is exact, so
 //          the only rounding is e4m3's (relative 2^-4 at most, absolute s 2^-10 below the normal range), and code * s
 //          is exact in bfloat16 too.
-//   int8 : s = max|x| / 127; code = x * (127 / max|x|) rounded to the nearest integer, half to even.
+//   int8 : s = max|x| / 127; code = x * (127 * (1 / max|x|)) rounded to the nearest integer, half to even; quotient, reciprocal and
+//          products are rounded to float32, which moves values within 2^-22 of a border between two codes at most.
 // A row of zeros has s = 1; s is at least 2^-126; a row that holds a NaN or an infinity gets s = NaN and codes 0, so that
 // reading it gives NaN everywhere and nothing else is touched.
 //
@@ -190,14 +191,10 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, Ragged
             codes = make_uint2(e4m3_x4(x[0], x[1], x[2], x[3]), e4m3_x4(x[4], x[5], x[6], x[7]));
         } else {
             // amax / 127 by a product with the rounded reciprocal and one residual correction, which gives the rounded quotient
-            // (Markstein 1990); 127 / amax by the approximate reciprocal (a unit in the last place), whose argument is kept
-            // where it neither over- nor underflows
+            // (Markstein 1990); the codes' factor is the rounded reciprocal times 127, rounded: the same bits wherever a row is quantised
             const float q0 = amax * (1.f / 127.f);
             s = fmaxf(fmaf(fmaf(-q0, 127.f, amax), 1.f / 127.f, q0), 1.17549435e-38f);
-            const float c = amax > 4.2e37f ? 0.0625f : 1.f; // 2^125
-            float inv;
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaxf(amax, 127.f * 1.17549435e-38f) * c));
-            inv *= 127.f * c;
+            const float inv = __fmul_rn(__frcp_rn(fmaxf(amax, 127.f * 1.17549435e-38f)), 127.f);
             codes = make_uint2(int8_x4(x, inv), int8_x4(x + 4, inv));
         }
         if (m == 0) s = 1.f;
