@@ -606,7 +606,9 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             rm[half * 128] = mx;
             asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
             mx = max_nan(mx, rm[(half ^ 1) * 128]);
-            if (mx != mx) l = mx; // a NaN among the scores: exp2_poly2 would lose it
+            // A NaN or +inf among the scores: no softmax.  Said here, because exp2_poly2 would make a weight of 0 of the NaN or inf - inf
+            // that is its argument then.
+            if (!(mx < INFINITY)) l = __uint_as_float(0x7fc00000u);
             const bool up = mx > m_used + 8.f; // -inf: a row's first keys
             if (__any_sync(0xffffffffu, up)) {
                 // all rows of the warp follow, so that rows whose first keys were few or low do not come one by one

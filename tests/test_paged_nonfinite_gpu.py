@@ -1,0 +1,96 @@
+"""Attention over a cache whose K rows give infinite scores, with finite V: what softmax makes of them, in every kernel."""
+import math
+
+import pytest
+import torch
+
+from paged_util import Batch
+from test_paged_gpu import TYPES, attend
+
+pytestmark = pytest.mark.gpu
+
+HEAD, DIM = 1, 7  # the KV head whose K rows are poisoned, and the head dim
+
+
+def batch(types, **kw):
+    bt = Batch(dtype=types[0], fmt=types[1], seed=21, **{**dict(nq=4, nkv=2, d=64, page=16), **kw})
+    bt.q = bt.q.abs() + 0.125  # the sign of a poisoned score is that of the infinity
+    return bt
+
+
+def poison(bt, dev, t, sign):
+    """Every score of key t (sequence 0) becomes sign * inf.  8-bit: codes of +-1 under an infinite scale, so that every term of the
+    score is the same infinity (a code of 0 would stand for 0 * inf)."""
+    p, s = bt.row_of(0, t)
+    k = dev["k_pages"][p, HEAD, s]
+    if dev["k_scales"] is None:
+        k[DIM] = sign * math.inf
+    else:
+        k.view(torch.uint8).fill_((0x38 if sign > 0 else 0xB8) if bt.fmt == "e4m3" else (1 if sign > 0 else 255))
+        dev["k_scales"][p, HEAD, s] = math.inf
+
+
+def reference(bt, gone):
+    """Sequence 0 as if the keys `gone` of the poisoned head did not exist; the tolerance is Batch.reference's.  NaN where no key is left."""
+    a, n, group = bt.lens[0], bt.new[0], bt.nq // bt.nkv
+    idx = torch.tensor([bt.row_of(0, t) for t in range(a + n)])
+    k, v = (bt.values[x][idx[:, 0], :, idx[:, 1]] for x in "kv")
+    t, p = torch.arange(a + n), torch.arange(a, a + n)[:, None]
+    see = t <= p
+    if bt.window:
+        see &= (t > p - bt.window) | (t < bt.sinks)
+    out = torch.full((n, bt.nq, bt.d), math.nan, dtype=torch.float64)
+    tol = torch.zeros_like(out)
+    q = bt.q.double()
+    for h in range(bt.nq):
+        left = see.clone()
+        if h // group == HEAD:
+            left[:, list(gone)] = False
+        kh, vh, scale = k[:, h // group], v[:, h // group], bt.d ** -0.5
+        w = torch.softmax((q[:, h] @ kh.t() * scale).masked_fill(~left, -math.inf), -1)
+        mag = (q[:, h].abs() @ kh.abs().t() * scale).masked_fill(~left, 0).amax(-1, keepdim=True)
+        aw = w @ vh.abs()
+        out[:, h] = w @ vh
+        tol[:, h] = (2 * (bt.d + 8) * 2.0 ** -24 * mag + 2.0 ** -18 + 2 * (a + n) * 2.0 ** -24) * aw
+        if bt.dtype == torch.bfloat16:
+            tol[:, h] += 1.01 * 2.0 ** -8 * (aw + out[:, h].abs())
+    return out, tol
+
+
+def check(got, ref, tol):
+    got, want = got.double().cpu(), ~torch.isnan(ref)
+    assert torch.isnan(got[~want]).all(), "a row without a softmax has to be NaN"
+    off = (got - ref).abs()[want] / tol[want]
+    assert torch.isfinite(off).all() and (off <= 1).all(), off.max()
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("new,page", [(1, 16), (3, 16), (40, 16), (40, 24), (1, 24)])
+@pytest.mark.parametrize("at", list(range(8)) + list(range(64, 72)))
+def test_a_score_of_infinity_is_nan_wherever_the_key_lies(types, new, page, at):
+    """Queries that see the key: inf - inf in every weight's sum.  The others, and the other KV head: nothing."""
+    lens = 128 + at - (new + 1) // 2  # some of the new tokens come before key 128 + at, where there are any
+    bt = batch(types, lens=[lens], new=[new], page=page)
+    dev = bt.device()
+    t = 128 + at if new > 1 else at
+    poison(bt, dev, t, 1)
+    out, err = attend(bt, dev)
+    assert err == 0
+    ref, tol = reference(bt, ())
+    p = torch.arange(lens, lens + new)
+    ref[p >= t, 2:] = math.nan
+    check(out, ref, tol)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("new", [2, 5, 100])
+def test_scores_of_minus_infinity_have_no_weight(types, new):
+    """Keys with such scores among others: as if they did not exist."""
+    bt = batch(types, lens=[150], new=[new])
+    dev = bt.device()
+    gone = list(range(3, 150, 7)) + [150]
+    for t in gone:
+        poison(bt, dev, t, -1)
+    out, err = attend(bt, dev)
+    assert err == 0
+    check(out, *reference(bt, gone))
