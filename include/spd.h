@@ -314,8 +314,8 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  *            between the sinks and the window may name anything (the pages may have been given back).
  *   workspace : device memory, 256-byte aligned, at least spd_paged_attention_workspace_bytes() (may be null where that is
  *            0); contents before and after do not matter; calls that may run at the same time need one each.
- * A key that a query does not see has no influence on it, whatever it holds.  A query with a visible score of NaN or +inf has no
- * softmax: its whole output row is NaN.  Scores, sums and the output are held in
+ * A key that a query does not see has no influence on it, whatever it holds.  A query with a visible score of NaN or +inf, or
+ * whose visible scores are all -inf, has no softmax: its whole output row is NaN.  Scores, sums and the output are held in
  * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product (two bfloat16s, 16 bits,
  * with an int8 cache).
  * A page id outside [0, n_pages) sets error bit 1; the output rows that needed it are undefined.

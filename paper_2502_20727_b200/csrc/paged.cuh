@@ -107,6 +107,10 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
     return true;
 }
 
+// What the weighted sum of a row is multiplied by.  Every query sees its own key, so a sum of 0 (all its scores -inf) has no softmax,
+// and neither has one of NaN.
+__device__ __forceinline__ float inverse_sum(float den) { return den > 0.f ? 1.f / den : __uint_as_float(0x7fc00000u); }
+
 // A kernel's dynamic shared-memory limit, raised once per device.
 struct SmemLimit {
     bool done[64] = {};

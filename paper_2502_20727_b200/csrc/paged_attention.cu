@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(G_THREADS) paged_attention_general_kernel(cons
         if (l[i] != l[i]) m[i] = fmaxf(m[i], 0.f); // scores that are all NaN leave no maximum
         if (a.part_o && tx == 0) { a.part_ml[w * 2] = m[i]; a.part_ml[w * 2 + 1] = l[i]; }
         if (D < 64 && tx >= D / 4) continue;
-        const float inv = a.part_o ? 1.f : (l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]));
+        const float inv = a.part_o ? 1.f : inverse_sum(l[i]);
 #pragma unroll
         for (int k = 0; k < OC; ++k) {
             const int c = tx * 4 + 64 * k;

@@ -580,7 +580,6 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         dst_of[r] = a.part_o ? (long)split * plane + (long)(row0 + i) * a.nq + head : (long)(row0 + i) * a.o_stride + (long)head * D;
     }
     __syncthreads();
-    auto inverse = [](float den) { return den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den); };
 #pragma unroll 4
     for (int idx = threadIdx.x; idx < rows * (D / 2); idx += R_THREADS) {
         const int r = idx / (D / 2), c = idx % (D / 2) * 2;
@@ -608,7 +607,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             }
         }
         if (a.splits == 1) {
-            const float inv = inverse(pml[2 * r + 1]);
+            const float inv = inverse_sum(pml[2 * r + 1]);
             *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x * inv, y * inv);
         } else if (clustered) // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
             *(float2 *)(mo + r * (D + 2) + c) = make_float2(x, y);
@@ -640,7 +639,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 q[s].x = q[s].x == -INFINITY ? 0.f : ex2(q[s].x - m);
                 den = fmaf(q[s].y, q[s].x, den);
             }
-            const float inv = inverse(den);
+            const float inv = inverse_sum(den);
 #pragma unroll
             for (int s = 0; s < PAGED_MAX_CLUSTER; ++s)
                 if (s < splits) cw[r * PAGED_MAX_CLUSTER + s] = q[s].x * inv;
@@ -721,7 +720,7 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
             for (int e = 0; e < VEC; ++e) o[e] = fmaf(v[k][e], f[k], o[e]);
         }
     }
-    const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
+    const float inv = inverse_sum(den);
     T *dst = (T *)a.out + (long)t * a.o_stride + (long)head * D + lane * VEC;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dst[e] = from_f<T>(o[e] * inv);

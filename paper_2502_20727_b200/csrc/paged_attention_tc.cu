@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             const float den = l + red[(half ^ 1) * 128 + row];
             float m = m_used;
             if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum
-            const float inv = a.part_o ? 1.f : (den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den));
+            const float inv = a.part_o ? 1.f : inverse_sum(den);
             const int head = kvh * a.group + head_of(row, my_token);
             const long token = row0 + tok0 + my_token;
             const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
