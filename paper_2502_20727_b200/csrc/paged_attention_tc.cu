@@ -699,41 +699,43 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2) && n_tiles > 0 && ok; c0 += 16) {
                 uint32_t y[16];
                 float v[16], x[16];
-                tmem_ld16u(tmem + lanes + T_O + c0, y); // warp-wide: lanes without a row load too
-                if (!live) continue;
+                __syncwarp(); // the load is the whole warp's; rows take their own ways below
+                tmem_ld16u(tmem + lanes + T_O + c0, y);
+                if (live) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(y[e]);
-                if (give_back) {
-                    for (int j = 0; j < n_tiles; ++j) {
-                        const int t0 = key0(j);
-                        for (int t = t0; t < t0 + TK && partial(t0); ++t) {
-                            if (t > pos || (a.window && t <= pos - a.window && t >= a.sinks)) continue;
-                            const int pi = t / a.kv.page, page = bt[pi];
-                            if (page < 0 || page >= a.kv.n_pages) continue;
-                            const bf16 *src = (const bf16 *)a.kv.v + (((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page)) * D + c0;
+                    for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(y[e]);
+                    if (give_back) {
+                        for (int j = 0; j < n_tiles; ++j) {
+                            const int t0 = key0(j);
+                            for (int t = t0; t < t0 + TK && partial(t0); ++t) {
+                                if (t > pos || (a.window && t <= pos - a.window && t >= a.sinks)) continue;
+                                const int pi = t / a.kv.page, page = bt[pi];
+                                if (page < 0 || page >= a.kv.n_pages) continue;
+                                const bf16 *src = (const bf16 *)a.kv.v + (((long)page * a.kv.nkv + kvh) * a.kv.page + (t - pi * a.kv.page)) * D + c0;
 #pragma unroll 1
-                            for (int e = 0; e < 16; ++e) {
-                                const float z = __bfloat162float(src[e]);
-                                if (!isfinite(z)) {
+                                for (int e = 0; e < 16; ++e) {
+                                    const float z = __bfloat162float(src[e]);
+                                    if (!isfinite(z)) {
 #pragma unroll
-                                    for (int k = 0; k < 16; ++k)
-                                        if (k == e) v[k] += z;
+                                        for (int k = 0; k < 16; ++k)
+                                            if (k == e) v[k] += z;
+                                    }
                                 }
                             }
                         }
                     }
-                }
-                // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
+                    // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
-                if (a.part_o) {
+                    for (int e = 0; e < 16; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
+                    if (a.part_o) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                } else { // through the Q tile, so that whole rows leave together
+                        for (int e = 0; e < 16; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    } else { // through the Q tile, so that whole rows leave together
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
-                        sts128(base + C::OFF_Q + tile_at(row, (c0 + e) >> 3),
-                               make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7])));
+                        for (int e = 0; e < 16; e += 8)
+                            sts128(base + C::OFF_Q + tile_at(row, (c0 + e) >> 3),
+                                   make_uint4(pack(x[e], x[e + 1]), pack(x[e + 2], x[e + 3]), pack(x[e + 4], x[e + 5]), pack(x[e + 6], x[e + 7])));
+                    }
                 }
             }
             if (!a.part_o && n_tiles > 0) {

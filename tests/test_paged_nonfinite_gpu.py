@@ -124,3 +124,22 @@ def test_key_ranges_of_minus_infinity(types, nq, lens, new):
         out, err = attend(bt, dev)
         assert err == 0
         check(out, *reference(bt, gone))
+
+
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("nq,nkv,lens,new", [(4, 2, 90, 45), (6, 2, 130, 43), (4, 1, 3000, 5), (2, 2, 0, 129), (8, 2, 200, 33)])
+def test_infinite_values_in_tiles_that_rows_do_not_fill(page, nq, nkv, lens, new):
+    """Row tiles with rows left over, whose warps' lanes differ in what they see of several infinities in V."""
+    bt = Batch(dtype="bf16", fmt="bf16", nq=nq, nkv=nkv, d=128, page=page, lens=[lens], new=[new], seed=22)
+    dev = bt.device()
+    ref, tol = bt.reference()
+    group, head = nq // nkv, nkv - 1
+    for i, dim in ((0, 3), (1, 40), (new // 2, 100), (new - 1, 17)):  # the i-th new token's value, in one dim
+        p, s = bt.row_of(0, lens + i)
+        dev["v_pages"][p, head, s, dim] = math.inf
+        ref[i:, head * group:, dim] = math.nan
+    out, err = attend(bt, dev)
+    assert err == 0
+    got, hit = out.double().cpu(), torch.isnan(ref)
+    assert (~torch.isfinite(got[hit])).all()
+    assert ((got - ref).abs()[~hit] <= tol[~hit]).all()
