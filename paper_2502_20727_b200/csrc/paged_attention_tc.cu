@@ -510,8 +510,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             } else
                 commit(o_done);
         }
-        if (*abort_flag && n_tiles > 0) { // products in flight end before tensor memory is freed
-            __syncwarp();
+        // one answer for the warp: another warp may raise the flag at this moment
+        if (__any_sync(0xffffffffu, *abort_flag) && n_tiles > 0) { // products in flight end before tensor memory is freed
             commit(drain);
             settle(drain, 0);
         }

@@ -41,3 +41,12 @@ def test_columns_are_owned_before_the_next_kernel_may_take_them(file, kernel, at
     assert min(at.values()) >= 0
     if at["wait"] < at["alloc"]:
         assert at["alloc"] < at["signal"], f"{file}: {kernel} lets the next kernel start before it owns its tensor memory"
+
+
+@pytest.mark.parametrize("path", spd_build.sources())
+def test_a_warp_takes_one_way_past_the_abort_flag(path):
+    """Any warp may raise the flag at any time, so lanes that read it for themselves can differ: where a warp-wide instruction
+    (tcgen05.commit by an elected lane) hangs on it, the warp has to have one answer."""
+    for m in re.finditer(r"if \(([^{;]*\babort_flag\b[^{;]*)\) \{([^}]*)\}", re.sub(r"//[^\n]*", "", open(path).read())):
+        if re.search(r"\bcommit\(|elect\.sync", m.group(2)):
+            assert re.search(r"__(any|all)_sync\(0xffffffffu, \*abort_flag\)", m.group(1)), m.group(0)
