@@ -60,10 +60,13 @@ __device__ __forceinline__ void stamp_exit(unsigned long long *slot)
     atomicMin(slot + 1, ~t);
 }
 
-// Launch with the programmatic-stream-serialization attribute (and an optional cluster size).
+// Launch with the programmatic-stream-serialization attribute (and an optional cluster size).  overlap false: without the attribute,
+// that is after everything before it in the stream has ended.  The first kernel of a decode step is launched so: the step's
+// attention asks for pages of earlier tokens before its own wait, and a chain of kernels that all signal at their tops gives no
+// other assurance that what was launched before the step (an append, a prompt, another step) has written them.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                                 int cluster_x, Args &&...args)
+inline cudaError_t launch_kernel_after(bool overlap, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
+                                       int cluster_x, Args &&...args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -72,9 +75,11 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     int n = 0;
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
+    if (overlap) {
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     if (cluster_x > 1) {
         at[n].id = cudaLaunchAttributeClusterDimension;
         at[n].val.clusterDim.x = (unsigned)cluster_x;
@@ -85,6 +90,11 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
     cfg.attrs = at;
     cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster_x, Args &&...args)
+{
+    return launch_kernel_after(true, kernel, grid, block, smem, st, cluster_x, args...);
 }
 
 // The same with a thread-block cluster along grid z.
@@ -179,13 +189,13 @@ struct NormArgs {
     // RMSNorm into a LayerNorm with that shift
     const void *bias, *shift;
 };
-template <typename T> cudaError_t launch_residual_norm(const NormArgs &a, cudaStream_t st);
+template <typename T> cudaError_t launch_residual_norm(const NormArgs &a, cudaStream_t st, bool overlap = true);
 
 // wg[n] = sum_k g[k] W[n][k], wb[n] = sum_k beta[k] W[n][k] + b[n] (b may be null); W bf16 [N][K] (block with bias, Sec. 4.1.2)
 cudaError_t launch_ln_fold(const void *W, int N, int K, const void *g, const void *beta, const void *b, float *wg, float *wb, cudaStream_t st);
 
 cudaError_t launch_rope_table(float2 *table, TokMap tm, int M, int head_dim, float base, cudaStream_t st,
-                              unsigned long long *stamp = nullptr);
+                              unsigned long long *stamp = nullptr, bool overlap = true);
 
 struct RopeKvArgs {
     const float *qkv;     // fp32 [splits][M][ldq]: columns [q | k | v]

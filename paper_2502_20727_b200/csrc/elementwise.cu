@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256) residual_norm_cluster_kernel(NormArgs a)
     }
 }
 
-template <typename T> cudaError_t launch_residual_norm(const NormArgs &a, cudaStream_t st)
+template <typename T> cudaError_t launch_residual_norm(const NormArgs &a, cudaStream_t st, bool overlap)
 {
     if (a.M <= 0) return cudaSuccess;
     if (a.H % 4 || a.n_groups > MAX_T) return cudaErrorInvalidValue;
@@ -232,14 +232,14 @@ template <typename T> cudaError_t launch_residual_norm(const NormArgs &a, cudaSt
         const int cpc = h4 / CS;
         const int threads = cpc >= 256 ? 256 : (cpc + 31) / 32 * 32;
         const dim3 grid((unsigned)(a.M * CS));
-        if (cpc <= threads) return launch_kernel(residual_norm_cluster_kernel<T, 1>, grid, dim3(threads), 0, st, CS, a);
-        return launch_kernel(residual_norm_cluster_kernel<T, 2>, grid, dim3(threads), 0, st, CS, a);
+        if (cpc <= threads) return launch_kernel_after(overlap, residual_norm_cluster_kernel<T, 1>, grid, dim3(threads), 0, st, CS, a);
+        return launch_kernel_after(overlap, residual_norm_cluster_kernel<T, 2>, grid, dim3(threads), 0, st, CS, a);
     }
     const int threads = h4 >= 512 ? 512 : (h4 + 31) / 32 * 32;
-    return launch_kernel(residual_norm_kernel<T>, dim3(a.M), dim3(threads), 0, st, 0, a);
+    return launch_kernel_after(overlap, residual_norm_kernel<T>, dim3(a.M), dim3(threads), 0, st, 0, a);
 }
-template cudaError_t launch_residual_norm<float>(const NormArgs &, cudaStream_t);
-template cudaError_t launch_residual_norm<bf16>(const NormArgs &, cudaStream_t);
+template cudaError_t launch_residual_norm<float>(const NormArgs &, cudaStream_t, bool);
+template cudaError_t launch_residual_norm<bf16>(const NormArgs &, cudaStream_t, bool);
 
 // Block with bias: the two vectors that let a LayerNorm commute with the projection that follows it,
 // wg[n] = sum_k g[k] W[n][k] and wb[n] = sum_k beta[k] W[n][k] + b[n] (one warp per weight row, fp32 sums of the
@@ -285,11 +285,12 @@ __global__ void rope_table_kernel(float2 *table, TokMap tm, int M, int half, dou
     if (threadIdx.x == 0) stamp_exit(stamp);
 }
 
-cudaError_t launch_rope_table(float2 *table, TokMap tm, int M, int head_dim, float base, cudaStream_t st, unsigned long long *stamp)
+cudaError_t launch_rope_table(float2 *table, TokMap tm, int M, int head_dim, float base, cudaStream_t st, unsigned long long *stamp,
+                              bool overlap)
 {
     int n = M * (head_dim / 2);
     if (n <= 0) return cudaSuccess;
-    return launch_kernel(rope_table_kernel, dim3((n + 255) / 256), dim3(256), 0, st, 0, table, tm, M, head_dim / 2,
+    return launch_kernel_after(overlap, rope_table_kernel, dim3((n + 255) / 256), dim3(256), 0, st, 0, table, tm, M, head_dim / 2,
                          log((double)base), head_dim, stamp);
 }
 

@@ -1013,7 +1013,7 @@ cudaError_t launch_decode_prologue(const PrologueArgs &a, cudaStream_t st)
     if (a.M <= 0) return cudaSuccess;
     const int h_tiles = (a.H + 127) / 128;
     const int table_blocks = a.rope_table ? (a.M * (a.head_dim / 2) + 127) / 128 : 0;
-    return launch_kernel(decode_prologue_kernel, dim3(h_tiles + table_blocks, a.n_z > 1 ? a.n_z : 1), dim3(128), 0, st, 0, a, h_tiles,
+    return launch_kernel_after(false, decode_prologue_kernel, dim3(h_tiles + table_blocks, a.n_z > 1 ? a.n_z : 1), dim3(128), 0, st, 0, a, h_tiles,
                          a.rope_table ? log((double)a.rope_base) : 0.0);
 }
 

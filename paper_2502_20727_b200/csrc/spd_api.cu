@@ -517,7 +517,7 @@ int run_tokens(Ctx *c, const void *x, void *out, int M, TokMap tm, const int32_t
     const bool opt = d.block_kind == 1;              // block with bias (Sec. 4.1.2): LayerNorm, biases, ReLU, no rotary
     const bool rope_on = d.rope_base > 0.f && !opt;
 
-    if (rope_on) LAUNCH(K_ROPE_TABLE, launch_rope_table(c->rope, tm, M, d.head_dim, d.rope_base, st));
+    if (rope_on) LAUNCH(K_ROPE_TABLE, launch_rope_table(c->rope, tm, M, d.head_dim, d.rope_base, st, nullptr, !decode));
 
     // block input -> fp32 residual stream and its attention RMSNorm
     {
@@ -525,7 +525,7 @@ int run_tokens(Ctx *c, const void *x, void *out, int M, TokMap tm, const int32_t
         a.x_in = x; a.res_out = c->res[0]; a.h_out = c->h; a.h_stride = Mc * H;
         a.gain = c->layers[0].attn_norm; a.n_groups = 1; a.per_group = 0; a.M = M; a.H = H; a.eps = d.rms_eps;
         if (opt) a.shift = c->layers[0].attn_norm_b;
-        LAUNCH(K_NORM, launch_residual_norm<T>(a, st));
+        LAUNCH(K_NORM, launch_residual_norm<T>(a, st, !decode || rope_on));
     }
     for (int l = 0; l < d.n_layers; ++l) {
         const spd_layer &w = c->layers[l];
@@ -718,12 +718,12 @@ int run_tp_baseline(Ctx *c, const void *x, void *out, int M, TokMap tm, const in
         return SPD_OK;
     };
 
-    if (rope_on) LAUNCH(K_ROPE_TABLE, launch_rope_table(c->rope, tm, M, d.head_dim, d.rope_base, st));
+    if (rope_on) LAUNCH(K_ROPE_TABLE, launch_rope_table(c->rope, tm, M, d.head_dim, d.rope_base, st, nullptr, !decode));
     {
         NormArgs a{};
         a.x_in = x; a.res_out = cur; a.h_out = c->h; a.h_stride = Mc * H;
         a.gain = c->layers[0].attn_norm; a.n_groups = 1; a.per_group = 0; a.M = M; a.H = H; a.eps = d.rms_eps;
-        LAUNCH(K_NORM, launch_residual_norm<bf16>(a, st));
+        LAUNCH(K_NORM, launch_residual_norm<bf16>(a, st, !decode || rope_on));
     }
     for (int l = 0; l < d.n_layers; ++l) {
         const spd_layer &w = c->layers[l];
