@@ -277,7 +277,8 @@ typedef struct {
 
 /* Token rows of a batch of B sequences of unequal lengths: rows cu_new[b] .. cu_new[b+1]-1 of a tensor with n_tokens
  * rows are sequence b's, at positions seq_lens[b], seq_lens[b]+1, ...  Rows before cu_new[0] or from cu_new[B] on belong
- * to nobody: they are neither computed nor written.  A sequence without rows is allowed. */
+ * to nobody: they are neither computed nor written.  A sequence without rows is allowed, and so is a batch of none (B 0, with
+ * null arrays if need be). */
 typedef struct {
     const int32_t *cu_new;      /* [B + 1] device, not decreasing                                            */
     const int32_t *seq_lens;    /* [B] device                                                                */

@@ -317,7 +317,7 @@ int check_cache(const spd_kv_cache *c, const spd_ragged *r, PagedKv *kv, RaggedB
     if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->kv_block_size < 1) return SPD_EINVAL;
     if (r->B < 0 || r->n_tokens < 0 || r->max_pages < 1) return SPD_EINVAL;
     if (!c->k_pages || !c->v_pages || (c->format >= SPD_KV_E4M3 && (!c->k_scales || !c->v_scales))) return SPD_ENULL;
-    if (!r->cu_new || !r->seq_lens || !r->block_table) return SPD_ENULL;
+    if (r->B && (!r->cu_new || !r->seq_lens || !r->block_table)) return SPD_ENULL; // arrays of no elements may be null
     if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || ((uintptr_t)c->k_scales & 3) || ((uintptr_t)c->v_scales & 3)) return SPD_EINVAL;
     *kv = PagedKv{c->k_pages, c->v_pages, c->k_scales, c->v_scales, c->n_pages, c->n_kv_heads, c->kv_block_size, c->head_dim, c->format};
     *rb = RaggedBatch{r->cu_new, r->seq_lens, r->block_table, r->B, r->max_pages, r->n_tokens, 0, 0};
