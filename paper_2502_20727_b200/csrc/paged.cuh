@@ -3,6 +3,7 @@
 #pragma once
 #include "common.cuh"
 
+#include <atomic>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -111,9 +112,9 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
 // and neither has one of NaN.
 __device__ __forceinline__ float inverse_sum(float den) { return den > 0.f ? 1.f / den : __uint_as_float(0x7fc00000u); }
 
-// A kernel's dynamic shared-memory limit, raised once per device.
+// A kernel's dynamic shared-memory limit, raised once per device (by any thread; twice does no harm).
 struct SmemLimit {
-    bool done[64] = {};
+    std::atomic<bool> done[64] = {};
     cudaError_t raise(const void *kernel, int bytes)
     {
         int dev = 0;

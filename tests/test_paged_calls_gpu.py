@@ -1,5 +1,7 @@
 """Calls of the paged-cache operators that the documentation allows: no sequences, no tokens, many query heads per KV head, windows
-that never end."""
+that never end, several threads at once."""
+import threading
+
 import pytest
 import torch
 
@@ -59,3 +61,35 @@ def test_windows_and_sinks_up_to_the_largest_number(types, new):
         check_attention(bt, out)
         if window != 1:
             assert torch.equal(out, want)
+
+
+def test_threads_that_call_at_once():
+    """First calls of several variants from several threads, each on a stream of its own."""
+    bts = [Batch(dtype=a, fmt=f, nq=8, nkv=2, d=d, page=page, lens=[200, 30], new=[new, 1], seed=34)
+           for a, f in TYPES for d, page, new in ((128, 16, 1), (64, 24, 40))]
+    ds = [bt.device() for bt in bts]
+    outs, bad = [None] * len(bts), []
+    torch.cuda.synchronize()
+    start = threading.Barrier(len(bts))
+
+    def work(i):
+        try:
+            bt, d = bts[i], ds[i]
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                for _ in range(3):
+                    outs[i] = spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], d["cu"], d["lens"], d["table"], max_new=bt.max_new(),
+                                                  max_context=bt.max_context(), err=d["err"], k_scales=d["k_scales"], v_scales=d["v_scales"])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            bad.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(bts))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad, bad
+    for bt, d, out in zip(bts, ds, outs):
+        assert int(d["err"]) == 0
+        check_attention(bt, out)
