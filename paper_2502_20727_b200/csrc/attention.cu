@@ -670,7 +670,8 @@ __global__ void __launch_bounds__(128) decode_attention_kernel(AttnArgs a)
 // read it.  Every page of the thread block's range is requested as early as the ring allows,
 // independent of the arithmetic, and pages that hold only earlier steps' tokens are requested
 // before the dependency wait (only the page receiving this step's token is written by the
-// preceding kernels of the step, and the step's first one starts after everything before it).  grid (n_q_heads / GT, B, splits); GT query heads share the KV head.
+// preceding kernels of the step, and the step's first one starts after everything before it).
+// grid (n_q_heads / GT, B, splits); GT query heads share the KV head.
 // DENSE: compiled for five resident blocks per SM instead of four (72 registers); each block is a little slower,
 // but a launch of 593-740 blocks (16 sequences x 40 heads, say) is resident at once instead of leaving a short
 // second wave - chosen by the launcher.

@@ -16,7 +16,8 @@ namespace {
 // token r / group, query head r % group, so that a group shares the K/V tiles) and walks tiles of 64 keys, widened to float32
 // in shared memory.  Thread (tx, ty) computes the scores of rows ty RPT .. and keys tx + 16 j, four head dims at a time (eight
 // products per 16-byte shared-memory load), the row maxima and sums over its half warp, and the output columns 4 tx + 64 j.
-// Bound: for chunks the FMA pipes, for few rows (RPT 1) the cache reads, which are cut into key ranges over thread blocks.
+// Bound: for chunks shared-memory loads beside the FMAs and the blocks of the longest sequences, for few rows (RPT 1) the cache
+// reads, which are cut into key ranges over thread blocks.
 // One warp per row, without tiles, took 259 us for 4 ragged chunks of up to 256 tokens where this takes 30 (head_dim 64).
 constexpr int GK = 64, G_THREADS = 256;
 
@@ -284,8 +285,8 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
     if (dtype != 1 || d == 32) {
-        // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64: 64 rows 38.7 us, 32
-        // rows 57); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
+        // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
+        // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);
         p.row_tile = rows <= 32 ? 16 : 64;
         long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);

@@ -5,7 +5,7 @@
 // padding: per 16 cached keys a warp issues head_dim / 8 MMAs for 8 query rows, a small part of an SM's issue slots at the
 // rate HBM delivers the keys.  mma.sync and registers are enough, and the rest serves the loads and, for 8-bit caches, the
 // widening of the codes:
-//   - every warp works on its own 16-key blocks (j, j + 4, ...) with a private ring of tiles, one TMA box each for K and V
+//   - every warp works on its own 16-key blocks (j, j + 4, ..., or j + 8 in the blocks of eight warps) with a private ring of tiles, one TMA box each for K and V
 //     (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled layout): no block-wide barrier between
 //     the first load and the merge;
 //   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 8 ranges
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 pl[n][1] = transpose8x8(left(p[2], p[3]));
             }
         }
-        if (!Q8) {
+        if constexpr (!Q8) {
             if (!all_seen) {
                 // 0 * NaN would reach rows that do not see the key: take non-finite values out here, give them back at the end
 #pragma unroll
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         }
     }
 
-    // the four warps' partial rows, merged through shared memory (the rings are done with)
+    // the warps' partial rows, merged through shared memory (the rings are done with)
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll

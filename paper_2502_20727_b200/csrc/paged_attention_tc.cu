@@ -4,8 +4,9 @@
 // The rows of a (sequence, KV head) are packed: row r = new token r / group, query head r % group of the KV head, so that the
 // query heads of a group share every K/V tile.  A thread block serves one tile of 128 rows, and two blocks share an SM (each 256
 // columns of tensor memory and 110 KB of shared memory): one's products run under the other's softmax, start and end.  One block
-// with two tiles that shared their K/V tiles and took turns was no faster on long contexts (2048 tokens on 14336, 64 heads: 1168
-// us against 1041) and slower on short ones (window of 1024: 181 against 141 us), where it waited for itself at both ends.
+// with two tiles that shared their K/V tiles and took turns waited for itself at both ends of short contexts (window of 1024: 181
+// against 141 us); on long ones the two forms are within what the clock changes (2048 tokens on 14336, 64 heads: 1168 us against 1041
+// when they were compared, and 1090 to 1190 since for the form that was kept).
 // Per tile of 128 keys and 128 rows:
 //   S = Q K^T      tcgen05.mma, Q and K as K-major 128B-swizzled tiles, accumulator in tensor memory
 //   P = softmax    thread = row and half of the keys: maximum (joined with the other half's), then the weights, which go back
@@ -218,7 +219,8 @@ constexpr int load_warps(bool tma, bool q8) { return tma ? 2 : q8 ? 8 : 4; }
 constexpr int SOFT_WARPS = 8, SOFT_THREADS = 32 * SOFT_WARPS;
 constexpr int tc_threads(bool tma, bool q8) { return SOFT_THREADS + 32 * (load_warps(tma, q8) + 1); } // two blocks: 80 registers a thread, 72 or 56
 // 8-bit caches: the load warps' way from one tile to the next is the longest, so there are eight of them, and of the 56 registers a thread
-// that 17 warps leave they give 16 to the softmax warps: 8 x 72 + 8 x 40 + 56 = 17 x 56
+// that 17 warps leave they give 16 to the softmax warps: 8 x 72 + 8 x 40 + 56 = 17 x 56.  (ptxas spills 4 to 72 bytes a thread in all variants
+// of this kernel but one.)
 constexpr int Q8_LAUNCH_REGS = 56, Q8_SOFT_REGS = 72, Q8_LOAD_REGS = 40;
 static_assert(8 * Q8_SOFT_REGS + 8 * Q8_LOAD_REGS + Q8_LAUNCH_REGS <= 17 * Q8_LAUNCH_REGS);
 
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 }
                 named_bar<BAR_LOAD, LT>();
             };
-            if (Q8) {
+            if constexpr (Q8) {
                 constexpr int CPR = D / 16, N = 64 * CPR / LT; // 16-code chunks per row; per thread and half a tile (64 keys)
                 const uint32_t c128 = widen_const();
                 const int c = tid % CPR;
@@ -637,7 +639,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
-                    // every fourth pair on the FMA pipes, which the exponentials otherwise leave idle
+                    // every second pair (bf16 pages by TMA) or every fourth on the FMA pipes, which the exponentials otherwise leave idle
                     float2 p = (TMA ? k % 2 == 1 : k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
                     ls = add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
