@@ -26,7 +26,7 @@
 //   - weights are rounded to bf16.  With int8 scales, which are not powers of two, even a row's only weight is off, and the errors
 //     came to 1.5 times that of the output's own rounding: there the rest of each weight is a second bf16 with products of its own
 //     (32 sequences of 9 to 16 thousand tokens: 192 us, 182 without; the same for the other formats cost 2 to 8 % and
-//     would take errors of 1.05 to 1.2 times, at most 1.45, to 1).
+//     would take errors of 1.05 to 1.3 times to 1).
 // Softmax: base 2, fp32, per warp; the accumulators follow the running maximum lazily (they are rescaled when it has grown by
 // more than 2^8: weights stay below 2^8, where bf16 rounds as finely as at 1).
 #include "gemm_tc.cuh"
