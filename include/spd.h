@@ -319,6 +319,8 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  * whose visible scores are all -inf, has no softmax: its whole output row is NaN.  Scores, sums and the output are held in
  * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product (two bfloat16s, 16 bits,
  * with an int8 cache).
+ * The sum over the keys is divided by the sum of the weights at the end, and weights may reach 2^8 before that: values of V
+ * beyond 2^100 or so can overflow on the way.
  * A page id outside [0, n_pages) sets error bit 1; the output rows that needed it are undefined.
  * Errors: SPD_ENULL, SPD_EINVAL, SPD_ECAPACITY (max_context beyond the block table), SPD_EWORKSPACE, SPD_ECUDA. */
 int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *batch, const void *q, int64_t q_stride, void *out,

@@ -5,9 +5,9 @@
 // padding: per 16 cached keys a warp issues head_dim / 8 MMAs for 8 query rows, a small part of an SM's issue slots at the
 // rate HBM delivers the keys.  mma.sync and registers are enough, and the rest serves the loads and, for 8-bit caches, the
 // widening of the codes:
-//   - every warp works on its own 16-key blocks (j, j + 4, ..., or j + 8 in the blocks of eight warps) with a private ring of tiles, one TMA box each for K and V
-//     (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled layout): no block-wide barrier between
-//     the first load and the merge;
+//   - every warp works on its own 16-key blocks (j, j + 4, ..., or j + 8 in thread blocks of eight warps) with a private ring of
+//     tiles, one TMA box each for K and V (page sizes that are multiples of 16; cp.async otherwise, into the same swizzled
+//     layout): no block-wide barrier between the first load and the merge;
 //   - the keys of a (sequence, KV head) are cut into ranges over thread blocks where there are few of them.  Up to 8 ranges
 //     are one thread-block cluster that adds up its partial rows through shared memory; more go through the workspace and
 //     paged_merge_kernel;
