@@ -251,7 +251,7 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
 /* ---- Paged-cache operators on their own ------------------------------------------------------------
  *
  * What a serving program needs next to the stack calls: appending rows to a cache of pages, plain or quantised to 8
- * bits, reading cached rows back, and the attention of a chunk of new tokens per sequence over such a cache (Sec. 3:
+ * or 4 bits, reading cached rows back, and the attention of a chunk of new tokens per sequence over such a cache (Sec. 3:
  * every shard attends over its own heads; a shard's call passes the shard's heads).
  *
  * Formats.  A cached row is the head_dim values of one token of one KV head.
@@ -262,15 +262,26 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  *                 the codes 0x7f and 0xff (NaN) are never written and must not be in a row that is read
  *   SPD_KV_INT8 : 8-bit integers and one float32 scale s = max|x| / 127 per row; code = x * (127 * (1 / max|x|)), the
  *                 reciprocal and both products rounded to float32, rounded to nearest (half to even) in -127 .. 127
- * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0. */
+ * A row of zeros has scale 1; a scale is at least 2^-126; a row with a NaN or an infinity gets scale NaN and codes 0.
+ *   SPD_KV_INT4 : 4-bit integers.  The first and the second half of the head dims have a bfloat16 scale s and a bfloat16
+ *                 smallest value m each: m = min x rounded down, s = (max x - m) / 15 rounded to nearest and at least
+ *                 2^-60, code = (x - m) / s rounded to nearest (half to even) in 0 .. 15; value = code * s + m in float32.
+ *                 A page row is head_dim / 2 bytes: byte i has the code of dim i in bits 0-3, of dim i + head_dim / 2 in bits
+ *                 4-7.  k_scales / v_scales point to [n_pages, n_kv_heads, kv_block_size, 2 halves, 2 (s, m)] bfloat16,
+ *                 8-byte aligned.  A row with a NaN or an infinity (or a half whose max - m is no float) gets four NaNs and
+ *                 codes 0; a row one of whose four parameters is not finite stands for NaNs.  Scales of V rows that queries
+ *                 see together should lie within 2^60 of one another, and values of V below 2^30 in magnitude: beyond, sums
+ *                 may lose the smaller ones or overflow. */
 #define SPD_KV_F32 0
 #define SPD_KV_BF16 1
 #define SPD_KV_E4M3 2
 #define SPD_KV_INT8 3
+#define SPD_KV_INT4 5 /* 4 is no format */
 
 typedef struct {
     void *k_pages, *v_pages;    /* [n_pages, n_kv_heads, kv_block_size, head_dim], 16-byte aligned           */
-    float *k_scales, *v_scales; /* [n_pages, n_kv_heads, kv_block_size]; 8-bit formats only, else may be null */
+    float *k_scales, *v_scales; /* [n_pages, n_kv_heads, kv_block_size]; 8-bit and 4-bit formats only (4 bits:
+                                 * see SPD_KV_INT4), else may be null                                       */
     int32_t n_pages, n_kv_heads, kv_block_size, head_dim; /* head_dim 32, 64 or 128; any block size          */
     int32_t format;
 } spd_kv_cache;
@@ -295,8 +306,14 @@ typedef struct {
 int spd_kv_write(const spd_kv_cache *cache, const spd_ragged *batch, const void *k, const void *v, int64_t k_stride,
                  int64_t v_stride, int32_t dtype, int32_t *err_flag, void *stream);
 
+/* The same for rows whose places the caller knows, e.g. from spd_plan_batch: row t becomes the cached row at slot
+ * slots[t] = page id * kv_block_size + row of the page.  A negative slot belongs to nobody and its row is skipped; a slot whose
+ * page id is outside [0, n_pages) sets error bit 1 and is skipped.  One plan serves the appends of all layers. */
+int spd_kv_write_slots(const spd_kv_cache *cache, const int32_t *slots, int32_t n_tokens, const void *k, const void *v,
+                       int64_t k_stride, int64_t v_stride, int32_t dtype, int32_t *err_flag, void *stream);
+
 /* Read rows back: row i of sequence b of k and v = the cached row at position seq_lens[b] + i, as the values the codes
- * stand for (code * scale), rounded once to dtype.  seq_lens is the first position to read.  Same layout rules and error
+ * stand for (code * scale; 4 bits: code * s + m), rounded once to dtype.  seq_lens is the first position to read.  Same layout rules and error
  * bits as spd_kv_write; rows that cannot be read are left as they are. */
 int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, void *v, int64_t k_stride, int64_t v_stride,
                 int32_t dtype, int32_t *err_flag, void *stream);
@@ -308,7 +325,8 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  * step, all of a prompt with seq_lens 0 a prefill, anything between a chunk, a continued conversation or a check of
  * drafted tokens.
  *   q, out : [n_tokens, n_q_heads, head_dim] of dtype (0 float32, 1 bfloat16), strided as in spd_kv_write; must not
- *            overlap.  A float32 q needs an SPD_KV_F32 or 8-bit cache, a bfloat16 q an SPD_KV_BF16 or 8-bit cache.
+ *            overlap.  A float32 q needs an SPD_KV_F32, 8-bit or 4-bit cache, a bfloat16 q any but
+ *            SPD_KV_F32.
  *   max_new, max_context : host bounds of a sequence's new tokens and of seq_lens[b] + new tokens (at most 2^30).  A sequence beyond
  *            them, or with rows outside the tensor, is skipped with error bit 2.
  *   window : only pages that hold a visible key are looked up, so that block-table entries of pages that lie wholly
@@ -328,6 +346,36 @@ int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *batch, cons
                         int32_t window, int32_t sinks, void *workspace, size_t workspace_bytes, int32_t *err_flag, void *stream);
 int spd_paged_attention_workspace_bytes(const spd_kv_cache *cache, int32_t B, int32_t n_tokens, int32_t dtype, int32_t n_q_heads,
                                         int32_t max_new, int32_t max_context, int32_t window, int32_t sinks, size_t *out_bytes);
+
+/* The plan of a serving step: where the rows of every request go, from the requests' lengths and a pool of free pages, in one launch
+ * and without the host (graph capture included).  Request b has seq_lens[b] cached tokens, whose pages are the first
+ * ceil(seq_lens[b] / kv_block_size) entries of its block-table row, and new_lens[b] new ones, or SPD_RELEASE (any negative
+ * number) if it is finished.
+ *   1. Pages of finished requests join the pool behind its first n_free[0] entries, in the order of the requests and of their
+ *      tables.  Their table entries stay as they are; the row may be used for another request from the next call on.
+ *   2. Every other request wants the pages that its new tokens reach.  It is served if the pages wanted up to and with it are no
+ *      more than the pool has (or it wants none) and the new tokens up to and with it are no more than n_tokens.  Otherwise
+ *      it gets no page and no row (error bit 2): it can be tried again, after others have finished or been set aside.
+ *   3. Pages are taken from the end of the pool, in the order of the requests, and written to the table.
+ *   seq_lens, new_lens : [B] device, B at most 16384
+ *   block_table : [B, max_pages] device, read and written; max_pages * kv_block_size and n_pages * kv_block_size below 2^31
+ *   cu_new      : [B + 1] device, out: row offsets of the served new tokens (spd_ragged.cu_new)
+ *   positions   : [n_tokens] device, out: position of every row in its sequence, -1 behind the last row
+ *   slots       : [n_tokens] device, out: page id * kv_block_size + row of the page (spd_kv_write_slots), -1 behind the last row
+ *   next_lens   : [B] device, out: lengths after the step, 0 for finished requests; not the same array as seq_lens or new_lens
+ *   err_flag    : device int32; bit 1 a page id outside [0, n_pages) in a table or the pool (skipped when given back, slot -1 when
+ *                 needed), bit 2 a request that is not served, or whose length is negative or beyond its table, or a pool that
+ *                 would hold more than n_pages pages (the surplus is dropped) */
+#define SPD_RELEASE (-1)
+typedef struct {
+    int32_t *free_pages;    /* [n_pages] device: ids of the free pages, in its first n_free[0] entries       */
+    const int32_t *n_free;  /* [1] device                                                                    */
+    int32_t *n_free_next;   /* [1] device, out: the pool's size after the step; may be n_free itself         */
+    int32_t n_pages, kv_block_size;
+} spd_page_pool;
+int spd_plan_batch(const spd_page_pool *pool, const int32_t *seq_lens, const int32_t *new_lens, int32_t B, int32_t *block_table,
+                   int32_t max_pages, int32_t n_tokens, int32_t *cu_new, int32_t *positions, int32_t *slots, int32_t *next_lens,
+                   int32_t *err_flag, void *stream);
 
 /* Replace the per-block mask of a context (same meaning as in spd_create).  A mask with an SPD
  * block needs the larger workspace of such a stack: SPD_EWORKSPACE if the context was created

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -34,7 +34,8 @@ EXPORTS = ("spd_workspace_bytes", "spd_create", "spd_prefill", "spd_decode_step"
            "spd_head_grouping_stats", "spd_head_scatter", "spd_mlp_match", "spd_timeline_begin", "spd_timeline_read",
            "spd_timeline_end", "spd_tp_region_bytes", "spd_tp_attach", "spd_tp_detach", "spd_tp_decode_step",
            "spd_tp_prefill", "spd_tp_baseline_decode_step", "spd_tp_baseline_prefill",
-           "spd_extend", "spd_set_window", "spd_kv_write", "spd_kv_read", "spd_paged_attention", "spd_paged_attention_workspace_bytes")
+           "spd_extend", "spd_set_window", "spd_kv_write", "spd_kv_read", "spd_paged_attention", "spd_paged_attention_workspace_bytes",
+           "spd_kv_write_slots", "spd_plan_batch")
 
 
 class SpdError(RuntimeError):
@@ -65,6 +66,11 @@ class spd_kv_cache(ctypes.Structure):
 class spd_ragged(ctypes.Structure):
     _fields_ = [("cu_new", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("B", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
+
+
+class spd_page_pool(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("n_free_next", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("kv_block_size", ctypes.c_int32)]
 
 
 _lib = None
@@ -117,7 +123,9 @@ def load_library() -> ctypes.CDLL:
     i64, f32 = ctypes.c_int64, ctypes.c_float
     cache, ragged = ctypes.POINTER(spd_kv_cache), ctypes.POINTER(spd_ragged)
     lib.spd_kv_write.argtypes = [cache, ragged, vp, vp, i64, i64, i32, vp, vp]
+    lib.spd_kv_write_slots.argtypes = [cache, vp, i32, vp, vp, i64, i64, i32, vp, vp]
     lib.spd_kv_read.argtypes = [cache, ragged, vp, vp, i64, i64, i32, vp, vp]
+    lib.spd_plan_batch.argtypes = [ctypes.POINTER(spd_page_pool), vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.spd_paged_attention.argtypes = [cache, ragged, vp, i64, vp, i64, i32, i32, i32, i32, f32, i32, i32, vp, sz, vp, vp]
     lib.spd_paged_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     lib.spd_profile_begin.argtypes = [vp]
@@ -205,8 +213,10 @@ def gemm_bf16_sum_static(a: torch.Tensor, w: torch.Tensor, out: torch.Tensor, er
     return out
 
 
-# Storage formats of a paged cache by the pages' dtype (SPD_KV_*); the 8-bit ones have one scale per cached row.
-KV_FORMATS = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3}
+# Storage formats of a paged cache by the pages' dtype (SPD_KV_*); the 8-bit ones have one scale per cached row, uint8 pages hold two
+# 4-bit codes per byte and have a (scale, smallest value) pair per half of a cached row.
+KV_FORMATS = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3, torch.uint8: 5}
+KV_INT4 = 5
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -216,16 +226,22 @@ def _kv_cache(k_pages, v_pages, k_scales, v_scales) -> spd_kv_cache:
     dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
     fmt = KV_FORMATS.get(dtype)
     if fmt is None or len(shape) != 4 or dev < 0 or not k_pages.is_contiguous():
-        raise ValueError("k_pages: contiguous CUDA tensor [n_pages, n_kv_heads, page, head_dim] of float32, bfloat16, float8_e4m3fn or int8")
+        raise ValueError("k_pages: contiguous CUDA tensor [n_pages, n_kv_heads, page, head_dim] of float32, bfloat16, float8_e4m3fn or int8, "
+                         "or uint8 with head_dim / 2 bytes per row (4 bits)")
     if v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev or not v_pages.is_contiguous():
         raise ValueError("v_pages: like k_pages")
+    if fmt == KV_INT4:
+        for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if s is None or s.get_device() != dev or s.dtype is not torch.bfloat16 or s.shape != shape[:3] + (2, 2) or not s.is_contiguous():
+                raise ValueError(f"{name}: contiguous bfloat16 [n_pages, n_kv_heads, page, 2, 2] on the pages' device (4-bit caches)")
+        return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *shape[:3], 2 * shape[3], fmt)
     if fmt >= 2:
         for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
             if s is None or s.get_device() != dev or s.dtype is not torch.float32 or s.shape != shape[:3] or not s.is_contiguous():
                 raise ValueError(f"{name}: contiguous float32 [n_pages, n_kv_heads, page] on the pages' device (8-bit caches)")
         return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *shape, fmt)
     if k_scales is not None or v_scales is not None:
-        raise ValueError("k_scales / v_scales: for 8-bit caches only")
+        raise ValueError("k_scales / v_scales: for 8-bit and 4-bit caches only")
     return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, *shape, fmt)
 
 
@@ -276,7 +292,8 @@ def _call_on(dev: int, fn, *args) -> int:
 def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
              block_table: torch.Tensor, *, err: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
              v_scales: Optional[torch.Tensor] = None) -> None:
-    """Append rows to a paged cache, quantised to 8 bits where the pages are float8_e4m3fn or int8; see spd_kv_write.
+    """Append rows to a paged cache, quantised to 8 bits where the pages are float8_e4m3fn or int8 and to 4 bits where they are uint8; see
+    spd_kv_write and, for the layout of 4-bit pages and their scales, SPD_KV_INT4.
 
     k, v: [n_tokens, n_kv_heads, head_dim]; rows cu_new[b] .. cu_new[b+1]-1 are sequence b's, at positions seq_lens[b] on.
     err: int32 tensor that collects error bits (1 page id out of range, 2 position outside the block table); it is not read
@@ -291,6 +308,23 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     rc = _call_on(dev, lib.spd_kv_write, c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, dev))
     if rc:
         _check("spd_kv_write", rc)
+
+
+def kv_write_slots(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor, *, err: torch.Tensor,
+                   k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None) -> None:
+    """kv_write for rows whose places are known: row t goes to slot slots[t] = page id * page size + row of the page (negative: nowhere),
+    e.g. of a BatchPlan; see spd_kv_write_slots."""
+    lib = load_library()
+    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
+    dev = k_pages.get_device()
+    if k.dtype is not v.dtype or k.shape != v.shape:
+        raise ValueError("k and v: same dtype and shape")
+    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
+    n = k.shape[0]
+    rc = _call_on(dev, lib.spd_kv_write_slots, c, _int32("slots", slots, dev, (n,)), n, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype],
+                  _flag(err, dev))
+    if rc:
+        _check("spd_kv_write_slots", rc)
 
 
 def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *,
@@ -360,6 +394,46 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
         rc = _call_on(dev, lib.spd_paged_attention, *args, workspace.data_ptr(), need.value, flag)
     if rc:
         _check("spd_paged_attention", rc)
+    return out
+
+
+RELEASE = -1  # new_lens entry of a request that is finished
+
+
+class BatchPlan(NamedTuple):
+    """A step's plan (all int32): row offsets [B + 1], positions and slots of the rows [n_tokens] (-1 behind the last one), the
+    requests' lengths after the step [B], the pool's size after it [1]."""
+    cu_new: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    next_lens: torch.Tensor
+    n_free: torch.Tensor
+
+
+def plan_batch(seq_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, *,
+               page: int, n_pages: int, n_tokens: int, err: torch.Tensor, out: Optional[BatchPlan] = None) -> BatchPlan:
+    """Row offsets, positions, slots and pages of a serving step from the requests' lengths; see spd_plan_batch.
+
+    Request b has seq_lens[b] cached tokens and new_lens[b] new ones (RELEASE: it is finished, its pages go back to the pool).
+    block_table [B, max_pages] gets the ids of new pages, which are taken from free_pages[:n_free]; n_tokens: room for rows.  The
+    plan's cu_new, with seq_lens and block_table, is what kv_write and paged_attention take; its slots are what kv_write_slots takes.
+    out: tensors to fill instead of new ones; its n_free may be the argument.  All tensors are contiguous int32."""
+    lib = load_library()
+    dev = block_table.get_device()
+    if block_table.dim() != 2 or dev < 0:
+        raise ValueError("block_table: CUDA tensor [B, max_pages]")
+    B, width = block_table.shape
+    if out is None:
+        buf = block_table.new_empty(2 * B + 2 + 2 * n_tokens, dtype=torch.int32)
+        out = BatchPlan(*buf.split((B + 1, n_tokens, n_tokens, B, 1)))
+    pool = spd_page_pool(_int32("free_pages", free_pages, dev, (n_pages,)), _int32("n_free", n_free, dev, (1,)),
+                         _int32("out.n_free", out.n_free, dev, (1,)), n_pages, page)
+    rc = _call_on(dev, lib.spd_plan_batch, pool, _int32("seq_lens", seq_lens, dev, (B,)), _int32("new_lens", new_lens, dev, (B,)), B,
+                  _int32("block_table", block_table, dev, (B, width)), width, n_tokens, _int32("out.cu_new", out.cu_new, dev, (B + 1,)),
+                  _int32("out.positions", out.positions, dev, (n_tokens,)), _int32("out.slots", out.slots, dev, (n_tokens,)),
+                  _int32("out.next_lens", out.next_lens, dev, (B,)), _flag(err, dev))
+    if rc:
+        _check("spd_plan_batch", rc)
     return out
 
 
@@ -561,6 +635,12 @@ class SpdStack:
     def set_window(self, window: int, sinks: int = 0):
         """Attend to the last `window` tokens and the first `sinks` ones from now on (0: to all); see spd_set_window."""
         _check("spd_set_window", self.lib.spd_set_window(self._ctx, int(window), int(sinks)))
+
+    def plan_batch(self, seq_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, *,
+                   n_tokens: int, err: torch.Tensor, out: Optional[BatchPlan] = None) -> BatchPlan:
+        """The step's plan over this stack's pages, e.g. the block tables for extend and decode_step; see plan_batch."""
+        return plan_batch(seq_lens, new_lens, block_table, free_pages, n_free, page=self.dims.kv_block_size, n_pages=self.n_pages, n_tokens=n_tokens,
+                          err=err, out=out)
 
     def read_cache(self, layer: int, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *, n_tokens: int, err: torch.Tensor):
         """Cached K and V rows of one layer, e.g. to keep a prefix or to move a sequence; see kv_read."""

@@ -8,6 +8,10 @@
 //          products are rounded to float32, which moves values within 2^-22 of a border between two codes at most.
 // A row of zeros has s = 1; s is at least 2^-126; a row that holds a NaN or an infinity gets s = NaN and codes 0, so that
 // reading it gives NaN everywhere and nothing else is touched.
+//   int4 : two halves of the head dims, each with its smallest value m rounded down to bf16 and a scale s = (max - m) / 15 rounded to
+//          bf16, at least 2^-60; code = (x - m) / s rounded to the nearest integer, half to even.  The quotients are the correctly
+//          rounded ones (from the rounded reciprocal with one residual correction, Markstein 1990), so that ties, which are common among
+//          bf16 values, fall as they do in exact arithmetic.  m <= x, and s is off by 2^-9 at most, so codes end at 15 by themselves.
 //
 // Bound: memory.  A thread block serves a few consecutive tokens and 16 cached rows (K and V of eight heads) of each; one warp
 // finds the tokens' sequences and pages for all of them, then every lane moves eight elements of UNITS rows with all loads in
@@ -26,9 +30,17 @@ constexpr int KV_THREADS = 256, ROWS = 16; // rows of a token a block serves
 
 // Where the block's tokens t0 .. t0 + TT - 1 are cached: the row of (page, head 0, slot), or -1 where a token is nobody's or does
 // not fit (error bit).  Warp 0; lane k < TT takes token k.  Sequence of token t: the last b with cu[b] <= t.
-template <int TT> __device__ __forceinline__ void locate_tokens(const PagedKv &kv, const RaggedBatch &rb, int t0, long (&base)[TT], int *err)
+template <int TT> __device__ __forceinline__ void locate_tokens(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, int t0, long (&base)[TT], int *err)
 {
     const int lane = threadIdx.x & 31;
+    if (slots) { // the caller knows: one load in place of the search and the table
+        if (lane >= TT) return;
+        const int slot = t0 + lane < rb.n_tokens ? slots[t0 + lane] : -1;
+        const int page = slot < 0 ? 0 : slot / kv.page;
+        if (slot >= 0 && page >= kv.n_pages) atomicOr(err, ERR_PAGE_RANGE);
+        base[lane] = slot >= 0 && page < kv.n_pages ? (long)page * kv.nkv * kv.page + (slot - page * kv.page) : -1;
+        return;
+    }
     int before[TT];
 #pragma unroll
     for (int k = 0; k < TT; ++k) before[k] = 0;
@@ -76,6 +88,14 @@ template <> __device__ __forceinline__ void store8<bf16>(bf16 *p, const float (&
         w[i] = *(const uint32_t *)&h;
     }
     *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T> __device__ __forceinline__ void store4(T *p, float a, float b, float c, float d);
+template <> __device__ __forceinline__ void store4<float>(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
+template <> __device__ __forceinline__ void store4<bf16>(bf16 *p, float a, float b, float c, float d)
+{
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(a, b), hi = __floats2bfloat162_rn(c, d);
+    *(uint2 *)p = make_uint2(*(const uint32_t *)&lo, *(const uint32_t *)&hi);
 }
 
 __device__ __forceinline__ uint32_t e4m3_x4(float a, float b, float c, float d)
@@ -136,6 +156,45 @@ __device__ __forceinline__ uint32_t top_of(const Raw8<float> &r)
     return max(max(a, b), max(c, d));
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) // NaN if either is
+{
+    float d;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+// smallest and largest of eight elements, NaN if one is
+__device__ __forceinline__ float2 range_of(const Raw8<bf16> &r)
+{
+    const uint4 u = r.u;
+    const auto h = [](uint32_t w) { return *(const __nv_bfloat162 *)&w; };
+    const __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(h(u.x), h(u.y)), __hmin2_nan(h(u.z), h(u.w)));
+    const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(h(u.x), h(u.y)), __hmax2_nan(h(u.z), h(u.w)));
+    return make_float2(min_nan(__low2float(lo), __high2float(lo)), max_nan(__low2float(hi), __high2float(hi)));
+}
+__device__ __forceinline__ float2 range_of(const Raw8<float> &r)
+{
+    const float4 a = r.a, b = r.b;
+    return make_float2(min_nan(min_nan(min_nan(a.x, a.y), min_nan(a.z, a.w)), min_nan(min_nan(b.x, b.y), min_nan(b.z, b.w))),
+                       max_nan(max_nan(max_nan(a.x, a.y), max_nan(a.z, a.w)), max_nan(max_nan(b.x, b.y), max_nan(b.z, b.w))));
+}
+// Four 4-bit codes, one per byte, of x >= m: (x - m) / s by its correctly rounded quotient, the integer as in int8_x4
+__device__ __forceinline__ uint32_t int4_x4(const float *x, float m, float s, float inv)
+{
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float d = __fsub_rn(x[i], m), q = __fmul_rn(d, inv);
+        b[i] = __float_as_uint(__fadd_rn(fmaf(fmaf(-q, s, d), inv, q), 12582912.f));
+    }
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+}
+
 // Rows a lane has in flight, tokens of a block.  FEW: few rows in all, which then spread over more blocks.
 template <typename T, int D, bool FEW> struct KvShape {
     static constexpr int LPR = D / 8, PER_PASS = KV_THREADS / LPR; // lanes per row, rows per pass of the block
@@ -143,7 +202,7 @@ template <typename T, int D, bool FEW> struct KvShape {
 };
 
 template <typename T, int FMT, int D, bool FEW>
-__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, RaggedBatch rb, const T *k, const T *v, long k_stride, long v_stride, int *err)
+__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, RaggedBatch rb, const int32_t *slots, const T *k, const T *v, long k_stride, long v_stride, int *err)
 {
     using S = KvShape<T, D, FEW>;
     constexpr int LPR = S::LPR, TT = S::TT, UNITS = S::UNITS;
@@ -160,7 +219,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, Ragged
         if (t < rb.n_tokens && (r >> 1) < kv.nkv)
             raw[i] = *(const Raw8<T> *)((r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)(r >> 1) * D + li * 8);
     }
-    if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, t0, base, err);
+    if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, slots, t0, base, err);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
@@ -171,6 +230,33 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, Ragged
         get(raw[i], x);
         if constexpr (FMT == KV_F32 || FMT == KV_BF16) {
             if (ok) store8<E>((E *)(r & 1 ? kv.v : kv.k) + row * D + li * 8, x);
+            continue;
+        }
+        if constexpr (FMT == KV_INT4) {
+            // lanes li and li ^ LPR / 2 hold the same bytes' low and high codes
+            constexpr int HALF = LPR / 2;
+            const bool high = li >= HALF;
+            float2 range = range_of(raw[i]);
+#pragma unroll
+            for (int o = HALF / 2; o > 0; o >>= 1) {
+                range.x = min_nan(range.x, __shfl_xor_sync(0xffffffffu, range.x, o));
+                range.y = max_nan(range.y, __shfl_xor_sync(0xffffffffu, range.y, o));
+            }
+            // down to bf16: towards zero, or away from it where negative
+            const uint32_t bits = __float_as_uint(range.x), mb = (range.x < 0.f ? bits + 0xffffu : bits) & 0xffff0000u;
+            const float m = __uint_as_float(mb), spread = __fsub_rn(range.y, m);
+            const float s = fmaxf(__bfloat162float(__float2bfloat16_rn(__fdiv_rn(spread, 15.f))), 0x1p-60f), inv = __frcp_rn(s);
+            const bool bad = !(spread < INFINITY); // a NaN or an infinity in the half, or a spread that is no float
+            uint32_t own = int4_x4(x, m, s, inv), other = int4_x4(x + 4, m, s, inv);
+            // this lane keeps the first four dims (low half) or the last four (high half); bit 7 of the others' codes: `bad`
+            if (high) { const uint32_t t = own; own = other; other = t; }
+            other = __shfl_xor_sync(0xffffffffu, bad ? 0x80u : other, HALF);
+            const bool row_bad = bad || (other & 0x80u);
+            if (!ok) continue;
+            *(uint32_t *)((uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + (li & (HALF - 1)) * 8 + high * 4) =
+                row_bad ? 0u : high ? other | (own << 4) : own | (other << 4);
+            if ((li & (HALF - 1)) == 0)
+                ((uint32_t *)(r & 1 ? kv.vs : kv.ks))[2 * row + high] = row_bad ? 0x7fc07fc0u : (__float_as_uint(s) >> 16) | mb;
             continue;
         }
         // largest magnitude of the row; a NaN wins (comparisons on the bit patterns of |x|)
@@ -215,8 +301,37 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedB
     pdl_launch_dependents();
     pdl_wait();
     const int t0 = blockIdx.x * TT, r0 = blockIdx.y * ROWS, li = threadIdx.x % LPR, g = threadIdx.x / LPR;
-    if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, t0, base, err);
+    if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, nullptr, t0, base, err);
     __syncthreads();
+    if constexpr (FMT == KV_INT4) { // a lane: four bytes of a row, hence four dims of either half
+        uint32_t codes[UNITS];
+        uint2 par[UNITS];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int id = i * S::PER_PASS + g, r = r0 + id % ROWS, h = r >> 1;
+            const long where = base[id / ROWS], row = where + (long)h * kv.page;
+            codes[i] = 0;
+            par[i] = make_uint2(0, 0);
+            if (where >= 0 && h < kv.nkv) {
+                codes[i] = *(const uint32_t *)((const uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + li * 4);
+                par[i] = kv4_params(r & 1 ? kv.vs : kv.ks, row);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int id = i * S::PER_PASS + g, t = t0 + id / ROWS, r = r0 + id % ROWS, h = r >> 1;
+            if (base[id / ROWS] < 0 || h >= kv.nkv) continue;
+            T *dst = (r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)h * D + li * 4;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t p = half ? par[i].y : par[i].x, c = codes[i] >> (4 * half);
+                const float s = kv4_scale(p), m = kv4_min(p);
+                store4<T>(dst + half * (D / 2), fmaf((float)(c & 15), s, m), fmaf((float)(c >> 8 & 15), s, m), fmaf((float)(c >> 16 & 15), s, m),
+                          fmaf((float)(c >> 24 & 15), s, m));
+            }
+        }
+        return;
+    }
     Raw8<E> raw[UNITS];
     float s[UNITS];
 #pragma unroll
@@ -245,7 +360,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedB
 }
 
 template <bool WRITE, typename T, int FMT, int D>
-cudaError_t launch(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
+cudaError_t launch(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
 {
     typedef typename std::conditional<WRITE, T, typename KvElem<FMT>::type>::type In;
     auto grid = [&](int tt) { return dim3((unsigned)((rb.n_tokens + tt - 1) / tt), (unsigned)((2 * kv.nkv + ROWS - 1) / ROWS)); };
@@ -253,47 +368,48 @@ cudaError_t launch(const PagedKv &kv, const RaggedBatch &rb, const void *k, cons
     const dim3 full = grid(KvShape<In, D, false>::TT);
     if ((long)full.x * full.y < sm_count()) {
         const dim3 few = grid(KvShape<In, D, true>::TT);
-        if (WRITE) return launch_kernel(kv_write_kernel<T, FMT, D, true>, few, dim3(KV_THREADS), 0, st, 0, kv, rb, (const T *)k, (const T *)v, ks, vs, err);
+        if (WRITE) return launch_kernel(kv_write_kernel<T, FMT, D, true>, few, dim3(KV_THREADS), 0, st, 0, kv, rb, slots, (const T *)k, (const T *)v, ks, vs, err);
         return launch_kernel(kv_read_kernel<T, FMT, D, true>, few, dim3(KV_THREADS), 0, st, 0, kv, rb, (T *)k, (T *)v, ks, vs, err);
     }
-    if (WRITE) return launch_kernel(kv_write_kernel<T, FMT, D, false>, full, dim3(KV_THREADS), 0, st, 0, kv, rb, (const T *)k, (const T *)v, ks, vs, err);
+    if (WRITE) return launch_kernel(kv_write_kernel<T, FMT, D, false>, full, dim3(KV_THREADS), 0, st, 0, kv, rb, slots, (const T *)k, (const T *)v, ks, vs, err);
     return launch_kernel(kv_read_kernel<T, FMT, D, false>, full, dim3(KV_THREADS), 0, st, 0, kv, rb, (T *)k, (T *)v, ks, vs, err);
 }
 
 template <bool WRITE, typename T, int FMT>
-cudaError_t by_dim(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
+cudaError_t by_dim(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
 {
     switch (kv.d) {
-    case 32: return launch<WRITE, T, FMT, 32>(kv, rb, k, v, ks, vs, err, st);
-    case 64: return launch<WRITE, T, FMT, 64>(kv, rb, k, v, ks, vs, err, st);
-    case 128: return launch<WRITE, T, FMT, 128>(kv, rb, k, v, ks, vs, err, st);
+    case 32: return launch<WRITE, T, FMT, 32>(kv, rb, slots, k, v, ks, vs, err, st);
+    case 64: return launch<WRITE, T, FMT, 64>(kv, rb, slots, k, v, ks, vs, err, st);
+    case 128: return launch<WRITE, T, FMT, 128>(kv, rb, slots, k, v, ks, vs, err, st);
     default: return cudaErrorInvalidValue;
     }
 }
 
 template <bool WRITE, typename T>
-cudaError_t by_format(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
+cudaError_t by_format(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, const void *k, const void *v, long ks, long vs, int *err, cudaStream_t st)
 {
     switch (kv.fmt) {
-    case KV_F32: return by_dim<WRITE, T, KV_F32>(kv, rb, k, v, ks, vs, err, st);
-    case KV_BF16: return by_dim<WRITE, T, KV_BF16>(kv, rb, k, v, ks, vs, err, st);
-    case KV_E4M3: return by_dim<WRITE, T, KV_E4M3>(kv, rb, k, v, ks, vs, err, st);
-    case KV_INT8: return by_dim<WRITE, T, KV_INT8>(kv, rb, k, v, ks, vs, err, st);
+    case KV_F32: return by_dim<WRITE, T, KV_F32>(kv, rb, slots, k, v, ks, vs, err, st);
+    case KV_BF16: return by_dim<WRITE, T, KV_BF16>(kv, rb, slots, k, v, ks, vs, err, st);
+    case KV_E4M3: return by_dim<WRITE, T, KV_E4M3>(kv, rb, slots, k, v, ks, vs, err, st);
+    case KV_INT8: return by_dim<WRITE, T, KV_INT8>(kv, rb, slots, k, v, ks, vs, err, st);
+    case KV_INT4: return by_dim<WRITE, T, KV_INT4>(kv, rb, slots, k, v, ks, vs, err, st);
     default: return cudaErrorInvalidValue;
     }
 }
 
 } // namespace
 
-cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long ks, long vs, int in_bf16, int *err,
-                            cudaStream_t st)
+cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, const void *k, const void *v, long ks, long vs, int in_bf16,
+                            int *err, cudaStream_t st)
 {
-    return in_bf16 ? by_format<true, bf16>(kv, rb, k, v, ks, vs, err, st) : by_format<true, float>(kv, rb, k, v, ks, vs, err, st);
+    return in_bf16 ? by_format<true, bf16>(kv, rb, slots, k, v, ks, vs, err, st) : by_format<true, float>(kv, rb, slots, k, v, ks, vs, err, st);
 }
 cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, void *v, long ks, long vs, int out_bf16, int *err,
                            cudaStream_t st)
 {
-    return out_bf16 ? by_format<false, bf16>(kv, rb, k, v, ks, vs, err, st) : by_format<false, float>(kv, rb, k, v, ks, vs, err, st);
+    return out_bf16 ? by_format<false, bf16>(kv, rb, nullptr, k, v, ks, vs, err, st) : by_format<false, float>(kv, rb, nullptr, k, v, ks, vs, err, st);
 }
 
 } // namespace spd
@@ -308,17 +424,20 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 namespace spd {
 
+bool known_format(int f) { return (f >= SPD_KV_F32 && f <= SPD_KV_INT8) || f == SPD_KV_INT4; }
+
 // Checks shared by the cache operators; fills the internal descriptions.
 int check_cache(const spd_kv_cache *c, const spd_ragged *r, PagedKv *kv, RaggedBatch *rb)
 {
     if (!c || !r) return SPD_ENULL;
-    if (c->format < SPD_KV_F32 || c->format > SPD_KV_INT8) return SPD_EINVAL;
+    if (!known_format(c->format)) return SPD_EINVAL;
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return SPD_EINVAL;
     if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->kv_block_size < 1) return SPD_EINVAL;
     if (r->B < 0 || r->n_tokens < 0 || r->max_pages < 1) return SPD_EINVAL;
     if (!c->k_pages || !c->v_pages || (c->format >= SPD_KV_E4M3 && (!c->k_scales || !c->v_scales))) return SPD_ENULL;
     if (r->B && (!r->cu_new || !r->seq_lens || !r->block_table)) return SPD_ENULL; // arrays of no elements may be null
-    if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || ((uintptr_t)c->k_scales & 3) || ((uintptr_t)c->v_scales & 3)) return SPD_EINVAL;
+    if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || (((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) & (c->format == SPD_KV_INT4 ? 7 : 3)))
+        return SPD_EINVAL;
     *kv = PagedKv{c->k_pages, c->v_pages, c->k_scales, c->v_scales, c->n_pages, c->n_kv_heads, c->kv_block_size, c->head_dim, c->format};
     *rb = RaggedBatch{r->cu_new, r->seq_lens, r->block_table, r->B, r->max_pages, r->n_tokens, 0, 0};
     return SPD_OK;
@@ -345,7 +464,25 @@ extern "C" int spd_kv_write(const spd_kv_cache *cache, const spd_ragged *batch, 
     if (rb.B == 0 || rb.n_tokens == 0) return SPD_OK;
     if (!k || !v) return SPD_ENULL;
     if (!rows_ok(k, k_stride, kv.nkv, kv.d, dtype) || !rows_ok(v, v_stride, kv.nkv, kv.d, dtype)) return SPD_EINVAL;
-    const cudaError_t e = launch_kv_write(kv, rb, k, v, k_stride, v_stride, dtype, err_flag, (cudaStream_t)stream);
+    const cudaError_t e = launch_kv_write(kv, rb, nullptr, k, v, k_stride, v_stride, dtype, err_flag, (cudaStream_t)stream);
+    if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }
+    return SPD_OK;
+}
+
+extern "C" int spd_kv_write_slots(const spd_kv_cache *cache, const int32_t *slots, int32_t n_tokens, const void *k, const void *v, int64_t k_stride,
+                                  int64_t v_stride, int32_t dtype, int32_t *err_flag, void *stream)
+{
+    PagedKv kv;
+    RaggedBatch rb;
+    const spd_ragged rows{nullptr, nullptr, nullptr, 0, 1, n_tokens};
+    const int rc = check_cache(cache, &rows, &kv, &rb);
+    if (rc) return rc;
+    if (!err_flag) return SPD_ENULL;
+    if (dtype != 0 && dtype != 1) return SPD_EINVAL;
+    if (n_tokens == 0) return SPD_OK;
+    if (!slots || !k || !v) return SPD_ENULL;
+    if (!rows_ok(k, k_stride, kv.nkv, kv.d, dtype) || !rows_ok(v, v_stride, kv.nkv, kv.d, dtype)) return SPD_EINVAL;
+    const cudaError_t e = launch_kv_write(kv, rb, slots, k, v, k_stride, v_stride, dtype, err_flag, (cudaStream_t)stream);
     if (e != cudaSuccess) { note_cuda_error(e); return SPD_ECUDA; }
     return SPD_OK;
 }

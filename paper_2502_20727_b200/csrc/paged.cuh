@@ -9,9 +9,10 @@
 
 namespace spd {
 
-enum KvFormat : int { KV_F32 = 0, KV_BF16 = 1, KV_E4M3 = 2, KV_INT8 = 3 };
+enum KvFormat : int { KV_F32 = 0, KV_BF16 = 1, KV_E4M3 = 2, KV_INT8 = 3, KV_INT4 = 5 };
 
-// [n_pages, n_kv_heads, page, head_dim] elements; 8-bit formats: one float32 scale per (page, head, row).
+// [n_pages, n_kv_heads, page, head_dim] elements; 8-bit formats: one float32 scale per (page, head, row).  4 bits: head_dim / 2 bytes per
+// row, and instead of a scale two words, one per half of the head dims: a bfloat16 scale (low bits) and a bfloat16 smallest value.
 struct PagedKv {
     void *k, *v;
     float *ks, *vs;
@@ -49,6 +50,7 @@ template <> struct KvElem<KV_F32> { typedef float type; };
 template <> struct KvElem<KV_BF16> { typedef bf16 type; };
 template <> struct KvElem<KV_E4M3> { typedef uint8_t type; };
 template <> struct KvElem<KV_INT8> { typedef int8_t type; };
+template <> struct KvElem<KV_INT4> { typedef uint8_t type; };
 
 // code -> the value it stands for before the row's scale
 template <int FMT> __device__ __forceinline__ float kv_value(typename KvElem<FMT>::type c);
@@ -59,6 +61,17 @@ template <> __device__ __forceinline__ float kv_value<KV_E4M3>(uint8_t c)
     return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));
 }
 template <> __device__ __forceinline__ float kv_value<KV_INT8>(int8_t c) { return (float)c; }
+
+// 4-bit rows: byte i holds the code of dim i (low bits) and of dim i + head_dim / 2; value = code * scale + smallest of the dim's half.
+__device__ __forceinline__ float kv4_scale(uint32_t half) { return __uint_as_float(half << 16); }
+__device__ __forceinline__ float kv4_min(uint32_t half) { return __uint_as_float(half & 0xffff0000u); }
+// A row's parameters; all four are NaN where one of them is not finite.
+__device__ __forceinline__ uint2 kv4_params(const float *params, long row)
+{
+    const uint2 p = *(const uint2 *)(params + 2 * row);
+    const uint32_t bad = (((p.x & 0x7f807f80u) + 0x00800080u) | ((p.y & 0x7f807f80u) + 0x00800080u)) & 0x80008000u;
+    return bad ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u) : p;
+}
 
 // Two 8-bit codes of a word -> bf16x2 of the values they stand for, exactly: bytes 0 and 2 (even), bytes 1 and 3 (odd).
 // c128: widen_const(), kept in a register by the caller.
@@ -126,8 +139,9 @@ struct SmemLimit {
     }
 };
 
-cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const void *k, const void *v, long k_stride, long v_stride,
-                            int in_bf16, int *err, cudaStream_t st);
+// slots non-null: row t goes to slot slots[t] = page id * page + row of the page (negative: nobody's), whatever rb says
+cudaError_t launch_kv_write(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slots, const void *k, const void *v, long k_stride,
+                            long v_stride, int in_bf16, int *err, cudaStream_t st);
 cudaError_t launch_kv_read(const PagedKv &kv, const RaggedBatch &rb, void *k, void *v, long k_stride, long v_stride, int out_bf16,
                            int *err, cudaStream_t st);
 

@@ -40,10 +40,18 @@ template <int FMT> __device__ __forceinline__ float4 cache4(const PagedKv &kv, c
         const uint2 u = *(const uint2 *)((const bf16 *)pages + row * D + c * 4);
         return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
     }
+    if constexpr (FMT == KV_INT4) { // four dims of one half
+        const bool high = c * 4 >= D / 2;
+        const uint32_t w = *(const uint32_t *)((const uint8_t *)pages + row * (D / 2) + (high ? c * 4 - D / 2 : c * 4)) >> (high ? 4 : 0);
+        const uint2 p = kv4_params(scales, row);
+        const float s = kv4_scale(high ? p.y : p.x), m = kv4_min(high ? p.y : p.x);
+        return make_float4(fmaf((float)(w & 15), s, m), fmaf((float)(w >> 8 & 15), s, m), fmaf((float)(w >> 16 & 15), s, m),
+                           fmaf((float)(w >> 24 & 15), s, m));
+    }
     typedef typename KvElem<FMT>::type E;
     const uint32_t w = *(const uint32_t *)((const uint8_t *)pages + row * D + c * 4);
     const float s = scales[row];
-    if constexpr (FMT >= KV_E4M3)
+    if constexpr (FMT == KV_E4M3 || FMT == KV_INT8)
         return make_float4(kv_value<FMT>((E)w) * s, kv_value<FMT>((E)(w >> 8)) * s, kv_value<FMT>((E)(w >> 16)) * s, kv_value<FMT>((E)(w >> 24)) * s);
     return make_float4(0.f, 0.f, 0.f, 0.f);
 }
@@ -255,11 +263,14 @@ template <int FMT> cudaError_t general_f32(const PagedAttnArgs &a, cudaStream_t 
 cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, cudaStream_t st)
 {
     if (q_bf16) {
+        if (a.kv.fmt == KV_INT4 && a.kv.d == 64) return general_by_rows<bf16, KV_INT4, 64>(a, st);
+        if (a.kv.fmt == KV_INT4 && a.kv.d == 128) return general_by_rows<bf16, KV_INT4, 128>(a, st);
         if (a.kv.d != 32) return cudaErrorInvalidValue; // 64 and 128: the tensor-core kernels
         switch (a.kv.fmt) {
         case KV_BF16: return general_by_rows<bf16, KV_BF16, 32>(a, st);
         case KV_E4M3: return general_by_rows<bf16, KV_E4M3, 32>(a, st);
         case KV_INT8: return general_by_rows<bf16, KV_INT8, 32>(a, st);
+        case KV_INT4: return general_by_rows<bf16, KV_INT4, 32>(a, st);
         default: return cudaErrorInvalidValue;
         }
     }
@@ -267,6 +278,7 @@ cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, c
     case KV_F32: return general_f32<KV_F32>(a, st);
     case KV_E4M3: return general_f32<KV_E4M3>(a, st);
     case KV_INT8: return general_f32<KV_INT8>(a, st);
+    case KV_INT4: return general_f32<KV_INT4>(a, st);
     default: return cudaErrorInvalidValue;
     }
 }
@@ -284,7 +296,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     const long rows = (long)max_new * (nq / nkv);
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
-    if (dtype != 1 || d == 32) {
+    if (dtype != 1 || d == 32 || fmt == KV_INT4) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
         // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);
@@ -345,6 +357,7 @@ cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, c
 }
 
 int check_cache(const spd_kv_cache *c, const spd_ragged *r, PagedKv *kv, RaggedBatch *rb); // kv_cache.cu
+bool known_format(int f);
 bool rows_ok(const void *p, int64_t stride, int heads, int d, int dtype);
 
 } // namespace spd
@@ -388,7 +401,7 @@ extern "C" int spd_paged_attention_workspace_bytes(const spd_kv_cache *cache, in
 {
     if (!cache || !out_bytes) return SPD_ENULL;
     if (B < 0 || n_tokens < 0 || (dtype != 0 && dtype != 1) || cache->n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % cache->n_kv_heads || max_new < 1 || max_context < 1 || window < 0 || sinks < 0) return SPD_EINVAL;
-    if (cache->format < SPD_KV_F32 || cache->format > SPD_KV_INT8) return SPD_EINVAL;
+    if (!known_format(cache->format)) return SPD_EINVAL;
     *out_bytes = plan_attention(cache->format, cache->head_dim, cache->n_kv_heads, dtype, n_q_heads, B, n_tokens, max_new, max_context, window,
                                 window ? sinks : 0).workspace;
     return SPD_OK;
