@@ -330,32 +330,32 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedB
                           fmaf((float)(c >> 24 & 15), s, m));
             }
         }
-        return;
-    }
-    Raw8<E> raw[UNITS];
-    float s[UNITS];
+    } else {
+        Raw8<E> raw[UNITS];
+        float s[UNITS];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const int id = i * S::PER_PASS + g, r = r0 + id % ROWS, h = r >> 1;
-        const long where = base[id / ROWS], row = where + (long)h * kv.page;
-        raw[i] = Raw8<E>{};
-        s[i] = 1.f;
-        if (where >= 0 && h < kv.nkv) {
-            raw[i] = *(const Raw8<E> *)((const E *)(r & 1 ? kv.v : kv.k) + row * D + li * 8);
-            if (sizeof(E) == 1) s[i] = (r & 1 ? kv.vs : kv.ks)[row];
+        for (int i = 0; i < UNITS; ++i) {
+            const int id = i * S::PER_PASS + g, r = r0 + id % ROWS, h = r >> 1;
+            const long where = base[id / ROWS], row = where + (long)h * kv.page;
+            raw[i] = Raw8<E>{};
+            s[i] = 1.f;
+            if (where >= 0 && h < kv.nkv) {
+                raw[i] = *(const Raw8<E> *)((const E *)(r & 1 ? kv.v : kv.k) + row * D + li * 8);
+                if (sizeof(E) == 1) s[i] = (r & 1 ? kv.vs : kv.ks)[row];
+            }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const int id = i * S::PER_PASS + g, t = t0 + id / ROWS, r = r0 + id % ROWS, h = r >> 1;
-        if (base[id / ROWS] < 0 || h >= kv.nkv) continue;
-        float x[8];
-        get(raw[i], x);
-        if (sizeof(E) == 1) {
+        for (int i = 0; i < UNITS; ++i) {
+            const int id = i * S::PER_PASS + g, t = t0 + id / ROWS, r = r0 + id % ROWS, h = r >> 1;
+            if (base[id / ROWS] < 0 || h >= kv.nkv) continue;
+            float x[8];
+            get(raw[i], x);
+            if (sizeof(E) == 1) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= s[i];
+                for (int e = 0; e < 8; ++e) x[e] *= s[i];
+            }
+            store8<T>((r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)h * D + li * 8, x);
         }
-        store8<T>((r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)h * D + li * 8, x);
     }
 }
 

@@ -296,7 +296,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     const long rows = (long)max_new * (nq / nkv);
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
-    if (dtype != 1 || d == 32 || fmt == KV_INT4) {
+    if (dtype != 1 || d == 32 || (fmt == KV_INT4 && rows > PAGED_MAX_FEW_ROWS)) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
         // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);
