@@ -263,8 +263,6 @@ template <int FMT> cudaError_t general_f32(const PagedAttnArgs &a, cudaStream_t 
 cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, cudaStream_t st)
 {
     if (q_bf16) {
-        if (a.kv.fmt == KV_INT4 && a.kv.d == 64) return general_by_rows<bf16, KV_INT4, 64>(a, st);
-        if (a.kv.fmt == KV_INT4 && a.kv.d == 128) return general_by_rows<bf16, KV_INT4, 128>(a, st);
         if (a.kv.d != 32) return cudaErrorInvalidValue; // 64 and 128: the tensor-core kernels
         switch (a.kv.fmt) {
         case KV_BF16: return general_by_rows<bf16, KV_BF16, 32>(a, st);
@@ -296,7 +294,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     const long rows = (long)max_new * (nq / nkv);
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
-    if (dtype != 1 || d == 32 || (fmt == KV_INT4 && rows > PAGED_MAX_FEW_ROWS)) {
+    if (dtype != 1 || d == 32) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
         // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);

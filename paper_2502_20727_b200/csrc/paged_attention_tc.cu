@@ -128,6 +128,34 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *(const uint32_t *)&v;
 }
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *(const uint32_t *)&v;
+}
+// 4-bit codes in bits 0-3 (4-7) of a word's halves -> float16x2 of code * s + m: the masked bits are code * 2^-24 (2^-20), so that
+// `s` holds the scale times 2^24 (2^20); one rounding.
+__device__ __forceinline__ uint32_t widen4(uint32_t codes, uint32_t s, uint32_t m)
+{
+    const __half2 v = __hfma2(*(const __half2 *)&codes, *(const __half2 *)&s, *(const __half2 *)&m);
+    return *(const uint32_t *)&v;
+}
+// A row's parameters (s, m of either half) in units of 2^(e + 6), where 2^e is the power of two at or under the largest of |m| and 16 s:
+// values are below 2^-4 then, and the scales as widen4 wants them below 2^16.  What rounding leaves of the smaller ones is 2^-20 of the
+// row's largest value at most.  unit = 2^(e + 6), at least 2^-60 and at most 2^36; a row that is not finite gives zeros and a NaN.
+__device__ __forceinline__ uint2 row_params(uint2 p, float &unit, int &exponent)
+{
+    const uint32_t mags = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu), sb = mags & 0xffffu, mb = mags >> 16;
+    const int ex = min(max((int)max((sb >> 7) + 4, mb >> 7) + 6, 127 - 60), 127 + 36);
+    unit = __uint_as_float((uint32_t)ex << 23);
+    exponent = ex - 127;
+    if (sb >= 0x7f80u || mb >= 0x7f80u) {
+        unit = __uint_as_float(0x7fc00000u);
+        return make_uint2(0, 0);
+    }
+    const float f = __uint_as_float((uint32_t)(254 - ex) << 23);
+    return make_uint2(pack_half(kv4_scale(p.x) * f * 0x1p24f, kv4_min(p.x) * f), pack_half(kv4_scale(p.y) * f * 0x1p20f, kv4_min(p.y) * f));
+}
 __device__ __forceinline__ float max_nan(float a, float b) // NaN if either is
 {
     float d;
@@ -229,9 +257,9 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                                                                           const __grid_constant__ PagedAttnArgs a)
 {
     using C = TcCfg<D>;
-    constexpr bool Q8 = FMT != KV_BF16;
+    constexpr bool Q4 = FMT == KV_INT4, Q8 = FMT == KV_E4M3 || FMT == KV_INT8, QC = Q4 || Q8;
     constexpr uint32_t T_COLS = 256, T_O = 128;
-    constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA, Q8), LT = 32 * load_warps(TMA, Q8);
+    constexpr int W_LOAD = SOFT_WARPS, W_MMA = SOFT_WARPS + load_warps(TMA, QC), LT = 32 * load_warps(TMA, QC);
     extern __shared__ uint8_t tc_raw[];
     uint8_t *gen = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(gen), bars = base + C::OFF_BAR;
@@ -239,6 +267,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     const uint32_t p_ready = bars + 56, p_rest = bars + 64; // weights of a tile's first 64 keys, of the others
     const uint32_t o_done = bars + 72, drain = bars + 80;
     auto sc_full = [&](int s) { return bars + 8u * (11 + s); };
+    constexpr int SC_SLOTS = Q4 ? 2 : 8; // tiles whose scales are kept
     uint32_t *tmem_slot = (uint32_t *)(gen + C::OFF_BAR + 8 * 40);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     volatile int *dirty = (volatile int *)(tmem_slot + 2);
@@ -301,7 +330,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     const uint32_t tmem = *tmem_slot;
     pdl_launch_dependents();
     if (warp >= W_LOAD && warp < W_MMA) {
-        if (Q8) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Q8_LOAD_REGS));
+        if (QC) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Q8_LOAD_REGS));
         const int tid = threadIdx.x - 32 * W_LOAD;
         // one box = 16 keys x 64 dims; lane = (16 keys, half of the head); 16 keys that no row needs come as zeros (a row beyond the map)
         constexpr int BOXES = 8 * (D / 64);
@@ -385,9 +414,71 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     sc[(j & 7) * 256 + 128 + tid] = row >= 0 ? a.kv.vs[row] : 0.f;
                     mbar_arrive(sc_full(j & 7)); // eight tiles later the slot's scores have long been weighted
                 }
+                if constexpr (Q4) {
+                    uint2 kp = make_uint2(0, 0), vp = kp;
+                    if (row >= 0) { kp = *(const uint2 *)(a.kv.ks + 2 * row); vp = *(const uint2 *)(a.kv.vs + 2 * row); }
+                    float *s = sc + (j & 1) * 384 + tid, ku, vu;
+                    int ke, ve;
+                    uint2 *par = (uint2 *)(gen + C::OFF_SC + 3072) + (j & 1) * 256 + tid;
+                    par[0] = row_params(kp, ku, ke);
+                    par[128] = row_params(vp, vu, ve);
+                    s[0] = ku;
+                    s[128] = vu == vu ? (float)ve : vu;
+                    s[256] = __uint_as_float((uint32_t)(127 - ve) << 23);
+                    mbar_arrive(sc_full(j & 1)); // the weights of the tile before last went into a product that the load warps have seen complete
+                }
                 named_bar<BAR_LOAD, LT>();
             };
-            if constexpr (Q8) {
+            if constexpr (Q4) {
+                // a thread: a quarter of a row, D / 8 bytes, of half a tile (64 keys); these are D / 8 dims of either half of the head
+                constexpr int W = D / 32;
+                const int c = tid & 3;
+                const uint32_t par = base + C::OFF_SC + 3072;
+                auto fetch = [&](int j, int h, const void *pages, uint32_t (&x)[W]) {
+                    const long row = rowoff[(j & 1) * 128 + h * 64 + tid / 4];
+                    const uint8_t *p = (const uint8_t *)pages + row * (D / 2) + c * (D / 8);
+                    if (W == 4) {
+                        const uint4 u = row >= 0 ? *(const uint4 *)p : make_uint4(0, 0, 0, 0);
+                        x[0] = u.x; x[1] = u.y; x[2 % W] = u.z; x[3 % W] = u.w;
+                    } else {
+                        const uint2 u = row >= 0 ? *(const uint2 *)p : make_uint2(0, 0);
+                        x[0] = u.x; x[1] = u.y;
+                    }
+                };
+                auto widen = [&](int j, bool is_v, int h, const uint32_t (&x)[W]) {
+                    const int r = h * 64 + tid / 4;
+                    const uint32_t tile_base = base + (is_v ? C::OFF_V : C::OFF_K);
+                    uint2 p;
+                    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(p.x), "=r"(p.y) : "r"(par + ((j & 1) * 256 + is_v * 128 + r) * 8) : "memory");
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t s = __byte_perm(half ? p.y : p.x, 0, 0x1010), m = __byte_perm(half ? p.y : p.x, 0, 0x3232), mask = half ? 0x00f000f0u : 0x000f000fu;
+#pragma unroll
+                        for (int i = 0; i < W; i += 2)
+                            sts128(tile_base + tile_at(r, half * (D / 16) + c * (W / 2) + i / 2),
+                                   make_uint4(widen4(x[i] & mask, s, m), widen4(x[i] >> 8 & mask, s, m), widen4(x[i + 1] & mask, s, m), widen4(x[i + 1] >> 8 & mask, s, m)));
+                    }
+                };
+                uint32_t x0[W], x1[W];
+                if (n_tiles > 0) { rows_of(0); fetch(0, 0, a.kv.k, x0); fetch(0, 1, a.kv.k, x1); }
+                for (int j = 0; j < n_tiles; ++j) {
+                    if (j > 0) mbar_wait(k_empty, (j - 1) & 1, a.err, abort_flag);
+                    widen(j, false, 0, x0);
+                    fetch(j, 0, a.kv.v, x0);
+                    widen(j, false, 1, x1);
+                    fetch(j, 1, a.kv.v, x1);
+                    fence_proxy_async();
+                    mbar_arrive(k_full);
+                    if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
+                    if (j + 1 < n_tiles) rows_of(j + 1);
+                    widen(j, true, 0, x0);
+                    if (j + 1 < n_tiles) fetch(j + 1, 0, a.kv.k, x0);
+                    widen(j, true, 1, x1);
+                    if (j + 1 < n_tiles) fetch(j + 1, 1, a.kv.k, x1);
+                    fence_proxy_async();
+                    mbar_arrive(v_full);
+                }
+            } else if constexpr (Q8) {
                 constexpr int CPR = D / 16, N = 64 * CPR / LT; // 16-code chunks per row; per thread and half a tile (64 keys)
                 const uint32_t c128 = widen_const();
                 const int c = tid % CPR;
@@ -470,7 +561,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     } else if (warp >= W_MMA) {
         // A wait that gives up raises the abort flag, after which every wait returns at once: the loops run out on whatever is there,
         // and the block ends with the error bit set.
-        constexpr uint32_t idesc_s = make_idesc(TK), idesc_o = make_idesc(D) | (1u << 16); // V: MN-major
+        constexpr uint32_t f16_ops = Q4 ? (1u << 7) | (1u << 10) : 0; // the operand types' bits: bf16, without them float16
+        constexpr uint32_t idesc_s = make_idesc(TK) & ~f16_ops, idesc_o = (make_idesc(D) & ~f16_ops) | (1u << 16); // V: MN-major
         const uint32_t q_lo = desc_lo(base + C::OFF_Q, 1), k_lo = desc_lo(base + C::OFF_K, 1), v_lo = desc_lo(base + C::OFF_V, HALF >> 4);
         auto wait = [&](uint32_t bar, int parity) {
             mbar_wait(bar, parity, a.err, abort_flag);
@@ -519,7 +611,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
         }
         __syncwarp();
     } else {
-        if (Q8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Q8_SOFT_REGS));
+        if (QC) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Q8_SOFT_REGS));
         const int half = warp >> 2, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + (warp & 3);
         // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
         {
@@ -534,12 +626,26 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const int idx = k * SOFT_THREADS + threadIdx.x, r = idx / CH, c = idx % CH;
-                const uint4 y = x[k];
+                uint4 y = x[k];
+                if constexpr (Q4) { // float16, each row times a power of two that brings it below 2^15
+                    uint32_t w[4] = {y.x, y.y, y.z, y.w}, top = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+#pragma unroll
+                    for (int o = CH / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const int ex = max((int)(top >> 7), 27) - 127;
+                    const float f = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = pack_half(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                    y = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (c == 0) ((float *)(gen + C::OFF_RED))[256 + r] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23); // where the maxima of tile 1 go
+                }
                 sts128(base + C::OFF_Q + tile_at(r, c),
-                       Q8 ? make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.z, y.w, 0x7632)) : y);
+                       QC ? make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.z, y.w, 0x7632)) : y);
             }
             fence_proxy_async();
             mbar_arrive(q_full);
+            if (Q4) named_bar<BAR_OUT, SOFT_THREADS>(); // the rows' factors
         }
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + half * 64u; // this thread's scores: 64 columns; its weights: the first 32 of them
@@ -547,14 +653,14 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
         const int my_token = token_of(row);
         const bool live = row < rows;
         const int pos = live ? len + tok0 + my_token : -1;
-        const float qs = a.scale_log2;
+        const float qs = a.scale_log2 * (Q4 ? ((const float *)(gen + C::OFF_RED))[256 + row] : 1.f);
         const float *sc = (const float *)(gen + C::OFF_SC);
         float *red = (float *)(gen + C::OFF_RED);
         float m_used = -INFINITY, l = 0.f;
         for (int j = 0; j < n_tiles; ++j) {
             const int t0 = key0(j) + half * 64;
             mbar_wait(s_full, j & 1, a.err, abort_flag); // see the MMA warp about waits that give up
-            if (Q8) mbar_wait(sc_full(j & 7), (j >> 3) & 1, a.err, abort_flag);
+            if (QC) mbar_wait(sc_full(j % SC_SLOTS), (j / SC_SLOTS) & 1, a.err, abort_flag);
             __syncwarp();
             fence_after();
             const bool masked = partial(key0(j));
@@ -564,9 +670,21 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 seen = below(pos - t0 + 1);
                 if (a.window) seen &= ~below(pos - a.window + 1 - t0) | below(a.sinks - t0);
             }
-            const float *ks = sc + (j & 7) * 256 + half * 64, *vs = ks + 128;
+            // 4 bits: the K rows' units, the exponents of the V rows' and their negative powers
+            const float *ks = sc + (Q4 ? (j & 1) * 384 : (j & 7) * 256) + half * 64, *vs = ks + 128;
             // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
+            // (4 bits: in base-2 units, the exponent of the key's V row added)
             auto finish = [&](int c0, uint32_t (&r)[32]) {
+                if constexpr (Q4) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 k4 = *(const float4 *)(ks + c0 + e), e4 = *(const float4 *)(vs + c0 + e);
+                        const float2 q2 = make_float2(qs, qs);
+                        const float2 x = fma2(mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(k4.x, k4.y)), q2, make_float2(e4.x, e4.y));
+                        const float2 y = fma2(mul2(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), make_float2(k4.z, k4.w)), q2, make_float2(e4.z, e4.w));
+                        r[e] = __float_as_uint(x.x); r[e + 1] = __float_as_uint(x.y); r[e + 2] = __float_as_uint(y.x); r[e + 3] = __float_as_uint(y.y);
+                    }
+                }
                 if (Q8) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
@@ -602,7 +720,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             tmem_ask32(t_s + 32, rb);
             tmem_wait32(rb);
             finish(32, rb);
-            mx = max_nan(mx, max_of(rb)) * qs;
+            mx = max_nan(mx, max_of(rb)) * (Q4 ? 1.f : qs);
             // join with the other half's maximum: both threads of a row then take the same decision
             float *rm = red + (j & 1) * 256 + row;
             rm[half * 128] = mx;
@@ -638,12 +756,13 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 uint32_t w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
+                    const float2 x = make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+                    const float2 t = Q4 ? add2(x, m2) : fma2(x, q2, m2);
                     // every second pair (bf16 pages by TMA) or every fourth on the FMA pipes, which the exponentials otherwise leave idle
                     float2 p = (TMA ? k % 2 == 1 : k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
-                    ls = add2(ls, p);
+                    ls = Q4 ? fma2(p, *(const float2 *)(vs + 128 + c0 + 2 * k), ls) : add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
-                    w[k] = pack(p.x, p.y);
+                    w[k] = Q4 ? pack_half(p.x, p.y) : pack(p.x, p.y);
                     if (FMT == KV_INT8) { r[2 * k] = __float_as_uint(p.x); r[2 * k + 1] = __float_as_uint(p.y); }
                 }
                 if (Q8 && masked) { // 0 times the scale of an unseen key, which may be anything
@@ -696,7 +815,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             const long token = row0 + tok0 + my_token;
             const long w = (long)split * ((long)a.rb.n_tokens * a.nq) + token * a.nq + head;
             if (a.part_o && live && half == 0) { a.part_ml[w * 2] = m; a.part_ml[w * 2 + 1] = den; }
-            const bool give_back = !Q8 && *dirty;
+            const bool give_back = !QC && *dirty;
 #pragma unroll 1
             for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2) && n_tiles > 0 && ok; c0 += 16) {
                 uint32_t y[16];
@@ -728,7 +847,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     }
                     // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[Q8 ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
+                    for (int e = 0; e < 16; ++e) x[QC ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
                     if (a.part_o) {
 #pragma unroll
                         for (int e = 0; e < 16; e += 4) *(float4 *)(a.part_o + w * D + c0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -805,6 +924,7 @@ cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st)
     case KV_BF16: return tc_by_dim<KV_BF16>(a, st);
     case KV_E4M3: return tc_by_dim<KV_E4M3>(a, st);
     case KV_INT8: return tc_by_dim<KV_INT8>(a, st);
+    case KV_INT4: return tc_by_dim<KV_INT4>(a, st);
     default: return cudaErrorInvalidValue;
     }
 }
