@@ -33,7 +33,7 @@ int make_operand_map(TcMap *out, const void *ptr, long k_inner, long rows, long 
                      long batch_stride_elems, int box_rows);
 // A paged K / V cache (16-token pages, head_dim 128) as a map whose {64, 16, 2} box is one (page, head): see gemm_tc.cu.
 int make_page_map(TcMap *out, const void *ptr, long rows);
-// A paged cache of rows of head_dim elements of `elem` bytes, 32, 64, 128 or 256 bytes in all: one box = 16 token rows of one (page, head).
+// A paged cache of any storage type (`elem` bytes) and head_dim 64 or 128: one box = 16 token rows of one (page, head).
 int make_cache_map(TcMap *out, const void *ptr, long rows, int head_dim, int elem);
 
 // Box rows of the token-side operand for a given token count (swap: 16/32/64, else 128).

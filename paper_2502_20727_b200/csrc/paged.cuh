@@ -154,6 +154,7 @@ constexpr int PAGED_MAX_CONTEXT = 1 << 30;
 // bf16 queries, head_dim 64 or 128, few rows (new tokens x query heads per KV head) per sequence and KV head
 constexpr int PAGED_MAX_FEW_ROWS = 16;
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
+cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, cudaStream_t st); // the same over 4-bit pages
 // bf16 queries, head_dim 64 or 128, any number of rows
 cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st);
 // Chooses a kernel and launches it (and the merge).  part_o / part_ml: room for `part_splits` ranges of partial rows, or null and 0;

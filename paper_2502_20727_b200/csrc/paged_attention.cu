@@ -347,7 +347,7 @@ cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, c
     cudaError_t e = cudaSuccess;
     switch (p.kernel) {
     case ATTN_GENERAL: e = launch_paged_attention_general(a, q_bf16, st); break;
-    case ATTN_ROWS: e = launch_paged_attention_rows(a, st); break;
+    case ATTN_ROWS: e = a.kv.fmt == KV_INT4 ? launch_paged_attention_rows4(a, st) : launch_paged_attention_rows(a, st); break;
     case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
     }
     if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, q_bf16, st);

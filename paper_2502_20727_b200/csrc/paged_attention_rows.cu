@@ -30,64 +30,41 @@
 // Softmax: base 2, fp32, per warp; the accumulators follow the running maximum lazily (they are rescaled when it has grown by
 // more than 2^8: weights stay below 2^8, where bf16 rounds as finely as at 1).
 #include "gemm_tc.cuh"
-#include "paged.cuh"
-#include "tc_ptx.cuh"
+#include "paged_rows.cuh"
 
 namespace spd {
 
 namespace {
 
+using namespace few;
+
 constexpr int BK16 = 16;
 
 // RW warps per thread block; `stages` tiles per warp (TMA: as many as the launch has shared memory for)
 template <int FMT, int D, int RW> struct RowsCfg {
-    static constexpr bool Q4 = FMT == KV_INT4;
-    static constexpr int RB = Q4 ? D / 2 : D * (FMT == KV_BF16 ? 2 : 1); // bytes of a cached row
-    static constexpr int PB = Q4 ? 8 : FMT == KV_BF16 ? 0 : 4; // of its scale or parameters
+    static constexpr bool Q8 = FMT != KV_BF16;
+    static constexpr int RB = D * (Q8 ? 1 : 2);            // bytes of a cached row
     static constexpr int TR = RB > 128 ? 128 : RB;         // bytes of a tile row; 256-byte rows are two tiles
     static constexpr int TILE = BK16 * RB;                 // K or V of one block
-    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : RB == 32 ? 8 : Q4 ? 5 : 6; // with the most thread blocks resident
+    static constexpr int STAGES = RB == 256 ? 2 : RB == 128 ? 3 : 6; // with the most thread blocks resident
     static constexpr int MAX_STAGES = 8;
     static constexpr int MERGE = RW * 16 * (D + 4) * 4;    // the warps' partial rows, over the tiles
-    // after the tiles: 16 K scales (parameters), 16 V scales per stage; a barrier per stage; abort flag; merged [16][2], weights [16][RW], rows' places [16], ranges' weights [16][8]
+    // after the tiles: 16 K scales, 16 V scales per stage; a barrier per stage; abort flag; merged [16][2], weights [16][RW], rows' places [16], ranges' weights [16][8]
     static constexpr int off_sc(int st) { return RW * st * 2 * TILE > MERGE ? RW * st * 2 * TILE : (MERGE + 1023) / 1024 * 1024; }
-    static constexpr int off_bar(int st) { return off_sc(st) + RW * st * 32 * PB; }
+    static constexpr int off_bar(int st) { return off_sc(st) + (Q8 ? RW * st * 128 : 0); }
     static constexpr int off_pml(int st) { return (off_bar(st) + RW * st * 8 + 16 + 15) / 16 * 16; }
     static constexpr int smem(int st) { return off_pml(st) + 128 + 16 * RW * 4 + 128 + 16 * PAGED_MAX_CLUSTER * 4 + 1024; } // + alignment slack
 };
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool valid)
 {
-    const int n = valid ? 16 : 0; // 0 source bytes: zero fill
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    const int n = valid ? 4 : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
-template <int BYTES> __device__ __forceinline__ void cp_small(uint32_t dst, const void *src, bool valid) // 4 or 8 bytes
+// 64 bytes, both sides 16-byte aligned
+__device__ __forceinline__ void bulk64(uint32_t dst, const void *src, uint32_t bar)
 {
-    const int n = valid ? BYTES : 0;
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(n), "n"(BYTES) : "memory");
-}
-// BYTES bytes, both sides 16-byte aligned
-template <int BYTES> __device__ __forceinline__ void bulk(uint32_t dst, const void *src, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %3, [%2];" ::"r"(dst), "l"(src), "r"(bar), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 64, [%2];" ::"r"(dst), "l"(src), "r"(bar) : "memory");
 }
 __device__ __forceinline__ float lds_f(uint32_t a)
 {
@@ -103,39 +80,6 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-template <bool F16>
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    if (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
-{
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *(const uint32_t *)&v;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *(const uint32_t *)&v;
-}
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // Two K codes of a word -> float16x2.  int8: codes with the sign bit flipped (code + 128), bytes 0, 1 or (SECOND) 2, 3, under the
 // exponent of 1024, minus 1152.  e4m3: bytes 0, 2 or 1, 3, sign, exponent and mantissa moved to float16's places: the value
 // times E4M3_UNIT = 2^-8, exactly (64 sequences of ragged lengths: 33.3 us, with a conversion instruction per pair 34.1).
@@ -148,39 +92,20 @@ template <int FMT, bool SECOND> __device__ __forceinline__ uint32_t half_of(uint
     return *(const uint32_t *)&v;
 }
 
-// 4-bit codes of a word -> float16x2 without arithmetic: a code in the lowest bits of a float16 is the subnormal number code * 2^-24, one
-// in bits 4-7 is 16 times that, and products with subnormals are exact.  Bytes 0, 2 of the word (shifted right by 8: bytes 1, 3).
-__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
-__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
-constexpr float LOW_UNIT = 0x1p24f, HIGH_UNIT = 0x1p20f;
-// Exponent field of the largest of a row's four parameters; at least 2^-60's, at most 2^30's (what is not finite says `bad`).
-__device__ __forceinline__ int row_exponent(uint2 p, bool &bad)
-{
-    const uint32_t m = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu), top = max(m & 0xffffu, m >> 16);
-    bad = top >= 0x7f80u;
-    return min(max((int)(top >> 7), 127 - 60), 127 + 30);
-}
-
-// keys t that a row at position pos (-1: no row) sees
-__device__ __forceinline__ bool sees(int t, int pos, int window, int sinks) { return t <= pos && (!window || t > pos - window || t < sinks); }
-
-// key of score row c (0-7) of eight
-__device__ __forceinline__ int key_of(int c) { return c & 1 ? (c & 6) ^ 5 : c; }
-
 // NR: groups of 8 query rows
 template <int FMT, int D, int NR, int RW, bool TMA>
 __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF16 ? 4 : 3) paged_attention_rows_kernel(const __grid_constant__ TcMap k_map, const __grid_constant__ TcMap v_map,
                                                                             const __grid_constant__ PagedAttnArgs a)
 {
     using C = RowsCfg<FMT, D, RW>;
-    constexpr bool Q4 = C::Q4, Q8 = FMT == KV_E4M3 || FMT == KV_INT8, QC = Q4 || Q8;
+    constexpr bool Q8 = C::Q8;
     constexpr int MT = D / 16, KS = D / 16, R_THREADS = 32 * RW;
     const int ST = TMA ? a.stages : C::STAGES;
     extern __shared__ uint8_t rows_raw[];
     uint8_t *gen = rows_raw + ((1024u - (tc::smem_u32(rows_raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(gen);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::off_sc(ST) + warp * ST * 32 * C::PB, bars = base + C::off_bar(ST) + warp * ST * 8;
+    const uint32_t ring = base + warp * ST * 2 * C::TILE, ring_sc = base + C::off_sc(ST) + warp * ST * 128, bars = base + C::off_bar(ST) + warp * ST * 8;
     volatile int *abort_flag = (volatile int *)(gen + C::off_bar(ST) + RW * ST * 8);
     if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
@@ -236,21 +161,17 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     auto at = [&](int r, int c) -> uint32_t {
         if (C::RB == 256) return (c >> 3) * (BK16 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
         if (C::RB == 128) return r * 128 + ((c ^ (r & 7)) << 4);
-        if (C::RB == 32) return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
         return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
     };
     auto load_block = [&](int stage, long where) {
-        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 32 * C::PB;
+        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
         if (TMA) {
             if (lane == 0) {
                 const uint32_t bar = bars + 8 * stage;
-                tc::mbar_expect_tx(bar, 2 * C::TILE + 32 * C::PB);
+                tc::mbar_expect_tx(bar, 2 * C::TILE + (Q8 ? 128 : 0));
                 tc::tma_load_3d(sK, (const CUtensorMap *)&k_map, 0, (int)where, 0, bar);
                 tc::tma_load_3d(sV, (const CUtensorMap *)&v_map, 0, (int)where, 0, bar);
-                if constexpr (QC) {
-                    bulk<16 * C::PB>(sS, (const uint8_t *)a.kv.ks + where * C::PB, bar);
-                    bulk<16 * C::PB>(sS + 16 * C::PB, (const uint8_t *)a.kv.vs + where * C::PB, bar);
-                }
+                if (Q8) { bulk64(sS, a.kv.ks + where, bar); bulk64(sS + 64, a.kv.vs + where, bar); }
             }
         } else {
             constexpr int CPR = C::RB / 16, RPI = 32 / CPR; // chunks per row, rows per instruction
@@ -263,7 +184,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 cp16(sK + at(r, c), (const uint8_t *)a.kv.k + off, row >= 0);
                 cp16(sV + at(r, c), (const uint8_t *)a.kv.v + off, row >= 0);
             }
-            if constexpr (QC) cp_small<C::PB>(sS + lane * C::PB, (const uint8_t *)(lane < 16 ? a.kv.ks : a.kv.vs) + (where >= 0 ? where * C::PB : 0), where >= 0);
+            if (Q8) cp4(sS + lane * 4, (lane < 16 ? a.kv.ks : a.kv.vs) + (where >= 0 ? where : 0), where >= 0);
         }
     };
 
@@ -283,8 +204,8 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
         const int i = live ? r / a.group : 0, head = live ? r - i * a.group : 0;
         const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
 #pragma unroll
-        for (int m = 0; m < D / 32; ++m) { // a 16-byte K chunk is 8 dims (bf16), 16 (codes) or 16 of either half (4 bits; D / 8 bytes are read)
-            const int dim = Q4 ? (D / 2) * (m / (D / 64)) + (D / 8) * t4 + 8 * (m % (D / 64)) : Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
+        for (int m = 0; m < D / 32; ++m) { // a 16-byte K chunk is 8 dims (bf16) or 16 (codes)
+            const int dim = Q8 ? 64 * (m >> 1) + 16 * t4 + 8 * (m & 1) : 32 * m + 8 * t4;
             q_raw[n][m] = live ? *(const uint4 *)(qp + dim) : make_uint4(0, 0, 0, 0);
         }
     }
@@ -302,13 +223,13 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     // Q fragments (column g of a group of 8 rows); rows beyond the tile's are zero.  qs: what turns the scores of this lane's
     // columns 2 t4 and 2 t4 + 1 into base-2 units
     uint32_t qf[NR][KS][2];
-    float qs[NR][2], qsum[NR][2][2]; // 4 bits: sums of the columns' halves
+    float qs[NR][2];
     int pos[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         uint4 (&u)[D / 32] = q_raw[n];
-        float my_qs = a.scale_log2, my_sum[2] = {0.f, 0.f};
-        if (QC) {
+        float my_qs = a.scale_log2;
+        if (Q8) {
             uint32_t top = 0; // largest magnitude's bits
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
@@ -329,27 +250,17 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 for (int e = 0; e < 4; ++e) {
                     const __half2 v = __floats2half2_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
                     x[e] = *(const uint32_t *)&v;
-                    if (Q4) my_sum[m / (D / 64)] += __low2float(v) + __high2float(v);
                 }
                 u[m] = make_uint4(x[0], x[1], x[2], x[3]);
             }
         }
 #pragma unroll
         for (int m = 0; m < D / 32; ++m) {
-            if (FMT == KV_E4M3 || Q4) { // as half_of or low_codes pairs the codes
+            if (FMT == KV_E4M3) { // as half_of pairs the codes
                 qf[n][2 * m][0] = __byte_perm(u[m].x, u[m].y, 0x5410); qf[n][2 * m][1] = __byte_perm(u[m].x, u[m].y, 0x7632);
                 qf[n][2 * m + 1][0] = __byte_perm(u[m].z, u[m].w, 0x5410); qf[n][2 * m + 1][1] = __byte_perm(u[m].z, u[m].w, 0x7632);
             } else {
                 qf[n][2 * m][0] = u[m].x; qf[n][2 * m][1] = u[m].y; qf[n][2 * m + 1][0] = u[m].z; qf[n][2 * m + 1][1] = u[m].w;
-            }
-        }
-        if (Q4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                my_sum[h] += __shfl_xor_sync(0xffffffffu, my_sum[h], 1);
-                my_sum[h] += __shfl_xor_sync(0xffffffffu, my_sum[h], 2);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) qsum[n][e][h] = __shfl_sync(0xffffffffu, my_sum[h], (2 * t4 + e) * 4);
             }
         }
 #pragma unroll
@@ -361,12 +272,11 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
     }
 
     // where this lane reads in a stage; chunk bits above the lane's own are XORs, rows + 8 a fixed distance
-    const uint32_t lane_k = C::RB == 32 ? at(key_of(g), t4 >> 1) + (t4 & 1) * 8 : at(key_of(g), t4);
+    const uint32_t lane_k = at(key_of(g), t4);
     const int vc = lane & 7;
-    auto v4_at = [&](int r) { return C::RB == 32 ? at(r, g >> 2) + (g & 3) * 4 : at(r, g >> 1) + (g & 1) * 8; }; // 4 bits: D / 16 bytes of row r
-    const uint32_t lane_v0 = Q4 ? v4_at(key_of(2 * t4)) : Q8 ? (D == 128 ? at(key_of(2 * t4), g) : at(key_of(2 * t4), g >> 1) + (g & 1) * 8) : at(key_of(vc) + (lane & 8), lane >> 4);
-    const uint32_t lane_v1 = Q4 ? v4_at(key_of(2 * t4 + 1)) : Q8 ? (D == 128 ? at(key_of(2 * t4 + 1), g) : at(key_of(2 * t4 + 1), g >> 1) + (g & 1) * 8) : 0u;
-    const uint32_t lane_s = key_of(g) * C::PB, c128 = widen_const();
+    const uint32_t lane_v0 = Q8 ? (D == 128 ? at(key_of(2 * t4), g) : at(key_of(2 * t4), g >> 1) + (g & 1) * 8) : at(key_of(vc) + (lane & 8), lane >> 4);
+    const uint32_t lane_v1 = Q8 ? (D == 128 ? at(key_of(2 * t4 + 1), g) : at(key_of(2 * t4 + 1), g >> 1) + (g & 1) * 8) : 0u;
+    const uint32_t lane_s = key_of(g) * 4, c128 = widen_const();
 
     float o[NR][MT][4];
 #pragma unroll
@@ -374,9 +284,9 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
 #pragma unroll
         for (int i = 0; i < MT; ++i) { o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f; }
     }
-    float m_used[NR][2], l[NR][2], om[NR][2][2]; // om, 4 bits: weighted sums of the halves' smallest values, this lane's keys
+    float m_used[NR][2], l[NR][2];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) { m_used[n][0] = m_used[n][1] = -INFINITY; l[n][0] = l[n][1] = om[n][0][0] = om[n][0][1] = om[n][1][0] = om[n][1][1] = 0.f; }
+    for (int n = 0; n < NR; ++n) { m_used[n][0] = m_used[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f; }
     bool dirty = false; // a NaN or infinity of V was taken out of a block that not every row sees
     bool ok = true;
     int stage = 0, phase = 0;
@@ -389,63 +299,12 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
             __syncwarp();
         }
-        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 32 * C::PB;
+        const uint32_t sK = ring + stage * 2 * C::TILE, sV = sK + C::TILE, sS = ring_sc + stage * 128;
         const int t0 = block_of(mine(it)) * BK16;
         float s[NR][4], ks[2], vs[2]; // rows g and g + 8
-        float v_unit[2], v_scale[2][2], v_min[2][2]; // 4 bits: 2^-exponent; scales in units of 2^exponent and smallest values [row][half]
 #pragma unroll
         for (int n = 0; n < NR; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-        if constexpr (Q4) {
-            // q . k = sum over the halves of s (q . codes) + m sum q, in float32 from the codes' exact products on.  The score of a key gets the
-            // exponent e of its V row: weights 2^(score + e - max), with which the V scales are products of numbers up to 1 whatever the
-            // scales are, are float16's; the same over 2^e is the key's weight in the softmax.
-            float acc[2][NR][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int n = 0; n < NR; ++n) acc[h][n][0] = acc[h][n][1] = acc[h][n][2] = acc[h][n][3] = 0.f;
-            uint32_t w0[D / 32], w1[D / 32];
-            if (D == 128) {
-                const uint4 u0 = lds128(sK + lane_k), u1 = lds128(sK + lane_k + 8 * C::TR);
-                w0[0] = u0.x; w0[1] = u0.y; w0[2 % (D / 32)] = u0.z; w0[3 % (D / 32)] = u0.w;
-                w1[0] = u1.x; w1[1] = u1.y; w1[2 % (D / 32)] = u1.z; w1[3 % (D / 32)] = u1.w;
-            } else {
-                const uint2 u0 = lds64(sK + lane_k), u1 = lds64(sK + lane_k + 8 * C::TR);
-                w0[0] = u0.x; w0[1] = u0.y; w1[0] = u1.x; w1[1] = u1.y;
-            }
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const uint32_t y0 = w0[i] >> 8, y1 = w1[i] >> 8;
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    mma16816<true>(acc[0][n], low_codes(w0[i]), low_codes(w1[i]), low_codes(y0), low_codes(y1), qf[n][i][0], qf[n][i][1]);
-                    mma16816<true>(acc[1][n], high_codes(w0[i]), high_codes(w1[i]), high_codes(y0), high_codes(y1), qf[n][D / 32 + i][0], qf[n][D / 32 + i][1]);
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) { // rows
-                const uint2 kp = lds64(sS + lane_s + h * 64), vp = lds64(sS + lane_s + 128 + h * 64);
-                const float s0 = kv4_scale(kp.x) * LOW_UNIT, s1 = kv4_scale(kp.y) * HIGH_UNIT, m0 = kv4_min(kp.x), m1 = kv4_min(kp.y);
-                bool bad;
-                const int ex = row_exponent(vp, bad);
-                v_unit[h] = __uint_as_float((uint32_t)(254 - ex) << 23);
-                v_scale[h][0] = kv4_scale(vp.x) * v_unit[h];
-                v_scale[h][1] = kv4_scale(vp.y) * v_unit[h];
-                v_min[h][0] = kv4_min(vp.x);
-                v_min[h][1] = kv4_min(vp.y);
-                const float ev = bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ex) - (8388608.f + 127.f); // 2^23 + ex
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float x = fmaf(m1, qsum[n][e][1], m0 * qsum[n][e][0]);
-                        x = fmaf(s1, acc[1][n][2 * h + e], fmaf(s0, acc[0][n][2 * h + e], x));
-                        x = fmaf(x, 0.f, x); // an infinity stands for a row that is not finite: NaN
-                        s[n][2 * h + e] = fmaf(x, qs[n][e], ev);
-                    }
-                }
-            }
-        } else if (!Q8) {
+        if (!Q8) {
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
                 const uint32_t p = ((sK + lane_k) ^ ((m & 1) << 6)) + (m >> 1) * (BK16 * 128);
@@ -497,7 +356,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                mx[n][e] = Q4 ? m : m * qs[n][e];
+                mx[n][e] = m * qs[n][e];
                 grow |= mx[n][e] > m_used[n][e] + 8.f; // first keys of a row included (-inf)
             }
         }
@@ -511,60 +370,39 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                     f[e] = m_used[n][e] == -INFINITY ? 0.f : ex2(m_used[n][e] - nm);
                     m_used[n][e] = nm;
                     l[n][e] *= f[e];
-                    if (Q4) { om[n][e][0] *= f[e]; om[n][e][1] *= f[e]; }
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
             }
         }
-        uint32_t pf[NR][2], pl[NR][2]; // pl: what rounding left (int8), the second half's weights (4 bits)
+        uint32_t pf[NR][2], pl[NR][2]; // pl: what rounding left, int8
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             float p[4];
-            if constexpr (Q4) {
-                float p1[4]; // weights times the scales of either half
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int h = e >> 1, c = e & 1;
-                    const bool seen = all_seen || s[n][e] != -INFINITY;
-                    const float x = ex2(s[n][e] - (m_used[n][c] == -INFINITY ? 0.f : m_used[n][c])), w = x * v_unit[h];
-                    l[n][c] += w;
-                    // 0 times the parameters of an unseen key, which may be anything
-                    om[n][c][0] = fmaf(w, seen ? v_min[h][0] : 0.f, om[n][c][0]);
-                    om[n][c][1] = fmaf(w, seen ? v_min[h][1] : 0.f, om[n][c][1]);
-                    p[e] = seen ? x * v_scale[h][0] : 0.f;
-                    p1[e] = seen ? x * v_scale[h][1] : 0.f;
-                }
-                pf[n][0] = transpose8x8(pack_half(p[0], p[1]));
-                pf[n][1] = transpose8x8(pack_half(p[2], p[3]));
-                pl[n][0] = transpose8x8(pack_half(p1[0], p1[1]));
-                pl[n][1] = transpose8x8(pack_half(p1[2], p1[3]));
-            } else {
+            for (int e = 0; e < 4; ++e) {
+                const float mb = m_used[n][e & 1] == -INFINITY ? 0.f : m_used[n][e & 1];
+                p[e] = ex2(fmaf(s[n][e], qs[n][e & 1], -mb));
+                l[n][e & 1] += p[e];
+                if (Q8) p[e] *= vs[e >> 1];
+            }
+            if (Q8 && !all_seen) { // 0 times the scale of a masked key, which may be anything
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float mb = m_used[n][e & 1] == -INFINITY ? 0.f : m_used[n][e & 1];
-                    p[e] = ex2(fmaf(s[n][e], qs[n][e & 1], -mb));
-                    l[n][e & 1] += p[e];
-                    if (Q8) p[e] *= vs[e >> 1];
-                }
-                if (Q8 && !all_seen) { // 0 times the scale of a masked key, which may be anything
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (s[n][e] == -INFINITY) p[e] = 0.f;
-                }
-                pf[n][0] = transpose8x8(pack(p[0], p[1]));
-                pf[n][1] = transpose8x8(pack(p[2], p[3]));
-                if (FMT == KV_INT8) {
-                    auto left = [](float lo, float hi) { // lo, hi minus their bf16s
-                        const uint32_t w = pack(lo, hi);
-                        return pack(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xffff0000u));
-                    };
-                    pl[n][0] = transpose8x8(left(p[0], p[1]));
-                    pl[n][1] = transpose8x8(left(p[2], p[3]));
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (s[n][e] == -INFINITY) p[e] = 0.f;
+            }
+            pf[n][0] = transpose8x8(pack(p[0], p[1]));
+            pf[n][1] = transpose8x8(pack(p[2], p[3]));
+            if (FMT == KV_INT8) {
+                auto left = [](float lo, float hi) { // lo, hi minus their bf16s
+                    const uint32_t w = pack(lo, hi);
+                    return pack(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xffff0000u));
+                };
+                pl[n][0] = transpose8x8(left(p[0], p[1]));
+                pl[n][1] = transpose8x8(left(p[2], p[3]));
             }
         }
-        if constexpr (FMT == KV_BF16) {
+        if constexpr (!Q8) {
             if (!all_seen) {
                 // 0 * NaN would reach rows that do not see the key: take non-finite values out here, give them back at the end
 #pragma unroll
@@ -589,32 +427,6 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 ldsm4t(vf, ((sV + lane_v0) ^ ((i & 3) << 5)) + (i >> 2) * (BK16 * 128));
 #pragma unroll
                 for (int n = 0; n < NR; ++n) mma16816<false>(o[n][i], vf[0], vf[2], vf[1], vf[3], pf[n][0], pf[n][1]);
-            }
-        } else if constexpr (Q4) {
-            constexpr int W = D / 64; // words per key and lane: bytes g * D / 16 .., hence dims from there on in either half
-            uint32_t v[4][W];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t p = sV + (q & 1 ? lane_v1 : lane_v0) + (q >> 1) * 8 * C::TR;
-                if (W == 2) {
-                    const uint2 u = lds64(p);
-                    v[q][0] = u.x; v[q][W - 1] = u.y;
-                } else
-                    v[q][0] = lds32(p);
-            }
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    // bytes (k0.2i, k0.2i+1, k1.2i, k1.2i+1)
-                    const uint32_t x0 = __byte_perm(v[0][w], v[1][w], i ? 0x7632 : 0x5410), x1 = __byte_perm(v[2][w], v[3][w], i ? 0x7632 : 0x5410);
-                    const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) {
-                        mma16816<true>(o[n][2 * w + i], low_codes(x0), low_codes(y0), low_codes(x1), low_codes(y1), pf[n][0], pf[n][1]);
-                        mma16816<true>(o[n][MT / 2 + 2 * w + i], high_codes(x0), high_codes(y0), high_codes(x1), high_codes(y1), pl[n][0], pl[n][1]);
-                    }
-                }
             }
         } else {
             constexpr int W = D / 32; // words per key and lane: dims g * D / 8 ..
@@ -673,19 +485,10 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 4);
             l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 8);
             l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 16);
-            if (Q4) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    om[n][e][h] += __shfl_xor_sync(0xffffffffu, om[n][e][h], 4);
-                    om[n][e][h] += __shfl_xor_sync(0xffffffffu, om[n][e][h], 8);
-                    om[n][e][h] += __shfl_xor_sync(0xffffffffu, om[n][e][h], 16);
-                }
-            }
         }
     }
     const int any_dirty = __syncthreads_or(dirty);
     float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
-    float *pml = (float *)(gen + C::off_pml(ST));
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
@@ -695,122 +498,30 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
                 float *dst = mo + (warp * 16 + r) * (D + 2);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    if (Q4) { // MMA row g: dim g D/16 + 2j of the half, row g + 8: + 1
-                        const int h = i / (MT / 2), j = i % (MT / 2);
-                        const float unit = h ? HIGH_UNIT : LOW_UNIT, low = om[n][e][h];
-                        *(float2 *)(dst + h * (D / 2) + g * (D / 16) + 2 * j) = make_float2(fmaf(o[n][i][e], unit, low), fmaf(o[n][i][2 + e], unit, low));
-                    } else if (!Q8) { dst[16 * i + g] = o[n][i][e]; dst[16 * i + 8 + g] = o[n][i][2 + e]; }
+                    if (!Q8) { dst[16 * i + g] = o[n][i][e]; dst[16 * i + 8 + g] = o[n][i][2 + e]; }
                     else *(float2 *)(dst + g * (D / 8) + 2 * i) = make_float2(o[n][i][e], o[n][i][2 + e]); // MMA row g: dims g D/8 + 2i, row g + 8: + 1
                 }
                 if (g == 0) { ml[(warp * 16 + r) * 2] = m_used[n][e]; ml[(warp * 16 + r) * 2 + 1] = l[n][e]; }
             }
         }
     }
-    __syncthreads();
-    // per row: the warps' weights relative to the block's maximum, its maximum and sum, where the row goes
-    const bool clustered = a.splits > 1 && !a.part_o;
-    const long plane = (long)a.rb.n_tokens * a.nq;
-    float *wt = pml + 32;                // [16][RW]
-    long *dst_of = (long *)(wt + 16 * RW); // [16]
-    float *cw = (float *)(dst_of + 16);    // [16][ranges of a cluster]
-    if (threadIdx.x < rows) {
-        const int r = threadIdx.x, i = r / a.group, head = kvh * a.group + r - i * a.group;
-        float m = -INFINITY, den = 0.f;
-#pragma unroll
-        for (int w = 0; w < RW; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
-#pragma unroll
-        for (int w = 0; w < RW; ++w) {
-            const float mw = ml[(w * 16 + r) * 2], f = mw == -INFINITY ? 0.f : ex2(mw - m);
-            wt[r * RW + w] = f;
-            den = fmaf(ml[(w * 16 + r) * 2 + 1], f, den);
-        }
-        if (den != den) m = fmaxf(m, 0.f); // scores that are all NaN leave no maximum: not an empty range
-        pml[2 * r] = m;
-        pml[2 * r + 1] = den;
-        dst_of[r] = a.part_o ? (long)split * plane + (long)(row0 + i) * a.nq + head : (long)(row0 + i) * a.o_stride + (long)head * D;
-    }
-    __syncthreads();
-#pragma unroll 4
-    for (int idx = threadIdx.x; idx < rows * (D / 2); idx += R_THREADS) {
-        const int r = idx / (D / 2), c = idx % (D / 2) * 2;
-        float x = 0.f, y = 0.f;
-#pragma unroll
-        for (int w = 0; w < RW; ++w) {
-            const float f = wt[r * RW + w];
-            const float2 v = *(const float2 *)(mo + (w * 16 + r) * (D + 2) + c);
-            x = fmaf(v.x, f, x);
-            y = fmaf(v.y, f, y);
-        }
-        if (FMT == KV_BF16 && any_dirty) { // the values taken out above, for the rows that see them
-            const int p = len + r / a.group;
-            for (int j = j_begin; j < j_end; ++j) {
-                const int t0 = block_of(j) * BK16;
-                for (int t = t0; t < t0 + BK16 && !seen_by_all(t0); ++t) {
-                    if (!sees(t, p, a.window, a.sinks)) continue;
-                    const long row = lookup(t);
-                    if (row < 0) continue;
-                    const __nv_bfloat162 v = *(const __nv_bfloat162 *)((const bf16 *)a.kv.v + row * D + c);
-                    const float vx = __bfloat162float(v.x), vy = __bfloat162float(v.y);
-                    if (!isfinite(vx)) x += vx;
-                    if (!isfinite(vy)) y += vy;
-                }
+    auto give_back = [&](int r, int c, float &x, float &y) { // the values taken out above, for the rows that see them
+        if (Q8 || !any_dirty) return;
+        const int p = len + r / a.group;
+        for (int j = j_begin; j < j_end; ++j) {
+            const int t0 = block_of(j) * BK16;
+            for (int t = t0; t < t0 + BK16 && !seen_by_all(t0); ++t) {
+                if (!sees(t, p, a.window, a.sinks)) continue;
+                const long row = lookup(t);
+                if (row < 0) continue;
+                const __nv_bfloat162 v = *(const __nv_bfloat162 *)((const bf16 *)a.kv.v + row * D + c);
+                const float vx = __bfloat162float(v.x), vy = __bfloat162float(v.y);
+                if (!isfinite(vx)) x += vx;
+                if (!isfinite(vy)) y += vy;
             }
         }
-        if (a.splits == 1) {
-            const float inv = inverse_sum(pml[2 * r + 1]);
-            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x * inv, y * inv);
-        } else if (clustered) // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
-            *(float2 *)(mo + r * (D + 2) + c) = make_float2(x, y);
-        else {
-            const float m = pml[2 * r];
-            if (m != -INFINITY) *(float2 *)(a.part_o + dst_of[r] * D + c) = make_float2(x, y);
-            if (c == 0) *(float2 *)(a.part_ml + dst_of[r] * 2) = make_float2(m, pml[2 * r + 1]);
-        }
-    }
-    if (clustered) {
-        tc::cluster_sync();
-        const uint32_t mo_addr = base, pml_addr = base + C::off_pml(ST);
-        auto peer2 = [](uint32_t addr, int rank) {
-            float2 v;
-            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(tc::mapa_shared(addr, rank)) : "memory");
-            return v;
-        };
-        // per row: the ranges' weights, with the sum's reciprocal in them (over the warps' weights, which have been used)
-        if (threadIdx.x < rows) {
-            const int r = threadIdx.x;
-            float2 q[PAGED_MAX_CLUSTER];
-            float m = -INFINITY, den = 0.f;
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) q[s] = s < splits ? peer2(pml_addr + 8 * r, s) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) m = fmaxf(m, q[s].x);
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) {
-                q[s].x = q[s].x == -INFINITY ? 0.f : ex2(q[s].x - m);
-                den = fmaf(q[s].y, q[s].x, den);
-            }
-            const float inv = inverse_sum(den);
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s)
-                if (s < splits) cw[r * PAGED_MAX_CLUSTER + s] = q[s].x * inv;
-        }
-        __syncthreads();
-        for (int idx = split + a.splits * (int)threadIdx.x; idx < rows * (D / 2); idx += a.splits * R_THREADS) {
-            const int r = idx / (D / 2), c = idx % (D / 2) * 2;
-            float2 v[PAGED_MAX_CLUSTER];
-            float x = 0.f, y = 0.f;
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) v[s] = s < splits ? peer2(mo_addr + (r * (D + 2) + c) * 4, s) : make_float2(0.f, 0.f);
-#pragma unroll
-            for (int s = 0; s < PAGED_MAX_CLUSTER; ++s) {
-                const float f = s < splits ? cw[r * PAGED_MAX_CLUSTER + s] : 0.f;
-                x = fmaf(v[s].x, f, x);
-                y = fmaf(v[s].y, f, y);
-            }
-            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x, y);
-        }
-        tc::cluster_sync(); // no block exits while a peer still reads its shared memory
-    }
+    };
+    join_rows<D, RW>(a, gen, C::off_pml(ST), rows, row0, len, kvh, split, splits, give_back);
     if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
@@ -897,9 +608,9 @@ template <int FMT, int D, int NR> cudaError_t rows_by_copy(const PagedAttnArgs &
     // 16-key blocks as TMA boxes: they lie in one page, row numbers fit a coordinate, scales start on 16 bytes
     TcMap km{}, vm{};
     const long rows = (long)a.kv.n_pages * a.kv.nkv * a.kv.page;
-    const int es = FMT == KV_BF16 ? 2 : 1, cols = FMT == KV_INT4 ? D / 2 : D;
+    const int es = FMT == KV_BF16 ? 2 : 1;
     if (a.kv.page % BK16 == 0 && rows <= 0x7fffffffL && !(((uintptr_t)a.kv.ks | (uintptr_t)a.kv.vs) & 15) &&
-        make_cache_map(&km, a.kv.k, rows, cols, es) == 0 && make_cache_map(&vm, a.kv.v, rows, cols, es) == 0) {
+        make_cache_map(&km, a.kv.k, rows, D, es) == 0 && make_cache_map(&vm, a.kv.v, rows, D, es) == 0) {
         if ((long)a.kv.nkv * a.rb.B * a.splits <= sm_count()) return launch_rows<FMT, D, NR, 8, true>(a, km, vm, st);
         return launch_rows<FMT, D, NR, 4, true>(a, km, vm, st);
     }
@@ -924,7 +635,6 @@ cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st)
     case KV_BF16: return rows_by_dim<KV_BF16>(a, st);
     case KV_E4M3: return rows_by_dim<KV_E4M3>(a, st);
     case KV_INT8: return rows_by_dim<KV_INT8>(a, st);
-    case KV_INT4: return rows_by_dim<KV_INT4>(a, st);
     default: return cudaErrorInvalidValue;
     }
 }
