@@ -106,6 +106,27 @@ template <> __device__ __forceinline__ uint32_t odd2<KV_E4M3>(uint32_t w, uint32
 template <> __device__ __forceinline__ uint32_t even2<KV_INT8>(uint32_t w, uint32_t c128) { return int8_fix(w, c128); }
 template <> __device__ __forceinline__ uint32_t odd2<KV_INT8>(uint32_t w, uint32_t c128) { return int8_fix(w >> 8, c128); }
 
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(unsigned long long *)&d)
+        : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b), "l"(*(const unsigned long long *)&c));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
+    return d;
+}
+
 // What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
 __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
 {
@@ -154,7 +175,11 @@ constexpr int PAGED_MAX_CONTEXT = 1 << 30;
 // bf16 queries, head_dim 64 or 128, few rows (new tokens x query heads per KV head) per sequence and KV head
 constexpr int PAGED_MAX_FEW_ROWS = 16;
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
-cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, cudaStream_t st); // the same over 4-bit pages
+// The same over 4-bit pages.  stream: all sequences' keys dealt out evenly to the warps that fit the GPU, through part_o (stream4_workspace bytes).
+cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, bool stream, cudaStream_t st);
+constexpr int STREAM_MAX_B = 512; // sequences of such a call: every block sums up their lengths
+int stream4_workers(int groups_of_8_rows);
+size_t stream4_workspace(int rows, int head_dim);
 // bf16 queries, head_dim 64 or 128, any number of rows
 cudaError_t launch_paged_attention_tc(const PagedAttnArgs &a, cudaStream_t st);
 // Chooses a kernel and launches it (and the merge).  part_o / part_ml: room for `part_splits` ranges of partial rows, or null and 0;

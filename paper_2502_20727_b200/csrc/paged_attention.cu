@@ -283,7 +283,7 @@ cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, c
 
 namespace {
 
-enum AttnKernel { ATTN_GENERAL, ATTN_ROWS, ATTN_TC };
+enum AttnKernel { ATTN_GENERAL, ATTN_ROWS, ATTN_STREAM, ATTN_TC };
 struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; int row_tile; };
 
 // Which kernel serves a call, and into how many ranges the keys of its row tiles are cut.
@@ -302,6 +302,11 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
         if (s > (keys + 127) / 128) s = (keys + 127) / 128;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    } else if (fmt == KV_INT4 && rows <= PAGED_MAX_FEW_ROWS && (long)B * nkv * (keys / 32) >= 16L * stream4_workers(rows <= 8 ? 1 : 2) && B <= STREAM_MAX_B &&
+               (long)B * nkv * ((keys + max_new) / 32 + 4) < (1L << 30)) { // steps of 32 keys: numbers of 32 bits
+        p.kernel = ATTN_STREAM;
+        p.workspace = stream4_workspace((int)rows, d);
+        return p;
     } else if (rows <= PAGED_MAX_FEW_ROWS) {
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
@@ -336,6 +341,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
 cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, cudaStream_t st)
 {
     AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, q_bf16, a.nq, a.rb.B, a.rb.n_tokens, a.max_new, a.max_context, a.window, a.sinks);
+    if (p.kernel == ATTN_STREAM && !part_splits) p = AttnPlan{ATTN_ROWS, 1, 0, 0}; // no workspace
     if (p.workspace && p.splits > part_splits) {
         const int own = p.kernel == ATTN_ROWS ? PAGED_MAX_CLUSTER : 1; // ranges that need no workspace
         p.splits = part_splits > own ? part_splits : own;
@@ -347,7 +353,8 @@ cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, c
     cudaError_t e = cudaSuccess;
     switch (p.kernel) {
     case ATTN_GENERAL: e = launch_paged_attention_general(a, q_bf16, st); break;
-    case ATTN_ROWS: e = a.kv.fmt == KV_INT4 ? launch_paged_attention_rows4(a, st) : launch_paged_attention_rows(a, st); break;
+    case ATTN_ROWS: e = a.kv.fmt == KV_INT4 ? launch_paged_attention_rows4(a, false, st) : launch_paged_attention_rows(a, st); break;
+    case ATTN_STREAM: return launch_paged_attention_rows4(a, true, st);
     case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
     }
     if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, q_bf16, st);

@@ -76,10 +76,6 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v)
 {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
 // Two K codes of a word -> float16x2.  int8: codes with the sign bit flipped (code + 128), bytes 0, 1 or (SECOND) 2, 3, under the
 // exponent of 1024, minus 1152.  e4m3: bytes 0, 2 or 1, 3, sign, exponent and mantissa moved to float16's places: the value
 // times E4M3_UNIT = 2^-8, exactly (64 sequences of ragged lengths: 33.3 us, with a conversion instruction per pair 34.1).

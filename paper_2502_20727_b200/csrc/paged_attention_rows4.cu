@@ -16,6 +16,8 @@
 // Measured, 32 sequences of 9 to 16 thousand tokens, 64 heads on 8: 190 us with 16 keys a step by TMA; REPLACED.
 #include "paged_rows.cuh"
 
+#include <type_traits>
+
 namespace spd {
 
 namespace {
@@ -24,13 +26,16 @@ using namespace few;
 
 constexpr int STEP = 32; // keys a warp takes at a time
 
-template <int D, int RW> struct Rows4Cfg {
+template <int D> struct Step4 {
     static constexpr int RB = D / 2, TILE = STEP * RB;                      // bytes of a row; of K or V of a step
     static constexpr int STAGE = 2 * TILE + 2 * STEP * 8;                   // tiles and parameters
+    static constexpr int FACTORS = STEP * 80;                               // a step's factors, each twice: a pair of columns is one operand
+};
+// Thread blocks of RW warps for one (sequence, KV head) and key range
+template <int D, int RW> struct Rows4Cfg : Step4<D> {
     static constexpr int STAGES = RW == 8 ? 4 : D == 128 ? 2 : 4;
-    static constexpr int FACTORS = STEP * 40;                               // a step's factors: K float4, V float4, (exponent, unit)
-    static constexpr int RING = RW * STAGES * STAGE, MERGE = RW * 16 * (D + 4) * 4;
-    static constexpr int OFF_FACTORS = RING > MERGE ? RING : MERGE, OFF_JOIN = OFF_FACTORS + RW * FACTORS;
+    static constexpr int RING = RW * STAGES * Step4<D>::STAGE, MERGE = RW * 16 * (D + 4) * 4;
+    static constexpr int OFF_FACTORS = RING > MERGE ? RING : MERGE, OFF_JOIN = OFF_FACTORS + RW * Step4<D>::FACTORS;
     static constexpr int SMEM = OFF_JOIN + join_bytes(RW) + 128;            // + alignment slack
 };
 
@@ -39,24 +44,15 @@ __device__ __forceinline__ void cp8(uint32_t dst, const void *src, bool valid)
     const int n = valid ? 8 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
+struct Pairs { float2 a, b; };
+__device__ __forceinline__ Pairs lds_pairs(uint32_t p)
 {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
+    const uint4 u = lds128(p);
+    return Pairs{make_float2(__uint_as_float(u.x), __uint_as_float(u.y)), make_float2(__uint_as_float(u.z), __uint_as_float(u.w))};
 }
-__device__ __forceinline__ float4 lds_f4(uint32_t a)
+__device__ __forceinline__ void sts_f4(uint32_t p, float x, float y) // x, x, y, y
 {
-    const uint4 u = lds128(a);
-    return make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
-}
-__device__ __forceinline__ void sts_f4(uint32_t a, float x, float y, float z, float w)
-{
-    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
-}
-__device__ __forceinline__ void sts_f2(uint32_t a, float x, float y)
-{
-    asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(a), "f"(x), "f"(y) : "memory");
+    asm volatile("st.shared.v4.f32 [%0], {%1,%1,%2,%2};" ::"r"(p), "f"(x), "f"(y) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
 {
@@ -68,95 +64,131 @@ __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
 constexpr float LOW_UNIT = 0x1p24f, HIGH_UNIT = 0x1p20f;
 
-// NR: groups of 8 query rows.  PAGE16: 16 keys lie in one page.
-template <int D, int NR, int RW, bool PAGE16>
-__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
-{
-    using C = Rows4Cfg<D, RW>;
-    constexpr int MT = D / 16, ST = C::STAGES, RB = C::RB, W = D / 32; // W: words of a lane per row
-    extern __shared__ uint8_t rows4_raw[];
-    uint8_t *gen = rows4_raw + ((128u - (tc::smem_u32(rows4_raw) & 127u)) & 127u);
-    const uint32_t base = tc::smem_u32(gen);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = base + warp * ST * C::STAGE, fk = base + C::OFF_FACTORS + warp * C::FACTORS, fv = fk + STEP * 16, fe = fv + STEP * 16;
-    if (threadIdx.x == 0) stamp_entry(a.stamp);
-    pdl_launch_dependents();
-    pdl_wait();
-    const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
-    int row0, n_new, len;
-    if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return; // the same for a whole cluster
-    const int rows = n_new * a.group; // <= 8 NR
-    const int kv_len = len + n_new, pos_max = kv_len - 1;
-    // steps of 32 keys that hold a key some row sees: sinks, then the window of the first query onwards
-    const int lo_min = a.window ? max(0, len - a.window + 1) : 0, first = lo_min / STEP;
-    const int n_sink = min((min(a.sinks, lo_min) + STEP - 1) / STEP, first);
-    const int n_steps = n_sink + (kv_len + STEP - 1) / STEP - first;
-    // short sequences are cut into fewer ranges, of at least 4 steps
-    const int splits = min(a.splits, (n_steps + 3) / 4);
-    const int per = splits > 1 ? n_steps / splits : n_steps, extra = n_steps - per * splits; // the first `extra` ranges get one more
-    const int j_begin = split < splits ? split * per + min(split, extra) : 0;
-    const int j_end = split < splits ? j_begin + per + (split < extra ? 1 : 0) : 0;
-    const int n_mine = (j_end - j_begin - warp + RW - 1) / RW; // steps j_begin + warp, + RW, ...
+// What a warp has of NR groups of 8 query rows: sums over its keys of weights times codes (tiles 0 .. MT / 2 - 1: first half of the head, in units of
+// 2^-24; the others 2^-20), of weights times smallest values, of weights; the maxima they are relative to.
+template <int D, int NR> struct Partial {
+    float o[NR][D / 16][4];
+    float2 m_used[NR], l[NR], om[NR][2]; // of this lane's columns 2 t4 and 2 t4 + 1
+};
 
-    const int32_t *bt = a.rb.table + (long)b * a.rb.max_pages;
-    const int bpp = a.kv.page / 16; // PAGE16: blocks of 16 keys per page
-    auto key0 = [&](int i) { const int j = j_begin + warp + i * RW; return (j < n_sink ? j : first + (j - n_sink)) * STEP; };
+// The query rows of a (sequence, KV head) and the keys they see
+struct Rows {
+    int b, kvh, row0, rows, len, kv_len;
+    int lo_min, first, n_sink, n_steps; // steps of 32 keys that hold a key some row sees: sinks, then the window of the first query onwards
+    __device__ __forceinline__ void keys(const PagedAttnArgs &a, int n_new)
+    {
+        rows = n_new * a.group;
+        kv_len = len + n_new;
+        lo_min = a.window ? max(0, len - a.window + 1) : 0;
+        first = lo_min / STEP;
+        n_sink = min((min(a.sinks, lo_min) + STEP - 1) / STEP, first);
+        n_steps = n_sink + (kv_len + STEP - 1) / STEP - first;
+    }
+};
+
+// One warp: steps j0, j0 + stride, ..., n_mine of them.  ring: its ST stages, fk: its factors' place.
+// PAGES: page sizes 16, 32, 64, ... with less than 2^31 bytes of codes per page; else any.
+template <int D, int NR, int ST, bool PAGES>
+__device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int j0, int n_mine, int stride, uint32_t ring, uint32_t fk, Partial<D, NR> &acc_out)
+{
+    using C = Step4<D>;
+    constexpr int MT = D / 16, RB = C::RB, W = D / 32; // W: words of a lane per row
+    const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    constexpr uint32_t F = STEP * 16; // factors: K scales, K smallest values, V scales, V smallest values, (exponent, unit)
+    const int rows = q.rows, row0 = q.row0, len = q.len, kv_len = q.kv_len, kvh = q.kvh, pos_max = kv_len - 1, lo_min = q.lo_min;
+    const int32_t *bt = a.rb.table + (long)q.b * a.rb.max_pages;
+    const int gap = q.first - q.n_sink;
+    auto key0 = [&](int i) { const int j = j0 + i * stride; return (j + (j < q.n_sink ? 0 : gap)) * STEP; };
+    // steps that may hold keys which no row sees
+    auto edge = [&](int i) { const int j = j0 + i * stride; return j == q.n_steps - 1 || (unsigned)(j - q.n_sink + 1) < 2u; };
     // every row sees every key of the 32 from t0 on
     auto seen_by_all = [&](int t0) { return t0 + STEP - 1 <= len && (!a.window || t0 > pos_max - a.window || t0 + STEP - 1 < a.sinks); };
-    auto row_in = [&](int page, int in_page) -> long {
-        if (page < 0 || page >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); return -1; }
-        return ((long)page * a.kv.nkv + kvh) * a.kv.page + in_page;
-    };
-    // PAGE16: cached rows of the step's keys 0 and 16; else (the first only) of this lane's key.  -1: no row needs them, or a bad page id.
-    struct Where { long r[2]; };
-    auto lookup = [&](int i) {
-        Where w{{-1, -1}};
-        const int t0 = key0(i);
-        if (PAGE16) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t = t0 + 16 * h, blk = t >> 4;
-                if (t < kv_len && (t + 15 >= lo_min || t < a.sinks)) w.r[h] = bpp == 1 ? row_in(bt[blk], 0) : row_in(bt[blk / bpp], blk % bpp * 16);
-            }
-        } else {
-            const int t = t0 + lane;
-            if (t < kv_len && (t >= lo_min || t < a.sinks)) w.r[0] = row_in(bt[t / a.kv.page], t % a.kv.page);
-        }
-        return w;
-    };
     // 16-byte chunk c of row r of a tile
     auto at = [&](int r, int c) -> uint32_t { return RB == 64 ? r * 64 + ((c ^ ((r >> 1) & 3)) << 4) : r * 32 + ((c ^ ((r >> 2) & 1)) << 4); };
     constexpr int CPR = RB / 16, RPI = 32 / CPR; // chunks per row, rows per copy instruction
     const uint32_t lane_dst = at(lane / CPR, lane % CPR);
-    auto load = [&](int stage, const Where &w) {
-        const uint32_t dst = ring + stage * C::STAGE;
+    // PAGES: ids of the pages of keys 0 and 16 of a step, asked for a step ahead (nothing looks at them before the copies); else the id of this
+    // lane's key's page.
+    struct Ids { int p[2]; };
+    const int lg = __ffs(a.kv.page) - 1;
+    auto needed = [&](int t, int n) { return t < kv_len && (t + n - 1 >= lo_min || t < a.sinks); }; // one of the keys t .. t + n - 1 is seen
+    auto ask = [&](int i) {
+        Ids w{{0, 0}};
+        const int t0 = key0(i);
+        if (PAGES) {
+            const bool some = edge(i);
+            if (!some || needed(t0, 16)) w.p[0] = bt[t0 >> lg];
+            if (!some || needed(t0 + 16, 16)) w.p[1] = bt[(t0 + 16) >> lg];
+        } else if (needed(t0 + lane, 1))
+            w.p[0] = bt[(t0 + lane) / a.kv.page];
+        return w;
+    };
+    // this lane's first chunk and parameters in page 0
+    const int in_row = PAGES ? lane / CPR % 16 : 0;
+    const uint8_t *k0 = (const uint8_t *)a.kv.k + ((long)kvh * a.kv.page + in_row) * RB + lane % CPR * 16;
+    const uint8_t *v0 = (const uint8_t *)a.kv.v + ((long)kvh * a.kv.page + in_row) * RB + lane % CPR * 16;
+    const uint2 *kp0 = (const uint2 *)a.kv.ks + (long)kvh * a.kv.page + (PAGES ? lane & 15 : 0), *vp0 = (const uint2 *)a.kv.vs + (long)kvh * a.kv.page + (PAGES ? lane & 15 : 0);
+    const typename std::conditional<PAGES, uint32_t, unsigned long long>::type page_rows = (unsigned long long)a.kv.nkv * a.kv.page;
+    auto load = [&](int stage, int i, const Ids &w) {
+        const uint32_t dst = ring + stage * C::STAGE + lane_dst, dst_p = ring + stage * C::STAGE + 2 * C::TILE + lane * 8;
+        const int t0 = key0(i);
+        if (PAGES) {
+            const uint32_t in0 = (uint32_t)t0 & (a.kv.page - 1), in1 = (uint32_t)(t0 + 16) & (a.kv.page - 1); // rows in the pages
+            auto copy = [&](int h, bool valid) {
+                const unsigned long long by = (unsigned long long)(uint32_t)w.p[h] * (page_rows * RB) + (h ? in1 : in0) * RB;
+                const uint8_t *k = valid ? k0 + by : k0, *v = valid ? v0 + by : v0;
 #pragma unroll
-        for (int i = 0; i < STEP / RPI; ++i) {
-            const int r = i * RPI + lane / CPR;
-            const long row = PAGE16 ? w.r[i * RPI / 16] + (r & 15) : __shfl_sync(0xffffffffu, w.r[0], r);
-            const bool valid = PAGE16 ? w.r[i * RPI / 16] >= 0 : row >= 0;
-            const long off = valid ? row * RB + (lane % CPR) * 16 : 0;
-            cp16(dst + lane_dst + i * RPI * RB, (const uint8_t *)a.kv.k + off, valid);
-            cp16(dst + C::TILE + lane_dst + i * RPI * RB, (const uint8_t *)a.kv.v + off, valid);
+                for (int c = 0; c < 16 / RPI; ++c) {
+                    cp16(dst + h * 16 * RB + c * RPI * RB, k + c * RPI * RB, valid);
+                    cp16(dst + C::TILE + h * 16 * RB + c * RPI * RB, v + c * RPI * RB, valid);
+                }
+            };
+            auto copy_params = [&](bool valid) {
+                const unsigned long long by = (unsigned long long)(uint32_t)(lane < 16 ? w.p[0] : w.p[1]) * page_rows + (lane < 16 ? in0 : in1);
+                cp8(dst_p, valid ? kp0 + by : kp0, valid);
+                cp8(dst_p + STEP * 8, valid ? vp0 + by : vp0, valid);
+            };
+            if (max((uint32_t)w.p[0], (uint32_t)w.p[1]) < (uint32_t)a.kv.n_pages && !edge(i)) {
+                copy(0, true);
+                copy(1, true);
+                copy_params(true);
+            } else {
+                bool valid[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    valid[h] = needed(t0 + 16 * h, 16);
+                    if (valid[h] && (uint32_t)w.p[h] >= (uint32_t)a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); valid[h] = false; }
+                    copy(h, valid[h]);
+                }
+                copy_params(lane < 16 ? valid[0] : valid[1]);
+            }
+        } else {
+            const int t = t0 + lane;
+            bool valid = needed(t, 1);
+            if (valid && (uint32_t)w.p[0] >= (uint32_t)a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); valid = false; }
+            const long row = valid ? (long)(w.p[0] * page_rows) + t % a.kv.page : -1; // from (page 0, this KV head, row 0)
+#pragma unroll
+            for (int k = 0; k < STEP / RPI; ++k) {
+                const long r = __shfl_sync(0xffffffffu, row, k * RPI + lane / CPR);
+                cp16(dst + k * RPI * RB, k0 + (r >= 0 ? r * RB : 0), r >= 0);
+                cp16(dst + C::TILE + k * RPI * RB, v0 + (r >= 0 ? r * RB : 0), r >= 0);
+            }
+            cp8(dst_p, kp0 + (valid ? row : 0), valid);
+            cp8(dst_p + STEP * 8, vp0 + (valid ? row : 0), valid);
         }
-        const long mine = PAGE16 ? (lane < 16 ? w.r[0] : w.r[1]) : w.r[0];
-        const bool valid = mine >= 0;
-        const long off = valid ? mine + (PAGE16 ? lane & 15 : 0) : 0;
-        cp8(dst + 2 * C::TILE + lane * 8, (const uint2 *)a.kv.ks + off, valid);
-        cp8(dst + 2 * C::TILE + STEP * 8 + lane * 8, (const uint2 *)a.kv.vs + off, valid);
     };
 
 #pragma unroll
     for (int s = 0; s < ST; ++s) {
-        if (s < n_mine) load(s, lookup(s));
+        if (s < n_mine) load(s, s, ask(s));
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    Where next{{-1, -1}};
-    if (ST < n_mine) next = lookup(ST);
+    Ids next{{0, 0}};
+    if (ST < n_mine) next = ask(ST);
 
     // Q fragments (column g of a group of 8 rows), in the order of the codes; rows beyond the last are zero.  A lane's dims: D / 8 of either half.
     uint32_t qf[NR][2 * W][2];
-    float qs[NR][2], qsum[NR][2][2]; // of this lane's columns 2 t4 and 2 t4 + 1: to base-2 units; sums of the halves in those
+    float2 qs[NR], qsum[NR][2]; // of this lane's columns 2 t4 and 2 t4 + 1: to base-2 units; sums of the halves in those
     int pos[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -200,28 +232,35 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
         for (int e = 0; e < 2; ++e) {
             const int c = 8 * n + 2 * t4 + e;
             pos[n][e] = c < rows ? len + c / a.group : -1;
-            qs[n][e] = __shfl_sync(0xffffffffu, my_qs, (2 * t4 + e) * 4);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) qsum[n][e][h] = __shfl_sync(0xffffffffu, sum[h], (2 * t4 + e) * 4) * qs[n][e];
         }
+        qs[n] = make_float2(__shfl_sync(0xffffffffu, my_qs, 2 * t4 * 4), __shfl_sync(0xffffffffu, my_qs, (2 * t4 + 1) * 4));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            qsum[n][h] = mul2(make_float2(__shfl_sync(0xffffffffu, sum[h], 2 * t4 * 4), __shfl_sync(0xffffffffu, sum[h], (2 * t4 + 1) * 4)), qs[n]);
     }
 
-    // where this lane reads in a tile; the second eight and sixteen rows are a fixed distance away
-    const uint32_t lane_k = RB == 64 ? at(key_of(g), t4) : at(key_of(g), t4 >> 1) + (t4 & 1) * 8;
-    auto v_at = [&](int r) { return RB == 64 ? at(r, g >> 1) + (g & 1) * 8 : at(r, g >> 2) + (g & 3) * 4; };
-    const uint32_t lane_v0 = v_at(key_of(2 * t4)), lane_v1 = v_at(key_of(2 * t4 + 1));
-    const int my_key = key_of(g);
+    // where this lane reads in a tile: K rows g (and 8, 16, 24 further on), the factors of these keys; V by transposing matrix loads of 8 keys x 16
+    // bytes, which give a lane bytes 2 g and 2 g + 1 of keys 2 t4 and 2 t4 + 1.
+    const uint32_t lane_k = RB == 64 ? at(g, t4) : at(g, t4 >> 1) + (t4 & 1) * 8, my_factors = fk + g * 16;
+    const uint32_t lane_v = at(lane & 15, lane >> 4); // matrices: keys 0-7 and 8-15 of chunk 0, of chunk 1
+    uint32_t shift8; // 2^24: products' high words are shifts by 8 on the FMA pipe, while masks fill the other one
+    asm volatile("mov.b32 %0, 0x1000000;" : "=r"(shift8));
 
-    float o[NR][MT][4]; // tiles 0 .. MT / 2 - 1: first half of the head, in units of 2^-24; the others 2^-20
-    float m_used[NR][2], l[NR][2], om[NR][2][2]; // om: weighted sums of the halves' smallest values, as l over this lane's keys
+    auto &o = acc_out.o;
+    auto &m_used = acc_out.m_used;
+    auto &l = acc_out.l;
+    auto &om = acc_out.om;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) { o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f; }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { m_used[n][e] = -INFINITY; l[n][e] = om[n][e][0] = om[n][e][1] = 0.f; }
+        m_used[n] = make_float2(-INFINITY, -INFINITY);
+        l[n] = om[n][0] = om[n][1] = make_float2(0.f, 0.f);
     }
 
+    float2 limit[NR], minus[NR]; // maxima beyond which the sums follow; what is added to a score
+#pragma unroll
+    for (int n = 0; n < NR; ++n) { limit[n] = make_float2(-INFINITY, -INFINITY); minus[n] = make_float2(3e38f, 3e38f); }
     int stage = 0;
     for (int it = 0; it < n_mine; ++it) {
         asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
@@ -233,24 +272,23 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
             const uint32_t km = __vmaxu2(kp.x & 0x7fff7fffu, kp.y & 0x7fff7fffu), vm = __vmaxu2(vp.x & 0x7fff7fffu, vp.y & 0x7fff7fffu);
             // a row that is not finite is a NaN for those who see its key, and nothing for the others
             const bool k_bad = ((km + 0x00800080u) & 0x80008000u) != 0;
-            sts_f4(fk + lane * 16, k_bad ? __uint_as_float(0x7fc00000u) : kv4_scale(kp.x) * LOW_UNIT, kv4_scale(kp.y) * HIGH_UNIT, kv4_min(kp.x), kv4_min(kp.y));
+            const float ks = k_bad ? __uint_as_float(0x7fc00000u) : kv4_scale(kp.x) * LOW_UNIT;
+            sts_f4(fk + lane * 16, ks, kv4_scale(kp.y) * HIGH_UNIT);
+            sts_f4(fk + F + lane * 16, kv4_min(kp.x), kv4_min(kp.y));
             const uint32_t top = max(vm & 0xffffu, vm >> 16);
             const bool v_bad = top >= 0x7f80u;
             const int ex = min(max((int)(top >> 7), 127 - 60), 127 + 30);
             const float unit = __uint_as_float((uint32_t)(254 - ex) << 23), f = v_bad ? 0.f : unit;
             const float ev = v_bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ex) - (8388608.f + 127.f); // 2^23 + ex
             const uint2 q = v_bad ? make_uint2(0, 0) : vp;
-            sts_f4(fv + lane * 16, kv4_scale(q.x) * f, kv4_scale(q.y) * f, kv4_min(q.x) * f, kv4_min(q.y) * f);
-            sts_f2(fe + lane * 8, ev, unit);
+            sts_f4(fk + 2 * F + lane * 16, kv4_scale(q.x) * f, kv4_scale(q.y) * f);
+            sts_f4(fk + 3 * F + lane * 16, kv4_min(q.x) * f, kv4_min(q.y) * f);
+            sts_f4(fk + 4 * F + lane * 16, ev, unit);
         }
-        float s[2][NR][4], unit[2][2]; // scores in base-2 units; [tile][rows g and g + 8]
+        float2 s[2][NR][2], unit[2][2]; // scores in base-2 units; [tile][rows g and g + 8]
         float acc[2][2][NR][4];        // q . codes [tile][half]
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int n = 0; n < NR; ++n) acc[u][h][n][0] = acc[u][h][n][1] = acc[u][h][n][2] = acc[u][h][n][3] = 0.f;
             const uint32_t p = sK + lane_k + u * 16 * RB;
             uint32_t w0[W], w1[W]; // rows g and g + 8
             if (W == 4) {
@@ -263,9 +301,14 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
             }
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                const uint32_t y0 = w0[i] >> 8, y1 = w1[i] >> 8;
+                const uint32_t y0 = __umulhi(w0[i], shift8), y1 = __umulhi(w1[i], shift8);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
+                    if (i == 0) {
+                        mma16816_zero(acc[u][0][n], low_codes(w0[i]), low_codes(w1[i]), low_codes(y0), low_codes(y1), qf[n][i][0], qf[n][i][1]);
+                        mma16816_zero(acc[u][1][n], high_codes(w0[i]), high_codes(w1[i]), high_codes(y0), high_codes(y1), qf[n][W + i][0], qf[n][W + i][1]);
+                        continue;
+                    }
                     mma16816<true>(acc[u][0][n], low_codes(w0[i]), low_codes(w1[i]), low_codes(y0), low_codes(y1), qf[n][i][0], qf[n][i][1]);
                     mma16816<true>(acc[u][1][n], high_codes(w0[i]), high_codes(w1[i]), high_codes(y0), high_codes(y1), qf[n][W + i][0], qf[n][W + i][1]);
                 }
@@ -276,17 +319,13 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int key = 16 * u + 8 * h + my_key;
-                const float4 k = lds_f4(fk + key * 16);
-                const uint2 eu = lds64(fe + key * 8);
-                unit[u][h] = __uint_as_float(eu.y);
+                const uint32_t p = my_factors + (16 * u + 8 * h) * 16;
+                const Pairs k = lds_pairs(p), km = lds_pairs(p + F), eu = lds_pairs(p + 4 * F);
+                unit[u][h] = eu.b;
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float shift = fmaf(k.w, qsum[n][e][1], fmaf(k.z, qsum[n][e][0], __uint_as_float(eu.x)));
-                        s[u][n][2 * h + e] = fmaf(fmaf(k.y, acc[u][1][n][2 * h + e], k.x * acc[u][0][n][2 * h + e]), qs[n][e], shift);
-                    }
+                    const float2 c0 = make_float2(acc[u][0][n][2 * h], acc[u][0][n][2 * h + 1]), c1 = make_float2(acc[u][1][n][2 * h], acc[u][1][n][2 * h + 1]);
+                    s[u][n][h] = fma2(fma2(k.b, c1, mul2(k.a, c0)), qs[n], fma2(km.b, qsum[n][1], fma2(km.a, qsum[n][0], eu.a)));
                 }
             }
         }
@@ -296,166 +335,384 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!sees(t0 + 16 * u + 8 * (e >> 1) + my_key, pos[n][e & 1], a.window, a.sinks)) s[u][n][e] = -INFINITY;
+                    for (int h = 0; h < 2; ++h) {
+                        const int t = t0 + 16 * u + 8 * h + g;
+                        if (!sees(t, pos[n][0], a.window, a.sinks)) s[u][n][h].x = -INFINITY;
+                        if (!sees(t, pos[n][1], a.window, a.sinks)) s[u][n][h].y = -INFINITY;
+                    }
         }
-        float mx[NR][2];
+        float2 mx[NR];
         bool grow = false;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float m = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
+            auto over_rows = [](float m) {
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                mx[n][e] = m;
-                grow |= m > m_used[n][e] + 8.f; // first keys of a row included (-inf)
-            }
+                return fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            };
+            mx[n].x = over_rows(fmaxf(fmaxf(s[0][n][0].x, s[0][n][1].x), fmaxf(s[1][n][0].x, s[1][n][1].x)));
+            mx[n].y = over_rows(fmaxf(fmaxf(s[0][n][0].y, s[0][n][1].y), fmaxf(s[1][n][0].y, s[1][n][1].y)));
+            grow |= mx[n].x > limit[n].x || mx[n].y > limit[n].y; // first keys of a row included (-inf)
         }
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                float f[2];
+                const float2 nm = make_float2(fmaxf(m_used[n].x, mx[n].x), fmaxf(m_used[n].y, mx[n].y));
+                const float2 f = make_float2(m_used[n].x == -INFINITY ? 0.f : ex2(m_used[n].x - nm.x), m_used[n].y == -INFINITY ? 0.f : ex2(m_used[n].y - nm.y));
+                m_used[n] = nm;
+                limit[n] = make_float2(nm.x + 8.f, nm.y + 8.f);
+                minus[n] = make_float2(fminf(-nm.x, 3e38f), fminf(-nm.y, 3e38f)); // no key seen so far: the weights are 2^-inf whatever this is
+                l[n] = mul2(l[n], f);
+                om[n][0] = mul2(om[n][0], f);
+                om[n][1] = mul2(om[n][1], f);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float nm = fmaxf(m_used[n][e], mx[n][e]);
-                    f[e] = m_used[n][e] == -INFINITY ? 0.f : ex2(m_used[n][e] - nm);
-                    m_used[n][e] = nm;
-                    l[n][e] *= f[e];
-                    om[n][e][0] *= f[e];
-                    om[n][e][1] *= f[e];
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
+                for (int i = 0; i < MT; ++i) { o[n][i][0] *= f.x; o[n][i][1] *= f.y; o[n][i][2] *= f.x; o[n][i][3] *= f.y; }
             }
         }
-        float mb[NR][2]; // no key seen so far: the weights are 2^-inf whatever this is
-#pragma unroll
-        for (int n = 0; n < NR; ++n) { mb[n][0] = fmaxf(m_used[n][0], -3e38f); mb[n][1] = fmaxf(m_used[n][1], -3e38f); }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             uint32_t pf[2][NR][2]; // [half]
-            float w[2][NR][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float4 v = lds_f4(fv + (16 * u + 8 * h + my_key) * 16);
+                const uint32_t p = my_factors + (16 * u + 8 * h) * 16;
+                const Pairs vs = lds_pairs(p + 2 * F), vm = lds_pairs(p + 3 * F);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
+                    const float2 y = add2(s[u][n][h], minus[n]), x = make_float2(ex2(y.x), ex2(y.y));
+                    l[n] = fma2(x, unit[u][h], l[n]);
+                    om[n][0] = fma2(x, vm.a, om[n][0]);
+                    om[n][1] = fma2(x, vm.b, om[n][1]);
+                    const float2 w0 = mul2(x, vs.a), w1 = mul2(x, vs.b);
+                    pf[0][n][h] = transpose8x8(pack_half(w0.x, w0.y));
+                    pf[1][n][h] = transpose8x8(pack_half(w1.x, w1.y));
+                }
+            }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x = ex2(s[u][n][2 * h + e] - mb[n][e]);
-                        l[n][e] = fmaf(x, unit[u][h], l[n][e]);
-                        om[n][e][0] = fmaf(x, v.z, om[n][e][0]);
-                        om[n][e][1] = fmaf(x, v.w, om[n][e][1]);
-                        w[0][n][2 * h + e] = x * v.x;
-                        w[1][n][2 * h + e] = x * v.y;
+            for (int c = 0; c < RB / 16; c += 2) { // 16-byte chunks: dims 16 c + 2 g and 16 c + 2 g + 1 of either half are MMA rows g and g + 8
+                uint32_t v[4];
+                ldsm4t(v, (sV + lane_v + u * 16 * RB) ^ (c << 4));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t x0 = v[2 * i], x1 = v[2 * i + 1], y0 = __umulhi(x0, shift8), y1 = __umulhi(x1, shift8);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        mma16816<true>(o[n][c + i], low_codes(x0), low_codes(y0), low_codes(x1), low_codes(y1), pf[0][n][0], pf[0][n][1]);
+                        mma16816<true>(o[n][W + c + i], high_codes(x0), high_codes(y0), high_codes(x1), high_codes(y1), pf[1][n][0], pf[1][n][1]);
                     }
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    pf[q][n][0] = transpose8x8(pack_half(w[q][n][0], w[q][n][1]));
-                    pf[q][n][1] = transpose8x8(pack_half(w[q][n][2], w[q][n][3]));
-                }
-            }
-            // bytes g D / 16 .. of four keys: dims from there on in either half
-            uint32_t v[4][W / 2];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t p = sV + (q & 1 ? lane_v1 : lane_v0) + ((q >> 1) * 8 + u * 16) * RB;
-                if (W == 4) {
-                    const uint2 x = lds64(p);
-                    v[q][0] = x.x; v[q][W / 2 - 1] = x.y;
-                } else
-                    v[q][0] = lds32(p);
-            }
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                // bytes (k0.2j, k0.2j+1, k1.2j, k1.2j+1), j = i & 1
-                const uint32_t sel = i & 1 ? 0x7632 : 0x5410;
-                const uint32_t x0 = __byte_perm(v[0][i >> 1], v[1][i >> 1], sel), x1 = __byte_perm(v[2][i >> 1], v[3][i >> 1], sel);
-                const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    mma16816<true>(o[n][i], low_codes(x0), low_codes(y0), low_codes(x1), low_codes(y1), pf[0][n][0], pf[0][n][1]);
-                    mma16816<true>(o[n][W + i], high_codes(x0), high_codes(y0), high_codes(x1), high_codes(y1), pf[1][n][0], pf[1][n][1]);
                 }
             }
         }
         __syncwarp(); // every lane has read the stage and the factors
         if (it + ST < n_mine) {
-            load(stage, next);
-            if (it + ST + 1 < n_mine) next = lookup(it + ST + 1);
+            load(stage, it + ST, next);
+            if (it + ST + 1 < n_mine) next = ask(it + ST + 1);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++stage == ST) stage = 0;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 
-    // the warps' partial rows, over the rings
+    // over the warp's lanes
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) {
-                l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], x);
-                om[n][e][0] += __shfl_xor_sync(0xffffffffu, om[n][e][0], x);
-                om[n][e][1] += __shfl_xor_sync(0xffffffffu, om[n][e][1], x);
-            }
+        for (int x = 4; x < 32; x <<= 1) {
+            auto other = [&](float2 v) { return add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, x), __shfl_xor_sync(0xffffffffu, v.y, x))); };
+            l[n] = other(l[n]);
+            om[n][0] = other(om[n][0]);
+            om[n][1] = other(om[n][1]);
         }
     }
-    __syncthreads();
+}
+
+__device__ __forceinline__ float column(float2 v, int e) { return e ? v.y : v.x; }
+
+template <int D, int NR, int RW, bool PAGES>
+__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    using C = Rows4Cfg<D, RW>;
+    constexpr int MT = D / 16, W = D / 32;
+    extern __shared__ uint8_t rows4_raw[];
+    uint8_t *gen = rows4_raw + ((128u - (tc::smem_u32(rows4_raw) & 127u)) & 127u);
+    const uint32_t base = tc::smem_u32(gen);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    if (threadIdx.x == 0) stamp_entry(a.stamp);
+    pdl_launch_dependents();
+    pdl_wait();
+    const int split = blockIdx.z;
+    Rows q;
+    int n_new;
+    q.kvh = blockIdx.x;
+    q.b = blockIdx.y;
+    if (!batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err)) return; // the same for a whole cluster
+    q.keys(a, n_new);
+    // short sequences are cut into fewer ranges, of at least 4 steps
+    const int splits = min(a.splits, (q.n_steps + 3) / 4);
+    const int per = splits > 1 ? q.n_steps / splits : q.n_steps, extra = q.n_steps - per * splits; // the first `extra` ranges get one more
+    const int j_begin = split < splits ? split * per + min(split, extra) : 0;
+    const int j_end = split < splits ? j_begin + per + (split < extra ? 1 : 0) : 0;
+    Partial<D, NR> p;
+    walk<D, NR, C::STAGES, PAGES>(a, q, j_begin + warp, (j_end - j_begin - warp + RW - 1) / RW, RW, base + warp * C::STAGES * C::STAGE,
+                                  base + C::OFF_FACTORS + warp * C::FACTORS, p);
+    __syncthreads(); // the partial rows go over the rings
     float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = 8 * n + 2 * t4 + e;
-            if (r < rows) {
-                float *dst = mo + (warp * 16 + r) * (D + 2) + g * (D / 16);
+            if (r < q.rows) {
+                float *dst = mo + (warp * 16 + r) * (D + 2) + 2 * g;
 #pragma unroll
-                for (int i = 0; i < MT; ++i) { // MMA row g: dim g D/16 + 2i of the tile's half, row g + 8: + 1
+                for (int i = 0; i < MT; ++i) { // MMA row g: dim 16 i + 2 g of the tile's half, row g + 8: + 1
                     const int h = i / W;
-                    const float x = h ? HIGH_UNIT : LOW_UNIT;
-                    *(float2 *)(dst + h * (D / 2) + 2 * (i % W)) = make_float2(fmaf(o[n][i][e], x, om[n][e][h]), fmaf(o[n][i][2 + e], x, om[n][e][h]));
+                    const float x = h ? HIGH_UNIT : LOW_UNIT, y = column(p.om[n][h], e);
+                    *(float2 *)(dst + h * (D / 2) + 16 * (i % W)) = make_float2(fmaf(p.o[n][i][e], x, y), fmaf(p.o[n][i][2 + e], x, y));
                 }
-                if (g == 0) { ml[(warp * 16 + r) * 2] = m_used[n][e]; ml[(warp * 16 + r) * 2 + 1] = l[n][e]; }
+                if (g == 0) { ml[(warp * 16 + r) * 2] = column(p.m_used[n], e); ml[(warp * 16 + r) * 2 + 1] = column(p.l[n], e); }
             }
         }
     }
-    join_rows<D, RW>(a, gen, C::OFF_JOIN, rows, row0, len, kvh, split, splits, [](int, int, float &, float &) {});
+    join_rows<D, RW>(a, gen, C::OFF_JOIN, q.rows, q.row0, q.len, q.kvh, split, splits, [](int, int, float &, float &) {});
     if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
-template <int D, int NR, int RW, bool PAGE16> cudaError_t launch_rows4(const PagedAttnArgs &a, cudaStream_t st)
+// ---- Many sequences: the steps of all (sequence, KV head) pairs, one after the other, are dealt out evenly to the warps that the GPU holds at a time.
+// A pair whose steps lie with one warp is finished by it; what a warp has of another pair goes to one of its two places in the workspace
+// (it can have the end of one and the start of another), and a second kernel adds those up.
+constexpr int STREAM_WARPS = 4;
+template <int D> struct StreamCfg : Step4<D> {
+    static constexpr int STAGES = D == 128 ? 2 : 4;
+    static constexpr int OFF_FACTORS = STREAM_WARPS * STAGES * Step4<D>::STAGE, OFF_STARTS = OFF_FACTORS + STREAM_WARPS * Step4<D>::FACTORS;
+    static constexpr int SMEM = OFF_STARTS + (STREAM_MAX_B + 1) * 4 + 128; // + alignment slack
+};
+
+// First step of every sequence's pairs in the order of all, [B + 1], in shared memory; by the whole block.
+__device__ __forceinline__ void stream_starts(const PagedAttnArgs &a, int *starts, int *part)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = blockDim.x;
+    int total = 0;
+    for (int b0 = 0; b0 < a.rb.B; b0 += n) {
+        const int b = b0 + tid;
+        int x = 0;
+        if (b < a.rb.B) {
+            Rows q;
+            int n_new;
+            if (batch_row(a.rb, b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err)) {
+                q.keys(a, n_new);
+                x = q.n_steps * a.kv.nkv;
+            }
+        }
+        int y = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int z = __shfl_up_sync(0xffffffffu, y, o);
+            if (lane >= o) y += z;
+        }
+        if (lane == 31) part[warp] = y;
+        __syncthreads();
+        int before = total, all = 0;
+        for (int w = 0; w < n / 32; ++w) {
+            if (w < warp) before += part[w];
+            all += part[w];
+        }
+        if (b < a.rb.B) starts[b] = before + y - x;
+        total += all;
+        __syncthreads();
+    }
+    if (tid == 0) starts[a.rb.B] = total;
+    __syncthreads();
+}
+// The last sequence that starts at or before step x and has steps
+__device__ __forceinline__ int stream_find(const int *starts, int B, int x)
+{
+    int lo = 0, hi = B; // starts[lo] <= x < starts[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+// How `total` steps are dealt out: no more workers than steps, the first `extra` of them one more than the others.
+struct Deal {
+    int workers, per, extra;
+    __device__ __forceinline__ Deal(int total, int warps)
+    {
+        workers = min(warps, total);
+        per = total / max(workers, 1);
+        extra = total - per * workers;
+    }
+    __device__ __forceinline__ int begin(int w) const { return w * per + min(w, extra); }
+    __device__ __forceinline__ int worker_of(int x) const { return x < extra * (per + 1) ? x / (per + 1) : extra + (x - extra * (per + 1)) / per; }
+};
+
+template <int D, int NR, bool PAGES>
+__global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 4 : 3) paged_attention_stream4_kernel(const __grid_constant__ PagedAttnArgs a, int *starts_out)
+{
+    using C = StreamCfg<D>;
+    constexpr int W = D / 32;
+    extern __shared__ uint8_t rows4_raw[];
+    uint8_t *gen = rows4_raw + ((128u - (tc::smem_u32(rows4_raw) & 127u)) & 127u);
+    const uint32_t base = tc::smem_u32(gen);
+    __shared__ int part[STREAM_WARPS];
+    int *starts = (int *)(gen + C::OFF_STARTS);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    if (threadIdx.x == 0) stamp_entry(a.stamp);
+    pdl_launch_dependents();
+    pdl_wait();
+    stream_starts(a, starts, part);
+    for (int b = threadIdx.x; blockIdx.x == 0 && b <= a.rb.B; b += 32 * STREAM_WARPS) starts_out[b] = starts[b]; // for the second kernel
+    const Deal deal(starts[a.rb.B], gridDim.x * STREAM_WARPS);
+    const int me = blockIdx.x * STREAM_WARPS + warp;
+    if (me >= deal.workers) return;
+    int x = deal.begin(me);
+    const int x_end = deal.begin(me + 1);
+    while (x < x_end) {
+        Rows q;
+        int n_new;
+        q.b = stream_find(starts, a.rb.B, x);
+        batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err);
+        q.keys(a, n_new);
+        const int in_seq = x - starts[q.b];
+        q.kvh = in_seq / q.n_steps;
+        const int j0 = in_seq - q.kvh * q.n_steps, n = min(q.n_steps - j0, x_end - x);
+        Partial<D, NR> p;
+        walk<D, NR, C::STAGES, PAGES>(a, q, j0, n, 1, base + warp * C::STAGES * C::STAGE, base + C::OFF_FACTORS + warp * C::FACTORS, p);
+        x += n;
+        const bool whole = n == q.n_steps;
+        const long slot = 2L * me + (j0 == 0);
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nr + 2 * t4 + e;
+                if (r >= q.rows) continue;
+                float inv = 1.f;
+                if (whole) inv = inverse_sum(column(p.l[nr], e));
+                const int i = r / a.group, head = q.kvh * a.group + r - i * a.group;
+#pragma unroll
+                for (int t = 0; t < 2 * W; ++t) { // dims 16 (t % W) + 2 g and the next of half t / W
+                    const float unit = t < W ? LOW_UNIT : HIGH_UNIT, low = column(p.om[nr][t / W], e);
+                    const float y0 = fmaf(p.o[nr][t][e], unit, low) * inv, y1 = fmaf(p.o[nr][t][2 + e], unit, low) * inv;
+                    const int dim = t / W * (D / 2) + 16 * (t % W) + 2 * g;
+                    if (whole) *(uint32_t *)((bf16 *)a.out + (long)(q.row0 + i) * a.o_stride + (long)head * D + dim) = pack(y0, y1);
+                    else *(float2 *)(a.part_o + (slot * (8 * NR) + r) * D + dim) = make_float2(y0, y1);
+                }
+                if (!whole && g == 0) {
+                    const float m = column(p.l[nr], e) != column(p.l[nr], e) ? fmaxf(column(p.m_used[nr], e), 0.f) : column(p.m_used[nr], e); // scores that are all NaN leave no maximum
+                    *(float2 *)(a.part_ml + (slot * (8 * NR) + r) * 2) = make_float2(m, column(p.l[nr], e));
+                }
+            }
+        }
+    }
+    if (threadIdx.x == 0) stamp_exit(a.stamp);
+}
+
+// Adds up what several warps have of a pair: a warp per query row.
+template <int D, int NR>
+__global__ void __launch_bounds__(128) paged_merge_stream4_kernel(const __grid_constant__ PagedAttnArgs a, int warps, const int *starts)
+{
+    constexpr int VEC = D / 32;
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, r = blockIdx.z * 4 + (threadIdx.x >> 5);
+    pdl_wait();
+    Rows q;
+    int n_new;
+    q.kvh = blockIdx.x;
+    q.b = blockIdx.y;
+    const int start = __ldcg(starts + q.b), total = __ldcg(starts + a.rb.B);
+    if (!batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err)) return;
+    q.keys(a, n_new);
+    if (r >= q.rows) return;
+    const Deal deal(total, warps);
+    const int x0 = start + q.kvh * q.n_steps, w0 = deal.worker_of(x0), w1 = deal.worker_of(x0 + q.n_steps - 1);
+    if (w0 == w1) return; // finished by its warp
+    float m = -INFINITY, den = 0.f, o[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o[e] = 0.f;
+    for (int wb = w0; wb <= w1; wb += 32) { // maxima and sums in the lanes, then eight workers' rows at a time
+        const int w = wb + lane, n = min(32, w1 - wb + 1);
+        const int slot = 2 * w + (deal.begin(w) <= x0);
+        const float2 ml = lane < n ? __ldcg((const float2 *)(a.part_ml + ((long)slot * (8 * NR) + r) * 2)) : make_float2(-INFINITY, 0.f);
+        float v[8][VEC];
+        auto fetch = [&](int k0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float *src = a.part_o + ((long)__shfl_sync(0xffffffffu, slot, (k0 + k) & 31) * (8 * NR) + r) * D + lane * VEC;
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const float2 x = k0 + k < n ? __ldcg((const float2 *)(src + e)) : make_float2(0.f, 0.f);
+                    v[k][e] = x.x; v[k][e + 1] = x.y;
+                }
+            }
+        };
+        fetch(0);
+        const float nm = fmaxf(m, warp_max(ml.x)), f = m == -INFINITY ? 0.f : ex2(m - nm), mine = ml.x == -INFINITY ? 0.f : ex2(ml.x - nm);
+        m = nm;
+        den = fmaf(den, f, warp_sum(ml.y * mine));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] *= f;
+        for (int k0 = 0; k0 < n; k0 += 8) {
+            if (k0) fetch(k0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float wt = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) o[e] = fmaf(v[k][e], wt, o[e]);
+            }
+        }
+    }
+    const float inv = inverse_sum(den);
+    const int i = r / a.group, head = q.kvh * a.group + r - i * a.group;
+    bf16 *dst = (bf16 *)a.out + (long)(q.row0 + i) * a.o_stride + (long)head * D + lane * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; e += 2) *(uint32_t *)(dst + e) = pack(o[e] * inv, o[e + 1] * inv);
+}
+
+template <int D, int NR, int RW, bool PAGES> cudaError_t launch_rows4(const PagedAttnArgs &a, cudaStream_t st)
 {
     using C = Rows4Cfg<D, RW>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_rows4_kernel<D, NR, RW, PAGE16>, C::SMEM);
+    const cudaError_t e = limit.raise((const void *)paged_attention_rows4_kernel<D, NR, RW, PAGES>, C::SMEM);
     if (e != cudaSuccess) return e;
-    return launch_kernel_z(paged_attention_rows4_kernel<D, NR, RW, PAGE16>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(32 * RW), C::SMEM, st, a.part_o ? 1 : a.splits, a);
+    return launch_kernel_z(paged_attention_rows4_kernel<D, NR, RW, PAGES>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(32 * RW), C::SMEM, st, a.part_o ? 1 : a.splits, a);
 }
-template <int D, int NR> cudaError_t rows4_by_page(const PagedAttnArgs &a, cudaStream_t st)
+template <int D, int NR, bool PAGES> cudaError_t launch_stream4(PagedAttnArgs a, cudaStream_t st)
 {
-    if (a.kv.page % 16) return launch_rows4<D, NR, 4, false>(a, st);
+    using C = StreamCfg<D>;
+    static SmemLimit limit;
+    cudaError_t e = limit.raise((const void *)paged_attention_stream4_kernel<D, NR, PAGES>, C::SMEM);
+    if (e != cudaSuccess) return e;
+    const int workers = stream4_workers(NR);
+    a.part_ml = a.part_o + (size_t)workers * 2 * 8 * NR * D;
+    int *starts = (int *)(a.part_ml + (size_t)workers * 2 * 8 * NR * 2);
+    e = launch_kernel(paged_attention_stream4_kernel<D, NR, PAGES>, dim3(workers / STREAM_WARPS), dim3(32 * STREAM_WARPS), C::SMEM, st, 0, a, starts);
+    if (e != cudaSuccess) return e;
+    const int rows = a.max_new * a.group;
+    return launch_kernel(paged_merge_stream4_kernel<D, NR>, dim3(a.kv.nkv, a.rb.B, (rows + 3) / 4), dim3(128), 0, st, 0, a, workers, starts);
+}
+template <int D, int NR> cudaError_t rows4_by_page(const PagedAttnArgs &a, bool stream, cudaStream_t st)
+{
+    const bool pages = a.kv.page >= 16 && !(a.kv.page & (a.kv.page - 1)) && (long)a.kv.nkv * a.kv.page * (D / 2) <= 0x7fffffffL;
+    if (stream) return pages ? launch_stream4<D, NR, true>(a, st) : launch_stream4<D, NR, false>(a, st);
+    if (!pages) return launch_rows4<D, NR, 4, false>(a, st);
     if ((long)a.kv.nkv * a.rb.B * a.splits <= sm_count()) return launch_rows4<D, NR, 8, true>(a, st);
     return launch_rows4<D, NR, 4, true>(a, st);
 }
-template <int D> cudaError_t rows4_by_count(const PagedAttnArgs &a, cudaStream_t st)
+template <int D> cudaError_t rows4_by_count(const PagedAttnArgs &a, bool stream, cudaStream_t st)
 {
-    return a.max_new * a.group <= 8 ? rows4_by_page<D, 1>(a, st) : rows4_by_page<D, 2>(a, st);
+    return a.max_new * a.group <= 8 ? rows4_by_page<D, 1>(a, stream, st) : rows4_by_page<D, 2>(a, stream, st);
 }
 
 } // namespace
 
-cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, cudaStream_t st)
+int stream4_workers(int nr) { return sm_count() * (nr == 1 ? 4 : 3) * STREAM_WARPS; }
+size_t stream4_workspace(int rows, int d) { return (size_t)stream4_workers(rows <= 8 ? 1 : 2) * 2 * (rows <= 8 ? 8 : 16) * (d + 2) * sizeof(float) + (STREAM_MAX_B + 1) * sizeof(int); }
+
+cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, bool stream, cudaStream_t st)
 {
-    if (a.kv.d == 128) return rows4_by_count<128>(a, st);
-    if (a.kv.d == 64) return rows4_by_count<64>(a, st);
+    if (a.kv.d == 128) return rows4_by_count<128>(a, stream, st);
+    if (a.kv.d == 64) return rows4_by_count<64>(a, stream, st);
     return cudaErrorInvalidValue;
 }
 

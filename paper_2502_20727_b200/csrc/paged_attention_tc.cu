@@ -162,26 +162,6 @@ __device__ __forceinline__ float max_nan(float a, float b) // NaN if either is
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-// two fp32 operations per instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(unsigned long long *)&d)
-        : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b), "l"(*(const unsigned long long *)&c));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*(unsigned long long *)&d) : "l"(*(const unsigned long long *)&a), "l"(*(const unsigned long long *)&b));
-    return d;
-}
 // 2^t of two values on the FMA pipes, for t <= 127 (t below -126 counts as -126): t = n + f with n = round(t), |f| <= 1/2; a
 // polynomial of degree 4 for 2^f (least maximum relative error over the interval by a Lawson iteration: 2.6e-6) whose exponent
 // field n is added to.
