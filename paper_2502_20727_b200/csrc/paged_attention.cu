@@ -314,7 +314,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         // More than a cluster's worth cost a second kernel (about 2 us) and pay from 512 keys each.  Measured, 8 KV heads of
         // 8 query heads, bf16, us by ranges: 1 x 4096 keys 8: 11.2, 20: 12.8; 1 x 16384 8: 24.9, 20: 22.4; 4 x 4096 2: 24.7,
         // 4: 18.9, 8: 19.1; 16 x 4096 2: 49, 8: 61.
-        const long pairs = (long)(B > 0 ? B : 1) * nkv, sms = sm_count(), resident = fmt != KV_BF16 && rows <= 8 ? 4 : 3;
+        const long pairs = (long)(B > 0 ? B : 1) * nkv, sms = sm_count(), resident = fmt == KV_INT4 ? (rows <= 8 ? 3 : 2) : fmt != KV_BF16 && rows <= 8 ? 4 : 3;
         long s = sms / pairs >= 2 ? sms / pairs : resident * sms / pairs;
         if (s > (keys + 255) / 256) s = (keys + 255) / 256;
         if (s < (keys + 2047) / 2048) s = (keys + 2047) / 2048;

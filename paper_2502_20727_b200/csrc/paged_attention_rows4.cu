@@ -33,7 +33,7 @@ template <int D> struct Step4 {
 };
 // Thread blocks of RW warps for one (sequence, KV head) and key range
 template <int D, int RW> struct Rows4Cfg : Step4<D> {
-    static constexpr int STAGES = RW == 8 ? 4 : D == 128 ? 2 : 4;
+    static constexpr int STAGES = RW == 8 || D == 64 ? 4 : 3;
     static constexpr int RING = RW * STAGES * Step4<D>::STAGE, MERGE = RW * 16 * (D + 4) * 4;
     static constexpr int OFF_FACTORS = RING > MERGE ? RING : MERGE, OFF_JOIN = OFF_FACTORS + RW * Step4<D>::FACTORS;
     static constexpr int SMEM = OFF_JOIN + join_bytes(RW) + 128;            // + alignment slack
@@ -243,9 +243,6 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
     // bytes, which give a lane bytes 2 g and 2 g + 1 of keys 2 t4 and 2 t4 + 1.
     const uint32_t lane_k = RB == 64 ? at(g, t4) : at(g, t4 >> 1) + (t4 & 1) * 8, my_factors = fk + g * 16;
     const uint32_t lane_v = at(lane & 15, lane >> 4); // matrices: keys 0-7 and 8-15 of chunk 0, of chunk 1
-    uint32_t shift8; // 2^24: products' high words are shifts by 8 on the FMA pipe, while masks fill the other one
-    asm volatile("mov.b32 %0, 0x1000000;" : "=r"(shift8));
-
     auto &o = acc_out.o;
     auto &m_used = acc_out.m_used;
     auto &l = acc_out.l;
@@ -301,7 +298,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
             }
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                const uint32_t y0 = __umulhi(w0[i], shift8), y1 = __umulhi(w1[i], shift8);
+                const uint32_t y0 = w0[i] >> 8, y1 = w1[i] >> 8;
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     if (i == 0) {
@@ -393,7 +390,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
                 ldsm4t(v, (sV + lane_v + u * 16 * RB) ^ (c << 4));
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint32_t x0 = v[2 * i], x1 = v[2 * i + 1], y0 = __umulhi(x0, shift8), y1 = __umulhi(x1, shift8);
+                    const uint32_t x0 = v[2 * i], x1 = v[2 * i + 1], y0 = x0 >> 8, y1 = x1 >> 8;
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
                         mma16816<true>(o[n][c + i], low_codes(x0), low_codes(y0), low_codes(x1), low_codes(y1), pf[0][n][0], pf[0][n][1]);
@@ -428,14 +425,14 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
 __device__ __forceinline__ float column(float2 v, int e) { return e ? v.y : v.x; }
 
 template <int D, int NR, int RW, bool PAGES>
-__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
+__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 3 : 2) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
 {
     using C = Rows4Cfg<D, RW>;
     constexpr int MT = D / 16, W = D / 32;
     extern __shared__ uint8_t rows4_raw[];
     uint8_t *gen = rows4_raw + ((128u - (tc::smem_u32(rows4_raw) & 127u)) & 127u);
     const uint32_t base = tc::smem_u32(gen);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3; // the same in all lanes, for the compiler too
     if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
     pdl_wait();
@@ -482,7 +479,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 4 : 3) paged_
 // (it can have the end of one and the start of another), and a second kernel adds those up.
 constexpr int STREAM_WARPS = 4;
 template <int D> struct StreamCfg : Step4<D> {
-    static constexpr int STAGES = D == 128 ? 2 : 4;
+    static constexpr int STAGES = D == 64 ? 4 : 3;
     static constexpr int OFF_FACTORS = STREAM_WARPS * STAGES * Step4<D>::STAGE, OFF_STARTS = OFF_FACTORS + STREAM_WARPS * Step4<D>::FACTORS;
     static constexpr int SMEM = OFF_STARTS + (STREAM_MAX_B + 1) * 4 + 128; // + alignment slack
 };
@@ -547,7 +544,7 @@ struct Deal {
 };
 
 template <int D, int NR, bool PAGES>
-__global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 4 : 3) paged_attention_stream4_kernel(const __grid_constant__ PagedAttnArgs a, int *starts_out)
+__global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 3 : 2) paged_attention_stream4_kernel(const __grid_constant__ PagedAttnArgs a, int *starts_out)
 {
     using C = StreamCfg<D>;
     constexpr int W = D / 32;
@@ -556,7 +553,7 @@ __global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 4 : 3) paged_atte
     const uint32_t base = tc::smem_u32(gen);
     __shared__ int part[STREAM_WARPS];
     int *starts = (int *)(gen + C::OFF_STARTS);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3; // the same in all lanes, for the compiler too
     if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_launch_dependents();
     pdl_wait();
@@ -706,7 +703,7 @@ template <int D> cudaError_t rows4_by_count(const PagedAttnArgs &a, bool stream,
 
 } // namespace
 
-int stream4_workers(int nr) { return sm_count() * (nr == 1 ? 4 : 3) * STREAM_WARPS; }
+int stream4_workers(int nr) { return sm_count() * (nr == 1 ? 3 : 2) * STREAM_WARPS; }
 size_t stream4_workspace(int rows, int d) { return (size_t)stream4_workers(rows <= 8 ? 1 : 2) * 2 * (rows <= 8 ? 8 : 16) * (d + 2) * sizeof(float) + (STREAM_MAX_B + 1) * sizeof(int); }
 
 cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, bool stream, cudaStream_t st)
