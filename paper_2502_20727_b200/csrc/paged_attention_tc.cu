@@ -133,29 +133,23 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     const __half2 v = __floats2half2_rn(lo, hi);
     return *(const uint32_t *)&v;
 }
-// 4-bit codes in bits 0-3 (4-7) of a word's halves -> float16x2 of code * s + m: the masked bits are code * 2^-24 (2^-20), so that
-// `s` holds the scale times 2^24 (2^20); one rounding.
-__device__ __forceinline__ uint32_t widen4(uint32_t codes, uint32_t s, uint32_t m)
+// 4-bit codes in bits 0-3 (4-7) of a word's halves -> float16x2 of code * s + m, one rounding.  The masked bits are code * 2^-24 (2^-20), and `s` holds
+// the scale times 2^24 (2^20), which bounds the values by 2^-4; if `normal`, the codes first become code (code * 16), and `s` holds the scale (over 16).
+__device__ __forceinline__ uint32_t widen4(bool normal, uint32_t w, uint32_t mask, uint32_t c1024, uint32_t s, uint32_t m)
 {
-    const __half2 v = __hfma2(*(const __half2 *)&codes, *(const __half2 *)&s, *(const __half2 *)&m);
+    const uint32_t x = normal ? and_or(w, mask, c1024) : w & mask;
+    __half2 c = *(const __half2 *)&x;
+    if (normal) c = __hsub2(c, *(const __half2 *)&c1024);
+    const __half2 v = __hfma2(c, *(const __half2 *)&s, *(const __half2 *)&m);
     return *(const uint32_t *)&v;
 }
-// A row's parameters (s, m of either half) in units of 2^(e + 6), where 2^e is the power of two at or under the largest of |m| and 16 s:
-// values are below 2^-4 then, and the scales as widen4 wants them below 2^16.  What rounding leaves of the smaller ones is 2^-20 of the
-// row's largest value at most.  unit = 2^(e + 6), at least 2^-60 and at most 2^36; a row that is not finite gives zeros and a NaN.
-__device__ __forceinline__ uint2 row_params(uint2 p, float &unit, int &exponent)
+// Exponent field of the power of two at or under the largest of |m| and 16 s of either half: values are below four times that.  0: not finite.
+__device__ __forceinline__ int row_exponent(uint2 p)
 {
     const uint32_t mags = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu), sb = mags & 0xffffu, mb = mags >> 16;
-    const int ex = min(max((int)max((sb >> 7) + 4, mb >> 7) + 6, 127 - 60), 127 + 36);
-    unit = __uint_as_float((uint32_t)ex << 23);
-    exponent = ex - 127;
-    if (sb >= 0x7f80u || mb >= 0x7f80u) {
-        unit = __uint_as_float(0x7fc00000u);
-        return make_uint2(0, 0);
-    }
-    const float f = __uint_as_float((uint32_t)(254 - ex) << 23);
-    return make_uint2(pack_half(kv4_scale(p.x) * f * 0x1p24f, kv4_min(p.x) * f), pack_half(kv4_scale(p.y) * f * 0x1p20f, kv4_min(p.y) * f));
+    return sb >= 0x7f80u || mb >= 0x7f80u ? 0 : (int)max((sb >> 7) + 4, mb >> 7);
 }
+__device__ __forceinline__ float pow2_of(int field) { return __uint_as_float((uint32_t)field << 23); }
 __device__ __forceinline__ float max_nan(float a, float b) // NaN if either is
 {
     float d;
@@ -394,26 +388,67 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     sc[(j & 7) * 256 + 128 + tid] = row >= 0 ? a.kv.vs[row] : 0.f;
                     mbar_arrive(sc_full(j & 7)); // eight tiles later the slot's scores have long been weighted
                 }
-                if constexpr (Q4) {
-                    uint2 kp = make_uint2(0, 0), vp = kp;
-                    if (row >= 0) { kp = *(const uint2 *)(a.kv.ks + 2 * row); vp = *(const uint2 *)(a.kv.vs + 2 * row); }
-                    float *s = sc + (j & 1) * 384 + tid, ku, vu;
-                    int ke, ve;
-                    uint2 *par = (uint2 *)(gen + C::OFF_SC + 3072) + (j & 1) * 256 + tid;
-                    par[0] = row_params(kp, ku, ke);
-                    par[128] = row_params(vp, vu, ve);
-                    s[0] = ku;
-                    s[128] = vu == vu ? (float)ve : vu;
-                    s[256] = __uint_as_float((uint32_t)(127 - ve) << 23);
-                    mbar_arrive(sc_full(j & 1)); // the weights of the tile before last went into a product that the load warps have seen complete
-                }
                 named_bar<BAR_LOAD, LT>();
             };
             if constexpr (Q4) {
+                // All rows of a tile get one power of two for K and one for V, so that the softmax warps need no factor per key (with one per row: 1603 us in
+                // place of REPLACED, chunk of 2048 on 14336).  K is scaled to below 2^-4, V to below 2^14: rows down to 2^-10 and 2^-28 of the tile's largest
+                // keep float16's 11 bits, and what is lost of smaller ones is 2^-21 of the largest in a score, nothing that counts in V.
+                // Threads 0-127 look after a key each: page id two tiles ahead, parameters one tile ahead.
+                const uint32_t par = base + C::OFF_SC + 1024;
+                int *exps = (int *)(gen + C::OFF_SC + 512); // [2][4 warps][K, V]
+                int page_next = 0;
+                bool need_next = false;
+                long row_next = -1;
+                uint2 kp = make_uint2(0, 0), vp = kp;
+                auto ask_page = [&](int j) {
+                    const int t = j < n_tiles ? key0(j) + tid : kv_len;
+                    need_next = tid < 128 && key_needed(t);
+                    page_next = need_next ? bt[t / a.kv.page] : 0;
+                };
+                auto ask_row = [&](int j) { // page_next is tile j's
+                    row_next = -1;
+                    kp = vp = make_uint2(0, 0);
+                    if (!need_next) return;
+                    if (page_next < 0 || page_next >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); return; }
+                    row_next = ((long)page_next * a.kv.nkv + kvh) * a.kv.page + (key0(j) + tid) % a.kv.page;
+                    kp = *(const uint2 *)(a.kv.ks + 2 * row_next);
+                    vp = *(const uint2 *)(a.kv.vs + 2 * row_next);
+                };
+                auto rows_now = [&](int j) { // tile j's rows for all load warps
+                    if (tid < 128) {
+                        const int k = __reduce_max_sync(0xffffffffu, row_exponent(kp)), v = __reduce_max_sync(0xffffffffu, row_exponent(vp));
+                        if (lane == 0) { exps[(j & 1) * 8 + 2 * (tid >> 5)] = k; exps[(j & 1) * 8 + 2 * (tid >> 5) + 1] = v; }
+                        rowoff[(j & 1) * 128 + tid] = row_next;
+                    }
+                    named_bar<BAR_LOAD, LT>();
+                };
+                auto params_now = [&](int j) { // ... and their parameters; the next tile's are asked for
+                    if (tid < 128) {
+                        const int *e = exps + (j & 1) * 8;
+                        const int k = min(max(max(max(e[0], e[2]), max(e[4], e[6])) + 6, 127 - 60), 127 + 36);  // K in units of 2^(k - 127): below 2^-4
+                        const int v = min(max(max(max(e[1], e[3]), max(e[5], e[7])) - 12, 127 - 60), 127 + 36); // V: below 2^14
+                        const float fk = pow2_of(254 - k), fv = pow2_of(254 - v), nan = __uint_as_float(0x7fc00000u);
+                        const bool v_bad = row_exponent(vp) == 0, bad = v_bad || row_exponent(kp) == 0; // a key with a row that is not finite: its scores are NaN
+                        uint2 *dst = (uint2 *)(gen + C::OFF_SC + 1024) + (j & 1) * 256 + tid;
+                        dst[0] = make_uint2(pack_half(kv4_scale(kp.x) * fk * 0x1p24f, bad ? nan : kv4_min(kp.x) * fk), pack_half(kv4_scale(kp.y) * fk * 0x1p20f, bad ? nan : kv4_min(kp.y) * fk));
+                        dst[128] = v_bad ? make_uint2(0, 0)
+                                         : make_uint2(pack_half(kv4_scale(vp.x) * fv, kv4_min(vp.x) * fv), pack_half(kv4_scale(vp.y) * fv * 0x1p-4f, kv4_min(vp.y) * fv));
+                        if (tid == 0) {
+                            sc[(j & 1) * 4] = pow2_of(k);
+                            sc[(j & 1) * 4 + 1] = (float)(v - 127);
+                            sc[(j & 1) * 4 + 2] = fv;
+                        }
+                        mbar_arrive(sc_full(j & 1)); // the weights of the tile before last went into a product that the load warps have seen complete
+                        if (j + 1 < n_tiles) { ask_row(j + 1); ask_page(j + 2); }
+                    }
+                    named_bar<BAR_LOAD, LT>();
+                };
                 // a thread: a quarter of a row, D / 8 bytes, of half a tile (64 keys); these are D / 8 dims of either half of the head
                 constexpr int W = D / 32;
                 const int c = tid & 3;
-                const uint32_t par = base + C::OFF_SC + 3072;
+                uint32_t c1024; // float16x2 of 1024, kept in a register
+                asm volatile("mov.b32 %0, 0x64006400;" : "=r"(c1024));
                 auto fetch = [&](int j, int h, const void *pages, uint32_t (&x)[W]) {
                     const long row = rowoff[(j & 1) * 128 + h * 64 + tid / 4];
                     const uint8_t *p = (const uint8_t *)pages + row * (D / 2) + c * (D / 8);
@@ -425,22 +460,31 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                         x[0] = u.x; x[1] = u.y;
                     }
                 };
-                auto widen = [&](int j, bool is_v, int h, const uint32_t (&x)[W]) {
+                auto widen = [&](int j, const bool V, int h, const uint32_t (&x)[W]) {
                     const int r = h * 64 + tid / 4;
-                    const uint32_t tile_base = base + (is_v ? C::OFF_V : C::OFF_K);
+                    const uint32_t tile_base = base + (V ? C::OFF_V : C::OFF_K);
                     uint2 p;
-                    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(p.x), "=r"(p.y) : "r"(par + ((j & 1) * 256 + is_v * 128 + r) * 8) : "memory");
+                    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(p.x), "=r"(p.y) : "r"(par + ((j & 1) * 256 + V * 128 + r) * 8) : "memory");
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t s = __byte_perm(half ? p.y : p.x, 0, 0x1010), m = __byte_perm(half ? p.y : p.x, 0, 0x3232), mask = half ? 0x00f000f0u : 0x000f000fu;
 #pragma unroll
                         for (int i = 0; i < W; i += 2)
                             sts128(tile_base + tile_at(r, half * (D / 16) + c * (W / 2) + i / 2),
-                                   make_uint4(widen4(x[i] & mask, s, m), widen4(x[i] >> 8 & mask, s, m), widen4(x[i + 1] & mask, s, m), widen4(x[i + 1] >> 8 & mask, s, m)));
+                                   make_uint4(widen4(V, x[i], mask, c1024, s, m), widen4(V, x[i] >> 8, mask, c1024, s, m), widen4(V, x[i + 1], mask, c1024, s, m),
+                                              widen4(V, x[i + 1] >> 8, mask, c1024, s, m)));
                     }
                 };
                 uint32_t x0[W], x1[W];
-                if (n_tiles > 0) { rows_of(0); fetch(0, 0, a.kv.k, x0); fetch(0, 1, a.kv.k, x1); }
+                if (n_tiles > 0) {
+                    ask_page(0);
+                    ask_row(0);
+                    ask_page(1);
+                    rows_now(0);
+                    fetch(0, 0, a.kv.k, x0);
+                    fetch(0, 1, a.kv.k, x1);
+                    params_now(0);
+                }
                 for (int j = 0; j < n_tiles; ++j) {
                     if (j > 0) mbar_wait(k_empty, (j - 1) & 1, a.err, abort_flag);
                     widen(j, false, 0, x0);
@@ -450,13 +494,14 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     fence_proxy_async();
                     mbar_arrive(k_full);
                     if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
-                    if (j + 1 < n_tiles) rows_of(j + 1);
+                    if (j + 1 < n_tiles) rows_now(j + 1);
                     widen(j, true, 0, x0);
                     if (j + 1 < n_tiles) fetch(j + 1, 0, a.kv.k, x0);
                     widen(j, true, 1, x1);
                     if (j + 1 < n_tiles) fetch(j + 1, 1, a.kv.k, x1);
                     fence_proxy_async();
                     mbar_arrive(v_full);
+                    if (j + 1 < n_tiles) params_now(j + 1);
                 }
             } else if constexpr (Q8) {
                 constexpr int CPR = D / 16, N = 64 * CPR / LT; // 16-code chunks per row; per thread and half a tile (64 keys)
@@ -650,21 +695,11 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 seen = below(pos - t0 + 1);
                 if (a.window) seen &= ~below(pos - a.window + 1 - t0) | below(a.sinks - t0);
             }
-            // 4 bits: the K rows' units, the exponents of the V rows' and their negative powers
-            const float *ks = sc + (Q4 ? (j & 1) * 384 : (j & 7) * 256) + half * 64, *vs = ks + 128;
+            const float *ks = sc + (j & 7) * 256 + half * 64, *vs = ks + 128;
+            // 4 bits: one factor for the tile's K, one exponent for its V (which the maxima have in them) and its negative power
+            const float kq = Q4 ? qs * sc[(j & 1) * 4] : qs, ev = Q4 ? sc[(j & 1) * 4 + 1] : 0.f, v_unit = Q4 ? sc[(j & 1) * 4 + 2] : 1.f;
             // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
-            // (4 bits: in base-2 units, the exponent of the key's V row added)
             auto finish = [&](int c0, uint32_t (&r)[32]) {
-                if constexpr (Q4) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 k4 = *(const float4 *)(ks + c0 + e), e4 = *(const float4 *)(vs + c0 + e);
-                        const float2 q2 = make_float2(qs, qs);
-                        const float2 x = fma2(mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(k4.x, k4.y)), q2, make_float2(e4.x, e4.y));
-                        const float2 y = fma2(mul2(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), make_float2(k4.z, k4.w)), q2, make_float2(e4.z, e4.w));
-                        r[e] = __float_as_uint(x.x); r[e + 1] = __float_as_uint(x.y); r[e + 2] = __float_as_uint(y.x); r[e + 3] = __float_as_uint(y.y);
-                    }
-                }
                 if (Q8) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
@@ -700,7 +735,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             tmem_ask32(t_s + 32, rb);
             tmem_wait32(rb);
             finish(32, rb);
-            mx = max_nan(mx, max_of(rb)) * (Q4 ? 1.f : qs);
+            mx = max_nan(mx, max_of(rb));
+            mx = Q4 ? fmaf(mx, kq, ev) : mx * qs;
             // join with the other half's maximum: both threads of a row then take the same decision
             float *rm = red + (j & 1) * 256 + row;
             rm[half * 128] = mx;
@@ -730,17 +766,16 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 }
             }
             const float mb = m_used == -INFINITY ? 0.f : m_used;
-            const float2 q2 = make_float2(qs, qs), m2 = make_float2(-mb, -mb);
+            const float2 q2 = make_float2(kq, kq), m2 = make_float2(ev - mb, ev - mb);
             float2 ls = make_float2(0.f, 0.f);
             auto weigh = [&](int c0, uint32_t (&r)[32]) {
                 uint32_t w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float2 x = make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
-                    const float2 t = Q4 ? add2(x, m2) : fma2(x, q2, m2);
+                    const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
                     // every second pair (bf16 pages by TMA) or every fourth on the FMA pipes, which the exponentials otherwise leave idle
                     float2 p = (TMA ? k % 2 == 1 : k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
-                    ls = Q4 ? fma2(p, *(const float2 *)(vs + 128 + c0 + 2 * k), ls) : add2(ls, p);
+                    ls = add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
                     w[k] = Q4 ? pack_half(p.x, p.y) : pack(p.x, p.y);
                     if (FMT == KV_INT8) { r[2 * k] = __float_as_uint(p.x); r[2 * k + 1] = __float_as_uint(p.y); }
@@ -770,7 +805,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             tmem_wait32(ra);
             finish(0, ra);
             weigh(0, ra);
-            l += ls.x + ls.y;
+            l = Q4 ? fmaf(ls.x + ls.y, v_unit, l) : l + (ls.x + ls.y);
             tmem_st_wait();
             fence_before();
             __syncwarp();
