@@ -133,17 +133,15 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     const __half2 v = __floats2half2_rn(lo, hi);
     return *(const uint32_t *)&v;
 }
-// 4-bit codes in bits 0-3 (4-7) of a word's halves -> float16x2 of code * s + m, one rounding.  The masked bits are code * 2^-24 (2^-20), and `s` holds
-// the scale times 2^24 (2^20), which bounds the values by 2^-4; if `normal`, the codes first become code (code * 16), and `s` holds the scale (over 16).
-__device__ __forceinline__ uint32_t widen4(bool normal, uint32_t w, uint32_t mask, uint32_t c1024, uint32_t s, uint32_t m)
+// 4-bit codes in bits 0-3 (4-7) of a word's halves -> float16x2 of code * s + m: the masked bits are code * 2^-24 (2^-20), so that `s` holds the scale
+// times 2^24 (2^20), which bounds the values by 2^-4; one rounding.
+__device__ __forceinline__ uint32_t widen4(uint32_t codes, uint32_t s, uint32_t m)
 {
-    const uint32_t x = normal ? and_or(w, mask, c1024) : w & mask;
-    __half2 c = *(const __half2 *)&x;
-    if (normal) c = __hsub2(c, *(const __half2 *)&c1024);
-    const __half2 v = __hfma2(c, *(const __half2 *)&s, *(const __half2 *)&m);
+    const __half2 v = __hfma2(*(const __half2 *)&codes, *(const __half2 *)&s, *(const __half2 *)&m);
     return *(const uint32_t *)&v;
 }
-// Exponent field of the power of two at or under the largest of |m| and 16 s of either half: values are below four times that.  0: not finite.
+// Exponent field of the power of two at or under the largest of |m| and 16 s of either half: values are below four times that.  0: not finite;
+// up to 4: zeros, or as good as.
 __device__ __forceinline__ int row_exponent(uint2 p)
 {
     const uint32_t mags = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu), sb = mags & 0xffffu, mb = mags >> 16;
@@ -291,7 +289,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
         mbar_init(p_rest, 4);
         mbar_init(o_done, 1);
         mbar_init(drain, 1);
-        for (int s = 0; s < 8; ++s) mbar_init(sc_full(s), 128);
+        for (int s = 0; s < 8; ++s) mbar_init(sc_full(s), Q4 ? LT : 128);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == W_MMA) {
@@ -391,64 +389,69 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 named_bar<BAR_LOAD, LT>();
             };
             if constexpr (Q4) {
-                // All rows of a tile get one power of two for K and one for V, so that the softmax warps need no factor per key (with one per row: 1603 us in
-                // place of REPLACED, chunk of 2048 on 14336).  K is scaled to below 2^-4, V to below 2^14: rows down to 2^-10 and 2^-28 of the tile's largest
-                // keep float16's 11 bits, and what is lost of smaller ones is 2^-21 of the largest in a score, nothing that counts in V.
-                // Threads 0-127 look after a key each: page id two tiles ahead, parameters one tile ahead.
-                const uint32_t par = base + C::OFF_SC + 1024;
-                int *exps = (int *)(gen + C::OFF_SC + 512); // [2][4 warps][K, V]
+                // K and V are scaled by powers of two to below 2^-4.  The rows of a tile share one for K and one for V where they are within 2^8 of one
+                // another: the softmax warps then need no factor per key, and a row keeps at least 2^-13 of its largest value.  Otherwise (`varied`: a row may
+                // hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on 14336; REPLACED.)
+                // Threads 0-127 look after a key's K row each, 128-255 after its V row: page id two tiles ahead, parameters one tile ahead.
+                const uint32_t par = base + C::OFF_SC + 3200;
+                int *exps = (int *)(gen + C::OFF_SC + 3200 + 4096); // [2][8 warps][largest, smallest, rows that are not finite, -]
+                const int key = tid & 127, lg = a.kv.page & (a.kv.page - 1) ? -1 : __ffs(a.kv.page) - 1;
+                const bool mine_v = tid >= 128;
                 int page_next = 0;
-                bool need_next = false;
-                long row_next = -1;
-                uint2 kp = make_uint2(0, 0), vp = kp;
-                auto ask_page = [&](int j) {
-                    const int t = j < n_tiles ? key0(j) + tid : kv_len;
-                    need_next = tid < 128 && key_needed(t);
-                    page_next = need_next ? bt[t / a.kv.page] : 0;
-                };
-                auto ask_row = [&](int j) { // page_next is tile j's
-                    row_next = -1;
-                    kp = vp = make_uint2(0, 0);
-                    if (!need_next) return;
-                    if (page_next < 0 || page_next >= a.kv.n_pages) { atomicOr(a.err, ERR_PAGE_RANGE); return; }
-                    row_next = ((long)page_next * a.kv.nkv + kvh) * a.kv.page + (key0(j) + tid) % a.kv.page;
-                    kp = *(const uint2 *)(a.kv.ks + 2 * row_next);
-                    vp = *(const uint2 *)(a.kv.vs + 2 * row_next);
+                uint2 prm = make_uint2(0, 0); // zeros stand for no row, too
+                auto needs = [&](int j) { return j < n_tiles && key_needed(key0(j) + key); };
+                auto page_of = [&](int t) { return lg >= 0 ? t >> lg : t / a.kv.page; };
+                auto ask_page = [&](int j) { page_next = needs(j) ? bt[page_of(key0(j) + key)] : 0; };
+                auto ask_row = [&](int j) { // page_next is tile j's.  The row numbers of the tile two before have been read.
+                    long row = -1;
+                    prm = make_uint2(0, 0);
+                    if (needs(j)) {
+                        if (page_next < 0 || page_next >= a.kv.n_pages) atomicOr(a.err, ERR_PAGE_RANGE);
+                        else {
+                            const int t = key0(j) + key;
+                            row = ((long)page_next * a.kv.nkv + kvh) * a.kv.page + (t - page_of(t) * a.kv.page);
+                            prm = *(const uint2 *)((mine_v ? a.kv.vs : a.kv.ks) + 2 * row);
+                        }
+                    }
+                    if (!mine_v) rowoff[(j & 1) * 128 + key] = row;
                 };
                 auto rows_now = [&](int j) { // tile j's rows for all load warps
-                    if (tid < 128) {
-                        const int k = __reduce_max_sync(0xffffffffu, row_exponent(kp)), v = __reduce_max_sync(0xffffffffu, row_exponent(vp));
-                        if (lane == 0) { exps[(j & 1) * 8 + 2 * (tid >> 5)] = k; exps[(j & 1) * 8 + 2 * (tid >> 5) + 1] = v; }
-                        rowoff[(j & 1) * 128 + tid] = row_next;
-                    }
+                    const int e = row_exponent(prm), most = __reduce_max_sync(0xffffffffu, e), least = __reduce_min_sync(0xffffffffu, e <= 4 ? 999 : e);
+                    const unsigned bad = __ballot_sync(0xffffffffu, e == 0);
+                    if (lane == 0) *(int4 *)(exps + (j & 1) * 32 + 4 * (tid >> 5)) = make_int4(most, least, (int)bad, 0);
                     named_bar<BAR_LOAD, LT>();
                 };
-                auto params_now = [&](int j) { // ... and their parameters; the next tile's are asked for
-                    if (tid < 128) {
-                        const int *e = exps + (j & 1) * 8;
-                        const int k = min(max(max(max(e[0], e[2]), max(e[4], e[6])) + 6, 127 - 60), 127 + 36);  // K in units of 2^(k - 127): below 2^-4
-                        const int v = min(max(max(max(e[1], e[3]), max(e[5], e[7])) - 12, 127 - 60), 127 + 36); // V: below 2^14
-                        const float fk = pow2_of(254 - k), fv = pow2_of(254 - v), nan = __uint_as_float(0x7fc00000u);
-                        const bool v_bad = row_exponent(vp) == 0, bad = v_bad || row_exponent(kp) == 0; // a key with a row that is not finite: its scores are NaN
-                        uint2 *dst = (uint2 *)(gen + C::OFF_SC + 1024) + (j & 1) * 256 + tid;
-                        dst[0] = make_uint2(pack_half(kv4_scale(kp.x) * fk * 0x1p24f, bad ? nan : kv4_min(kp.x) * fk), pack_half(kv4_scale(kp.y) * fk * 0x1p20f, bad ? nan : kv4_min(kp.y) * fk));
-                        dst[128] = v_bad ? make_uint2(0, 0)
-                                         : make_uint2(pack_half(kv4_scale(vp.x) * fv, kv4_min(vp.x) * fv), pack_half(kv4_scale(vp.y) * fv * 0x1p-4f, kv4_min(vp.y) * fv));
-                        if (tid == 0) {
-                            sc[(j & 1) * 4] = pow2_of(k);
-                            sc[(j & 1) * 4 + 1] = (float)(v - 127);
-                            sc[(j & 1) * 4 + 2] = fv;
-                        }
-                        mbar_arrive(sc_full(j & 1)); // the weights of the tile before last went into a product that the load warps have seen complete
-                        if (j + 1 < n_tiles) { ask_row(j + 1); ask_page(j + 2); }
+                auto params_now = [&](int j) { // ... and their parameters; then the next tile's are asked for
+                    const int4 *e = (const int4 *)(exps + (j & 1) * 32);
+                    int most[2] = {0, 0}, least[2] = {999, 999}; // K, V
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) {
+                        const int2 x = *(const int2 *)(e + w);
+                        most[w >> 2] = max(most[w >> 2], x.x);
+                        least[w >> 2] = min(least[w >> 2], x.y);
                     }
+                    const bool varied = most[0] - least[0] > 8 || most[1] - least[1] > 8;
+                    const int mine = row_exponent(prm), tile = mine_v ? most[1] : most[0];
+                    const int unit = min(max((varied ? mine : tile) + 6, 127 - 60), 127 + 36); // field of the power of two that the values are divided by
+                    const float f = pow2_of(254 - unit);
+                    uint2 out = make_uint2(pack_half(kv4_scale(prm.x) * f * 0x1p24f, kv4_min(prm.x) * f), pack_half(kv4_scale(prm.y) * f * 0x1p20f, kv4_min(prm.y) * f));
+                    if (mine == 0) out = make_uint2(0, 0);
+                    if (!mine_v && ((e[4 + (tid >> 5)].z >> lane & 1) || mine == 0)) out = make_uint2(0x7e000000u, 0x7e000000u); // a row of the key is not finite: its scores are NaN
+                    *((uint2 *)(gen + C::OFF_SC + 3200) + (j & 1) * 256 + tid) = out;
+                    float *dst = sc + (j & 1) * 400 + key;
+                    if (mine_v) {
+                        dst[128] = (float)(unit - 127);
+                        dst[256] = f;
+                    } else
+                        dst[0] = pow2_of(unit);
+                    if (tid == 0) dst[384] = varied ? 1.f : 0.f;
+                    mbar_arrive(sc_full(j & 1)); // the weights of the tile before last went into a product that the load warps have seen complete
                     named_bar<BAR_LOAD, LT>();
+                    if (j + 1 < n_tiles) { ask_row(j + 1); ask_page(j + 2); }
                 };
                 // a thread: a quarter of a row, D / 8 bytes, of half a tile (64 keys); these are D / 8 dims of either half of the head
                 constexpr int W = D / 32;
                 const int c = tid & 3;
-                uint32_t c1024; // float16x2 of 1024, kept in a register
-                asm volatile("mov.b32 %0, 0x64006400;" : "=r"(c1024));
                 auto fetch = [&](int j, int h, const void *pages, uint32_t (&x)[W]) {
                     const long row = rowoff[(j & 1) * 128 + h * 64 + tid / 4];
                     const uint8_t *p = (const uint8_t *)pages + row * (D / 2) + c * (D / 8);
@@ -471,8 +474,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
 #pragma unroll
                         for (int i = 0; i < W; i += 2)
                             sts128(tile_base + tile_at(r, half * (D / 16) + c * (W / 2) + i / 2),
-                                   make_uint4(widen4(V, x[i], mask, c1024, s, m), widen4(V, x[i] >> 8, mask, c1024, s, m), widen4(V, x[i + 1], mask, c1024, s, m),
-                                              widen4(V, x[i + 1] >> 8, mask, c1024, s, m)));
+                                   make_uint4(widen4(x[i] & mask, s, m), widen4(x[i] >> 8 & mask, s, m), widen4(x[i + 1] & mask, s, m), widen4(x[i + 1] >> 8 & mask, s, m)));
                     }
                 };
                 uint32_t x0[W], x1[W];
@@ -493,8 +495,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     fetch(j, 1, a.kv.v, x1);
                     fence_proxy_async();
                     mbar_arrive(k_full);
-                    if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
                     if (j + 1 < n_tiles) rows_now(j + 1);
+                    if (j > 0) mbar_wait(v_empty, (j - 1) & 1, a.err, abort_flag);
                     widen(j, true, 0, x0);
                     if (j + 1 < n_tiles) fetch(j + 1, 0, a.kv.k, x0);
                     widen(j, true, 1, x1);
@@ -696,10 +698,20 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 if (a.window) seen &= ~below(pos - a.window + 1 - t0) | below(a.sinks - t0);
             }
             const float *ks = sc + (j & 7) * 256 + half * 64, *vs = ks + 128;
-            // 4 bits: one factor for the tile's K, one exponent for its V (which the maxima have in them) and its negative power
-            const float kq = Q4 ? qs * sc[(j & 1) * 4] : qs, ev = Q4 ? sc[(j & 1) * 4 + 1] : 0.f, v_unit = Q4 ? sc[(j & 1) * 4 + 2] : 1.f;
+            // 4 bits: factors of the K rows, exponents of the V rows (which the scores have in them) and their negative powers; one of each for the tile unless `varied`
+            const float *f4 = sc + (j & 1) * 400 + half * 64;
+            const bool varied = Q4 && sc[(j & 1) * 400 + 384] != 0.f;
+            const float kq = !Q4 ? qs : varied ? 1.f : qs * f4[0], ev = Q4 && !varied ? f4[128] : 0.f, v_unit = Q4 && !varied ? f4[256] : 1.f;
             // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
             auto finish = [&](int c0, uint32_t (&r)[32]) {
+                if (Q4 && varied) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 x = fma2(mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), *(const float2 *)(f4 + c0 + e)), make_float2(qs, qs),
+                                              *(const float2 *)(f4 + 128 + c0 + e));
+                        r[e] = __float_as_uint(x.x); r[e + 1] = __float_as_uint(x.y);
+                    }
+                }
                 if (Q8) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
@@ -768,14 +780,15 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             const float mb = m_used == -INFINITY ? 0.f : m_used;
             const float2 q2 = make_float2(kq, kq), m2 = make_float2(ev - mb, ev - mb);
             float2 ls = make_float2(0.f, 0.f);
-            auto weigh = [&](int c0, uint32_t (&r)[32]) {
+            auto weigh = [&](int c0, uint32_t (&r)[32], const bool own_units) {
                 uint32_t w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     const float2 t = fma2(make_float2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), q2, m2);
-                    // every second pair (bf16 pages by TMA) or every fourth on the FMA pipes, which the exponentials otherwise leave idle
-                    float2 p = (TMA ? k % 2 == 1 : k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
-                    ls = add2(ls, p);
+                    // every second pair (bf16 pages by TMA) or every fourth (8 bits) on the FMA pipes, which the exponentials otherwise leave idle; with 4 bits the
+                    // issue slots are short instead (every fourth: 1451 us, chunk of 2048 on 14336; none: 1384)
+                    float2 p = (TMA ? k % 2 == 1 : !Q4 && k % 4 == 3) ? exp2_poly2(t) : make_float2(ex2(t.x), ex2(t.y));
+                    ls = own_units ? fma2(p, *(const float2 *)(f4 + 256 + c0 + 2 * k), ls) : add2(ls, p);
                     if (Q8) p = mul2(p, *(const float2 *)(vs + c0 + 2 * k));
                     w[k] = Q4 ? pack_half(p.x, p.y) : pack(p.x, p.y);
                     if (FMT == KV_INT8) { r[2 * k] = __float_as_uint(p.x); r[2 * k + 1] = __float_as_uint(p.y); }
@@ -800,11 +813,11 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     tmem_st16(t_s + rest_column(c0), w);
                 }
             };
-            weigh(32, rb);
+            if (Q4 && varied) weigh(32, rb, true); else weigh(32, rb, false);
             tmem_ask32(t_s, ra);
             tmem_wait32(ra);
             finish(0, ra);
-            weigh(0, ra);
+            if (Q4 && varied) weigh(0, ra, true); else weigh(0, ra, false);
             l = Q4 ? fmaf(ls.x + ls.y, v_unit, l) : l + (ls.x + ls.y);
             tmem_st_wait();
             fence_before();
