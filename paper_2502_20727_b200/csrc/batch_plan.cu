@@ -26,116 +26,178 @@ struct PlanArgs {
     int *err;
 };
 
+// Sums that stop at the largest number: what is wanted may be more than there is by any amount.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { const uint32_t s = a + b; return s < a ? 0xffffffffu : s; }
+__device__ __forceinline__ uint2 add_sat(uint2 a, uint2 b) { return make_uint2(add_sat(a.x, b.x), add_sat(a.y, b.y)); }
+
 // Exclusive prefix sums of two numbers over the block's threads; the totals in `all`.
-__device__ __forceinline__ longlong2 block_scan(longlong2 v, longlong2 &all, longlong2 *part)
+__device__ __forceinline__ uint2 block_scan(uint2 v, uint2 &all, uint2 *part)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    longlong2 x = v;
+    auto before = [&](uint2 x) { // inclusive sums over the lanes, then one lane up
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long a = __shfl_up_sync(0xffffffffu, x.x, o), b = __shfl_up_sync(0xffffffffu, x.y, o);
-        if (lane >= o) { x.x += a; x.y += b; }
-    }
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint2 y = make_uint2(__shfl_up_sync(0xffffffffu, x.x, o), __shfl_up_sync(0xffffffffu, x.y, o));
+            if (lane >= o) x = add_sat(x, y);
+        }
+        return x;
+    };
+    const uint2 x = before(v);
     if (lane == 31) part[warp] = x;
     __syncthreads();
-    longlong2 w = lane < PLAN_WARPS ? part[lane] : make_longlong2(0, 0);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long a = __shfl_up_sync(0xffffffffu, w.x, o), b = __shfl_up_sync(0xffffffffu, w.y, o);
-        if (lane >= o) { w.x += a; w.y += b; }
-    }
-    all = make_longlong2(__shfl_sync(0xffffffffu, w.x, 31), __shfl_sync(0xffffffffu, w.y, 31));
-    const int before = warp ? warp - 1 : 0;
-    const long long bx = __shfl_sync(0xffffffffu, w.x, before), by = __shfl_sync(0xffffffffu, w.y, before);
+    const uint2 w = before(part[lane]);
+    all = make_uint2(__shfl_sync(0xffffffffu, w.x, 31), __shfl_sync(0xffffffffu, w.y, 31));
+    const uint2 warps = make_uint2(__shfl_sync(0xffffffffu, w.x, (warp + 31) & 31), __shfl_sync(0xffffffffu, w.y, (warp + 31) & 31));
+    const uint2 lanes = make_uint2(__shfl_up_sync(0xffffffffu, x.x, 1), __shfl_up_sync(0xffffffffu, x.y, 1));
     __syncthreads(); // `part` may be written again
-    return make_longlong2(x.x - v.x + (warp ? bx : 0), x.y - v.y + (warp ? by : 0));
+    const uint2 zero = make_uint2(0, 0);
+    return add_sat(warp ? warps : zero, lane ? lanes : zero);
 }
+static_assert(PLAN_WARPS == 32, "a lane per warp");
+
+// Positions and slots of the rows, entries of the tables' new pages.  cu: row offsets; at: places of the requests' first new pages among those taken.
+struct Fill {
+    const int *cu, *at;
+    int served, top, lg;
+    __device__ __forceinline__ int page_of(int pos, int page) const { return lg >= 0 ? pos >> lg : pos / page; }
+    template <int ROWS> __device__ __forceinline__ void rows(const PlanArgs &a, int rank, int ranks) const
+    {
+        for (int r0 = (rank * PLAN_THREADS + (int)threadIdx.x) * ROWS; r0 < a.n_tokens; r0 += ranks * PLAN_THREADS * ROWS) {
+            int b[ROWS], id[ROWS], pos[ROWS], j[ROWS];
+            if (r0 < served) {
+                int lo = 0, end = a.B; // cu[lo] <= r0 < cu[end]
+                while (end - lo > 1) {
+                    const int mid = (lo + end) >> 1;
+                    if (cu[mid] <= r0) lo = mid; else end = mid;
+                }
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    while (r0 + i < served && cu[lo + 1] <= r0 + i) ++lo; // ends: the last request's rows end at `served`
+                    b[i] = lo;
+                }
+            }
+            // the loads of all rows at once, one kind after the other
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) pos[i] = r0 + i < served ? a.lens[b[i]] : 0;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                id[i] = j[i] = -1;
+                if (r0 + i >= served) continue;
+                const int have = pos[i] ? page_of(pos[i] - 1, a.page) + 1 : 0;
+                pos[i] += r0 + i - cu[b[i]];
+                j[i] = page_of(pos[i], a.page);
+                id[i] = j[i] < have ? a.table[(long)b[i] * a.max_pages + j[i]] : __ldcg(a.free_pages + (top - 1 - (at[b[i]] + j[i] - have)));
+                if (j[i] < have) j[i] |= 0x80000000; // not a new page
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const int r = r0 + i, in_page = pos[i] - (j[i] & 0x7fffffff) * a.page;
+                if (r >= a.n_tokens) break;
+                const bool mine = r < served, good = mine && (uint32_t)id[i] < (uint32_t)a.n_pages;
+                if (mine && in_page == 0 && j[i] >= 0) a.table[(long)b[i] * a.max_pages + j[i]] = id[i]; // a new page's first row is always a new one
+                if (mine && !good) atomicOr(a.err, ERR_PAGE_RANGE);
+                a.positions[r] = mine ? pos[i] : -1;
+                a.slots[r] = good ? id[i] * a.page + in_page : -1;
+            }
+        }
+    }
+};
 
 __global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_constant__ PlanArgs a)
 {
     extern __shared__ int plan_sm[];
     int *cu = plan_sm, *at = cu + a.B + 1; // row offsets; a request's place among the pages given back or taken
-    __shared__ longlong2 part[PLAN_WARPS];
-    __shared__ int any_done;
+    int *list = cu; // before the row offsets are made: finished requests that this block looks after
+    __shared__ uint2 part[PLAN_WARPS];
+    __shared__ int n_done;
+    __shared__ volatile int any_bad;
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, rank = blockIdx.x, ranks = gridDim.x, warp = tid >> 5;
     const long capacity = (long)a.max_pages * a.page;
-    auto pages_of = [&](long n) { return (int)((n + a.page - 1) / a.page); };
+    const int lg = a.page & (a.page - 1) ? -1 : __ffs(a.page) - 1; // page sizes are mostly powers of two
+    auto page_of = [&](int pos) { return lg >= 0 ? pos >> lg : pos / a.page; };
+    auto pages_of = [&](int n) { return n ? page_of(n - 1) + 1 : 0; };
     auto flag = [&](int bit) { atomicOr(a.err, bit); };
+    auto set_flag = [&](int block) { // any_bad of a block of the cluster
+        const uint32_t mine = tc::smem_u32((const void *)&any_bad);
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ranks > 1 ? tc::mapa_shared(mine, block) : mine), "r"(1) : "memory");
+    };
 
     int n_free = *a.n_free;
     if (n_free < 0 || n_free > a.n_pages) {
         n_free = n_free < 0 ? 0 : a.n_pages;
         if (rank == 0 && tid == 0) flag(ERR_CAPACITY);
     }
-    if (tid == 0) any_done = 0;
+    // Finished requests: their pages join the pool.  Once as if all their entries named pages (then how many there are is known from the lengths);
+    // if that is not so, once more with entries outside the cache passed over.
+    if (tid == 0) n_done = any_bad = 0;
     __syncthreads();
-    // Finished requests: their pages are counted (by a warp each, as entries outside the cache are passed over), placed, and given back by the
-    // block whose turn it is.
+    bool some = false;
     for (int b = tid; b < a.B; b += PLAN_THREADS) {
-        const bool done = a.news[b] < 0;
-        at[b] = done ? -1 : 0;
-        if (done) any_done = 1;
+        at[b] = 0;
+        if (a.news[b] >= 0) continue;
+        some = true;
+        const int len = a.lens[b];
+        if (len >= 0 && len <= capacity) at[b] = pages_of(len);
+        else if (rank == 0) flag(ERR_CAPACITY);
+        if (b % ranks == rank) list[atomicAdd(&n_done, 1)] = b; // this block's; their order does not matter
     }
-    __syncthreads();
+    const bool any_done = __syncthreads_or(some);
     int top = n_free; // pages in the pool once all have been given back
-    if (any_done) {
-        for (int b = warp; b < a.B; b += PLAN_WARPS) {
-            if (at[b] == 0) continue; // the same for the whole warp
-            const long len = a.lens[b];
-            int count = 0;
-            if (len >= 0 && len <= capacity) {
-                const int have = pages_of(len);
-                for (int j0 = 0; j0 < have; j0 += 32) {
-                    const int id = j0 + lane < have ? a.table[(long)b * a.max_pages + j0 + lane] : -1;
-                    const bool good = id >= 0 && id < a.n_pages;
-                    if (rank == 0 && !good && j0 + lane < have) flag(ERR_PAGE_RANGE);
-                    count += __popc(__ballot_sync(0xffffffffu, good));
-                }
-            } else if (rank == 0 && lane == 0)
-                flag(ERR_CAPACITY);
-            __syncwarp();
-            if (lane == 0) at[b] = count;
+    for (bool again = false; any_done; again = true) {
+        if (again) { // pages that exist
+            for (int b = warp; b < a.B; b += PLAN_WARPS) {
+                if (a.news[b] >= 0) continue;
+                const int len = a.lens[b], have = len >= 0 && len <= capacity ? pages_of(len) : 0;
+                int count = 0;
+                for (int j = lane; j < have; j += 32) count += (uint32_t)a.table[(long)b * a.max_pages + j] < (uint32_t)a.n_pages;
+                count = __reduce_add_sync(0xffffffffu, count);
+                if (lane == 0) at[b] = count;
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        long long sum = n_free;
+        uint32_t sum = n_free;
         for (int b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
             const int b = b0 + tid;
-            longlong2 all;
-            const longlong2 before = block_scan(make_longlong2(b < a.B ? at[b] : 0, 0), all, part);
-            if (b < a.B) at[b] = (int)(sum + before.x < a.n_pages ? sum + before.x : a.n_pages);
-            sum += all.x;
+            uint2 all;
+            const uint2 before = block_scan(make_uint2(b < a.B && a.news[b] < 0 ? at[b] : 0, 0), all, part);
+            if (b < a.B) at[b] = (int)min(add_sat(sum, before.x), (uint32_t)a.n_pages);
+            sum = add_sat(sum, all.x);
         }
-        if (sum > a.n_pages) { // more pages than there are: some came back twice
-            if (rank == 0 && tid == 0) flag(ERR_CAPACITY);
-            sum = a.n_pages;
-        }
-        top = (int)sum;
-        __syncthreads();
-        for (int b = warp * ranks + rank; b < a.B; b += PLAN_WARPS * ranks) {
-            if (a.news[b] >= 0) continue;
-            const long len = a.lens[b];
-            if (len < 0 || len > capacity) continue;
-            const int have = pages_of(len);
+        top = (int)min(sum, (uint32_t)a.n_pages);
+        if (ranks > 1 && !again) tc::cluster_sync(); else __syncthreads(); // the places; and every block's flag is set to 0 before another one raises it
+        for (int k = warp; k < n_done; k += PLAN_WARPS) {
+            const int b = list[k], len = a.lens[b], have = len >= 0 && len <= capacity ? pages_of(len) : 0;
             int to = at[b];
+#pragma unroll 4
             for (int j0 = 0; j0 < have; j0 += 32) {
-                const int id = j0 + lane < have ? a.table[(long)b * a.max_pages + j0 + lane] : -1;
-                const unsigned good = __ballot_sync(0xffffffffu, id >= 0 && id < a.n_pages);
-                const int place = to + __popc(good & ((1u << lane) - 1));
-                if ((good >> lane & 1) && place < top) a.free_pages[place] = id;
-                to += __popc(good);
+                const int id = j0 + lane < have ? a.table[(long)b * a.max_pages + j0 + lane] : 0;
+                const bool good = j0 + lane < have && (uint32_t)id < (uint32_t)a.n_pages;
+                const unsigned all = __ballot_sync(0xffffffffu, good);
+                const int place = again ? to + __popc(all & ((1u << lane) - 1)) : to + lane;
+                if (good && place < top) a.free_pages[place] = id;
+                if (!again && j0 + lane < have && !good) {
+                    flag(ERR_PAGE_RANGE);
+                    for (int c = 0; c < ranks; ++c) set_flag(c);
+                }
+                to += again ? __popc(all) : 32;
             }
+        }
+        // Pages given back are in the pool.
+        if (ranks > 1) tc::cluster_sync(); else __syncthreads();
+        if (again || !any_bad) {
+            if (sum > (uint32_t)a.n_pages && rank == 0 && tid == 0) flag(ERR_CAPACITY); // more pages than there are: some came back twice
+            break;
         }
     }
 
     // Requests with new tokens: pages and rows wanted up to each, then the rows of those that are served.
-    long long wanted = 0, rows = 0;
+    uint32_t wanted = 0, rows = 0;
     int served = 0, taken = 0;
     for (int b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
-        long len = 0, n = 0;
-        int take = 0;
+        int len = 0, n = 0, take = 0;
         bool done = false, bad = false;
         if (b < a.B) {
             len = a.lens[b];
@@ -145,57 +207,39 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_c
             else if (len < 0 || len > capacity - n) { bad = true; n = 0; }
             if (n > 0) take = pages_of(len + n) - pages_of(len);
         }
-        longlong2 all, mine;
-        const longlong2 before = block_scan(make_longlong2(take, n), all, part);
-        const long long take_to = wanted + before.x + take, rows_to = rows + before.y + n;
-        const bool ok = (take == 0 || take_to <= top) && rows_to <= a.n_tokens;
-        const int n_ok = ok ? (int)n : 0, take_ok = ok ? take : 0;
-        const longlong2 got_before = block_scan(make_longlong2(n_ok, take_ok), mine, part);
+        uint2 all, mine;
+        const uint2 before = block_scan(make_uint2(take, n), all, part);
+        const uint32_t take_to = add_sat(add_sat(wanted, before.x), take), rows_to = add_sat(add_sat(rows, before.y), n);
+        const bool ok = (take == 0 || take_to <= (uint32_t)top) && rows_to <= (uint32_t)a.n_tokens;
+        const int n_ok = ok ? n : 0, take_ok = ok ? take : 0;
+        uint2 got = before;
+        if (__syncthreads_and(ok)) mine = all; // the usual case: all of them are served
+        else got = block_scan(make_uint2(take_ok, n_ok), mine, part);
         if (b < a.B) {
-            cu[b] = served + (int)got_before.x;
-            if (!done) at[b] = taken + (int)got_before.y;
+            cu[b] = served + (int)got.y;
+            if (!done) at[b] = taken + (int)got.x;
             if (b % ranks == rank) {
                 a.cu[b] = cu[b];
-                a.next_lens[b] = done ? 0 : (int)len + n_ok;
+                a.next_lens[b] = done ? 0 : len + n_ok;
                 if (bad || !ok) flag(ERR_CAPACITY);
             }
         }
-        wanted += all.x;
-        rows += all.y;
-        served += (int)mine.x;
-        taken += (int)mine.y;
+        wanted = add_sat(wanted, all.x);
+        rows = add_sat(rows, all.y);
+        served += (int)mine.y;
+        taken += (int)mine.x;
     }
     if (tid == 0) {
         cu[a.B] = served;
         if (rank == 0) a.cu[a.B] = served;
     }
-    // Pages given back are in the pool, and every block has read its size.
-    if (ranks > 1) tc::cluster_sync(); else __syncthreads();
+    if (ranks > 1 && !any_done) tc::cluster_sync(); else __syncthreads(); // every block has read the pool's size, and the offsets are there
     if (rank == 0 && tid == 0) *a.n_free_next = top - taken;
 
-    for (int r = rank * PLAN_THREADS + tid; r < a.n_tokens; r += ranks * PLAN_THREADS) {
-        int pos = -1, slot = -1;
-        if (r < served) {
-            int b = 0, end = a.B; // cu[b] <= r < cu[end]
-            while (end - b > 1) {
-                const int mid = (b + end) >> 1;
-                if (cu[mid] <= r) b = mid; else end = mid;
-            }
-            const int len = a.lens[b];
-            pos = len + (r - cu[b]);
-            const int j = pos / a.page, in_page = pos - j * a.page, have = pages_of(len);
-            int id;
-            if (j < have) id = a.table[(long)b * a.max_pages + j];
-            else {
-                id = __ldcg(a.free_pages + (top - 1 - (at[b] + j - have)));
-                if (in_page == 0) a.table[(long)b * a.max_pages + j] = id; // a new page's first row is always a new one
-            }
-            if (id < 0 || id >= a.n_pages) flag(ERR_PAGE_RANGE);
-            else slot = id * a.page + in_page;
-        }
-        a.positions[r] = pos;
-        a.slots[r] = slot;
-    }
+    // where the rows are many, four to a thread share a search
+    const Fill f{cu, at, served, top, lg};
+    if (a.n_tokens > ranks * PLAN_THREADS) f.rows<4>(a, rank, ranks);
+    else f.rows<1>(a, rank, ranks);
 }
 
 } // namespace

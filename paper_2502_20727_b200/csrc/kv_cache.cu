@@ -90,12 +90,36 @@ template <> __device__ __forceinline__ void store8<bf16>(bf16 *p, const float (&
     *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <typename T> __device__ __forceinline__ void store4(T *p, float a, float b, float c, float d);
-template <> __device__ __forceinline__ void store4<float>(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
-template <> __device__ __forceinline__ void store4<bf16>(bf16 *p, float a, float b, float c, float d)
+// The values of eight bytes of a 4-bit row: eight dims of the first half and eight of the second.  code * scale + smallest is rounded once: to float32,
+// or, by a product in bf16x2, to bf16.  A code is exact under the exponent of 2^23 (2^7 in bf16), less that.
+__device__ __forceinline__ void values4(uint2 w, uint2 par, float *low, float *high)
 {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(a, b), hi = __floats2bfloat162_rn(c, d);
-    *(uint2 *)p = make_uint2(*(const uint32_t *)&lo, *(const uint32_t *)&hi);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint32_t p = half ? par.y : par.x;
+        const float s = kv4_scale(p), m = kv4_min(p);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fmaf(__uint_as_float(0x4b000000u | ((i < 4 ? w.x : w.y) >> (8 * (i & 3) + 4 * half) & 15u)) - 8388608.f, s, m);
+        store8<float>(half ? high : low, x);
+    }
+}
+__device__ __forceinline__ void values4(uint2 w, uint2 par, bf16 *low, bf16 *high)
+{
+    const uint32_t c128 = widen_const();
+    const uint32_t b[4] = {__byte_perm(w.x, 0, 0x4140), __byte_perm(w.x, 0, 0x4342), __byte_perm(w.y, 0, 0x4140), __byte_perm(w.y, 0, 0x4342)};
+    const auto h = [](uint32_t x) { return *(const __nv_bfloat162 *)&x; };
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint32_t p = half ? par.y : par.x, s = __byte_perm(p, 0, 0x1010), m = __byte_perm(p, 0, 0x3232);
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 v = __hfma2(__hsub2(h(and_or(b[i] >> (4 * half), 0x000f000fu, c128)), h(c128)), h(s), h(m));
+            x[i] = *(const uint32_t *)&v;
+        }
+        *(uint4 *)(half ? high : low) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
 }
 
 __device__ __forceinline__ uint32_t e4m3_x4(float a, float b, float c, float d)
@@ -168,56 +192,86 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-// smallest and largest of eight elements, NaN if one is
-__device__ __forceinline__ float2 range_of(const Raw8<bf16> &r)
+// Smallest and largest element of the 16 x LANES elements of a group of lanes, NaN if one is.
+template <int LANES> __device__ __forceinline__ float2 range_of(const Raw8<bf16> (&r)[2])
 {
-    const uint4 u = r.u;
+    const uint4 u = r[0].u, v = r[1].u;
     const auto h = [](uint32_t w) { return *(const __nv_bfloat162 *)&w; };
-    const __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(h(u.x), h(u.y)), __hmin2_nan(h(u.z), h(u.w)));
-    const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(h(u.x), h(u.y)), __hmax2_nan(h(u.z), h(u.w)));
-    return make_float2(min_nan(__low2float(lo), __high2float(lo)), max_nan(__low2float(hi), __high2float(hi)));
+    const auto w = [](__nv_bfloat162 v) { return *(const uint32_t *)&v; };
+    const auto least = [&](uint4 a) { return __hmin2_nan(__hmin2_nan(h(a.x), h(a.y)), __hmin2_nan(h(a.z), h(a.w))); };
+    const auto most = [&](uint4 a) { return __hmax2_nan(__hmax2_nan(h(a.x), h(a.y)), __hmax2_nan(h(a.z), h(a.w))); };
+    const uint32_t lo = w(__hmin2_nan(least(u), least(v))), hi = w(__hmax2_nan(most(u), most(v))) ^ 0x80008000u;
+    __nv_bfloat162 x = __hmin2_nan(h(__byte_perm(lo, hi, 0x5410)), h(__byte_perm(lo, hi, 0x7632))); // (smallest, minus the largest)
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) x = __hmin2_nan(x, h(__shfl_xor_sync(0xffffffffu, w(x), o)));
+    return make_float2(__uint_as_float(w(x) << 16), __uint_as_float((w(x) & 0xffff0000u) ^ 0x80000000u));
 }
-__device__ __forceinline__ float2 range_of(const Raw8<float> &r)
+template <int LANES> __device__ __forceinline__ float2 range_of(const Raw8<float> (&r)[2])
 {
-    const float4 a = r.a, b = r.b;
-    return make_float2(min_nan(min_nan(min_nan(a.x, a.y), min_nan(a.z, a.w)), min_nan(min_nan(b.x, b.y), min_nan(b.z, b.w))),
-                       max_nan(max_nan(max_nan(a.x, a.y), max_nan(a.z, a.w)), max_nan(max_nan(b.x, b.y), max_nan(b.z, b.w))));
+    const auto least = [](const Raw8<float> &q) {
+        return min_nan(min_nan(min_nan(q.a.x, q.a.y), min_nan(q.a.z, q.a.w)), min_nan(min_nan(q.b.x, q.b.y), min_nan(q.b.z, q.b.w)));
+    };
+    const auto most = [](const Raw8<float> &q) {
+        return max_nan(max_nan(max_nan(q.a.x, q.a.y), max_nan(q.a.z, q.a.w)), max_nan(max_nan(q.b.x, q.b.y), max_nan(q.b.z, q.b.w)));
+    };
+    float lo = min_nan(least(r[0]), least(r[1])), hi = max_nan(most(r[0]), most(r[1]));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    return make_float2(lo, hi);
 }
-// Four 4-bit codes, one per byte, of x >= m: (x - m) / s by its correctly rounded quotient, the integer as in int8_x4
+// 1 / s, rounded to nearest, for a bf16 number s from 2^-60 on: one Newton step from the approximate reciprocal (the same bits as the division's for
+// every such s; the division's own code has a branch for numbers that do not occur here)
+__device__ __forceinline__ float reciprocal(float s)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+    return fmaf(fmaf(-s, y, 1.f), y, y);
+}
+// Four 4-bit codes, one per byte, of x >= m: (x - m) / s by its correctly rounded quotient, the integer as in int8_x4; two at a time
 __device__ __forceinline__ uint32_t int4_x4(const float *x, float m, float s, float inv)
 {
     uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float d = __fsub_rn(x[i], m), q = __fmul_rn(d, inv);
-        b[i] = __float_as_uint(__fadd_rn(fmaf(fmaf(-q, s, d), inv, q), 12582912.f));
+    for (int i = 0; i < 4; i += 2) {
+        const float2 d = add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), q = mul2(d, make_float2(inv, inv));
+        const float2 c = add2(fma2(fma2(q, make_float2(-s, -s), d), make_float2(inv, inv), q), make_float2(12582912.f, 12582912.f));
+        b[i] = __float_as_uint(c.x);
+        b[i + 1] = __float_as_uint(c.y);
     }
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 
 // Rows a lane has in flight, tokens of a block.  FEW: few rows in all, which then spread over more blocks.
-template <typename T, int D, bool FEW> struct KvShape {
-    static constexpr int LPR = D / 8, PER_PASS = KV_THREADS / LPR; // lanes per row, rows per pass of the block
-    static constexpr int TT = (FEW ? 1 : sizeof(T) == 4 ? 4 : 8) * PER_PASS / ROWS, UNITS = TT * ROWS / PER_PASS;
+// 4 bits: a lane has 16 elements of a row (read: eight bytes, eight elements of either half; written: of one half, two Raw8) of four rows, so that what is
+// done once per half row is done by half as many lanes.
+template <typename T, int D, bool FEW, bool INT4> struct KvShape {
+    static constexpr int LPR = D / (INT4 ? 16 : 8), PER_PASS = KV_THREADS / LPR; // lanes per row, rows per pass of the block
+    static constexpr int TT = (FEW ? 1 : (sizeof(T) == 4 ? 4 : 8) / (INT4 ? 2 : 1)) * PER_PASS / ROWS, UNITS = TT * ROWS / PER_PASS;
 };
 
 template <typename T, int FMT, int D, bool FEW>
 __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, RaggedBatch rb, const int32_t *slots, const T *k, const T *v, long k_stride, long v_stride, int *err)
 {
-    using S = KvShape<T, D, FEW>;
-    constexpr int LPR = S::LPR, TT = S::TT, UNITS = S::UNITS;
+    using S = KvShape<T, D, FEW, FMT == KV_INT4>;
+    constexpr int LPR = S::LPR, TT = S::TT, UNITS = S::UNITS, PARTS = FMT == KV_INT4 ? 2 : 1; // Raw8s of a lane and row
     typedef typename KvElem<FMT>::type E;
     __shared__ long base[TT];
     pdl_launch_dependents();
     pdl_wait();
     const int t0 = blockIdx.x * TT, r0 = blockIdx.y * ROWS, li = threadIdx.x % LPR, g = threadIdx.x / LPR;
-    Raw8<T> raw[UNITS];
+    Raw8<T> raw[UNITS][PARTS];
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) { // row 2h: K of head h, 2h + 1: V
         const int id = i * S::PER_PASS + g, t = t0 + id / ROWS, r = r0 + id % ROWS;
-        raw[i] = Raw8<T>{};
-        if (t < rb.n_tokens && (r >> 1) < kv.nkv)
-            raw[i] = *(const Raw8<T> *)((r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)(r >> 1) * D + li * 8);
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            raw[i][q] = Raw8<T>{};
+            if (t < rb.n_tokens && (r >> 1) < kv.nkv)
+                raw[i][q] = *(const Raw8<T> *)((r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)(r >> 1) * D + (li * PARTS + q) * 8);
+        }
     }
     if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, slots, t0, base, err);
     __syncthreads();
@@ -227,40 +281,40 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(PagedKv kv, Ragged
         const long where = base[id / ROWS], row = where + (long)h * kv.page;
         const bool ok = where >= 0 && h < kv.nkv;
         float x[8];
-        get(raw[i], x);
+        get(raw[i][0], x);
         if constexpr (FMT == KV_F32 || FMT == KV_BF16) {
             if (ok) store8<E>((E *)(r & 1 ? kv.v : kv.k) + row * D + li * 8, x);
             continue;
         }
         if constexpr (FMT == KV_INT4) {
-            // lanes li and li ^ LPR / 2 hold the same bytes' low and high codes
+            // lanes li and li ^ LPR / 2 have the same bytes' low and high codes
             constexpr int HALF = LPR / 2;
             const bool high = li >= HALF;
-            float2 range = range_of(raw[i]);
-#pragma unroll
-            for (int o = HALF / 2; o > 0; o >>= 1) {
-                range.x = min_nan(range.x, __shfl_xor_sync(0xffffffffu, range.x, o));
-                range.y = max_nan(range.y, __shfl_xor_sync(0xffffffffu, range.y, o));
-            }
+            const float2 range = range_of<HALF>(raw[i]);
             // down to bf16: towards zero, or away from it where negative
             const uint32_t bits = __float_as_uint(range.x), mb = (range.x < 0.f ? bits + 0xffffu : bits) & 0xffff0000u;
             const float m = __uint_as_float(mb), spread = __fsub_rn(range.y, m);
-            const float s = fmaxf(__bfloat162float(__float2bfloat16_rn(__fdiv_rn(spread, 15.f))), 0x1p-60f), inv = __frcp_rn(s);
+            // spread / 15 as amax / 127 below
+            const float q0 = spread * (1.f / 15.f), step = fmaf(fmaf(-q0, 15.f, spread), 1.f / 15.f, q0);
+            const float s = fmaxf(__bfloat162float(__float2bfloat16_rn(step)), 0x1p-60f), inv = reciprocal(s);
             const bool bad = !(spread < INFINITY); // a NaN or an infinity in the half, or a spread that is no float
-            uint32_t own = int4_x4(x, m, s, inv), other = int4_x4(x + 4, m, s, inv);
-            // this lane keeps the first four dims (low half) or the last four (high half); bit 7 of the others' codes: `bad`
-            if (high) { const uint32_t t = own; own = other; other = t; }
-            other = __shfl_xor_sync(0xffffffffu, bad ? 0x80u : other, HALF);
-            const bool row_bad = bad || (other & 0x80u);
+            float y[8];
+            get(raw[i][1], y);
+            uint2 own = make_uint2(int4_x4(x, m, s, inv), int4_x4(x + 4, m, s, inv)), other = make_uint2(int4_x4(y, m, s, inv), int4_x4(y + 4, m, s, inv));
+            // this lane keeps the first eight dims (low half) or the last eight (high half); bit 7 of the others' codes: `bad`
+            if (high) { const uint2 t = own; own = other; other = t; }
+            other = make_uint2(__shfl_xor_sync(0xffffffffu, bad ? 0x80u : other.x, HALF), __shfl_xor_sync(0xffffffffu, other.y, HALF));
+            const bool row_bad = bad || (other.x & 0x80u);
             if (!ok) continue;
-            *(uint32_t *)((uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + (li & (HALF - 1)) * 8 + high * 4) =
-                row_bad ? 0u : high ? other | (own << 4) : own | (other << 4);
+            const uint2 lo = high ? other : own, hi = high ? own : other;
+            *(uint2 *)((uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + (li & (HALF - 1)) * 16 + high * 8) =
+                row_bad ? make_uint2(0, 0) : make_uint2(lo.x | (hi.x << 4), lo.y | (hi.y << 4));
             if ((li & (HALF - 1)) == 0)
                 ((uint32_t *)(r & 1 ? kv.vs : kv.ks))[2 * row + high] = row_bad ? 0x7fc07fc0u : (__float_as_uint(s) >> 16) | mb;
             continue;
         }
         // largest magnitude of the row; a NaN wins (comparisons on the bit patterns of |x|)
-        uint32_t m = top_of(raw[i]);
+        uint32_t m = top_of(raw[i][0]);
 #pragma unroll
         for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
         const float amax = __uint_as_float(m);
@@ -295,7 +349,7 @@ template <typename T, int FMT, int D, bool FEW>
 __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedBatch rb, T *k, T *v, long k_stride, long v_stride, int *err)
 {
     typedef typename KvElem<FMT>::type E;
-    using S = KvShape<E, D, FEW>;
+    using S = KvShape<E, D, FEW, FMT == KV_INT4>;
     constexpr int LPR = S::LPR, TT = S::TT, UNITS = S::UNITS;
     __shared__ long base[TT];
     pdl_launch_dependents();
@@ -303,17 +357,15 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedB
     const int t0 = blockIdx.x * TT, r0 = blockIdx.y * ROWS, li = threadIdx.x % LPR, g = threadIdx.x / LPR;
     if (threadIdx.x < 32) locate_tokens<TT>(kv, rb, nullptr, t0, base, err);
     __syncthreads();
-    if constexpr (FMT == KV_INT4) { // a lane: four bytes of a row, hence four dims of either half
-        uint32_t codes[UNITS];
-        uint2 par[UNITS];
+    if constexpr (FMT == KV_INT4) {
+        uint2 codes[UNITS], par[UNITS];
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             const int id = i * S::PER_PASS + g, r = r0 + id % ROWS, h = r >> 1;
             const long where = base[id / ROWS], row = where + (long)h * kv.page;
-            codes[i] = 0;
-            par[i] = make_uint2(0, 0);
+            codes[i] = par[i] = make_uint2(0, 0);
             if (where >= 0 && h < kv.nkv) {
-                codes[i] = *(const uint32_t *)((const uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + li * 4);
+                codes[i] = *(const uint2 *)((const uint8_t *)(r & 1 ? kv.v : kv.k) + row * (D / 2) + li * 8);
                 par[i] = kv4_params(r & 1 ? kv.vs : kv.ks, row);
             }
         }
@@ -321,14 +373,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(PagedKv kv, RaggedB
         for (int i = 0; i < UNITS; ++i) {
             const int id = i * S::PER_PASS + g, t = t0 + id / ROWS, r = r0 + id % ROWS, h = r >> 1;
             if (base[id / ROWS] < 0 || h >= kv.nkv) continue;
-            T *dst = (r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)h * D + li * 4;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const uint32_t p = half ? par[i].y : par[i].x, c = codes[i] >> (4 * half);
-                const float s = kv4_scale(p), m = kv4_min(p);
-                store4<T>(dst + half * (D / 2), fmaf((float)(c & 15), s, m), fmaf((float)(c >> 8 & 15), s, m), fmaf((float)(c >> 16 & 15), s, m),
-                          fmaf((float)(c >> 24 & 15), s, m));
-            }
+            T *dst = (r & 1 ? v + (long)t * v_stride : k + (long)t * k_stride) + (long)h * D + li * 8;
+            values4(codes[i], par[i], dst, dst + D / 2);
         }
     } else {
         Raw8<E> raw[UNITS];
@@ -365,9 +411,9 @@ cudaError_t launch(const PagedKv &kv, const RaggedBatch &rb, const int32_t *slot
     typedef typename std::conditional<WRITE, T, typename KvElem<FMT>::type>::type In;
     auto grid = [&](int tt) { return dim3((unsigned)((rb.n_tokens + tt - 1) / tt), (unsigned)((2 * kv.nkv + ROWS - 1) / ROWS)); };
     // under one block per SM the copy is a matter of latency (64 tokens x 16 rows appended and read back: 9.5 -> 7.2 us)
-    const dim3 full = grid(KvShape<In, D, false>::TT);
+    const dim3 full = grid(KvShape<In, D, false, FMT == KV_INT4>::TT);
     if ((long)full.x * full.y < sm_count()) {
-        const dim3 few = grid(KvShape<In, D, true>::TT);
+        const dim3 few = grid(KvShape<In, D, true, FMT == KV_INT4>::TT);
         if (WRITE) return launch_kernel(kv_write_kernel<T, FMT, D, true>, few, dim3(KV_THREADS), 0, st, 0, kv, rb, slots, (const T *)k, (const T *)v, ks, vs, err);
         return launch_kernel(kv_read_kernel<T, FMT, D, true>, few, dim3(KV_THREADS), 0, st, 0, kv, rb, (T *)k, (T *)v, ks, vs, err);
     }
