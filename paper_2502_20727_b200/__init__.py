@@ -216,77 +216,22 @@ def gemm_bf16_sum_static(a: torch.Tensor, w: torch.Tensor, out: torch.Tensor, er
 # Storage formats of a paged cache by the pages' dtype (SPD_KV_*); the 8-bit ones have one scale per cached row, uint8 pages hold two
 # 4-bit codes per byte and have a (scale, smallest value) pair per half of a cached row.
 KV_FORMATS = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3, torch.uint8: 5}
-KV_INT4 = 5
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+_ops = None
 
 
-# These run once per layer and token of a serving loop, so their checks stay cheap: device indices instead of device objects,
-# one comparison where one says it.
-def _kv_cache(k_pages, v_pages, k_scales, v_scales) -> spd_kv_cache:
-    dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
-    fmt = KV_FORMATS.get(dtype)
-    if fmt is None or len(shape) != 4 or dev < 0 or not k_pages.is_contiguous():
-        raise ValueError("k_pages: contiguous CUDA tensor [n_pages, n_kv_heads, page, head_dim] of float32, bfloat16, float8_e4m3fn or int8, "
-                         "or uint8 with head_dim / 2 bytes per row (4 bits)")
-    if v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev or not v_pages.is_contiguous():
-        raise ValueError("v_pages: like k_pages")
-    if fmt == KV_INT4:
-        for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
-            if s is None or s.get_device() != dev or s.dtype is not torch.bfloat16 or s.shape != shape[:3] + (2, 2) or not s.is_contiguous():
-                raise ValueError(f"{name}: contiguous bfloat16 [n_pages, n_kv_heads, page, 2, 2] on the pages' device (4-bit caches)")
-        return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *shape[:3], 2 * shape[3], fmt)
-    if fmt >= 2:
-        for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
-            if s is None or s.get_device() != dev or s.dtype is not torch.float32 or s.shape != shape[:3] or not s.is_contiguous():
-                raise ValueError(f"{name}: contiguous float32 [n_pages, n_kv_heads, page] on the pages' device (8-bit caches)")
-        return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *shape, fmt)
-    if k_scales is not None or v_scales is not None:
-        raise ValueError("k_scales / v_scales: for 8-bit and 4-bit caches only")
-    return spd_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, *shape, fmt)
-
-
-def _int32(name: str, t: torch.Tensor, dev: int, shape) -> int:
-    if t.dtype is not torch.int32 or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous int32 tensor {list(shape)} on the pages' device")
-    return t.data_ptr()
-
-
-def _ragged(dev: int, cu_new, seq_lens, block_table, n_tokens: int) -> spd_ragged:
-    if block_table.dim() != 2:
-        raise ValueError("block_table: [B, max_pages]")
-    B, width = block_table.shape
-    return spd_ragged(_int32("cu_new", cu_new, dev, (B + 1,)), _int32("seq_lens", seq_lens, dev, (B,)),
-                      _int32("block_table", block_table, dev, (B, width)), B, width, n_tokens)
-
-
-def _rows(name: str, t: torch.Tensor, dev: int, heads: int, d: int) -> int:
-    """Checks a [n_tokens, heads, head_dim] tensor whose heads lie side by side; returns the elements between its rows."""
-    n, h, e = t.shape
-    row, head, one = t.stride()
-    if t.get_device() != dev or t.dtype not in _DTYPES or h != heads or e != d or one != 1 or (head != d and heads > 1):
-        raise ValueError(f"{name}: float32 or bfloat16 [n_tokens, {heads}, {d}] on the pages' device, heads side by side in a row")
-    return row if n > 1 else heads * d
-
-
-def _flag(err: torch.Tensor, dev: int) -> int:
-    if err.get_device() != dev or err.dtype is not torch.int32 or err.numel() < 1:
-        raise ValueError("err: int32 tensor on the pages' device")
-    return err.data_ptr()
-
-
-try:
-    _raw_stream = torch._C._cuda_getCurrentRawStream
-except AttributeError:  # a torch built without CUDA
-    def _raw_stream(dev: int) -> int:
-        return torch.cuda.current_stream(dev).cuda_stream
-
-
-def _call_on(dev: int, fn, *args) -> int:
-    """fn(*args, stream) with `dev` current, on its current stream."""
-    if torch.cuda.current_device() == dev:
-        return fn(*args, _raw_stream(dev))
-    with torch.cuda.device(dev):
-        return fn(*args, _raw_stream(dev))
+def _operators():
+    """The operators' calls (csrc/binding.cpp): checks, marshalling and allocation without the interpreter, as they run once per layer and token
+    of a serving loop."""
+    global _ops
+    if _ops is None:
+        load_library()
+        try:
+            from . import _calls
+        except ImportError as e:
+            raise ImportError("the package's _calls module is missing: run `python -m paper_2502_20727_b200.build`") from e
+        _calls.set_check(_check)
+        _ops = _calls
+    return _ops
 
 
 def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
@@ -298,33 +243,14 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     k, v: [n_tokens, n_kv_heads, head_dim]; rows cu_new[b] .. cu_new[b+1]-1 are sequence b's, at positions seq_lens[b] on.
     err: int32 tensor that collects error bits (1 page id out of range, 2 position outside the block table); it is not read
     back here."""
-    lib = load_library()
-    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
-    dev = k_pages.get_device()
-    if k.dtype is not v.dtype or k.shape != v.shape:
-        raise ValueError("k and v: same dtype and shape")
-    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
-    r = _ragged(dev, cu_new, seq_lens, block_table, k.shape[0])
-    rc = _call_on(dev, lib.spd_kv_write, c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, dev))
-    if rc:
-        _check("spd_kv_write", rc)
+    (_ops or _operators()).kv_write(k, v, k_pages, v_pages, cu_new, seq_lens, block_table, err, k_scales, v_scales)
 
 
 def kv_write_slots(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor, *, err: torch.Tensor,
                    k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None) -> None:
     """kv_write for rows whose places are known: row t goes to slot slots[t] = page id * page size + row of the page (negative: nowhere),
     e.g. of a BatchPlan; see spd_kv_write_slots."""
-    lib = load_library()
-    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
-    dev = k_pages.get_device()
-    if k.dtype is not v.dtype or k.shape != v.shape:
-        raise ValueError("k and v: same dtype and shape")
-    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
-    n = k.shape[0]
-    rc = _call_on(dev, lib.spd_kv_write_slots, c, _int32("slots", slots, dev, (n,)), n, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype],
-                  _flag(err, dev))
-    if rc:
-        _check("spd_kv_write_slots", rc)
+    (_ops or _operators()).kv_write_slots(k, v, k_pages, v_pages, slots, err, k_scales, v_scales)
 
 
 def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, *,
@@ -333,24 +259,11 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, cu: torch.Tensor, star
     """Cached rows as values: row i of sequence b (rows cu[b] .. cu[b+1]-1) is position starts[b] + i; see spd_kv_read.
     Returns (k, v), each [n_tokens, n_kv_heads, head_dim] of dtype; `out` gives both tensors instead of n_tokens and dtype.
     Rows outside every sequence are left as they are (undefined where the tensors are made here)."""
-    lib = load_library()
-    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
-    dev = k_pages.get_device()
-    if out is None:
-        if n_tokens is None or dtype not in _DTYPES:
-            raise ValueError("n_tokens and a dtype of float32 or bfloat16, or out")
-        k = torch.empty((n_tokens, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_pages.device)
-        v = torch.empty_like(k)
-    else:
-        k, v = out
-        if k.dtype is not v.dtype or k.shape != v.shape:
-            raise ValueError("out: two tensors of one dtype and shape")
-    ks, vs = _rows("k", k, dev, c.n_kv_heads, c.head_dim), _rows("v", v, dev, c.n_kv_heads, c.head_dim)
-    r = _ragged(dev, cu, starts, block_table, k.shape[0])
-    rc = _call_on(dev, lib.spd_kv_read, c, r, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPES[k.dtype], _flag(err, dev))
-    if rc:
-        _check("spd_kv_read", rc)
-    return k, v
+    if out is not None:
+        return (_ops or _operators()).kv_read(k_pages, v_pages, cu, starts, block_table, err, 0, -1, k_scales, v_scales, *out)
+    if n_tokens is None or dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("n_tokens and a dtype of float32 or bfloat16, or out")
+    return (_ops or _operators()).kv_read(k_pages, v_pages, cu, starts, block_table, err, n_tokens, dtype is torch.bfloat16, k_scales, v_scales, None, None)
 
 
 def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
@@ -364,37 +277,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     the cache already.  max_new, max_context: host bounds of a sequence's new tokens and of its whole length.  scale:
     1/sqrt(head_dim) by default.  workspace: uint8 tensor to use instead of allocating one where the call needs one (calls
     that may overlap need one each).  err collects error bits as in kv_write."""
-    lib = load_library()
-    c = _kv_cache(k_pages, v_pages, k_scales, v_scales)
-    dev = k_pages.get_device()
-    n, nq, d = q.shape
-    qs = _rows("q", q, dev, nq, c.head_dim)
-    if out is None:
-        out = q.new_empty((n, nq, d))
-        os_ = nq * d
-    else:
-        if out.dtype is not q.dtype or out.shape != q.shape:
-            raise ValueError("out: shape and dtype of q")
-        os_ = _rows("out", out, dev, nq, d)
-    r = _ragged(dev, cu_new, seq_lens, block_table, n)
-    dtype = _DTYPES[q.dtype]
-    ws_ptr = ws_bytes = 0
-    if workspace is not None:
-        if workspace.get_device() != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-            raise ValueError("workspace: contiguous uint8 tensor on the pages' device")
-        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
-    args = (c, r, q.data_ptr(), qs, out.data_ptr(), os_, dtype, nq, max_new, max_context, d ** -0.5 if scale is None else scale, window, sinks)
-    flag = _flag(err, dev)
-    rc = _call_on(dev, lib.spd_paged_attention, *args, ws_ptr, ws_bytes, flag)
-    if rc == SPD_EWORKSPACE and workspace is None:  # nothing ran: this call wants one
-        need = ctypes.c_size_t(0)
-        _check("spd_paged_attention_workspace_bytes", lib.spd_paged_attention_workspace_bytes(
-            c, r.B, n, dtype, nq, max_new, max_context, window, sinks, need))
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        rc = _call_on(dev, lib.spd_paged_attention, *args, workspace.data_ptr(), need.value, flag)
-    if rc:
-        _check("spd_paged_attention", rc)
-    return out
+    return (_ops or _operators()).paged_attention(q, k_pages, v_pages, cu_new, seq_lens, block_table, max_new, max_context, err, window, sinks, scale,
+                                                    k_scales, v_scales, out, workspace)
 
 
 RELEASE = -1  # new_lens entry of a request that is finished
@@ -418,23 +302,8 @@ def plan_batch(seq_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torc
     block_table [B, max_pages] gets the ids of new pages, which are taken from free_pages[:n_free]; n_tokens: room for rows.  The
     plan's cu_new, with seq_lens and block_table, is what kv_write and paged_attention take; its slots are what kv_write_slots takes.
     out: tensors to fill instead of new ones; its n_free may be the argument.  All tensors are contiguous int32."""
-    lib = load_library()
-    dev = block_table.get_device()
-    if block_table.dim() != 2 or dev < 0:
-        raise ValueError("block_table: CUDA tensor [B, max_pages]")
-    B, width = block_table.shape
-    if out is None:
-        buf = block_table.new_empty(2 * B + 2 + 2 * n_tokens, dtype=torch.int32)
-        out = BatchPlan(*buf.split((B + 1, n_tokens, n_tokens, B, 1)))
-    pool = spd_page_pool(_int32("free_pages", free_pages, dev, (n_pages,)), _int32("n_free", n_free, dev, (1,)),
-                         _int32("out.n_free", out.n_free, dev, (1,)), n_pages, page)
-    rc = _call_on(dev, lib.spd_plan_batch, pool, _int32("seq_lens", seq_lens, dev, (B,)), _int32("new_lens", new_lens, dev, (B,)), B,
-                  _int32("block_table", block_table, dev, (B, width)), width, n_tokens, _int32("out.cu_new", out.cu_new, dev, (B + 1,)),
-                  _int32("out.positions", out.positions, dev, (n_tokens,)), _int32("out.slots", out.slots, dev, (n_tokens,)),
-                  _int32("out.next_lens", out.next_lens, dev, (B,)), _flag(err, dev))
-    if rc:
-        _check("spd_plan_batch", rc)
-    return out
+    plan = (_ops or _operators()).plan_batch(seq_lens, new_lens, block_table, free_pages, n_free, page, n_pages, n_tokens, err, out)
+    return plan if out is not None else BatchPlan._make(plan)
 
 
 TIER_NAMES = ("TP", "ISB", "SB", "ESB")
