@@ -56,42 +56,59 @@ __device__ __forceinline__ uint2 block_scan(uint2 v, uint2 &all, uint2 *part)
 static_assert(PLAN_WARPS == 32, "a lane per warp");
 
 // Positions and slots of the rows, entries of the tables' new pages.  cu: row offsets; at: places of the requests' first new pages among those taken.
+// A warp takes GROUPS x 32 consecutive rows: one search for the first one's request, then, 32 rows at a time, the next 32 offsets in the lanes.  (A search
+// per row, or one per thread with four rows each, whose stores then lie apart: 13 us of a mixed step's 26.)
 struct Fill {
     const int *cu, *at;
     int served, top, lg;
     __device__ __forceinline__ int page_of(int pos, int page) const { return lg >= 0 ? pos >> lg : pos / page; }
-    template <int ROWS> __device__ __forceinline__ void rows(const PlanArgs &a, int rank, int ranks) const
+    template <int GROUPS> __device__ __forceinline__ void rows(const PlanArgs &a, int rank, int ranks) const
     {
-        for (int r0 = (rank * PLAN_THREADS + (int)threadIdx.x) * ROWS; r0 < a.n_tokens; r0 += ranks * PLAN_THREADS * ROWS) {
-            int b[ROWS], id[ROWS], pos[ROWS], j[ROWS];
-            if (r0 < served) {
-                int lo = 0, end = a.B; // cu[lo] <= r0 < cu[end]
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        for (int w0 = (rank * PLAN_WARPS + warp) * 32 * GROUPS; w0 < a.n_tokens; w0 += ranks * PLAN_THREADS * GROUPS) {
+            int b[GROUPS], id[GROUPS], pos[GROUPS], j[GROUPS];
+            if (w0 < served) {
+                int lo = 0, end = a.B; // cu[lo] <= w0 < cu[end]; the same for the warp
                 while (end - lo > 1) {
                     const int mid = (lo + end) >> 1;
-                    if (cu[mid] <= r0) lo = mid; else end = mid;
+                    if (cu[mid] <= w0) lo = mid; else end = mid;
                 }
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i) {
-                    while (r0 + i < served && cu[lo + 1] <= r0 + i) ++lo; // ends: the last request's rows end at `served`
-                    b[i] = lo;
+                for (int i = 0; i < GROUPS; ++i) {
+                    const int r = w0 + 32 * i + lane, last = min(w0 + 32 * i + 31, served - 1);
+                    while (true) { // lanes' requests: lo and how many of the next 32 start at or before the row
+                        const int start = lo + 1 + lane < a.B ? cu[lo + 1 + lane] : served;
+                        int n = 0;
+                        if (__shfl_sync(0xffffffffu, start, 0) <= last) {
+#pragma unroll
+                            for (int step = 16; step > 0; step >>= 1) n += __shfl_sync(0xffffffffu, start, n + step - 1) <= r ? step : 0;
+                            n += __shfl_sync(0xffffffffu, start, n) <= r;
+                        }
+                        if (cu[lo] <= r) b[i] = lo + n; // always so in the first turn
+                        // all 32 start within the group: there may be more
+                        if (__shfl_sync(0xffffffffu, start, 31) > last) break;
+                        lo += 32;
+                    }
+                    lo = __shfl_sync(0xffffffffu, b[i], last - (w0 + 32 * i) < 0 ? 0 : last - (w0 + 32 * i)); // the last row's, for the next group
                 }
             }
             // the loads of all rows at once, one kind after the other
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) pos[i] = r0 + i < served ? a.lens[b[i]] : 0;
+            for (int i = 0; i < GROUPS; ++i) pos[i] = w0 + 32 * i + lane < served ? a.lens[b[i]] : 0;
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
+            for (int i = 0; i < GROUPS; ++i) {
+                const int r = w0 + 32 * i + lane;
                 id[i] = j[i] = -1;
-                if (r0 + i >= served) continue;
+                if (r >= served) continue;
                 const int have = pos[i] ? page_of(pos[i] - 1, a.page) + 1 : 0;
-                pos[i] += r0 + i - cu[b[i]];
+                pos[i] += r - cu[b[i]];
                 j[i] = page_of(pos[i], a.page);
                 id[i] = j[i] < have ? a.table[(long)b[i] * a.max_pages + j[i]] : __ldcg(a.free_pages + (top - 1 - (at[b[i]] + j[i] - have)));
                 if (j[i] < have) j[i] |= 0x80000000; // not a new page
             }
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                const int r = r0 + i, in_page = pos[i] - (j[i] & 0x7fffffff) * a.page;
+            for (int i = 0; i < GROUPS; ++i) {
+                const int r = w0 + 32 * i + lane, in_page = pos[i] - (j[i] & 0x7fffffff) * a.page;
                 if (r >= a.n_tokens) break;
                 const bool mine = r < served, good = mine && (uint32_t)id[i] < (uint32_t)a.n_pages;
                 if (mine && in_page == 0 && j[i] >= 0) a.table[(long)b[i] * a.max_pages + j[i]] = id[i]; // a new page's first row is always a new one
@@ -103,7 +120,7 @@ struct Fill {
     }
 };
 
-__global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_constant__ PlanArgs a)
+__global__ void __launch_bounds__(PLAN_THREADS, 1) plan_batch_kernel(const __grid_constant__ PlanArgs a)
 {
     extern __shared__ int plan_sm[];
     int *cu = plan_sm, *at = cu + a.B + 1; // row offsets; a request's place among the pages given back or taken
@@ -133,6 +150,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_c
     // if that is not so, once more with entries outside the cache passed over.
     if (tid == 0) n_done = any_bad = 0;
     __syncthreads();
+    // every block has read the pool's size and set its flag to 0: waited for where that matters
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    auto all_started = [&] {
+        if (ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        __syncthreads();
+    };
     bool some = false;
     for (int b = tid; b < a.B; b += PLAN_THREADS) {
         at[b] = 0;
@@ -166,7 +189,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_c
             sum = add_sat(sum, all.x);
         }
         top = (int)min(sum, (uint32_t)a.n_pages);
-        if (ranks > 1 && !again) tc::cluster_sync(); else __syncthreads(); // the places; and every block's flag is set to 0 before another one raises it
+        if (again) __syncthreads(); else all_started(); // the places are there, and the other blocks' flags may be raised
         for (int k = warp; k < n_done; k += PLAN_WARPS) {
             const int b = list[k], len = a.lens[b], have = len >= 0 && len <= capacity ? pages_of(len) : 0;
             int to = at[b];
@@ -233,10 +256,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_batch_kernel(const __grid_c
         cu[a.B] = served;
         if (rank == 0) a.cu[a.B] = served;
     }
-    if (ranks > 1 && !any_done) tc::cluster_sync(); else __syncthreads(); // every block has read the pool's size, and the offsets are there
+    if (any_done) __syncthreads(); else all_started(); // the offsets are there, and every block has read the pool's size
     if (rank == 0 && tid == 0) *a.n_free_next = top - taken;
 
-    // where the rows are many, four to a thread share a search
+    // where the rows are many, four groups of them share a search and the waiting for their loads
     const Fill f{cu, at, served, top, lg};
     if (a.n_tokens > ranks * PLAN_THREADS) f.rows<4>(a, rank, ranks);
     else f.rows<1>(a, rank, ranks);
