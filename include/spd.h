@@ -269,9 +269,8 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  *                 A page row is head_dim / 2 bytes: byte i has the code of dim i in bits 0-3, of dim i + head_dim / 2 in bits
  *                 4-7.  k_scales / v_scales point to [n_pages, n_kv_heads, kv_block_size, 2 halves, 2 (s, m)] bfloat16,
  *                 8-byte aligned.  A row with a NaN or an infinity (or a half whose max - m is no float) gets four NaNs and
- *                 codes 0; a row one of whose four parameters is not finite stands for NaNs.  Scales of V rows that queries
- *                 see together should lie within 2^60 of one another, and values of V below 2^30 in magnitude: beyond, sums
- *                 may lose the smaller ones or overflow. */
+ *                 codes 0; a row one of whose four parameters is not finite stands for NaNs.  bfloat16 calls may take a row with values of
+ *                 2^30 and more for one that is not finite, and V rows that a query sees together should be within 2^60 of one another. */
 #define SPD_KV_F32 0
 #define SPD_KV_BF16 1
 #define SPD_KV_E4M3 2

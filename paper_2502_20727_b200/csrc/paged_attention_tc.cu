@@ -140,12 +140,13 @@ __device__ __forceinline__ uint32_t widen4(uint32_t codes, uint32_t s, uint32_t 
     const __half2 v = __hfma2(*(const __half2 *)&codes, *(const __half2 *)&s, *(const __half2 *)&m);
     return *(const uint32_t *)&v;
 }
-// Exponent field of the power of two at or under the largest of |m| and 16 s of either half: values are below four times that.  0: not finite;
-// up to 4: zeros, or as good as.
+// Exponent field of the power of two at or under the largest of |m| and 16 s of either half: values are below four times that.  0: not finite, or 2^34 and
+// more, which float16 beside other rows does not reach; up to 4: zeros, or as good as.
 __device__ __forceinline__ int row_exponent(uint2 p)
 {
-    const uint32_t mags = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu), sb = mags & 0xffffu, mb = mags >> 16;
-    return sb >= 0x7f80u || mb >= 0x7f80u ? 0 : (int)max((sb >> 7) + 4, mb >> 7);
+    const uint32_t mags = __vmaxu2(p.x & 0x7fff7fffu, p.y & 0x7fff7fffu);
+    const int e = (int)max(((mags & 0xffffu) >> 7) + 4, mags >> 23);
+    return e >= 127 + 34 ? 0 : e;
 }
 __device__ __forceinline__ float pow2_of(int field) { return __uint_as_float((uint32_t)field << 23); }
 __device__ __forceinline__ float max_nan(float a, float b) // NaN if either is
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                     }
                     const bool varied = most[0] - least[0] > 8 || most[1] - least[1] > 8;
                     const int mine = row_exponent(prm), tile = mine_v ? most[1] : most[0];
-                    const int unit = min(max((varied ? mine : tile) + 6, 127 - 60), 127 + 36); // field of the power of two that the values are divided by
+                    const int unit = max((varied ? mine : tile) + 6, 127 - 60); // field of the power of two that the values are divided by
                     const float f = pow2_of(254 - unit);
                     uint2 out = make_uint2(pack_half(kv4_scale(prm.x) * f * 0x1p24f, kv4_min(prm.x) * f), pack_half(kv4_scale(prm.y) * f * 0x1p20f, kv4_min(prm.y) * f));
                     if (mine == 0) out = make_uint2(0, 0);

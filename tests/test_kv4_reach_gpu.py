@@ -1,0 +1,280 @@
+"""Attention over a 4-bit cache at the far ends: batches whose keys are dealt out over the whole GPU, rows of any finite size that a query does not see,
+caches beyond 32-bit offsets, calls that overlap."""
+import math
+import random
+import threading
+
+import pytest
+import torch
+
+import paper_2502_20727_b200 as spd
+from kv4_util import Batch4
+from paged_util import check_attention
+from test_paged_gpu import attend, run_and_check
+
+pytestmark = pytest.mark.gpu
+BOUND = 4096  # the host's bound of a sequence's length, by which such a batch is told from small ones
+
+
+def many(B=70, top=260, new=1, nq=16, nkv=8, d=128, page=16, seed=0, **kw):
+    """More (sequence, KV head, 32 keys) than 16 for each warp that 148 SMs hold, by the bound."""
+    assert B * nkv * (BOUND // 32) >= 16 * 148 * 12 and B <= 512
+    rng = random.Random(seed)
+    lens = [rng.choice([0, 1, 31, 32, 33, top, rng.randint(0, top)]) for _ in range(B)]
+    bt = Batch4(dtype="bf16", nq=nq, nkv=nkv, d=d, page=page, lens=lens, new=[rng.randint(0, new) if new > 1 else 1 for _ in range(B)], lead=1, behind=2,
+                seed=seed, offset=0.3, **kw)
+    bt.table = torch.cat([bt.table, torch.full((B, -(-BOUND // page)), -7, dtype=torch.int32)], 1)
+    return bt
+
+
+def run(bt):
+    out, err = attend(bt, max_context=BOUND)
+    assert err == 0
+    live = check_attention(bt, out)
+    assert (out.cpu()[~live] == 77.0).all()
+    return out
+
+
+@pytest.mark.parametrize("nq,new", [(8, 1), (16, 1), (64, 1), (16, 4), (16, 8), (64, 2), (72, 1), (128, 1), (8, 16)])
+@pytest.mark.parametrize("d", [128, 64])
+def test_many_sequences(nq, new, d):
+    run(many(nq=nq, new=new, d=d, seed=nq + new))
+
+
+@pytest.mark.parametrize("page", [1, 8, 24, 32, 48, 64])
+@pytest.mark.parametrize("new", [1, 6])
+def test_many_sequences_page_sizes(page, new):
+    run(many(nq=16, new=new, page=page, seed=page))
+
+
+@pytest.mark.parametrize("window", [(1, 0), (17, 3), (100, 40), (64, 130)])
+def test_many_sequences_with_a_window(window):
+    for new in (1, 5):
+        run(many(nq=16, new=new, top=400, window=window[0], sinks=window[1], seed=7 + new))
+
+
+def test_many_sequences_several_steps_a_warp():
+    run(many(B=64, top=2500, nq=8, seed=3))
+    run(many(B=40, top=1500, new=2, nq=56, seed=4))
+
+
+def test_many_sequences_replay_and_overlap():
+    """The same bits every time; two streams at once, each call with a workspace of its own; a workspace that two captured graphs share in turn."""
+    bt = many(seed=5)
+    first = run(bt)
+    d = bt.device()
+    torch.cuda.synchronize()
+    call = lambda **kw: spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], d["cu"], d["lens"], d["table"], max_new=1, max_context=BOUND, err=d["err"],  # noqa: E731
+                                            k_scales=d["k_scales"], v_scales=d["v_scales"], **kw)
+    outs = []
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append(call())
+    torch.cuda.synchronize()
+    live = torch.arange(bt.cu[0], bt.cu[-1])
+    assert all(torch.equal(o[live], first[live]) for o in outs)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    static = [torch.zeros_like(first) for _ in range(2)]
+    side = streams[0]
+    graphs = []
+    with torch.cuda.stream(side):
+        for o in static:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                call(out=o, workspace=ws)
+            graphs.append(g)
+        ws.fill_(255)
+        for g in graphs * 2:
+            g.replay()
+    side.synchronize()
+    assert all(torch.equal(o[live], first[live]) for o in static) and int(d["err"]) == 0
+    with pytest.raises(spd.SpdError):
+        call(workspace=ws[:1024])
+
+
+def test_many_sequences_what_does_not_fit():
+    bt = many(seed=6)
+    ref, tol = bt.reference()
+    for what in ("negative", "context", "rows", "page"):
+        dev = bt.device()
+        b = max(range(bt.B), key=lambda i: bt.lens[i])
+        if what == "negative":
+            dev["lens"][b] = -1
+        elif what == "context":
+            dev["lens"][b] = BOUND
+        elif what == "rows":
+            b = bt.B - 1
+            dev["cu"][bt.B] = bt.n + 1
+        else:
+            dev["table"][b, 0] = bt.n_pages
+        out, err = attend(bt, dev, max_context=BOUND)
+        assert err == (1 if what == "page" else 2), what
+        row = bt.cu[b]
+        keep = [i for i in range(bt.cu[0], bt.cu[-1]) if i != row]
+        assert ((out.double().cpu() - ref).abs() <= tol)[keep].all(), what
+        if what != "page":
+            assert (out[row] == 77).all(), what
+
+
+def test_many_sequences_rows_that_are_not_finite():
+    """One sequence's row in one KV head, anywhere in its keys: that sequence's heads there are NaN, nothing else changes."""
+    bt = many(seed=8)
+    ref, tol = bt.reference()
+    b = max(range(bt.B), key=lambda i: bt.lens[i])
+    for t in (0, 31, bt.lens[b] // 2, bt.lens[b]):
+        for what in ("k_scales", "v_scales"):
+            dev = bt.device()
+            p, s = bt.row_of(b, t)
+            dev[what][p, 5, s, 1, 0] = math.nan
+            out, err = attend(bt, dev, max_context=BOUND)
+            assert err == 0
+            got = out.double().cpu()
+            hit = torch.zeros_like(ref, dtype=torch.bool)
+            hit[bt.cu[b], 10:12] = True
+            dead = torch.isnan(ref)
+            assert torch.isnan(got[hit]).all()
+            assert ((got - ref).abs() <= tol)[~hit & ~dead].all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 29, 2.0 ** 60, 3.0e38])
+@pytest.mark.parametrize("new", [2, 8, 150])
+@pytest.mark.parametrize("nq", [4, 8])
+def test_finite_rows_of_any_size_that_are_not_seen(size, new, nq):
+    """The last cached row's values are huge: the queries before it are as if it were not there, to the last bit of what they are bounded by."""
+    tried = 0
+    for window, at in ((0, -1), (33, 8), (40, 10)):  # the newest row; rows that the window has passed for all but the first queries
+        bt = Batch4(dtype="bf16", nq=nq, nkv=4, d=128, page=16, lens=[40], new=[new], window=window, seed=11)
+        dev = bt.device()
+        t = 40 + new - 1 if at < 0 else at
+        p, s = bt.row_of(0, t)
+        if int(bt.table[0, t // 16]) != p:
+            continue
+        for name in ("k_scales", "v_scales"):
+            dev[name][p, :, s, :, 0] = size / 16
+            dev[name][p, :, s, :, 1] = -size
+        out, err = attend(bt, dev)
+        assert err == 0
+        ref, tol = bt.reference()
+        pos = torch.arange(40, 40 + new)
+        blind = (pos < t) | ((pos - window >= t) if window else torch.zeros_like(pos, dtype=torch.bool))
+        got = out.double().cpu()
+        assert ((got - ref).abs() <= tol)[blind].all()
+        tried += int(blind.any())
+    assert tried >= 2
+
+
+@pytest.mark.parametrize("page", [16, 24])
+def test_pages_beyond_32_bit_offsets(page):
+    """The batch's pages are the last ones of a cache of more than 2^32 bytes (K and V share it, at different pages)."""
+    bts = [Batch4(dtype="bf16", nq=4, nkv=2, d=128, page=page, lens=[70, 9], new=new, seed=3) for new in ([1, 1], [12, 3], [60, 1])]
+    bts.append(Batch4(dtype="f32", nq=4, nkv=2, d=128, page=page, lens=[70, 9], new=[5, 1], seed=3))
+    n_big = 2 ** 32 // (2 * page * 64) + 200
+    pages = torch.empty((n_big, 2, page, 64), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((n_big, 2, page, 2, 2), dtype=torch.bfloat16, device="cuda")
+    for bt in bts:
+        d = bt.device()
+        n = bt.n_pages
+        assert n <= 100
+        kp, ks, vp, vs = pages[100:], scales[100:], pages[:n_big - 100], scales[:n_big - 100]
+        for t, key in ((kp, "k_pages"), (ks, "k_scales"), (vp, "v_pages"), (vs, "v_scales")):
+            t[-n:].copy_(d[key])
+        table = torch.where((d["table"] >= 0) & (d["table"] < n), d["table"] + (n_big - 100 - n), d["table"])
+        out = torch.full((bt.n, 4, 128), 77.0, dtype=bt.dtype, device="cuda")
+        kw = dict(k_scales=ks, v_scales=vs, err=d["err"])
+        spd.paged_attention(d["q"], kp, vp, d["cu"], d["lens"], table, max_new=bt.max_new(), max_context=bt.max_context(), out=out, **kw)
+        assert int(d["err"]) == 0
+        check_attention(bt, out)
+        cu, zero = torch.tensor([0, 50], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        k, v = spd.kv_read(kp, vp, cu, zero, table[:1], n_tokens=50, dtype=bt.dtype, **kw)
+        k2, v2 = spd.kv_read(d["k_pages"], d["v_pages"], cu, zero, d["table"][:1], n_tokens=50, dtype=bt.dtype, err=d["err"], k_scales=d["k_scales"], v_scales=d["v_scales"])
+        assert torch.equal(k, k2) and torch.equal(v, v2)
+        # what was read, appended again: by slots at the far end of the cache
+        t = torch.arange(50, device="cuda")
+        slots = (table[0].long()[t // page] * page + t % page).to(torch.int32)
+        spd.kv_write_slots(k, k, kp, vp, slots, **kw)
+        k3, v3 = spd.kv_read(kp, vp, cu, zero, table[:1], n_tokens=50, dtype=torch.float32, **kw)
+        assert torch.equal(k3, v3) and int(d["err"]) == 0
+        # values of a 4-bit row, quantised again: m is m again, s within its two roundings
+        assert (k3 - k.float()).abs().max() <= 2.0 ** -7 * 16 * k.float().abs().max()
+    del pages, scales, kp, ks, vp, vs
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_sequences_that_share_pages(new):
+    """The same pages under two sequences of a batch (a shared prefix): both see what one alone sees."""
+    bt = Batch4(dtype="bf16", nq=8, nkv=2, d=128, page=16, lens=[100], new=[new], seed=5)
+    d = bt.device()
+    kw = dict(max_new=new, max_context=100 + new, err=d["err"], k_scales=d["k_scales"], v_scales=d["v_scales"])
+    one = spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], d["cu"], d["lens"], d["table"], **kw)
+    two = spd.paged_attention(torch.cat([d["q"], d["q"]]), d["k_pages"], d["v_pages"], torch.tensor([0, new, 2 * new], dtype=torch.int32, device="cuda"),
+                              d["lens"].repeat(2), d["table"].repeat(2, 1), **kw)
+    check_attention(bt, one)
+    assert torch.equal(two[:new], two[new:]) and int(d["err"]) == 0
+    check_attention(bt, two[:new])
+
+
+@pytest.mark.parametrize("nq,nkv", [(32, 1), (71, 1), (128, 1), (400, 2)])
+def test_many_query_heads_per_kv_head(nq, nkv):
+    run_and_check(Batch4(dtype="bf16", nq=nq, nkv=nkv, d=64, page=16, lens=[150, 0, 40], new=[1, 1, 1], seed=31))
+    run_and_check(Batch4(dtype="bf16", nq=nq, nkv=nkv, d=64, page=16, lens=[97], new=[4], window=50, sinks=3, seed=32))
+
+
+def test_threads_that_call_at_once():
+    """First calls of several variants from several threads, each on a stream of its own."""
+    bts = [Batch4(dtype=t, nq=8, nkv=2, d=d, page=page, lens=[200, 30], new=[new, 1], seed=34) for t in ("bf16", "f32") for d, page, new in ((128, 16, 1), (64, 24, 40), (64, 16, 5))]
+    bts.append(many(seed=35))
+    ds = [bt.device() for bt in bts]
+    outs, bad = [None] * len(bts), []
+    torch.cuda.synchronize()
+    start = threading.Barrier(len(bts))
+
+    def work(i):
+        try:
+            bt, d = bts[i], ds[i]
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                for _ in range(3):
+                    outs[i] = spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], d["cu"], d["lens"], d["table"], max_new=bt.max_new(),
+                                                  max_context=BOUND if bt.B > 3 else bt.max_context(), err=d["err"], k_scales=d["k_scales"], v_scales=d["v_scales"])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            bad.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(bts))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad, bad
+    for bt, d, out in zip(bts, ds, outs):
+        assert int(d["err"]) == 0
+        check_attention(bt, out)
+
+
+def test_tensors_of_another_stream_and_strides():
+    """Rows that are slices of one projection output, made on the stream that then attends; refusals of what does not fit the pages."""
+    bt = Batch4(dtype="bf16", nq=8, nkv=2, d=128, page=16, lens=[20, 3], new=[1, 7], seed=9)
+    d = bt.device()
+    kw = dict(max_new=7, max_context=27, err=d["err"], k_scales=d["k_scales"], v_scales=d["v_scales"])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        fused = torch.cat([d["q"] * 0, d["q"], d["q"] * 0], 1)
+        out = spd.paged_attention(fused[:, 8:16], d["k_pages"], d["v_pages"], d["cu"], d["lens"], d["table"], **kw)
+        torch.cuda.current_stream().synchronize()
+    check_attention(bt, out)
+    at = (d["cu"], d["lens"], d["table"])
+    for q in (d["q"][:, :, ::2], d["q"].transpose(0, 1), d["q"].half(), d["q"][0], d["q"].cpu()):
+        with pytest.raises(ValueError):
+            spd.paged_attention(q, d["k_pages"], d["v_pages"], *at, **kw)
+    for bad in (dict(k_scales=None), dict(v_scales=d["v_scales"].float()), dict(k_scales=d["k_scales"][..., :1]), dict(v_scales=d["v_scales"][:-1])):
+        with pytest.raises(ValueError):
+            spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], *at, **{**kw, **bad})
+    with pytest.raises(ValueError):
+        spd.paged_attention(d["q"], d["k_pages"][..., :32], d["v_pages"], *at, **kw)
+    with pytest.raises(spd.SpdError):
+        spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], *at, **{**kw, "max_new": 0})
+    with pytest.raises(TypeError):
+        spd.paged_attention([1.0], d["k_pages"], d["v_pages"], *at, **kw)
