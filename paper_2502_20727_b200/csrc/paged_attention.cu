@@ -276,7 +276,7 @@ cudaError_t launch_paged_attention_general(const PagedAttnArgs &a, int q_bf16, c
     case KV_F32: return general_f32<KV_F32>(a, st);
     case KV_E4M3: return general_f32<KV_E4M3>(a, st);
     case KV_INT8: return general_f32<KV_INT8>(a, st);
-    case KV_INT4: return general_f32<KV_INT4>(a, st);
+    case KV_INT4: return a.kv.d == 32 ? general_by_rows<float, KV_INT4, 32>(a, st) : cudaErrorInvalidValue; // others: paged_attention_rows4.cu
     default: return cudaErrorInvalidValue;
     }
 }
@@ -294,7 +294,14 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     const long rows = (long)max_new * (nq / nkv);
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
-    if (dtype != 1 || d == 32) {
+    if (fmt == KV_INT4 && dtype == 0 && d != 32) {
+        // tiles of 8 rows; ranges of the keys, joined in a cluster, where the tiles do not fill the GPU, none under 256 keys
+        p.kernel = ATTN_ROWS;
+        const long blocks = (rows + 7) / 8 * nkv * (B > 0 ? B : 1), sms = sm_count();
+        long s = sms / blocks >= 2 ? sms / blocks : 2 * sms / blocks;
+        if (s > (keys + 255) / 256) s = (keys + 255) / 256;
+        p.splits = (int)(s < 1 ? 1 : s > PAGED_MAX_CLUSTER ? PAGED_MAX_CLUSTER : s);
+    } else if (dtype != 1 || d == 32) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
         // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
         const long pairs = (long)nkv * (B > 0 ? B : 1);
@@ -353,8 +360,8 @@ cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, c
     cudaError_t e = cudaSuccess;
     switch (p.kernel) {
     case ATTN_GENERAL: e = launch_paged_attention_general(a, q_bf16, st); break;
-    case ATTN_ROWS: e = a.kv.fmt == KV_INT4 ? launch_paged_attention_rows4(a, false, st) : launch_paged_attention_rows(a, st); break;
-    case ATTN_STREAM: return launch_paged_attention_rows4(a, true, st);
+    case ATTN_ROWS: e = a.kv.fmt == KV_INT4 ? launch_paged_attention_rows4(a, q_bf16, false, st) : launch_paged_attention_rows(a, st); break;
+    case ATTN_STREAM: return launch_paged_attention_rows4(a, q_bf16, true, st);
     case ATTN_TC: e = launch_paged_attention_tc(a, st); break;
     }
     if (e == cudaSuccess && p.workspace) e = launch_paged_merge(a, q_bf16, st);

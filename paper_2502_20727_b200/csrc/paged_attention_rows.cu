@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && FMT != KV_BF
             }
         }
     };
-    join_rows<D, RW>(a, gen, C::off_pml(ST), rows, row0, len, kvh, split, splits, give_back);
+    join_rows<bf16, D, RW>(a, gen, C::off_pml(ST), rows, row0, 0, kvh, split, splits, give_back);
     if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 

@@ -62,7 +62,24 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
 // codes of bytes 0 and 2 of a word (shifted right by 8: bytes 1 and 3) as float16x2, in units of 2^-24 and 2^-20
 __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
-constexpr float LOW_UNIT = 0x1p24f, HIGH_UNIT = 0x1p20f;
+// float32 queries: code - 8 and 16 (code - 8), so that sums of weighted codes do not cancel against weighted smallest values
+__device__ __forceinline__ uint32_t centred(uint32_t w, uint32_t mask, uint32_t c1024, uint32_t minus)
+{
+    const uint32_t x = and_or(w, mask, c1024);
+    const __half2 v = __hsub2(*(const __half2 *)&x, *(const __half2 *)&minus);
+    return *(const uint32_t *)&v;
+}
+// What a float16 leaves of a float32 operand is a second float16: 22 bits, in products of their own
+__device__ __forceinline__ void split_half(float x, float y, uint32_t &high, uint32_t &low)
+{
+    const __half2 h = __floats2half2_rn(x, y);
+    high = *(const uint32_t *)&h;
+    low = pack_half(x - __low2float(h), y - __high2float(h));
+}
+template <typename T> struct Code4 { // the operands' units; what the weights are scaled by, and how far the maximum may be exceeded (powers of two)
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr float LOW = F32 ? 1.f : 0x1p24f, HIGH = F32 ? 0x1p-4f : 0x1p20f, WEIGHT = F32 ? 0x1p12f : 1.f, SLACK = F32 ? 0.f : 8.f;
+};
 
 // What a warp has of NR groups of 8 query rows: sums over its keys of weights times codes (tiles 0 .. MT / 2 - 1: first half of the head, in units of
 // 2^-24; the others 2^-20), of weights times smallest values, of weights; the maxima they are relative to.
@@ -73,12 +90,15 @@ template <int D, int NR> struct Partial {
 
 // The query rows of a (sequence, KV head) and the keys they see
 struct Rows {
-    int b, kvh, row0, rows, len, kv_len;
+    int b, kvh, row0, r0, rows, len, kv_len; // packed rows r0 .. r0 + rows - 1: row r = new token r / group, query head r % group; len: the first one's position
     int lo_min, first, n_sink, n_steps; // steps of 32 keys that hold a key some row sees: sinks, then the window of the first query onwards
-    __device__ __forceinline__ void keys(const PagedAttnArgs &a, int n_new)
+    // the `most` rows from `from` on, of n_new tokens behind the cached ones in `len`
+    __device__ __forceinline__ void keys(const PagedAttnArgs &a, int n_new, int from = 0, int most = 0x7fffffff)
     {
-        rows = n_new * a.group;
-        kv_len = len + n_new;
+        r0 = from;
+        rows = min(n_new * a.group - from, most);
+        kv_len = len + (from + rows - 1) / a.group + 1;
+        len += from / a.group;
         lo_min = a.window ? max(0, len - a.window + 1) : 0;
         first = lo_min / STEP;
         n_sink = min((min(a.sinks, lo_min) + STEP - 1) / STEP, first);
@@ -88,10 +108,12 @@ struct Rows {
 
 // One warp: steps j0, j0 + stride, ..., n_mine of them.  ring: its ST stages, fk: its factors' place.
 // PAGES: page sizes 16, 32, 64, ... with less than 2^31 bytes of codes per page; else any.
-template <int D, int NR, int ST, bool PAGES>
+template <typename T, int D, int NR, int ST, bool PAGES>
 __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int j0, int n_mine, int stride, uint32_t ring, uint32_t fk, Partial<D, NR> &acc_out)
 {
     using C = Step4<D>;
+    using U = Code4<T>;
+    constexpr bool F32 = U::F32;
     constexpr int MT = D / 16, RB = C::RB, W = D / 32; // W: words of a lane per row
     const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     constexpr uint32_t F = STEP * 16; // factors: K scales, K smallest values, V scales, V smallest values, (exponent, unit)
@@ -187,41 +209,60 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
     if (ST < n_mine) next = ask(ST);
 
     // Q fragments (column g of a group of 8 rows), in the order of the codes; rows beyond the last are zero.  A lane's dims: D / 8 of either half.
-    uint32_t qf[NR][2 * W][2];
+    uint32_t qf[NR][2 * W][2], ql[F32 ? NR : 1][2 * W][2]; // ql: what float16 leaves of float32
     float2 qs[NR], qsum[NR][2]; // of this lane's columns 2 t4 and 2 t4 + 1: to base-2 units; sums of the halves in those
     int pos[NR][2];
+    const int first_in_group = q.r0 % a.group; // the rows' tokens are counted from the first row's
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         const int r = g + 8 * n;
         const bool live = r < rows;
-        const int i = live ? r / a.group : 0, head = live ? r - i * a.group : 0;
-        const bf16 *qp = (const bf16 *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
-        uint4 u[W];
-        uint32_t top = 0; // largest magnitude's bits
+        const int i = live ? (q.r0 + r) / a.group : 0, head = live ? q.r0 + r - i * a.group : 0;
+        const T *qp = (const T *)a.q + (long)(row0 + i) * a.q_stride + (long)(kvh * a.group + head) * D;
+        float x[W][8];
+        uint32_t top = 0; // largest magnitude's bits (float32's)
 #pragma unroll
         for (int m = 0; m < W; ++m) {
-            u[m] = live ? *(const uint4 *)(qp + (D / 2) * (m / (W / 2)) + (D / 8) * t4 + 8 * (m % (W / 2))) : make_uint4(0, 0, 0, 0);
-            const uint32_t x = __vmaxu2(__vmaxu2(u[m].x & 0x7fff7fffu, u[m].y & 0x7fff7fffu), __vmaxu2(u[m].z & 0x7fff7fffu, u[m].w & 0x7fff7fffu));
-            top = max(top, max(x & 0xffffu, x >> 16));
+            const T *src = qp + (D / 2) * (m / (W / 2)) + (D / 8) * t4 + 8 * (m % (W / 2));
+            if constexpr (F32) {
+                const float4 u = live ? *(const float4 *)src : make_float4(0.f, 0.f, 0.f, 0.f), v = live ? *(const float4 *)(src + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                x[m][0] = u.x; x[m][1] = u.y; x[m][2] = u.z; x[m][3] = u.w; x[m][4] = v.x; x[m][5] = v.y; x[m][6] = v.z; x[m][7] = v.w;
+            } else {
+                const uint4 u = live ? *(const uint4 *)src : make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { x[m][2 * e] = __uint_as_float(w[e] << 16); x[m][2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[m][e]) & 0x7fffffffu);
         }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int ex = max((int)(top >> 7), 27) - 127;                    // 2^ex <= largest < 2^(ex + 1), ex >= -100
+        const int ex = max((int)(top >> 23), 27) - 127;                   // 2^ex <= largest < 2^(ex + 1), ex >= -100
         const float f = __uint_as_float((uint32_t)(127 + 14 - ex) << 23); // to [2^14, 2^15)
         const float my_qs = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int m = 0; m < W; ++m) {
-            const uint32_t w[4] = {u[m].x, u[m].y, u[m].z, u[m].w};
-            uint32_t x[4];
+            uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const __half2 v = __floats2half2_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
-                x[e] = *(const uint32_t *)&v;
-                sum[m / (W / 2)] += __low2float(v) + __high2float(v);
+                const float a0 = x[m][2 * e] * f, a1 = x[m][2 * e + 1] * f;
+                if (F32) {
+                    split_half(a0, a1, hi[e], lo[e]);
+                    sum[m / (W / 2)] += a0 + a1;
+                } else {
+                    hi[e] = pack_half(a0, a1);
+                    const __half2 v = *(const __half2 *)&hi[e];
+                    sum[m / (W / 2)] += __low2float(v) + __high2float(v);
+                }
             }
-            qf[n][2 * m][0] = __byte_perm(x[0], x[1], 0x5410); qf[n][2 * m][1] = __byte_perm(x[0], x[1], 0x7632);
-            qf[n][2 * m + 1][0] = __byte_perm(x[2], x[3], 0x5410); qf[n][2 * m + 1][1] = __byte_perm(x[2], x[3], 0x7632);
+            qf[n][2 * m][0] = __byte_perm(hi[0], hi[1], 0x5410); qf[n][2 * m][1] = __byte_perm(hi[0], hi[1], 0x7632);
+            qf[n][2 * m + 1][0] = __byte_perm(hi[2], hi[3], 0x5410); qf[n][2 * m + 1][1] = __byte_perm(hi[2], hi[3], 0x7632);
+            if constexpr (F32) {
+                ql[n][2 * m][0] = __byte_perm(lo[0], lo[1], 0x5410); ql[n][2 * m][1] = __byte_perm(lo[0], lo[1], 0x7632);
+                ql[n][2 * m + 1][0] = __byte_perm(lo[2], lo[3], 0x5410); ql[n][2 * m + 1][1] = __byte_perm(lo[2], lo[3], 0x7632);
+            }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -231,7 +272,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int c = 8 * n + 2 * t4 + e;
-            pos[n][e] = c < rows ? len + c / a.group : -1;
+            pos[n][e] = c < rows ? len + (first_in_group + c) / a.group : -1;
         }
         qs[n] = make_float2(__shfl_sync(0xffffffffu, my_qs, 2 * t4 * 4), __shfl_sync(0xffffffffu, my_qs, (2 * t4 + 1) * 4));
 #pragma unroll
@@ -243,6 +284,10 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
     // bytes, which give a lane bytes 2 g and 2 g + 1 of keys 2 t4 and 2 t4 + 1.
     const uint32_t lane_k = RB == 64 ? at(g, t4) : at(g, t4 >> 1) + (t4 & 1) * 8, my_factors = fk + g * 16;
     const uint32_t lane_v = at(lane & 15, lane >> 4); // matrices: keys 0-7 and 8-15 of chunk 0, of chunk 1
+    uint32_t c1024 = 0, c1032 = 0, c1152 = 0; // float16x2, in registers
+    if (F32) asm volatile("mov.b32 %0, 0x64006400;\n\tmov.b32 %1, 0x64086408;\n\tmov.b32 %2, 0x64806480;" : "=r"(c1024), "=r"(c1032), "=r"(c1152));
+    auto low = [&](uint32_t w) { return F32 ? centred(w, 0x000f000fu, c1024, c1032) : low_codes(w); };
+    auto high = [&](uint32_t w) { return F32 ? centred(w, 0x00f000f0u, c1024, c1152) : high_codes(w); };
     auto &o = acc_out.o;
     auto &m_used = acc_out.m_used;
     auto &l = acc_out.l;
@@ -269,17 +314,18 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
             const uint32_t km = __vmaxu2(kp.x & 0x7fff7fffu, kp.y & 0x7fff7fffu), vm = __vmaxu2(vp.x & 0x7fff7fffu, vp.y & 0x7fff7fffu);
             // a row that is not finite is a NaN for those who see its key, and nothing for the others
             const bool k_bad = ((km + 0x00800080u) & 0x80008000u) != 0;
-            const float ks = k_bad ? __uint_as_float(0x7fc00000u) : kv4_scale(kp.x) * LOW_UNIT;
-            sts_f4(fk + lane * 16, ks, kv4_scale(kp.y) * HIGH_UNIT);
-            sts_f4(fk + F + lane * 16, kv4_min(kp.x), kv4_min(kp.y));
+            const float ks = k_bad ? __uint_as_float(0x7fc00000u) : kv4_scale(kp.x) * U::LOW;
+            sts_f4(fk + lane * 16, ks, kv4_scale(kp.y) * U::HIGH);
+            auto middle = [](uint32_t p) { return F32 ? fmaf(8.f, kv4_scale(p), kv4_min(p)) : kv4_min(p); }; // what a code of 0, float32: of 8, stands for
+            sts_f4(fk + F + lane * 16, middle(kp.x), middle(kp.y));
             const uint32_t top = max(vm & 0xffffu, vm >> 16);
             const bool v_bad = top >= 0x7f80u;
             const int ex = min(max((int)(top >> 7), 127 - 60), 127 + 30);
             const float unit = __uint_as_float((uint32_t)(254 - ex) << 23), f = v_bad ? 0.f : unit;
             const float ev = v_bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ex) - (8388608.f + 127.f); // 2^23 + ex
             const uint2 q = v_bad ? make_uint2(0, 0) : vp;
-            sts_f4(fk + 2 * F + lane * 16, kv4_scale(q.x) * f, kv4_scale(q.y) * f);
-            sts_f4(fk + 3 * F + lane * 16, kv4_min(q.x) * f, kv4_min(q.y) * f);
+            sts_f4(fk + 2 * F + lane * 16, kv4_scale(q.x) * (f * U::WEIGHT), kv4_scale(q.y) * (f * U::WEIGHT));
+            sts_f4(fk + 3 * F + lane * 16, middle(q.x) * f, middle(q.y) * f);
             sts_f4(fk + 4 * F + lane * 16, ev, unit);
         }
         float2 s[2][NR][2], unit[2][2]; // scores in base-2 units; [tile][rows g and g + 8]
@@ -299,15 +345,20 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
 #pragma unroll
             for (int i = 0; i < W; ++i) {
                 const uint32_t y0 = w0[i] >> 8, y1 = w1[i] >> 8;
+                const uint32_t l0 = low(w0[i]), l1 = low(w1[i]), l2 = low(y0), l3 = low(y1), h0 = high(w0[i]), h1 = high(w1[i]), h2 = high(y0), h3 = high(y1);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     if (i == 0) {
-                        mma16816_zero(acc[u][0][n], low_codes(w0[i]), low_codes(w1[i]), low_codes(y0), low_codes(y1), qf[n][i][0], qf[n][i][1]);
-                        mma16816_zero(acc[u][1][n], high_codes(w0[i]), high_codes(w1[i]), high_codes(y0), high_codes(y1), qf[n][W + i][0], qf[n][W + i][1]);
-                        continue;
+                        mma16816_zero(acc[u][0][n], l0, l1, l2, l3, qf[n][i][0], qf[n][i][1]);
+                        mma16816_zero(acc[u][1][n], h0, h1, h2, h3, qf[n][W + i][0], qf[n][W + i][1]);
+                    } else {
+                        mma16816<true>(acc[u][0][n], l0, l1, l2, l3, qf[n][i][0], qf[n][i][1]);
+                        mma16816<true>(acc[u][1][n], h0, h1, h2, h3, qf[n][W + i][0], qf[n][W + i][1]);
                     }
-                    mma16816<true>(acc[u][0][n], low_codes(w0[i]), low_codes(w1[i]), low_codes(y0), low_codes(y1), qf[n][i][0], qf[n][i][1]);
-                    mma16816<true>(acc[u][1][n], high_codes(w0[i]), high_codes(w1[i]), high_codes(y0), high_codes(y1), qf[n][W + i][0], qf[n][W + i][1]);
+                    if constexpr (F32) {
+                        mma16816<true>(acc[u][0][n], l0, l1, l2, l3, ql[n][i][0], ql[n][i][1]);
+                        mma16816<true>(acc[u][1][n], h0, h1, h2, h3, ql[n][W + i][0], ql[n][W + i][1]);
+                    }
                 }
             }
         }
@@ -357,7 +408,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
                 const float2 nm = make_float2(fmaxf(m_used[n].x, mx[n].x), fmaxf(m_used[n].y, mx[n].y));
                 const float2 f = make_float2(m_used[n].x == -INFINITY ? 0.f : ex2(m_used[n].x - nm.x), m_used[n].y == -INFINITY ? 0.f : ex2(m_used[n].y - nm.y));
                 m_used[n] = nm;
-                limit[n] = make_float2(nm.x + 8.f, nm.y + 8.f);
+                limit[n] = make_float2(nm.x + U::SLACK, nm.y + U::SLACK);
                 minus[n] = make_float2(fminf(-nm.x, 3e38f), fminf(-nm.y, 3e38f)); // no key seen so far: the weights are 2^-inf whatever this is
                 l[n] = mul2(l[n], f);
                 om[n][0] = mul2(om[n][0], f);
@@ -368,7 +419,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            uint32_t pf[2][NR][2]; // [half]
+            uint32_t pf[2][NR][2], pl[2][F32 ? NR : 1][2]; // weights [half], and what float16 leaves of them
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t p = my_factors + (16 * u + 8 * h) * 16;
@@ -380,8 +431,18 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
                     om[n][0] = fma2(x, vm.a, om[n][0]);
                     om[n][1] = fma2(x, vm.b, om[n][1]);
                     const float2 w0 = mul2(x, vs.a), w1 = mul2(x, vs.b);
-                    pf[0][n][h] = transpose8x8(pack_half(w0.x, w0.y));
-                    pf[1][n][h] = transpose8x8(pack_half(w1.x, w1.y));
+                    if constexpr (F32) {
+                        uint32_t hi, lo;
+                        split_half(w0.x, w0.y, hi, lo);
+                        pf[0][n][h] = transpose8x8(hi);
+                        pl[0][n][h] = transpose8x8(lo);
+                        split_half(w1.x, w1.y, hi, lo);
+                        pf[1][n][h] = transpose8x8(hi);
+                        pl[1][n][h] = transpose8x8(lo);
+                    } else {
+                        pf[0][n][h] = transpose8x8(pack_half(w0.x, w0.y));
+                        pf[1][n][h] = transpose8x8(pack_half(w1.x, w1.y));
+                    }
                 }
             }
 #pragma unroll
@@ -391,10 +452,15 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t x0 = v[2 * i], x1 = v[2 * i + 1], y0 = x0 >> 8, y1 = x1 >> 8;
+                    const uint32_t l0 = low(x0), l1 = low(y0), l2 = low(x1), l3 = low(y1), h0 = high(x0), h1 = high(y0), h2 = high(x1), h3 = high(y1);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
-                        mma16816<true>(o[n][c + i], low_codes(x0), low_codes(y0), low_codes(x1), low_codes(y1), pf[0][n][0], pf[0][n][1]);
-                        mma16816<true>(o[n][W + c + i], high_codes(x0), high_codes(y0), high_codes(x1), high_codes(y1), pf[1][n][0], pf[1][n][1]);
+                        mma16816<true>(o[n][c + i], l0, l1, l2, l3, pf[0][n][0], pf[0][n][1]);
+                        mma16816<true>(o[n][W + c + i], h0, h1, h2, h3, pf[1][n][0], pf[1][n][1]);
+                        if constexpr (F32) {
+                            mma16816<true>(o[n][c + i], l0, l1, l2, l3, pl[0][n][0], pl[0][n][1]);
+                            mma16816<true>(o[n][W + c + i], h0, h1, h2, h3, pl[1][n][0], pl[1][n][1]);
+                        }
                     }
                 }
             }
@@ -424,8 +490,8 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
 
 __device__ __forceinline__ float column(float2 v, int e) { return e ? v.y : v.x; }
 
-template <int D, int NR, int RW, bool PAGES>
-__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 3 : 2) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
+template <typename T, int D, int NR, int RW, bool PAGES>
+__global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && sizeof(T) == 2 ? 3 : 2) paged_attention_rows4_kernel(const __grid_constant__ PagedAttnArgs a)
 {
     using C = Rows4Cfg<D, RW>;
     constexpr int MT = D / 16, W = D / 32;
@@ -439,17 +505,19 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 3 : 2) paged_
     const int split = blockIdx.z;
     Rows q;
     int n_new;
-    q.kvh = blockIdx.x;
+    const int tile = blockIdx.x / a.kv.nkv; // of 8 NR rows
+    q.kvh = blockIdx.x - tile * a.kv.nkv;
     q.b = blockIdx.y;
-    if (!batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err)) return; // the same for a whole cluster
-    q.keys(a, n_new);
+    // the same for a whole cluster
+    if (!batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err) || n_new * a.group <= tile * 8 * NR) return;
+    q.keys(a, n_new, tile * 8 * NR, 8 * NR);
     // short sequences are cut into fewer ranges, of at least 4 steps
     const int splits = min(a.splits, (q.n_steps + 3) / 4);
     const int per = splits > 1 ? q.n_steps / splits : q.n_steps, extra = q.n_steps - per * splits; // the first `extra` ranges get one more
     const int j_begin = split < splits ? split * per + min(split, extra) : 0;
     const int j_end = split < splits ? j_begin + per + (split < extra ? 1 : 0) : 0;
     Partial<D, NR> p;
-    walk<D, NR, C::STAGES, PAGES>(a, q, j_begin + warp, (j_end - j_begin - warp + RW - 1) / RW, RW, base + warp * C::STAGES * C::STAGE,
+    walk<T, D, NR, C::STAGES, PAGES>(a, q, j_begin + warp, (j_end - j_begin - warp + RW - 1) / RW, RW, base + warp * C::STAGES * C::STAGE,
                                   base + C::OFF_FACTORS + warp * C::FACTORS, p);
     __syncthreads(); // the partial rows go over the rings
     float *mo = (float *)gen, *ml = mo + RW * 16 * (D + 2); // [warp][16][D + 2], [warp][16][2]
@@ -463,14 +531,14 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 ? 3 : 2) paged_
 #pragma unroll
                 for (int i = 0; i < MT; ++i) { // MMA row g: dim 16 i + 2 g of the tile's half, row g + 8: + 1
                     const int h = i / W;
-                    const float x = h ? HIGH_UNIT : LOW_UNIT, y = column(p.om[n][h], e);
+                    const float x = (h ? Code4<T>::HIGH : Code4<T>::LOW) / Code4<T>::WEIGHT, y = column(p.om[n][h], e);
                     *(float2 *)(dst + h * (D / 2) + 16 * (i % W)) = make_float2(fmaf(p.o[n][i][e], x, y), fmaf(p.o[n][i][2 + e], x, y));
                 }
                 if (g == 0) { ml[(warp * 16 + r) * 2] = column(p.m_used[n], e); ml[(warp * 16 + r) * 2 + 1] = column(p.l[n], e); }
             }
         }
     }
-    join_rows<D, RW>(a, gen, C::OFF_JOIN, q.rows, q.row0, q.len, q.kvh, split, splits, [](int, int, float &, float &) {});
+    join_rows<T, D, RW>(a, gen, C::OFF_JOIN, q.rows, q.row0, q.r0, q.kvh, split, splits, [](int, int, float &, float &) {});
     if (threadIdx.x == 0) stamp_exit(a.stamp);
 }
 
@@ -574,7 +642,7 @@ __global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 3 : 2) paged_atte
         q.kvh = in_seq / q.n_steps;
         const int j0 = in_seq - q.kvh * q.n_steps, n = min(q.n_steps - j0, x_end - x);
         Partial<D, NR> p;
-        walk<D, NR, C::STAGES, PAGES>(a, q, j0, n, 1, base + warp * C::STAGES * C::STAGE, base + C::OFF_FACTORS + warp * C::FACTORS, p);
+        walk<bf16, D, NR, C::STAGES, PAGES>(a, q, j0, n, 1, base + warp * C::STAGES * C::STAGE, base + C::OFF_FACTORS + warp * C::FACTORS, p);
         x += n;
         const bool whole = n == q.n_steps;
         const long slot = 2L * me + (j0 == 0);
@@ -589,7 +657,7 @@ __global__ void __launch_bounds__(32 * STREAM_WARPS, NR == 1 ? 3 : 2) paged_atte
                 const int i = r / a.group, head = q.kvh * a.group + r - i * a.group;
 #pragma unroll
                 for (int t = 0; t < 2 * W; ++t) { // dims 16 (t % W) + 2 g and the next of half t / W
-                    const float unit = t < W ? LOW_UNIT : HIGH_UNIT, low = column(p.om[nr][t / W], e);
+                    const float unit = t < W ? Code4<bf16>::LOW : Code4<bf16>::HIGH, low = column(p.om[nr][t / W], e);
                     const float y0 = fmaf(p.o[nr][t][e], unit, low) * inv, y1 = fmaf(p.o[nr][t][2 + e], unit, low) * inv;
                     const int dim = t / W * (D / 2) + 16 * (t % W) + 2 * g;
                     if (whole) *(uint32_t *)((bf16 *)a.out + (long)(q.row0 + i) * a.o_stride + (long)head * D + dim) = pack(y0, y1);
@@ -666,13 +734,15 @@ __global__ void __launch_bounds__(128) paged_merge_stream4_kernel(const __grid_c
     for (int e = 0; e < VEC; e += 2) *(uint32_t *)(dst + e) = pack(o[e] * inv, o[e + 1] * inv);
 }
 
-template <int D, int NR, int RW, bool PAGES> cudaError_t launch_rows4(const PagedAttnArgs &a, cudaStream_t st)
+template <typename T, int D, int NR, int RW, bool PAGES> cudaError_t launch_rows4(const PagedAttnArgs &a, cudaStream_t st)
 {
     using C = Rows4Cfg<D, RW>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise((const void *)paged_attention_rows4_kernel<D, NR, RW, PAGES>, C::SMEM);
+    const cudaError_t e = limit.raise((const void *)paged_attention_rows4_kernel<T, D, NR, RW, PAGES>, C::SMEM);
     if (e != cudaSuccess) return e;
-    return launch_kernel_z(paged_attention_rows4_kernel<D, NR, RW, PAGES>, dim3(a.kv.nkv, a.rb.B, a.splits), dim3(32 * RW), C::SMEM, st, a.part_o ? 1 : a.splits, a);
+    const long tiles = ((long)a.max_new * a.group + 8 * NR - 1) / (8 * NR);
+    if (tiles * a.kv.nkv > 0x7fffffffL) return cudaErrorInvalidConfiguration;
+    return launch_kernel_z(paged_attention_rows4_kernel<T, D, NR, RW, PAGES>, dim3((unsigned)(a.kv.nkv * tiles), a.rb.B, a.splits), dim3(32 * RW), C::SMEM, st, a.part_o ? 1 : a.splits, a);
 }
 template <int D, int NR, bool PAGES> cudaError_t launch_stream4(PagedAttnArgs a, cudaStream_t st)
 {
@@ -688,17 +758,19 @@ template <int D, int NR, bool PAGES> cudaError_t launch_stream4(PagedAttnArgs a,
     const int rows = a.max_new * a.group;
     return launch_kernel(paged_merge_stream4_kernel<D, NR>, dim3(a.kv.nkv, a.rb.B, (rows + 3) / 4), dim3(128), 0, st, 0, a, workers, starts);
 }
-template <int D, int NR> cudaError_t rows4_by_page(const PagedAttnArgs &a, bool stream, cudaStream_t st)
+template <typename T, int D, int NR> cudaError_t rows4_by_page(const PagedAttnArgs &a, bool stream, cudaStream_t st)
 {
     const bool pages = a.kv.page >= 16 && !(a.kv.page & (a.kv.page - 1)) && (long)a.kv.nkv * a.kv.page * (D / 2) <= 0x7fffffffL;
-    if (stream) return pages ? launch_stream4<D, NR, true>(a, st) : launch_stream4<D, NR, false>(a, st);
-    if (!pages) return launch_rows4<D, NR, 4, false>(a, st);
-    if ((long)a.kv.nkv * a.rb.B * a.splits <= sm_count()) return launch_rows4<D, NR, 8, true>(a, st);
-    return launch_rows4<D, NR, 4, true>(a, st);
+    if constexpr (sizeof(T) == 2)
+        if (stream) return pages ? launch_stream4<D, NR, true>(a, st) : launch_stream4<D, NR, false>(a, st);
+    if (!pages) return launch_rows4<T, D, NR, 4, false>(a, st);
+    if ((long)a.kv.nkv * a.rb.B * a.splits * (((long)a.max_new * a.group + 8 * NR - 1) / (8 * NR)) <= sm_count()) return launch_rows4<T, D, NR, 8, true>(a, st);
+    return launch_rows4<T, D, NR, 4, true>(a, st);
 }
-template <int D> cudaError_t rows4_by_count(const PagedAttnArgs &a, bool stream, cudaStream_t st)
+template <int D> cudaError_t rows4_by_type(const PagedAttnArgs &a, int q_bf16, bool stream, cudaStream_t st)
 {
-    return a.max_new * a.group <= 8 ? rows4_by_page<D, 1>(a, stream, st) : rows4_by_page<D, 2>(a, stream, st);
+    if (!q_bf16) return rows4_by_page<float, D, 1>(a, false, st);
+    return a.max_new * a.group <= 8 ? rows4_by_page<bf16, D, 1>(a, stream, st) : rows4_by_page<bf16, D, 2>(a, stream, st);
 }
 
 } // namespace
@@ -706,10 +778,10 @@ template <int D> cudaError_t rows4_by_count(const PagedAttnArgs &a, bool stream,
 int stream4_workers(int nr) { return sm_count() * (nr == 1 ? 3 : 2) * STREAM_WARPS; }
 size_t stream4_workspace(int rows, int d) { return (size_t)stream4_workers(rows <= 8 ? 1 : 2) * 2 * (rows <= 8 ? 8 : 16) * (d + 2) * sizeof(float) + (STREAM_MAX_B + 1) * sizeof(int); }
 
-cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, bool stream, cudaStream_t st)
+cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, int q_bf16, bool stream, cudaStream_t st)
 {
-    if (a.kv.d == 128) return rows4_by_count<128>(a, stream, st);
-    if (a.kv.d == 64) return rows4_by_count<64>(a, stream, st);
+    if (a.kv.d == 128) return rows4_by_type<128>(a, q_bf16, stream, st);
+    if (a.kv.d == 64) return rows4_by_type<64>(a, q_bf16, stream, st);
     return cudaErrorInvalidValue;
 }
 

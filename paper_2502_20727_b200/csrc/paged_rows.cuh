@@ -68,13 +68,16 @@ __device__ __forceinline__ bool sees(int t, int pos, int window, int sinks) { re
 // key of score row c (0-7) of eight
 __device__ __forceinline__ int key_of(int c) { return c & 1 ? (c & 6) ^ 5 : c; }
 
+__device__ __forceinline__ void store2(bf16 *p, float x, float y) { *(uint32_t *)p = pack(x, y); }
+__device__ __forceinline__ void store2(float *p, float x, float y) { *(float2 *)p = make_float2(x, y); }
+
 // Shared memory behind the partial rows, from `off_pml` on: merged [16][2], weights [16][RW], rows' places [16], ranges' weights [16][8].
 constexpr int join_bytes(int RW) { return 128 + 16 * RW * 4 + 128 + 16 * PAGED_MAX_CLUSTER * 4; }
 
-// The warps' partial rows lie at gen: [warp][16][D + 2] sums, then [warp][16][2] maxima and weights' sums.  extra(r, c, x, y): called for columns
+// The warps' partial rows (packed rows r0 .. r0 + rows - 1 of the sequence) lie at gen: [warp][16][D + 2] sums, then [warp][16][2] maxima and weights' sums.  extra(r, c, x, y): called for columns
 // c and c + 1 of row r once their warps' sums are added up in x and y.
-template <int D, int RW, typename Extra>
-__device__ __forceinline__ void join_rows(const PagedAttnArgs &a, uint8_t *gen, int off_pml, int rows, int row0, int len, int kvh, int split, int splits, Extra extra)
+template <typename T, int D, int RW, typename Extra>
+__device__ __forceinline__ void join_rows(const PagedAttnArgs &a, uint8_t *gen, int off_pml, int rows, int row0, int r0, int kvh, int split, int splits, Extra extra)
 {
     constexpr int R_THREADS = 32 * RW;
     const uint32_t base = tc::smem_u32(gen);
@@ -87,7 +90,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs &a, uint8_t *gen, 
     long *dst_of = (long *)(wt + 16 * RW); // [16]
     float *cw = (float *)(dst_of + 16);    // [16][ranges of a cluster]
     if (threadIdx.x < rows) {
-        const int r = threadIdx.x, i = r / a.group, head = kvh * a.group + r - i * a.group;
+        const int r = threadIdx.x, i = (r0 + r) / a.group, head = kvh * a.group + r0 + r - i * a.group;
         float m = -INFINITY, den = 0.f;
 #pragma unroll
         for (int w = 0; w < RW; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
@@ -117,7 +120,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs &a, uint8_t *gen, 
         extra(r, c, x, y);
         if (a.splits == 1) {
             const float inv = inverse_sum(pml[2 * r + 1]);
-            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x * inv, y * inv);
+            store2((T *)a.out + dst_of[r] + c, x * inv, y * inv);
         } else if (clustered) // only this thread reads (r, c) of the warps' partials: the first one's place keeps the sum
             *(float2 *)(mo + r * (D + 2) + c) = make_float2(x, y);
         else {
@@ -166,7 +169,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs &a, uint8_t *gen, 
                 x = fmaf(v[s].x, f, x);
                 y = fmaf(v[s].y, f, y);
             }
-            *(uint32_t *)((bf16 *)a.out + dst_of[r] + c) = pack(x, y);
+            store2((T *)a.out + dst_of[r] + c, x, y);
         }
         tc::cluster_sync(); // no block exits while a peer still reads its shared memory
     }
