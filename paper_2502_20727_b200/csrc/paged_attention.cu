@@ -314,14 +314,17 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         p.kernel = ATTN_STREAM;
         p.workspace = stream4_workspace((int)rows, d);
         return p;
-    } else if (rows <= PAGED_MAX_FEW_ROWS) {
+    } else if (rows <= PAGED_MAX_FEW_ROWS || (fmt == KV_INT4 && rows <= 2 * PAGED_MAX_FEW_ROWS && (keys <= 4096 || 4L * B * nkv >= sm_count()))) {
+        // 4 bits: up to 32 rows as two tiles of 16, except on long contexts of few (sequence, KV head) pairs.  Measured, 64 heads on 8, us this way and on
+        // tcgen05: 3 tokens, 32 sequences of 500 to 2300 keys 59, 62; 4 tokens, 4 such sequences 14, 19; 4 tokens on 8000 keys 28, 22; five tokens (40 rows),
+        // 32 sequences 82, 61.
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
         // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
         // More than a cluster's worth cost a second kernel (about 2 us) and pay from 512 keys each.  Measured, 8 KV heads of
         // 8 query heads, bf16, us by ranges: 1 x 4096 keys 8: 11.2, 20: 12.8; 1 x 16384 8: 24.9, 20: 22.4; 4 x 4096 2: 24.7,
         // 4: 18.9, 8: 19.1; 16 x 4096 2: 49, 8: 61.
-        const long pairs = (long)(B > 0 ? B : 1) * nkv, sms = sm_count(), resident = fmt == KV_INT4 ? (rows <= 8 ? 3 : 2) : fmt != KV_BF16 && rows <= 8 ? 4 : 3;
+        const long pairs = (long)(B > 0 ? B : 1) * nkv * ((rows + 15) / 16), sms = sm_count(), resident = fmt == KV_INT4 ? (rows <= 8 ? 3 : 2) : fmt != KV_BF16 && rows <= 8 ? 4 : 3;
         long s = sms / pairs >= 2 ? sms / pairs : resident * sms / pairs;
         if (s > (keys + 255) / 256) s = (keys + 255) / 256;
         if (s < (keys + 2047) / 2048) s = (keys + 2047) / 2048;
