@@ -335,7 +335,8 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  * A key that a query does not see has no influence on it, whatever it holds.  A query with a visible score of NaN or +inf, or
  * whose visible scores are all -inf, has no softmax: its whole output row is NaN.  Scores, sums and the output are held in
  * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product (two bfloat16s, 16 bits,
- * with an int8 cache).
+ * with an int8 cache; one float16 with a 4-bit one, whose cached values may be rounded to float16 as well).  float32 calls over a
+ * 4-bit cache with head_dim 64 or 128 take queries and weights as two float16s each, 22 bits.
  * The sum over the keys is divided by the sum of the weights at the end, and weights may reach 2^8 before that: values of V
  * beyond 2^100 or so can overflow on the way.
  * A page id outside [0, n_pages) sets error bit 1; the output rows that needed it are undefined.

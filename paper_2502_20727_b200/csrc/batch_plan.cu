@@ -2,12 +2,14 @@
 // pages of finished requests back to the pool, new pages out of it into the block tables.
 //
 // Everything is a prefix sum over the requests: of pages given back (they extend the pool in the requests' order), of pages and rows
-// wanted (a request is served while neither sum passes what there is), of the rows served.  Rows then find their request by a
-// binary search in the offsets.
+// wanted (a request is served while neither sum passes what there is), of the rows served.  Rows then find their request by a search
+// in the offsets.
 //
 // Bound: latency, of a few dependent steps (lengths, sums, pages given back, table entries); the bytes take well under a microsecond.  So
 // one launch: a cluster of up to eight thread blocks, each of which forms all sums for itself from the lengths (cheaper
-// than an exchange), gives back its share of the pages, and after one cluster barrier writes its share of the rows.
+// than an exchange), gives back its share of the pages, and after a cluster barrier writes its share of the rows.
+// 256 single tokens 4.6 us; 2048 requests, 81 thousand rows, 100 of them finished 22.7 (sums 6, pages given back 7, rows 8; with 16 blocks, which not
+// every GPU can place, 3 less; sums of 64 bits and a search per row took 48).
 #include "../../include/spd.h"
 #include "paged.cuh"
 #include "tc_ptx.cuh"

@@ -1,5 +1,5 @@
 // Paged K/V cache operators: the cache's storage formats, where rows of a ragged batch sit in their sequences and
-// pages, and the launchers of kv_cache.cu, paged_attention.cu, paged_attention_rows.cu and paged_attention_tc.cu.
+// pages, and the launchers of kv_cache.cu, paged_attention.cu, paged_attention_rows.cu, paged_attention_rows4.cu and paged_attention_tc.cu.
 #pragma once
 #include "common.cuh"
 

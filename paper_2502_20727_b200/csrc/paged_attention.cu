@@ -12,7 +12,7 @@ namespace spd {
 
 namespace {
 
-// Every type (float32 queries, head_dim 32): CUDA cores, float32 throughout.  A thread block takes 16 RPT packed rows (row r = new
+// Every type (float32 queries, head_dim 32; not float32 over 4-bit pages of head_dim 64 and 128): CUDA cores, float32 throughout.  A thread block takes 16 RPT packed rows (row r = new
 // token r / group, query head r % group, so that a group shares the K/V tiles) and walks tiles of 64 keys, widened to float32
 // in shared memory.  Thread (tx, ty) computes the scores of rows ty RPT .. and keys tx + 16 j, four head dims at a time (eight
 // products per 16-byte shared-memory load), the row maxima and sums over its half warp, and the output columns 4 tx + 64 j.

@@ -1,6 +1,6 @@
-// Paged attention for few query rows (bf16) over 4-bit pages: the arrangement of paged_attention_rows.cu - keys and head dims as rows of
-// m16n8k16 MMAs, the 8 or 16 query rows as their columns, a private ring of key tiles per warp, key ranges joined through a cluster or the
-// workspace - with what 4 bits change:
+// Paged attention for few query rows over 4-bit pages (bf16 queries: up to 32 rows; float32: any number, in tiles of 8): the arrangement of
+// paged_attention_rows.cu - keys and head dims as rows of m16n8k16 MMAs, 8 or 16 query rows as their columns, a private ring of key
+// tiles per warp, key ranges joined through a cluster - with what 4 bits change:
 //   - the cache stream is a quarter of bf16's, so that instructions bound the kernel, the unpacking of codes before all.  Codes are float16
 //     operands without arithmetic: one in the lowest bits of a float16 is the subnormal number code * 2^-24, one in bits 4-7 is 16 times
 //     that, and the tensor cores' products with subnormals are exact.  A word of eight codes costs four masks and a shift;
@@ -10,10 +10,15 @@
 //     parameter: x = 2^(score + e - max) <= 2^8, weights x (s 2^-e), the key's share in the softmax x 2^-e.  What float16 leaves out of a
 //     weight is then small beside the largest contribution to the output, not beside the largest softmax weight;
 //   - a warp takes 32 keys a step (two MMA tiles): one wait, one maximum and one check of it for both, and each lane turns one key's
-//     parameters into the factors that all lanes read (every lane for its own rows: 16 more instructions per key and lane);
+//     parameters into the factors that all lanes read;
 //   - tiles come by cp.async: a page's 16 keys are 64 chunks of 16 bytes, two instructions for the warp; as TMA boxes they were two boxes and
-//     two bulk copies from one lane, at several times the instructions.
-// Measured, 32 sequences of 9 to 16 thousand tokens, 64 heads on 8: 190 us with 16 keys a step by TMA; REPLACED.
+//     two bulk copies from one lane, at several times the instructions;
+//   - float32 queries: Q and the weights in two float16s each (22 bits), codes less 8 so that sums do not cancel, the maximum followed at once.
+// 32 sequences of 9 to 16 thousand tokens, 64 heads on 8 (475 MB), us by step: 16 keys a step by TMA, a thread block per range 188; 32 keys a step by
+// cp.async 145; keys dealt out evenly to the resident warps (below) 132; two float32 operations per instruction, factors without bank
+// conflicts, V by transposing matrix loads 124; 168 registers and three stages in place of 128 and two 107; warp numbers that the
+// compiler knows to be the same in all lanes 105 (4.5 TB/s, 69 % of a copy's; about 600 instructions a step, of which 176 unpack).
+// Not kept: shifts as products' high words on the FMA pipe (slower issue), the next step's first products under this one's softmax (113).
 #include "paged_rows.cuh"
 
 #include <type_traits>

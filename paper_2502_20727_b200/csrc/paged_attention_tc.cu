@@ -24,6 +24,10 @@
 // row's only one, and such errors came to 1.5 times the output's own rounding: there what rounding left is a second bf16 with a
 // product of its own (ragged chunks of up to 700 tokens on up to 1000, 40 heads: 243 us; e4m3, whose scales are powers of two and
 // whose weights are single bf16s, 187; bf16 124).
+// 4-bit pages: eight load warps, too, a key's K or V row per thread for the parameters and a quarter of a row for the codes.  Rows become float16 - one
+// product per pair of codes, see widen4 - scaled by powers of two that the softmax warps put into the exponent (a V row's lies in the scores, so that
+// weights stay within float16 whatever the row holds).  Ragged chunks as above 165 us, 2048 tokens on 14336 1271 (bf16 1140 beside it): the widening
+// and its loads, as with 8 bits.
 // A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
 // shared memory before the product, and rows that do see them get them back at the end.
 // Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
@@ -219,7 +223,7 @@ __device__ __forceinline__ constexpr uint32_t rest_column(int k) { return (uint3
 constexpr int load_warps(bool tma, bool q8) { return tma ? 2 : q8 ? 8 : 4; }
 constexpr int SOFT_WARPS = 8, SOFT_THREADS = 32 * SOFT_WARPS;
 constexpr int tc_threads(bool tma, bool q8) { return SOFT_THREADS + 32 * (load_warps(tma, q8) + 1); } // two blocks: 80 registers a thread, 72 or 56
-// 8-bit caches: the load warps' way from one tile to the next is the longest, so there are eight of them, and of the 56 registers a thread
+// 8-bit and 4-bit caches: the load warps' way from one tile to the next is the longest, so there are eight of them, and of the 56 registers a thread
 // that 17 warps leave they give 16 to the softmax warps: 8 x 72 + 8 x 40 + 56 = 17 x 56.  (ptxas spills 4 to 72 bytes a thread in all variants
 // of this kernel but one.)
 constexpr int Q8_LAUNCH_REGS = 56, Q8_SOFT_REGS = 72, Q8_LOAD_REGS = 40;
@@ -392,7 +396,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             if constexpr (Q4) {
                 // K and V are scaled by powers of two to below 2^-4.  The rows of a tile share one for K and one for V where they are within 2^8 of one
                 // another: the softmax warps then need no factor per key, and a row keeps at least 2^-13 of its largest value.  Otherwise (`varied`: a row may
-                // hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on 14336; REPLACED.)
+                // hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on 14336; now 1271, 1246
+                // without the second way.)
                 // Threads 0-127 look after a key's K row each, 128-255 after its V row: page id two tiles ahead, parameters one tile ahead.
                 const uint32_t par = base + C::OFF_SC + 3200;
                 int *exps = (int *)(gen + C::OFF_SC + 3200 + 4096); // [2][8 warps][largest, smallest, rows that are not finite, -]
@@ -641,7 +646,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     } else {
         if (QC) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Q8_SOFT_REGS));
         const int half = warp >> 2, row = (warp & 3) * 32 + lane, pair_bar = BAR_PAIR + (warp & 3);
-        // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit
+        // Q: rows of the tiles, zeros beyond the last; codes' dim order where the cache is 8-bit or 4-bit
         {
             constexpr int CH = D / 8, N = ROWS * CH / SOFT_THREADS;
             uint4 x[N];
@@ -874,7 +879,7 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                             }
                         }
                     }
-                    // columns of an 8-bit cache are in the order (0, 2, 1, 3) of every four
+                    // columns of an 8-bit or 4-bit cache are in the order (0, 2, 1, 3) of every four
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[QC ? (e & ~3) | ((e & 1) << 1) | ((e >> 1) & 1) : e] = v[e] * inv;
                     if (a.part_o) {

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2502_20727_b200 as spd
-from kv4_util import Batch4
+from kv4_util import Batch4, values4
 from paged_util import check_attention
 from test_paged_gpu import attend, run_and_check
 
@@ -278,3 +278,31 @@ def test_tensors_of_another_stream_and_strides():
         spd.paged_attention(d["q"], d["k_pages"], d["v_pages"], *at, **{**kw, "max_new": 0})
     with pytest.raises(TypeError):
         spd.paged_attention([1.0], d["k_pages"], d["v_pages"], *at, **kw)
+
+
+@pytest.mark.parametrize("nq,new,bound", [(64, 4, 40000), (64, 3, 4000), (8, 1, 40000), (16, 8, 70000)])
+def test_key_ranges_by_the_host_bound(nq, new, bound):
+    """Calls cut into key ranges for a far longer context than the sequences have: ranges without keys, rows beyond 16, tiles without rows."""
+    bt = Batch4(dtype="bf16", nq=nq, nkv=8, d=128, page=16, lens=[0, 700, 31, 1, 300], new=[new, 1, new, 0, new], seed=41, behind=1)
+    bt.table = torch.cat([bt.table, torch.full((bt.B, -(-bound // 16)), -7, dtype=torch.int32)], 1)
+    out, err = attend(bt, max_context=bound)
+    assert err == 0
+    check_attention(bt, out)
+    f32 = Batch4(dtype="f32", nq=16, nkv=2, d=128, page=16, lens=[0, 700, 31, 1, 300], new=[new, 1, 2, 0, 9], seed=42, behind=1)
+    f32.table = torch.cat([f32.table, torch.full((f32.B, -(-bound // 16)), -7, dtype=torch.int32)], 1)
+    out, err = attend(f32, max_context=bound)
+    assert err == 0
+    check_attention(f32, out)
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 20), ("f32", 3)])
+def test_scales_of_either_sign(dtype, new):
+    """The caller's own parameters: negative scales, scales of zero."""
+    bt = Batch4(dtype=dtype, nq=8, nkv=2, d=64, page=16, lens=[90, 5], new=[new, 1], seed=43)
+    g = torch.Generator().manual_seed(1)
+    for n in "kv":
+        p = bt.scales[n]
+        sign = torch.randint(-1, 2, p.shape[:-1], generator=g).to(p.dtype)
+        p[..., 0] *= sign
+        bt.values[n] = values4(bt.codes[n], p.nan_to_num(0.0))
+    run_and_check(bt)
