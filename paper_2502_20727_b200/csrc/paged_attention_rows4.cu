@@ -13,11 +13,13 @@
 //     parameters into the factors that all lanes read;
 //   - tiles come by cp.async: a page's 16 keys are 64 chunks of 16 bytes, two instructions for the warp; as TMA boxes they were two boxes and
 //     two bulk copies from one lane, at several times the instructions;
-//   - float32 queries: Q and the weights in two float16s each (22 bits), codes less 8 so that sums do not cancel, the maximum followed at once.
+//   - float32 queries: Q and the weights in two float16s each (22 bits), codes less 8 so that sums do not cancel, the maximum followed at once; the tensor cores add up
+//     16 products at a time, float32 additions the rest: their own longer sums are cut off at every step (errors of 3.6e-7 to 1.5e-6 relative to
+//     float64 in place of 1.5e-7 to 3.6e-7, and 3 to 10 % less time).
 // 32 sequences of 9 to 16 thousand tokens, 64 heads on 8 (475 MB), us by step: 16 keys a step by TMA, a thread block per range 188; 32 keys a step by
 // cp.async 145; keys dealt out evenly to the resident warps (below) 132; two float32 operations per instruction, factors without bank
 // conflicts, V by transposing matrix loads 124; 168 registers and three stages in place of 128 and two 107; warp numbers that the
-// compiler knows to be the same in all lanes 105 (4.5 TB/s, 69 % of a copy's; about 600 instructions a step, of which 176 unpack).
+// compiler knows to be the same in all lanes 105 (4.5 TB/s, 69 % of a copy's; about 500 instructions a step, of which 176 unpack).
 // Not kept: shifts as products' high words on the FMA pipe (slower issue), the next step's first products under this one's softmax (113).
 #include "paged_rows.cuh"
 
@@ -353,16 +355,24 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
                 const uint32_t l0 = low(w0[i]), l1 = low(w1[i]), l2 = low(y0), l3 = low(y1), h0 = high(w0[i]), h1 = high(w1[i]), h2 = high(y0), h3 = high(y1);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
-                    if (i == 0) {
+                    if constexpr (F32) {
+                        // sums of 16 products at a time, added in float32: a longer chain in the tensor cores is cut off, not rounded, at every step
+                        float c0[4], c1[4], d0[4], d1[4];
+                        mma16816_zero(c0, l0, l1, l2, l3, qf[n][i][0], qf[n][i][1]);
+                        mma16816_zero(c1, h0, h1, h2, h3, qf[n][W + i][0], qf[n][W + i][1]);
+                        mma16816_zero(d0, l0, l1, l2, l3, ql[n][i][0], ql[n][i][1]);
+                        mma16816_zero(d1, h0, h1, h2, h3, ql[n][W + i][0], ql[n][W + i][1]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            acc[u][0][n][e] = (i ? acc[u][0][n][e] : 0.f) + (c0[e] + d0[e]);
+                            acc[u][1][n][e] = (i ? acc[u][1][n][e] : 0.f) + (c1[e] + d1[e]);
+                        }
+                    } else if (i == 0) {
                         mma16816_zero(acc[u][0][n], l0, l1, l2, l3, qf[n][i][0], qf[n][i][1]);
                         mma16816_zero(acc[u][1][n], h0, h1, h2, h3, qf[n][W + i][0], qf[n][W + i][1]);
                     } else {
                         mma16816<true>(acc[u][0][n], l0, l1, l2, l3, qf[n][i][0], qf[n][i][1]);
                         mma16816<true>(acc[u][1][n], h0, h1, h2, h3, qf[n][W + i][0], qf[n][W + i][1]);
-                    }
-                    if constexpr (F32) {
-                        mma16816<true>(acc[u][0][n], l0, l1, l2, l3, ql[n][i][0], ql[n][i][1]);
-                        mma16816<true>(acc[u][1][n], h0, h1, h2, h3, ql[n][W + i][0], ql[n][W + i][1]);
                     }
                 }
             }
@@ -460,11 +470,17 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
                     const uint32_t l0 = low(x0), l1 = low(y0), l2 = low(x1), l3 = low(y1), h0 = high(x0), h1 = high(y0), h2 = high(x1), h3 = high(y1);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
-                        mma16816<true>(o[n][c + i], l0, l1, l2, l3, pf[0][n][0], pf[0][n][1]);
-                        mma16816<true>(o[n][W + c + i], h0, h1, h2, h3, pf[1][n][0], pf[1][n][1]);
                         if constexpr (F32) {
-                            mma16816<true>(o[n][c + i], l0, l1, l2, l3, pl[0][n][0], pl[0][n][1]);
-                            mma16816<true>(o[n][W + c + i], h0, h1, h2, h3, pl[1][n][0], pl[1][n][1]);
+                            float c0[4], c1[4];
+                            mma16816_zero(c0, l0, l1, l2, l3, pl[0][n][0], pl[0][n][1]);
+                            mma16816_zero(c1, h0, h1, h2, h3, pl[1][n][0], pl[1][n][1]);
+                            mma16816<true>(c0, l0, l1, l2, l3, pf[0][n][0], pf[0][n][1]);
+                            mma16816<true>(c1, h0, h1, h2, h3, pf[1][n][0], pf[1][n][1]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) { o[n][c + i][e] += c0[e]; o[n][W + c + i][e] += c1[e]; }
+                        } else {
+                            mma16816<true>(o[n][c + i], l0, l1, l2, l3, pf[0][n][0], pf[0][n][1]);
+                            mma16816<true>(o[n][W + c + i], h0, h1, h2, h3, pf[1][n][0], pf[1][n][1]);
                         }
                     }
                 }
