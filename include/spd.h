@@ -307,7 +307,8 @@ int spd_kv_write(const spd_kv_cache *cache, const spd_ragged *batch, const void 
 
 /* The same for rows whose places the caller knows, e.g. from spd_plan_batch: row t becomes the cached row at slot
  * slots[t] = page id * kv_block_size + row of the page.  A negative slot belongs to nobody and its row is skipped; a slot whose
- * page id is outside [0, n_pages) sets error bit 1 and is skipped.  One plan serves the appends of all layers. */
+ * page id is outside [0, n_pages) sets error bit 1 and is skipped.  Of two rows with the same slot either may be cached, or a
+ * mixture of both.  One plan serves the appends of all layers. */
 int spd_kv_write_slots(const spd_kv_cache *cache, const int32_t *slots, int32_t n_tokens, const void *k, const void *v,
                        int64_t k_stride, int64_t v_stride, int32_t dtype, int32_t *err_flag, void *stream);
 
@@ -336,9 +337,10 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  * whose visible scores are all -inf, has no softmax: its whole output row is NaN.  Scores, sums and the output are held in
  * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product (two bfloat16s, 16 bits,
  * with an int8 cache; one float16 with a 4-bit one, whose cached values may be rounded to float16 as well).  float32 calls over a
- * 4-bit cache with head_dim 64 or 128 take queries and weights as two float16s each, 22 bits.
+ * 4-bit cache with head_dim 64 or 128 take queries and weights as two float16s each, 22 bits, and round the sum of a score in
+ * base 2 and the exponent of its V row to float32.
  * The sum over the keys is divided by the sum of the weights at the end, and weights may reach 2^8 before that: values of V
- * beyond 2^100 or so can overflow on the way.
+ * beyond 2^100 or so (4 bits: of K too) can overflow on the way.
  * A page id outside [0, n_pages) sets error bit 1; the output rows that needed it are undefined.
  * Errors: SPD_ENULL, SPD_EINVAL, SPD_ECAPACITY (max_context beyond the block table), SPD_EWORKSPACE, SPD_ECUDA. */
 int spd_paged_attention(const spd_kv_cache *cache, const spd_ragged *batch, const void *q, int64_t q_stride, void *out,
@@ -360,6 +362,7 @@ int spd_paged_attention_workspace_bytes(const spd_kv_cache *cache, int32_t B, in
  *   seq_lens, new_lens : [B] device, B at most 16384
  *   block_table : [B, max_pages] device, read and written; max_pages * kv_block_size and n_pages * kv_block_size below 2^31
  *   cu_new      : [B + 1] device, out: row offsets of the served new tokens (spd_ragged.cu_new)
+ *   n_tokens    : rows of positions and slots, at most 2^30
  *   positions   : [n_tokens] device, out: position of every row in its sequence, -1 behind the last row
  *   slots       : [n_tokens] device, out: page id * kv_block_size + row of the page (spd_kv_write_slots), -1 behind the last row
  *   next_lens   : [B] device, out: lengths after the step, 0 for finished requests; not the same array as seq_lens or new_lens

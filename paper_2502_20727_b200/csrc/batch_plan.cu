@@ -20,6 +20,7 @@ namespace {
 
 constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32, PLAN_MAX_CLUSTER = 8;
 constexpr int PLAN_MAX_B = 16384; // two words of shared memory each
+constexpr int PLAN_MAX_TOKENS = 1 << 30; // row numbers and strides between them stay within 32 bits
 
 struct PlanArgs {
     const int32_t *lens, *news, *n_free;
@@ -279,7 +280,7 @@ extern "C" int spd_plan_batch(const spd_page_pool *pool, const int32_t *seq_lens
 {
     if (!pool) return SPD_ENULL;
     if (pool->n_pages < 1 || pool->kv_block_size < 1 || (int64_t)pool->n_pages * pool->kv_block_size > 0x7fffffffLL) return SPD_EINVAL;
-    if (B < 0 || B > PLAN_MAX_B || max_pages < 1 || n_tokens < 0 || (int64_t)max_pages * pool->kv_block_size > 0x7fffffffLL) return SPD_EINVAL;
+    if (B < 0 || B > PLAN_MAX_B || max_pages < 1 || n_tokens < 0 || n_tokens > PLAN_MAX_TOKENS || (int64_t)max_pages * pool->kv_block_size > 0x7fffffffLL) return SPD_EINVAL;
     if (!pool->free_pages || !pool->n_free || !pool->n_free_next || !cu_new || !err_flag) return SPD_ENULL;
     if (B && (!seq_lens || !new_lens || !block_table || !next_lens)) return SPD_ENULL;
     if (n_tokens && (!positions || !slots)) return SPD_ENULL;

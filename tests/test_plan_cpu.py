@@ -27,3 +27,7 @@ def test_binding_refuses_what_does_not_match():
     i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
     with pytest.raises(ValueError):  # no CPU tensors
         spd.plan_batch(i(2), i(2), i(2, 4), i(8), i(1), page=16, n_pages=8, n_tokens=3, err=i(1))
+
+
+def test_more_rows_than_row_numbers(lib):  # noqa: F811
+    assert plan(lib, n=2 ** 30 + 1) == -1 and plan(lib, n=2 ** 31 - 1) == -1
