@@ -327,7 +327,7 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
             sts_f4(fk + F + lane * 16, middle(kp.x), middle(kp.y));
             const uint32_t top = max(vm & 0xffffu, vm >> 16);
             const bool v_bad = top >= 0x7f80u;
-            const int ex = min(max((int)(top >> 7), 127 - 60), 127 + 30);
+            const int ex = min(max((int)(top >> 7), 127 - 60), 127 + 100);
             const float unit = __uint_as_float((uint32_t)(254 - ex) << 23), f = v_bad ? 0.f : unit;
             const float ev = v_bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ex) - (8388608.f + 127.f); // 2^23 + ex
             const uint2 q = v_bad ? make_uint2(0, 0) : vp;

@@ -306,3 +306,21 @@ def test_scales_of_either_sign(dtype, new):
         p[..., 0] *= sign
         bt.values[n] = values4(bt.codes[n], p.nan_to_num(0.0))
     run_and_check(bt)
+
+
+@pytest.mark.parametrize("power", [33, 45, 90])
+@pytest.mark.parametrize("name", ["k", "v"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("new", [1, 40])
+def test_float32_calls_over_very_large_values(power, name, d, new):
+    """K is brought back by the softmax scale.  V: three roundings at a size below 128 (half a step, 2^-18) of a score with its V row's exponent, in a
+    weight and in the weights' sum: 6 ln 2 2^-18, under 2^-15.9 of the largest value that takes part."""
+    bt = Batch4(dtype="f32", nq=8, nkv=2, d=d, page=16, lens=[120, 9], new=[new, 1], seed=44, rows=lambda n, x: x * 2.0 ** power if n == name else x)
+    scale = d ** -0.5 * (2.0 ** -power if name == "k" else 1.0)
+    out, err = attend(bt, scale=scale)
+    assert err == 0
+    ref, tol = bt.reference(scale)
+    live = ~torch.isnan(ref[:, 0, 0])
+    if name == "v":
+        tol = tol + 2.0 ** -15.9 * bt.values["v"].nan_to_num(0.0).abs().max()
+    assert ((out.double().cpu() - ref).abs() <= tol)[live].all()
