@@ -12,8 +12,8 @@
 //          bf16, at least 2^-60; code = (x - m) / s rounded to the nearest integer, half to even.  The quotients are the correctly
 //          rounded ones (from the rounded reciprocal with one residual correction, Markstein 1990), so that ties, which are common among
 //          bf16 values, fall as they do in exact arithmetic.  m <= x, and s is off by 2^-9 at most, so codes end at 15 by themselves.
-//          16 prompts of about 1024 tokens, 40 heads, stored and read back: 131 us (5.4 TB/s; storing is bound by its 120 instructions per
-//          eight elements; eight elements a lane in place of 16: 155).
+//          16 prompts of about 1024 tokens, 40 heads, stored and read back: 131 us (5.4 TB/s; storing is bound by its instructions: with
+//          eight elements a lane in place of 16 155 us at 78 % of the issue slots).
 //
 // Bound: memory.  A thread block serves a few consecutive tokens and 16 cached rows (K and V of eight heads) of each; one warp
 // finds the tokens' sequences and pages for all of them, then every lane moves eight elements of UNITS rows with all loads in
@@ -224,8 +224,8 @@ template <int LANES> __device__ __forceinline__ float2 range_of(const Raw8<float
     }
     return make_float2(lo, hi);
 }
-// 1 / s, rounded to nearest, for a bf16 number s from 2^-60 on: one Newton step from the approximate reciprocal (the same bits as the division's for
-// every such s; the division's own code has a branch for numbers that do not occur here)
+// 1 / s, rounded to nearest, for a bf16 number s from 2^-60 on: one Newton step from the approximate reciprocal (the correctly rounded
+// quotient for every such s: all of them were compared with the division's)
 __device__ __forceinline__ float reciprocal(float s)
 {
     float y;

@@ -351,7 +351,6 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
 cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, cudaStream_t st)
 {
     AttnPlan p = plan_attention(a.kv.fmt, a.kv.d, a.kv.nkv, q_bf16, a.nq, a.rb.B, a.rb.n_tokens, a.max_new, a.max_context, a.window, a.sinks);
-    if (p.kernel == ATTN_STREAM && !part_splits) p = AttnPlan{ATTN_ROWS, 1, 0, 0}; // no workspace
     if (p.workspace && p.splits > part_splits) {
         const int own = p.kernel == ATTN_ROWS ? PAGED_MAX_CLUSTER : 1; // ranges that need no workspace
         p.splits = part_splits > own ? part_splits : own;
