@@ -40,6 +40,7 @@ struct PagedAttnArgs {
     int splits;                   // ranges the keys of a row tile are cut into
     int row_tile;                 // general kernel: rows of a thread block (16 or 64)
     int stages;                   // paged_attention_rows.cu: set by its launcher
+    int longest_first;            // 4-bit caches: thread blocks take the sequences by length (batch_row_by_length)
     float *part_o, *part_ml;      // ranges that no cluster adds up (else null): fp32 [splits][n_tokens * nq][d], [splits][n_tokens * nq][2]
     int *err;
     unsigned long long *stamp;    // the stack's launch timeline, or null
@@ -128,11 +129,8 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
 }
 
 // What a sequence's batch row says, checked once: false (and an error bit) where it does not fit the call.
-__device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
+__device__ __forceinline__ bool batch_row_fits(const RaggedBatch &rb, int max_new, int max_context, int row0, int &n_new, int len, int *err)
 {
-    row0 = rb.cu ? rb.cu[b] : b * rb.uniform;
-    n_new = rb.cu ? rb.cu[b + 1] - row0 : rb.uniform;
-    len = (rb.lens ? rb.lens[b] : 0) + rb.first;
     if (n_new == 0) return false;
     if (row0 < 0 || n_new < 0 || n_new > rb.n_tokens - row0 || n_new > max_new || len < 0 || len > max_context - n_new) {
         atomicOr(err, ERR_CAPACITY);
@@ -140,6 +138,47 @@ __device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_
         return false;
     }
     return true;
+}
+__device__ __forceinline__ bool batch_row(const RaggedBatch &rb, int b, int max_new, int max_context, int &row0, int &n_new, int &len, int *err)
+{
+    row0 = rb.cu ? rb.cu[b] : b * rb.uniform;
+    n_new = rb.cu ? rb.cu[b + 1] - row0 : rb.uniform;
+    len = (rb.lens ? rb.lens[b] : 0) + rb.first;
+    return batch_row_fits(rb, max_new, max_context, row0, n_new, len, err);
+}
+// The same for the sequence b with `place` longer ones: thread blocks start in the order of their numbers, and long sequences that start last are what a
+// launch ends with.  By the whole block (128 threads or more), of a batch with cu and lens of at most ORDER_MAX_B sequences; sm: ORDER_MAX_B + 4 words,
+// 16-byte aligned.  Lengths count up to 2^24, sequences of one length go by their numbers; whatever the lengths hold, every sequence has one place.
+constexpr int ORDER_MAX_B = 128;
+__device__ __forceinline__ bool batch_row_by_length(const RaggedBatch &rb, int place, int max_new, int max_context, int &b, int &row0, int &n_new, int &len, int *err, uint32_t *sm)
+{
+    const int i = threadIdx.x;
+    uint32_t mine = ORDER_MAX_B - 1 - i;
+    if (i < ORDER_MAX_B) {
+        if (i < rb.B) {
+            row0 = rb.cu[i];
+            n_new = rb.cu[i + 1] - row0;
+            len = rb.lens[i];
+            mine |= min((uint32_t)len + (uint32_t)n_new, 0xffffffu) << 7;
+        }
+        sm[i] = mine; // behind the last sequence: less than any
+    }
+    __syncthreads();
+    if (i < rb.B) {
+        int longer = 0;
+        for (int k0 = 0; k0 < rb.B; k0 += 32) {
+            uint4 u[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[k] = *(const uint4 *)(sm + k0 + 4 * k);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) longer += (u[k].x > mine) + (u[k].y > mine) + (u[k].z > mine) + (u[k].w > mine);
+        }
+        if (longer == place) *(int4 *)(sm + ORDER_MAX_B) = make_int4(i, row0, n_new, len);
+    }
+    __syncthreads();
+    const int4 row = *(const int4 *)(sm + ORDER_MAX_B);
+    b = row.x; row0 = row.y; n_new = row.z; len = row.w;
+    return batch_row_fits(rb, max_new, max_context, row0, n_new, len, err);
 }
 
 // What the weighted sum of a row is multiplied by.  Every query sees its own key, so a sum of 0 (all its scores -inf) has no softmax,

@@ -529,8 +529,9 @@ __global__ void __launch_bounds__(32 * RW, RW == 8 ? 1 : NR == 1 && sizeof(T) ==
     const int tile = blockIdx.x / a.kv.nkv; // of 8 NR rows
     q.kvh = blockIdx.x - tile * a.kv.nkv;
     q.b = blockIdx.y;
-    // the same for a whole cluster
-    if (!batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err) || n_new * a.group <= tile * 8 * NR) return;
+    const bool fits = a.longest_first ? batch_row_by_length(a.rb, q.b, a.max_new, a.max_context, q.b, q.row0, n_new, q.len, a.err, (uint32_t *)(gen + C::OFF_JOIN))
+                                      : batch_row(a.rb, q.b, a.max_new, a.max_context, q.row0, n_new, q.len, a.err); // OFF_JOIN: written again after the walk
+    if (!fits || n_new * a.group <= tile * 8 * NR) return; // the same for a whole cluster
     q.keys(a, n_new, tile * 8 * NR, 8 * NR);
     // short sequences are cut into fewer ranges, of at least 4 steps
     const int splits = min(a.splits, (q.n_steps + 3) / 4);

@@ -252,9 +252,13 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) stamp_entry(a.stamp);
     pdl_wait(); // pdl_launch_dependents: below, once the block owns its tensor memory
-    const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kvh = blockIdx.y;
+    int b = blockIdx.z / a.splits;
+    const int split = blockIdx.z % a.splits, kvh = blockIdx.y;
     int row0, n_new, len;
-    if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err)) return;
+    if (Q4 && a.longest_first) { // in a place that is not used before the barrier below
+        if (!batch_row_by_length(a.rb, b, a.max_new, a.max_context, b, row0, n_new, len, a.err, (uint32_t *)(gen + C::OFF_RED))) return;
+    } else if (!batch_row(a.rb, b, a.max_new, a.max_context, row0, n_new, len, a.err))
+        return;
     constexpr int ROWS = TQ;
     const int all_rows = n_new * a.group;
     const int tile = (int)gridDim.x - 1 - (int)blockIdx.x; // the longest rows first

@@ -324,3 +324,60 @@ def test_float32_calls_over_very_large_values(power, name, d, new):
     if name == "v":
         tol = tol + 2.0 ** -15.9 * bt.values["v"].nan_to_num(0.0).abs().max()
     assert ((out.double().cpu() - ref).abs() <= tol)[live].all()
+
+
+def by_length(B, new, dtype="bf16", nq=64, d=128, seed=50):
+    """One tile of rows per sequence and KV head, 19 to 128 sequences of 8 heads: more thread blocks than SMs, at most eight times as many."""
+    rng = random.Random(seed)
+    lens = [rng.choice([0, 0, 7, 31, 64, 64, rng.randint(0, 330)]) for _ in range(B)]
+    return Batch4(dtype=dtype, nq=nq, nkv=8, d=d, page=16, lens=lens, new=[rng.choice([0, 1, new, new]) for _ in range(B)], lead=1, behind=2, seed=seed)
+
+
+@pytest.mark.parametrize("dtype,nq,new,d", [("bf16", 64, 1, 128), ("bf16", 64, 1, 64), ("bf16", 16, 6, 128), ("bf16", 64, 5, 128), ("bf16", 64, 16, 64), ("f32", 8, 8, 64),
+                                            ("f32", 64, 1, 128)])
+@pytest.mark.parametrize("B", [19, 33, 127, 128, 129])
+def test_sequences_by_length(dtype, nq, new, d, B):
+    bt = by_length(B, new, dtype, nq, d, seed=B)
+    run_and_check(bt)
+
+
+@pytest.mark.parametrize("new", [1, 5])
+def test_sequences_by_length_that_do_not_fit(new):
+    bt = by_length(40, new)
+    ref, tol = bt.reference()
+    live = ~torch.isnan(ref[:, 0, 0])
+    b = max((i for i in range(bt.B) if bt.new[i]), key=lambda i: bt.lens[i])
+    for bad in (-1, -2 ** 31, 2 ** 31 - 1, bt.max_context()):
+        dev = bt.device()
+        dev["lens"][b] = bad
+        out, err = attend(bt, dev)
+        assert err == 2, bad
+        keep = live.clone()
+        keep[bt.cu[b]:bt.cu[b + 1]] = False
+        assert ((out.double().cpu() - ref).abs() <= tol)[keep].all(), bad
+        assert (out[bt.cu[b]:bt.cu[b + 1]] == 77).all(), bad
+    dev = bt.device()  # offsets that run backwards: a sequence of a negative number of rows, and one that would have too many
+    at = next(i for i in range(1, bt.B) if bt.new[i - 1] and bt.new[i])
+    dev["cu"][at] = bt.n
+    out, err = attend(bt, dev)
+    assert err == 2
+    keep = live.clone()
+    keep[bt.cu[at - 1]:bt.cu[at + 1]] = False
+    assert ((out.double().cpu() - ref).abs() <= tol)[keep].all()
+
+
+def test_sequences_by_length_give_the_same_bits_in_any_order():
+    bt = by_length(60, 1)
+    first, _ = attend(bt)
+    live = ~torch.isnan(bt.reference()[0][:, 0, 0]).cuda()
+    dev = bt.device()
+    order = torch.randperm(bt.B, generator=torch.Generator().manual_seed(1))
+    new = torch.tensor(bt.new)[order]
+    start = torch.cat([torch.zeros(1, dtype=torch.long), new.cumsum(0)])
+    rows = torch.cat([torch.arange(bt.cu[b], bt.cu[b] + bt.new[b]) for b in order.tolist()]).cuda()
+    dev["q"] = dev["q"][rows].contiguous()
+    dev["cu"], dev["lens"], dev["table"] = start.int().cuda(), dev["lens"][order.cuda()].contiguous(), dev["table"][order.cuda()].contiguous()
+    out = spd.paged_attention(dev["q"], dev["k_pages"], dev["v_pages"], dev["cu"], dev["lens"], dev["table"], max_new=bt.max_new(), max_context=bt.max_context(),
+                              err=dev["err"], k_scales=dev["k_scales"], v_scales=dev["v_scales"])
+    assert int(dev["err"]) == 0 and live[rows].all()
+    assert torch.equal(out, first[rows])
