@@ -309,15 +309,21 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 4L * sm_count() / ((rows + p.row_tile - 1) / p.row_tile * pairs);
         if (s > (keys + 127) / 128) s = (keys + 127) / 128;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-    } else if (fmt == KV_INT4 && rows <= PAGED_MAX_FEW_ROWS && (long)B * nkv * (keys / 32) >= 16L * stream4_workers(rows <= 8 ? 1 : 2) && B <= STREAM_MAX_B &&
+    } else if (fmt == KV_INT4 && rows <= PAGED_MAX_FEW_ROWS && keys >= 2048 && B <= STREAM_MAX_B &&
+               (long)B * nkv * (keys / 32) >= (rows <= 8 ? 32L * stream4_workers(1) : 24L * stream4_workers(2)) &&
                (long)B * nkv * ((keys + max_new) / 32 + 4) < (1L << 30)) { // steps of 32 keys: numbers of 32 bits
+        // Dealt out evenly where the sequences are not short and every warp has 32 (16 rows: 24) steps or more by the bounds: below that the second kernel and
+        // the warps' new starts cost more than the balance gains.  Measured, single tokens, 64 heads on 8, us this way and as thread blocks per sequence: 18 steps
+        // (128 sequences of 129 to 1023 keys) 36, 31; 27 (32 of 1000 to 6000) 49, 38; 36 (32 of 4000 to 8000) 61, 69; 54 (32 of 3000 to 12000) 66, 79; 67 (16 of
+        // 20000 to 30000) 101, 118; on 16 heads 56 steps (200 of 100 to 1000) 87, 79.  128 heads on 8: 30 (24 of 1000 to 6000) 45, 53; 31 (100 of 300 to 1500) 59,
+        // 50; 54 (16 of 4000 to 16000) 69, 99.
         p.kernel = ATTN_STREAM;
         p.workspace = stream4_workspace((int)rows, d);
         return p;
-    } else if (rows <= PAGED_MAX_FEW_ROWS || (fmt == KV_INT4 && rows <= 2 * PAGED_MAX_FEW_ROWS && (keys <= 4096 || 4L * B * nkv >= sm_count()))) {
-        // 4 bits: up to 32 rows as two tiles of 16, except on long contexts of few (sequence, KV head) pairs.  Measured, 64 heads on 8, us this way and on
-        // tcgen05: 3 tokens, 32 sequences of 500 to 2300 keys 59, 62; 4 tokens, 4 such sequences 14, 19; 4 tokens on 8000 keys 28, 22; five tokens (40 rows),
-        // 32 sequences 82, 61.
+    } else if (rows <= PAGED_MAX_FEW_ROWS || (fmt == KV_INT4 && rows <= 2 * PAGED_MAX_FEW_ROWS && (long)B * nkv <= sm_count() && (keys <= 4096 || 4L * B * nkv >= sm_count()))) {
+        // 4 bits: up to 32 rows as two tiles of 16, except for more (sequence, KV head) pairs than SMs and on long contexts of few pairs.  Measured, 64 heads on
+        // 8, us this way and on tcgen05: 4 tokens, 500 to 2300 keys, 4 sequences 14, 19, 8: 21, 28, 16: 36, 39, 32: 62, 50, 64: 118, 83; 4 tokens on 8000 keys
+        // 28, 22; five tokens (40 rows), 32 sequences 82, 50.
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
         // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
@@ -363,7 +369,7 @@ cudaError_t run_paged_attention(PagedAttnArgs &a, int q_bf16, int part_splits, c
         // length 22.4 -> 23.2), five tokens, 32 sequences of 500 to 2300 keys 62 -> 50.  Not for several tiles of rows per sequence, whose short blocks pay
         // the 0.4 us for nothing (ragged chunks 162 -> 161, in float32 12.0 -> 12.6).
         const long rows = (long)a.max_new * a.group, blocks = (long)a.kv.nkv * a.rb.B * p.splits;
-        a.longest_first = rows <= (p.kernel == ATTN_TC ? 128 : q_bf16 && rows > 8 ? 16 : 8) && blocks > sm_count() && blocks <= 8 * sm_count();
+        a.longest_first = rows <= (p.kernel == ATTN_TC ? 128 : q_bf16 ? 2 * PAGED_MAX_FEW_ROWS : 8) && blocks > sm_count() && blocks <= 8 * sm_count();
     }
     if (!p.workspace) a.part_o = a.part_ml = nullptr;
     cudaError_t e = cudaSuccess;

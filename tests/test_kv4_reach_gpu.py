@@ -381,3 +381,10 @@ def test_sequences_by_length_give_the_same_bits_in_any_order():
                               err=dev["err"], k_scales=dev["k_scales"], v_scales=dev["v_scales"])
     assert int(dev["err"]) == 0 and live[rows].all()
     assert torch.equal(out, first[rows])
+
+
+@pytest.mark.parametrize("window,sinks", [(2500, 40), (2048, 0), (2100, 1000)])
+def test_many_sequences_with_a_long_window(window, sinks):
+    """Windows of as many keys as batches that are dealt out have."""
+    run(many(top=3700, window=window, sinks=sinks, seed=60))
+    run(many(B=64, top=3500, new=3, nq=32, window=window, sinks=sinks, seed=61))
