@@ -286,6 +286,23 @@ namespace {
 enum AttnKernel { ATTN_GENERAL, ATTN_ROWS, ATTN_STREAM, ATTN_TC };
 struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; int row_tile; };
 
+// tcgen05 over 4-bit pages: ranges by a model of the time, in units of 50 ns: a key tile takes 2.2 us in a thread block with an SM to itself, 3.6 in each of
+// two; partial rows and their sum 5 us and 0.35 per thousand rows and range.  Against ranges that fill two blocks per SM, of 512 keys or more (the
+// other formats'), us: 6 prompts of 743 tokens, 4 heads on 2, 42 -> 22; 134 tokens on 1000, 64 heads on 8, 34 -> 26; 16 tokens, 2 sequences of 8000 keys, 38 ->
+// 32; 8 sequences of 900 keys, 40 tokens, 32 heads on 8, 37 -> 24; 64 tokens on 6000 keys 44 either way.
+int tc4_splits(long blocks, long tiles, long rows)
+{
+    const long sms = sm_count();
+    long best = 0;
+    int splits = 1;
+    for (int s = 1; s <= 64 && s <= tiles; ++s) {
+        const long running = blocks * s, tile = running <= sms ? 44 : (running + 2 * sms - 1) / (2 * sms) * 72;
+        const long cost = (tiles + s - 1) / s * tile + (s > 1 ? 100 + rows * s * 7 / 1000 : 0);
+        if (s == 1 || cost < best) { best = cost; splits = s; }
+    }
+    return splits;
+}
+
 // Which kernel serves a call, and into how many ranges the keys of its row tiles are cut.
 AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long n_tokens, int max_new, int max_context, int window, int sinks)
 {
@@ -347,6 +364,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 2L * sm_count() / blocks;
         if (s > (keys + 511) / 512) s = (keys + 511) / 512;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+        if (fmt == KV_INT4) p.splits = tc4_splits(blocks, (keys + 127) / 128, n_tokens * nq);
     }
     if (p.kernel == ATTN_ROWS ? p.splits > PAGED_MAX_CLUSTER : p.splits > 1) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
