@@ -214,7 +214,7 @@ constexpr int PAGED_MAX_CONTEXT = 1 << 30;
 // bf16 queries, head_dim 64 or 128, few rows (new tokens x query heads per KV head) per sequence and KV head
 constexpr int PAGED_MAX_FEW_ROWS = 16;
 cudaError_t launch_paged_attention_rows(const PagedAttnArgs &a, cudaStream_t st);
-// The same over 4-bit pages; float32 queries: any number of rows.  stream: all sequences' keys dealt out evenly to the warps that fit the GPU, through part_o (stream4_workspace bytes).
+// The same over 4-bit pages, any number of rows.  stream: all sequences' keys dealt out evenly to the warps that fit the GPU, through part_o (stream4_workspace bytes).
 cudaError_t launch_paged_attention_rows4(const PagedAttnArgs &a, int q_bf16, bool stream, cudaStream_t st);
 constexpr int STREAM_MAX_B = 512; // sequences of such a call: every block sums up their lengths
 int stream4_workers(int groups_of_8_rows);

@@ -303,6 +303,18 @@ int tc4_splits(long blocks, long tiles, long rows)
     return splits;
 }
 
+// Ranges (s, a cluster) that `tiles` row tiles over 4-bit pages are cut into, or fewer where not all clusters would find their SMs at once: these lie in
+// groups of unequal size.  places: clusters of 1 .. 8 thread blocks that a B200 holds with 1, 2 and 3 blocks per SM, as the runtime says.  One cluster too
+// many waits for all the others: single tokens on 2300 keys, 64 heads on 8, 2 sequences as 16 clusters of 8 15 us, of 6 8.3; 6 as 48 of 3 18, of 2 11.6.
+long clusters_that_fit(long s, long tiles, int resident)
+{
+    static const int places[3][PAGED_MAX_CLUSTER] = {{148, 74, 45, 33, 26, 22, 15, 15}, {296, 148, 93, 71, 56, 45, 37, 33}, {444, 222, 142, 104, 82, 71, 56, 48}};
+    const int per_sm = tiles * s <= sm_count() ? 1 : resident;
+    if (s <= PAGED_MAX_CLUSTER && tiles * s <= (long)per_sm * sm_count())
+        while (s > 1 && tiles > places[per_sm - 1][s - 1]) --s;
+    return s;
+}
+
 // Which kernel serves a call, and into how many ranges the keys of its row tiles are cut.
 AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long n_tokens, int max_new, int max_context, int window, int sinks)
 {
@@ -311,13 +323,14 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
     const long rows = (long)max_new * (nq / nkv);
     long keys = max_context;
     if (window && keys > (long)window + max_new + sinks) keys = (long)window + max_new + sinks;
+    const long tiles16 = (rows + 15) / 16 * nkv * (B > 0 ? B : 1);
     if (fmt == KV_INT4 && dtype == 0 && d != 32) {
         // tiles of 8 rows; ranges of the keys, joined in a cluster, where the tiles do not fill the GPU, none under 256 keys
         p.kernel = ATTN_ROWS;
         const long blocks = (rows + 7) / 8 * nkv * (B > 0 ? B : 1), sms = sm_count();
         long s = sms / blocks >= 2 ? sms / blocks : 2 * sms / blocks;
         if (s > (keys + 255) / 256) s = (keys + 255) / 256;
-        p.splits = (int)(s < 1 ? 1 : s > PAGED_MAX_CLUSTER ? PAGED_MAX_CLUSTER : s);
+        p.splits = (int)(s < 1 ? 1 : clusters_that_fit(s > PAGED_MAX_CLUSTER ? PAGED_MAX_CLUSTER : s, blocks, 2));
     } else if (dtype != 1 || d == 32) {
         // 64-row tiles do the most products per shared-memory load (four chunks of up to 512 rows, head_dim 64, with ranges of four
         // tiles or more: 64 rows 38.7 us, 32 rows 57; with the finer ranges below 64 rows take 30); ranges where the tiles do not give every SM four thread blocks, of at least two tiles of 64 keys
@@ -337,17 +350,21 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         p.kernel = ATTN_STREAM;
         p.workspace = stream4_workspace((int)rows, d);
         return p;
-    } else if (rows <= PAGED_MAX_FEW_ROWS || (fmt == KV_INT4 && rows <= 2 * PAGED_MAX_FEW_ROWS && (long)B * nkv <= sm_count() && (keys <= 4096 || 4L * B * nkv >= sm_count()))) {
+    } else if (rows <= PAGED_MAX_FEW_ROWS ||
+               (fmt == KV_INT4 && rows <= 2 * PAGED_MAX_FEW_ROWS && (long)B * nkv <= sm_count() && (keys <= 4096 || 4L * B * nkv >= sm_count())) ||
+               (fmt == KV_INT4 && tiles16 <= sm_count() && keys <= 4096 && tiles16 * keys <= 2048L * sm_count())) {
         // 4 bits: up to 32 rows as two tiles of 16, except for more (sequence, KV head) pairs than SMs and on long contexts of few pairs.  Measured, 64 heads on
         // 8, us this way and on tcgen05: 4 tokens, 500 to 2300 keys, 4 sequences 14, 19, 8: 21, 28, 16: 36, 39, 32: 62, 50, 64: 118, 83; 4 tokens on 8000 keys
-        // 28, 22; five tokens (40 rows), 32 sequences 82, 50.
+        // 28, 22; five tokens (40 rows), 32 sequences 82, 50.  More rows where their tiles of 16 find an SM each and the contexts are short; one sequence, 64 heads
+        // on 8: 8 tokens on 200 keys 7, 11, on 2300: 13, 17; 35 tokens on 1000 keys 15, 19, on 3900 (not here) 31, 28.
         p.kernel = ATTN_ROWS;
         // Ranges enough to give every SM one (wide) thread block, or, where there are many (sequence, KV head) pairs, to fill
         // the resident ones; at least one per 2048 keys, which evens out sequences of unequal length; none under 256 keys.
         // More than a cluster's worth cost a second kernel (about 2 us) and pay from 512 keys each.  Measured, 8 KV heads of
         // 8 query heads, bf16, us by ranges: 1 x 4096 keys 8: 11.2, 20: 12.8; 1 x 16384 8: 24.9, 20: 22.4; 4 x 4096 2: 24.7,
         // 4: 18.9, 8: 19.1; 16 x 4096 2: 49, 8: 61.
-        const long pairs = (long)(B > 0 ? B : 1) * nkv * ((rows + 15) / 16), sms = sm_count(), resident = fmt == KV_INT4 ? (rows <= 8 ? 3 : 2) : fmt != KV_BF16 && rows <= 8 ? 4 : 3;
+        const long pairs = (long)(B > 0 ? B : 1) * nkv * ((rows + 15) / 16), sms = sm_count();
+        const int resident = fmt == KV_INT4 ? (rows <= 8 ? 3 : 2) : fmt != KV_BF16 && rows <= 8 ? 4 : 3;
         long s = sms / pairs >= 2 ? sms / pairs : resident * sms / pairs;
         if (s > (keys + 255) / 256) s = (keys + 255) / 256;
         if (s < (keys + 2047) / 2048) s = (keys + 2047) / 2048;
@@ -356,6 +373,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
             if (s > 64) s = 64;
             if (s < 12) s = PAGED_MAX_CLUSTER;
         }
+        if (fmt == KV_INT4) s = clusters_that_fit(s, pairs, resident);
         p.splits = (int)(s < 1 ? 1 : s);
     } else {
         // two thread blocks per SM: ranges where the row tiles leave some idle, of at least four tiles of 128 keys

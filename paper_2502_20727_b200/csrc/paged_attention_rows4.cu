@@ -1,4 +1,4 @@
-// Paged attention for few query rows over 4-bit pages (bf16 queries: up to 32 rows; float32: any number, in tiles of 8): the arrangement of
+// Paged attention for few query rows over 4-bit pages (bf16 queries: up to 32 rows, more in small calls; float32: any number, in tiles of 8): the arrangement of
 // paged_attention_rows.cu - keys and head dims as rows of m16n8k16 MMAs, 8 or 16 query rows as their columns, a private ring of key
 // tiles per warp, key ranges joined through a cluster - with what 4 bits change:
 //   - the cache stream is a quarter of bf16's, so that instructions bound the kernel, the unpacking of codes before all.  Codes are float16

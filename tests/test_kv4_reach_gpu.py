@@ -388,3 +388,13 @@ def test_many_sequences_with_a_long_window(window, sinks):
     """Windows of as many keys as batches that are dealt out have."""
     run(many(top=3700, window=window, sinks=sinks, seed=60))
     run(many(B=64, top=3500, new=3, nq=32, window=window, sinks=sinks, seed=61))
+
+
+@pytest.mark.parametrize("B,nq,nkv,new", [(1, 64, 8, 5), (1, 64, 8, 36), (2, 64, 8, 9), (1, 8, 1, 140), (1, 32, 32, 64), (1, 8, 8, 287), (3, 16, 2, 100), (4, 64, 8, 6), (1, 12, 4, 300),
+                                          (2, 20, 4, 71), (6, 64, 8, 1), (2, 64, 8, 1), (3, 64, 8, 2), (11, 64, 8, 1), (1, 108, 108, 1)])
+@pytest.mark.parametrize("d,window", [(128, 0), (64, 0), (128, 150)])
+def test_many_rows_of_small_calls(B, nq, nkv, new, d, window):
+    """Rows in tiles of 16 with an SM each, beside calls that just pass that bound; ranges as clusters that fill the GPU."""
+    rng = random.Random(B + new)
+    run_and_check(Batch4(dtype="bf16", nq=nq, nkv=nkv, d=d, page=16, lens=[rng.choice([0, 40, 700, 1300]) for _ in range(B)], new=[new] + [rng.randint(0, new) for _ in range(B - 1)],
+                         window=window, sinks=9 if window else 0, lead=1, behind=2, seed=70))
