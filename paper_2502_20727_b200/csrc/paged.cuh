@@ -181,6 +181,13 @@ __device__ __forceinline__ bool batch_row_by_length(const RaggedBatch &rb, int p
     return batch_row_fits(rb, max_new, max_context, row0, n_new, len, err);
 }
 
+// Tiles of `per` packed rows that a sequence can have.  max_new is a host bound of up to 2^30, but no sequence has more rows than the tensors, which fit the
+// GPU: in a launch of this many tiles the rows' numbers stay within 32 bits.
+inline long row_tiles(const PagedAttnArgs &a, int per)
+{
+    return ((long)(a.max_new < a.rb.n_tokens ? a.max_new : a.rb.n_tokens) * a.group + per - 1) / per;
+}
+
 // What the weighted sum of a row is multiplied by.  Every query sees its own key, so a sum of 0 (all its scores -inf) has no softmax,
 // and neither has one of NaN.
 __device__ __forceinline__ float inverse_sum(float den) { return den > 0.f ? 1.f / den : __uint_as_float(0x7fc00000u); }

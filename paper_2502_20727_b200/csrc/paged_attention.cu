@@ -238,7 +238,7 @@ template <typename T, int FMT, int D, int RPT> cudaError_t launch_general(const 
     static SmemLimit limit;
     const cudaError_t e = limit.raise((const void *)paged_attention_general_kernel<T, FMT, D, RPT>, C::SMEM);
     if (e != cudaSuccess) return e;
-    const long tiles = ((long)a.max_new * a.group + C::RT - 1) / C::RT;
+    const long tiles = row_tiles(a, C::RT);
     return launch_kernel(paged_attention_general_kernel<T, FMT, D, RPT>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(G_THREADS), C::SMEM, st, 0, a);
 }
 template <typename T, int FMT, int D> cudaError_t general_by_rows(const PagedAttnArgs &a, cudaStream_t st)

@@ -762,8 +762,7 @@ template <typename T, int D, int NR, int RW, bool PAGES> cudaError_t launch_rows
     static SmemLimit limit;
     const cudaError_t e = limit.raise((const void *)paged_attention_rows4_kernel<T, D, NR, RW, PAGES>, C::SMEM);
     if (e != cudaSuccess) return e;
-    const long tiles = ((long)a.max_new * a.group + 8 * NR - 1) / (8 * NR);
-    if (tiles * a.kv.nkv > 0x7fffffffL) return cudaErrorInvalidConfiguration;
+    const long tiles = row_tiles(a, 8 * NR);
     return launch_kernel_z(paged_attention_rows4_kernel<T, D, NR, RW, PAGES>, dim3((unsigned)(a.kv.nkv * tiles), a.rb.B, a.splits), dim3(32 * RW), C::SMEM, st, a.part_o ? 1 : a.splits, a);
 }
 template <int D, int NR, bool PAGES> cudaError_t launch_stream4(PagedAttnArgs a, cudaStream_t st)
@@ -786,7 +785,7 @@ template <typename T, int D, int NR> cudaError_t rows4_by_page(const PagedAttnAr
     if constexpr (sizeof(T) == 2)
         if (stream) return pages ? launch_stream4<D, NR, true>(a, st) : launch_stream4<D, NR, false>(a, st);
     if (!pages) return launch_rows4<T, D, NR, 4, false>(a, st);
-    if ((long)a.kv.nkv * a.rb.B * a.splits * (((long)a.max_new * a.group + 8 * NR - 1) / (8 * NR)) <= sm_count()) return launch_rows4<T, D, NR, 8, true>(a, st);
+    if ((long)a.kv.nkv * a.rb.B * a.splits * row_tiles(a, 8 * NR) <= sm_count()) return launch_rows4<T, D, NR, 8, true>(a, st);
     return launch_rows4<T, D, NR, 4, true>(a, st);
 }
 template <int D> cudaError_t rows4_by_type(const PagedAttnArgs &a, int q_bf16, bool stream, cudaStream_t st)

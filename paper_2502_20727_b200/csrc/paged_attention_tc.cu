@@ -932,7 +932,7 @@ template <int FMT, int D, bool TMA> cudaError_t launch_tc(const PagedAttnArgs &a
     }
     const cudaError_t e = limit.raise((const void *)paged_attention_tc_kernel<FMT, D, TMA>, TcCfg<D>::SMEM);
     if (e != cudaSuccess) return e;
-    const long tiles = ((long)a.max_new * a.group + TQ - 1) / TQ;
+    const long tiles = row_tiles(a, TQ);
     return launch_kernel(paged_attention_tc_kernel<FMT, D, TMA>, dim3((unsigned)tiles, a.kv.nkv, a.rb.B * a.splits), dim3(tc_threads(TMA, FMT != KV_BF16)),
                          TcCfg<D>::SMEM, st, 0, km, vm, a);
 }
