@@ -711,7 +711,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             // 4 bits: factors of the K rows, exponents of the V rows (which the scores have in them) and their negative powers; one of each for the tile unless `varied`
             const float *f4 = sc + (j & 1) * 400 + half * 64;
             const bool varied = Q4 && sc[(j & 1) * 400 + 384] != 0.f;
-            const float kq = !Q4 ? qs : varied ? 1.f : qs * f4[0], ev = Q4 && !varied ? f4[128] : 0.f, v_unit = Q4 && !varied ? f4[256] : 1.f;
+            // A product of queries and keys next to zero must not become 0: masked scores are -inf before it.
+            const float kq = !Q4 ? qs : varied ? 1.f : fmaxf(qs * f4[0], 0x1p-126f), ev = Q4 && !varied ? f4[128] : 0.f, v_unit = Q4 && !varied ? f4[256] : 1.f;
             // 32 scores (as read) in columns c0 ..: scaled by the keys' scales, -inf where the row does not see the key
             auto finish = [&](int c0, uint32_t (&r)[32]) {
                 if (Q4 && varied) {
