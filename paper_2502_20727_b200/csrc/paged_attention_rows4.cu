@@ -332,7 +332,9 @@ __device__ __forceinline__ void walk(const PagedAttnArgs &a, const Rows &q, int 
             const float ev = v_bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ex) - (8388608.f + 127.f); // 2^23 + ex
             const uint2 q = v_bad ? make_uint2(0, 0) : vp;
             sts_f4(fk + 2 * F + lane * 16, kv4_scale(q.x) * (f * U::WEIGHT), kv4_scale(q.y) * (f * U::WEIGHT));
-            sts_f4(fk + 3 * F + lane * 16, middle(q.x) * f, middle(q.y) * f);
+            // the power of two first: 8 s of a finite row that nobody sees may be no float, and its weight of 0 would make a NaN of that
+            auto scaled_middle = [f](uint32_t p) { return F32 ? fmaf(8.f, kv4_scale(p) * f, kv4_min(p) * f) : kv4_min(p) * f; };
+            sts_f4(fk + 3 * F + lane * 16, scaled_middle(q.x), scaled_middle(q.y));
             sts_f4(fk + 4 * F + lane * 16, ev, unit);
         }
         float2 s[2][NR][2], unit[2][2]; // scores in base-2 units; [tile][rows g and g + 8]
