@@ -287,18 +287,23 @@ enum AttnKernel { ATTN_GENERAL, ATTN_ROWS, ATTN_STREAM, ATTN_TC };
 struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; int row_tile; };
 
 // tcgen05 over 4-bit pages: ranges by a model of the time, in units of 50 ns: a key tile takes 2.2 us in a thread block with an SM to itself, 3.6 in each of
-// two; partial rows and their sum 5 us and 0.35 per thousand rows and range.  Against ranges that fill two blocks per SM, of 512 keys or more (the
-// other formats'), us: 6 prompts of 743 tokens, 4 heads on 2, 42 -> 22; 134 tokens on 1000, 64 heads on 8, 34 -> 26; 16 tokens, 2 sequences of 8000 keys, 38 ->
-// 32; 8 sequences of 900 keys, 40 tokens, 32 heads on 8, 37 -> 24; 64 tokens on 6000 keys 44 either way.
-int tc4_splits(long blocks, long tiles, long rows)
+// two; partial rows and their sum 5 us and 0.35 per thousand rows and range.  The model takes all sequences for as long as the bound.  Several are mostly not,
+// and thread blocks beyond one per SM even that out by themselves: there ranges have to gain 15 %, and beyond those that run at a time there are none.  At most four
+// times as many blocks as run at a time (79 MB of partial rows of 128 on 148 SMs), which keeps the launch within its limits, too.  Measured, us in one range
+// and by this rule, 64 heads on 8 unless said: one sequence, 128 tokens on 14000 keys (64 blocks) 236, 112; 300 on 16000 (152) 388, 285; 600 (304) 610, 515; 700 (352) 618, 552; 2000
+// on 8000, 8 heads on 8 (128) 170, 148; 16 sequences, up to 8 tokens on 2000 to 8000 keys (128) 133, 90; 20, five tokens on 8000 (160) 199, 156; 24, on 2000 to 8000 (192) 154,
+// 110.  Where there are none, us in one range and in two or three: one sequence, 1024 tokens on 14336 keys (512) 698, 698; 2048 (1024) 1258, 1408; 40 sequences, five tokens on 2000
+// to 8000 keys (320) 162, 165; 100 to 128 tokens on 500 to 4000 keys, 40 heads on 40, 4 sequences (160) 74, 90; 8 (320) 112, 168.
+int tc4_splits(long blocks, long tiles, long rows, int B)
 {
-    const long sms = sm_count();
-    long best = 0;
+    const long sms = sm_count(), two = 2 * sms; // two: blocks that run at a time
+    if (B > 1 && blocks > two) return 1;
+    auto pace = [=](long n) { return n / two * 72 + (n % two == 0 ? 0 : n % two <= sms ? 44 : 72); }; // time of a key tile in each of n blocks
+    long best = tiles * pace(blocks) * (B == 1 ? 95 : blocks > sms ? 85 : 100) / 100;
     int splits = 1;
-    for (int s = 1; s <= 64 && s <= tiles; ++s) {
-        const long running = blocks * s, tile = running <= sms ? 44 : (running + 2 * sms - 1) / (2 * sms) * 72;
-        const long cost = (tiles + s - 1) / s * tile + (s > 1 ? 100 + rows * s * 7 / 1000 : 0);
-        if (s == 1 || cost < best) { best = cost; splits = s; }
+    for (int s = 2; s <= 64 && s <= tiles && blocks * s <= 4 * two; ++s) {
+        const long cost = (tiles + s - 1) / s * pace(blocks * s) + 100 + rows * s * 7 / 1000;
+        if (cost < best) { best = cost; splits = s; }
     }
     return splits;
 }
@@ -382,7 +387,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 2L * sm_count() / blocks;
         if (s > (keys + 511) / 512) s = (keys + 511) / 512;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-        if (fmt == KV_INT4) p.splits = tc4_splits(blocks, (keys + 127) / 128, n_tokens * nq);
+        if (fmt == KV_INT4) p.splits = tc4_splits(blocks, (keys + 127) / 128, n_tokens * nq, B);
     }
     if (p.kernel == ATTN_ROWS ? p.splits > PAGED_MAX_CLUSTER : p.splits > 1) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
