@@ -789,7 +789,9 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
                 }
             }
             const float mb = m_used == -INFINITY ? 0.f : m_used;
-            const float2 q2 = make_float2(kq, kq), m2 = make_float2(ev - mb, ev - mb);
+            // 4 bits: weights reach 2^15 in place of 2^8, so that float16 keeps those down to 2^-31 of the largest; a row's sum is the same times larger
+            const float shift = ev - mb + (Q4 ? 7.f : 0.f);
+            const float2 q2 = make_float2(kq, kq), m2 = make_float2(shift, shift);
             float2 ls = make_float2(0.f, 0.f);
             auto weigh = [&](int c0, uint32_t (&r)[32], const bool own_units) {
                 uint32_t w[16];
