@@ -132,6 +132,16 @@ int32_t *flag(PyObject *o, int dev)
     return (int32_t *)t.data_ptr();
 }
 
+// f() without the interpreter's lock: other threads run while the driver makes a call wait (a full queue, an allocation)
+template <typename F> auto unlocked(F f)
+{
+    struct Lock {
+        PyThreadState *state = PyEval_SaveThread();
+        ~Lock() { PyEval_RestoreThread(state); }
+    } lock;
+    return f();
+}
+
 struct OnDevice { // makes `dev` current; its current stream
     c10::cuda::OptionalCUDAGuard guard;
     void *stream;
@@ -171,7 +181,8 @@ PyObject *kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
         const spd_ragged r = ragged(a[4], a[5], a[6], dev, k.size(0));
         int32_t *err = flag(a[7], dev);
         const OnDevice on(dev);
-        check("spd_kv_write", spd_kv_write(&c, &r, k.data_ptr(), v.data_ptr(), ks, vs, dtype_of(k), err, on.stream));
+        void *kd = k.data_ptr(), *vd = v.data_ptr();
+        check("spd_kv_write", unlocked([&] { return spd_kv_write(&c, &r, kd, vd, ks, vs, dtype_of(k), err, on.stream); }));
         Py_RETURN_NONE;
     });
 }
@@ -189,7 +200,8 @@ PyObject *kv_write_slots(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (tokens > 0x7fffffff) value_error("k: sizes beyond 32 bits");
         int32_t *err = flag(a[5], dev);
         const OnDevice on(dev);
-        check("spd_kv_write_slots", spd_kv_write_slots(&c, slots, (int32_t)tokens, k.data_ptr(), v.data_ptr(), ks, vs, dtype_of(k), err, on.stream));
+        void *kd = k.data_ptr(), *vd = v.data_ptr();
+        check("spd_kv_write_slots", unlocked([&] { return spd_kv_write_slots(&c, slots, (int32_t)tokens, kd, vd, ks, vs, dtype_of(k), err, on.stream); }));
         Py_RETURN_NONE;
     });
 }
@@ -206,8 +218,10 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
             const int64_t tokens = PyLong_AsLongLong(a[6]);
             if (PyErr_Occurred()) throw Raised{};
             const auto options = tensor(a[0], "k_pages").options().dtype(bf16 ? at::kBFloat16 : at::kFloat);
-            k = at::empty({tokens, c.n_kv_heads, c.head_dim}, options);
-            v = at::empty({tokens, c.n_kv_heads, c.head_dim}, options);
+            unlocked([&] {
+                k = at::empty({tokens, c.n_kv_heads, c.head_dim}, options);
+                v = at::empty({tokens, c.n_kv_heads, c.head_dim}, options);
+            });
         } else {
             k = tensor(a[10], "out");
             v = tensor(a[11], "out");
@@ -218,7 +232,8 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
         int32_t *err = flag(a[5], dev);
         {
             const OnDevice on(dev);
-            check("spd_kv_read", spd_kv_read(&c, &r, k.data_ptr(), v.data_ptr(), ks, vs, dtype_of(k), err, on.stream));
+            void *kd = k.data_ptr(), *vd = v.data_ptr();
+            check("spd_kv_read", unlocked([&] { return spd_kv_read(&c, &r, kd, vd, ks, vs, dtype_of(k), err, on.stream); }));
         }
         PyObject *pair = PyTuple_New(2);
         if (!pair) throw Raised{};
@@ -240,7 +255,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (nq > 0x7fffffff) value_error("q: sizes beyond 32 bits");
         at::Tensor out;
         int64_t os = nq * d;
-        if (a[14] == Py_None) out = at::empty({tokens, nq, d}, q.options());
+        if (a[14] == Py_None) unlocked([&] { out = at::empty({tokens, nq, d}, q.options()); });
         else {
             out = tensor(a[14], "out");
             if (out.scalar_type() != q.scalar_type() || !out.sizes().equals(q.sizes())) value_error("out: shape and dtype of q");
@@ -265,14 +280,18 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         {
             const OnDevice on(dev);
-            // what the arguments ask for; what they are refused for the call itself says
-            if (a[15] == Py_None && spd_paged_attention_workspace_bytes(&c, r.B, r.n_tokens, dtype_of(q), (int32_t)nq, max_new, max_context, window, sinks, &ws_bytes) == SPD_OK &&
-                ws_bytes && r.B && r.n_tokens) {
-                ws = at::empty({(int64_t)ws_bytes}, q.options().dtype(at::kByte));
-                ws_ptr = ws.data_ptr();
-            }
-            check("spd_paged_attention", spd_paged_attention(&c, &r, q.data_ptr(), qs, out.data_ptr(), os, dtype_of(q), (int32_t)nq, max_new, max_context, (float)scale,
-                                                             window, sinks, ws_ptr, ws_ptr ? ws_bytes : 0, err, on.stream));
+            void *qd = q.data_ptr(), *od = out.data_ptr();
+            const bool own_ws = a[15] == Py_None;
+            check("spd_paged_attention", unlocked([&] {
+                // what the arguments ask for; what they are refused for the call itself says
+                if (own_ws && spd_paged_attention_workspace_bytes(&c, r.B, r.n_tokens, dtype_of(q), (int32_t)nq, max_new, max_context, window, sinks, &ws_bytes) == SPD_OK &&
+                    ws_bytes && r.B && r.n_tokens) {
+                    ws = at::empty({(int64_t)ws_bytes}, q.options().dtype(at::kByte));
+                    ws_ptr = ws.data_ptr();
+                }
+                return spd_paged_attention(&c, &r, qd, qs, od, os, dtype_of(q), (int32_t)nq, max_new, max_context, (float)scale, window, sinks, ws_ptr, ws_ptr ? ws_bytes : 0, err,
+                                           on.stream);
+            }));
         }
         if (a[14] != Py_None) {
             Py_INCREF(a[14]);
@@ -301,7 +320,7 @@ PyObject *plan_batch(PyObject *, PyObject *const *a, Py_ssize_t n)
             result = PyTuple_New(5);
             if (!result) throw Raised{};
             at::AutoDispatchBelowADInplaceOrView views;
-            const at::Tensor all = at::empty({2 * B + 2 + 2 * (int64_t)n_tokens}, table.options().dtype(at::kInt));
+            const at::Tensor all = unlocked([&] { return at::empty({2 * B + 2 + 2 * (int64_t)n_tokens}, table.options().dtype(at::kInt)); });
             int64_t at_ = 0;
             for (int i = 0; i < 5; ++i) {
                 const at::Tensor t = all.narrow(0, at_, sizes[i]);
@@ -320,7 +339,7 @@ PyObject *plan_batch(PyObject *, PyObject *const *a, Py_ssize_t n)
             const int32_t *lens = int32s(a[0], "seq_lens", dev, {B}), *news = int32s(a[1], "new_lens", dev, {B});
             int32_t *entries = int32s(a[2], "block_table", dev, {B, width}), *err = flag(a[8], dev);
             const OnDevice on(dev);
-            check("spd_plan_batch", spd_plan_batch(&pool, lens, news, (int32_t)B, entries, (int32_t)width, n_tokens, p[0], p[1], p[2], p[3], err, on.stream));
+            check("spd_plan_batch", unlocked([&] { return spd_plan_batch(&pool, lens, news, (int32_t)B, entries, (int32_t)width, n_tokens, p[0], p[1], p[2], p[3], err, on.stream); }));
         } catch (...) {
             Py_DECREF(result);
             throw;
