@@ -311,7 +311,7 @@ PyObject *plan_batch(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t B = table.size(0), width = table.size(1);
         if (B > 0x7ffffffe || width > 0x7fffffff) value_error("block_table: sizes beyond 32 bits");
         const int32_t page = int32_arg(a[5]), n_pages = int32_arg(a[6]), n_tokens = int32_arg(a[7]);
-        if (n_tokens < 0) check("spd_plan_batch", SPD_EINVAL);
+        if (n_tokens < 0 || n_tokens > 1 << 30) check("spd_plan_batch", SPD_EINVAL); // before there are outputs of such a size
         const int64_t sizes[5] = {B + 1, n_tokens, n_tokens, B, 1};
         static const char *const names[5] = {"out.cu_new", "out.positions", "out.slots", "out.next_lens", "out.n_free"};
         PyObject *result = nullptr;
