@@ -270,7 +270,8 @@ int spd_gemm_bf16_sum_static(const void *a, const void *w, float *c, int32_t M, 
  *                 4-7.  k_scales / v_scales point to [n_pages, n_kv_heads, kv_block_size, 2 halves, 2 (s, m)] bfloat16,
  *                 8-byte aligned.  A row with a NaN or an infinity (or a half whose max - m is no float) gets four NaNs and
  *                 codes 0; a row one of whose four parameters is not finite stands for NaNs.  bfloat16 calls may take a row with values of
- *                 2^30 and more for one that is not finite, and V rows that a query sees together should be within 2^60 of one another. */
+ *                 2^30 and more for one that is not finite.  V rows that a query sees together should be within 2^100 of one another, a
+ *                 row of zeros counting as 2^-60: a key may drop out of the softmax beside one whose V row is larger than that. */
 #define SPD_KV_F32 0
 #define SPD_KV_BF16 1
 #define SPD_KV_E4M3 2
