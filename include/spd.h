@@ -334,10 +334,11 @@ int spd_kv_read(const spd_kv_cache *cache, const spd_ragged *batch, void *k, voi
  *            between the sinks and the window may name anything (the pages may have been given back).
  *   workspace : device memory, 256-byte aligned, at least spd_paged_attention_workspace_bytes() (may be null where that is
  *            0); contents before and after do not matter; calls that may run at the same time need one each.
- * A key that a query does not see has no influence on it, whatever it holds.  A query with a visible score of NaN or +inf, or
+ * A key that a query does not see has no influence on it, whatever it holds, but on which way the roundings named here go.  A query with a visible score of NaN or +inf, or
  * whose visible scores are all -inf, has no softmax: its whole output row is NaN.  Scores, sums and the output are held in
  * float32 until the end; bfloat16 calls round the softmax weights to bfloat16 for the second product (two bfloat16s, 16 bits,
- * with an int8 cache; one float16 with a 4-bit one, whose cached values may be rounded to float16 as well).  float32 calls over a
+ * with an int8 cache; one float16 with a 4-bit one, whose cached values may be rounded to float16 as well, and be off by 2^-10 of
+ * the larger of 16 s and |m| of their row where a neighbouring row is much larger).  float32 calls over a
  * 4-bit cache with head_dim 64 or 128 take queries and weights as two float16s each, 22 bits, and round the sum of a score in
  * base 2 and the exponent of its V row to float32.
  * The sum over the keys is divided by the sum of the weights at the end, and weights may reach 2^8 before that: values of V

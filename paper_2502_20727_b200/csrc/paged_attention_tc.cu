@@ -399,7 +399,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             };
             if constexpr (Q4) {
                 // K and V are scaled by powers of two to below 2^-4.  The rows of a tile share one for K and one for V where they are within 2^8 of one
-                // another: the softmax warps then need no factor per key, and a row keeps at least 2^-13 of its largest value.  Otherwise (`varied`: a row may
+                // another, seen by all queries or not: the softmax warps then need no factor per key, and a value is off by 2^-10 of its row's largest power of two at
+                // most.  Otherwise (`varied`: a row may
                 // hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on 14336; now 1271, 1246
                 // without the second way.)
                 // Threads 0-127 look after a key's K row each, 128-255 after its V row: page id two tiles ahead, parameters one tile ahead.
