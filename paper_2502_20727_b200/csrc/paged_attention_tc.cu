@@ -26,8 +26,8 @@
 // whose weights are single bf16s, 187; bf16 124).
 // 4-bit pages: eight load warps, too, a key's K or V row per thread for the parameters and a quarter of a row for the codes.  Rows become float16 - one
 // product per pair of codes, see widen4 - scaled by powers of two that the softmax warps put into the exponent (a V row's lies in the scores, so that
-// weights stay within float16 whatever the row holds).  Ragged chunks as above 165 us, 2048 tokens on 14336 1271 (bf16 1140 beside it): the widening
-// and its loads, as with 8 bits.
+// weights stay within float16 whatever the row holds).  Ragged chunks as above 162 to 168 us, 2048 tokens on 14336 1255 to 1300 (bf16 1160 to 1180):
+// the widening and its loads, as with 8 bits.
 // A key that only some of the rows see may hold anything in V: tiles with such keys have their NaNs and infinities taken out of
 // shared memory before the product, and rows that do see them get them back at the end.
 // Key tiles can be cut into ranges over thread blocks (fp32 partial rows in the workspace, paged_merge_kernel).
@@ -400,9 +400,8 @@ __global__ void __launch_bounds__(tc_threads(TMA, FMT != KV_BF16), 2) paged_atte
             if constexpr (Q4) {
                 // K and V are scaled by powers of two to below 2^-4.  The rows of a tile share one for K and one for V where they are within 2^8 of one
                 // another, seen by all queries or not: the softmax warps then need no factor per key, and a value is off by 2^-10 of its row's largest power of two at
-                // most.  Otherwise (`varied`: a row may
-                // hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on 14336; now 1271, 1246
-                // without the second way.)
+                // most.  Otherwise (`varied`: a row may hold anything for the queries that do not see it) every row has its own.  (Always its own: 1603 us, chunk of 2048 on
+                // 14336, where this took 1271, and 1246 without the second way.)
                 // Threads 0-127 look after a key's K row each, 128-255 after its V row: page id two tiles ahead, parameters one tile ahead.
                 const uint32_t par = base + C::OFF_SC + 3200;
                 int *exps = (int *)(gen + C::OFF_SC + 3200 + 4096); // [2][8 warps][largest, smallest, rows that are not finite, -]
