@@ -289,7 +289,8 @@ struct AttnPlan { AttnKernel kernel; int splits; size_t workspace; int row_tile;
 // tcgen05 over 4-bit pages: ranges by a model of the time, in units of 50 ns: a key tile takes 2.2 us in a thread block with an SM to itself, 3.6 in each of
 // two; partial rows and their sum 5 us and 0.35 per thousand rows and range.  The model takes all sequences for as long as the bound.  Several are mostly not,
 // and thread blocks beyond one per SM even that out by themselves: there ranges have to gain 15 %, and beyond those that run at a time there are none.  At most four
-// times as many blocks as run at a time (79 MB of partial rows of 128 on 148 SMs), which keeps the launch within its limits, too.  Measured, us in one range
+// times as many blocks as run at a time (79 MB of partial rows of 128 on 148 SMs), which keeps the launch within its limits, too.  rows: by the bounds, not the tokens at hand, so that
+// a workspace for a step of many tokens serves one of fewer.  Measured, us in one range
 // and by this rule, 64 heads on 8 unless said: one sequence, 128 tokens on 14000 keys (64 blocks) 236, 112; 300 on 16000 (152) 388, 285; 600 (304) 610, 515; 700 (352) 618, 552; 2000
 // on 8000, 8 heads on 8 (128) 170, 148; 16 sequences, up to 8 tokens on 2000 to 8000 keys (128) 133, 90; 20, five tokens on 8000 (160) 199, 156; 24, on 2000 to 8000 (192) 154,
 // 110.  Where there are none, us in one range and in two or three: one sequence, 1024 tokens on 14336 keys (512) 698, 698; 2048 (1024) 1258, 1408; 40 sequences, five tokens on 2000
@@ -387,7 +388,7 @@ AttnPlan plan_attention(int fmt, int d, int nkv, int dtype, int nq, int B, long 
         long s = 2L * sm_count() / blocks;
         if (s > (keys + 511) / 512) s = (keys + 511) / 512;
         p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-        if (fmt == KV_INT4) p.splits = tc4_splits(blocks, (keys + 127) / 128, n_tokens * nq, B);
+        if (fmt == KV_INT4) p.splits = tc4_splits(blocks, (keys + 127) / 128, (long)(B > 0 ? B : 1) * max_new * nq, B);
     }
     if (p.kernel == ATTN_ROWS ? p.splits > PAGED_MAX_CLUSTER : p.splits > 1) p.workspace = (size_t)p.splits * n_tokens * nq * (d + 2) * sizeof(float);
     return p;
